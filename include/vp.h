@@ -11,6 +11,10 @@
  *   4. the top-K_t visual tokens by the head-averaged score S_i    (Eq. 2, Eq. 3)
  *   5. attention over the kept visual tokens plus every text token (Sec. 4.2, Sec. 5.7)
  *
+ * Beside it: vp_attend_new (attention of newly appended tokens: decode steps,
+ * drafted tokens, prompts; sliding window, sinks, accumulated weights) and
+ * vp_evict (eviction of cached tokens by accumulated weight).
+ *
  * Conventions shared by every entry point:
  *   - Tensors are caller-owned DEVICE memory unless stated otherwise; the
  *     library never frees or retains them beyond the call.  The context owns
@@ -242,6 +246,137 @@ vp_status vp_compact_kv(vp_ctx* ctx, int32_t batch, const vp_kv* src, const vp_k
                         const vp_span* visual_span, const int32_t* text_len,
                         const int32_t* kept_idx, int32_t kept_cap, const int32_t* kept_count,
                         void* cuda_stream);
+
+/*
+ * ---- Attention of newly appended tokens, and eviction from the cache ----
+ *
+ * VisionPulse prunes the visual tokens of a step; the text of a long
+ * generation still grows.  The entry points below serve the layers and the
+ * tokens that pruning leaves alone: attention of one or more new tokens over
+ * the cache (a decode step, drafted tokens, a prompt or a chunk of one) with
+ * an optional sliding window and sink tokens, a running sum of the attention
+ * weight that every cached token received, and eviction of the tokens with
+ * the smallest such sums.  They use the same contexts, caches (vp_kv), error
+ * codes and device checks as vp_decode_step.
+ */
+
+/* Which cached tokens a new token at position t sees: those at j <= t with
+ * j > t - window (its own position counts) or j < sinks. */
+#define VP_NO_WINDOW (-1)
+typedef struct {
+  int32_t window; /* tokens of the window, >= 0; VP_NO_WINDOW: every j <= t       */
+  int32_t sinks;  /* first tokens of the sequence that stay visible, >= 0          */
+  float scale;    /* logit scale; 0 means 1/sqrt(D)                                */
+} vp_visible;
+
+/* Rows of query heads: element (sequence b, new token i, head h, dim d) lives at
+ * data + b*stride_b + i*stride_n + h*stride_h + d (strides in elements; every
+ * row on a 16-byte boundary, as in vp_kv). */
+typedef struct {
+  void* data;
+  int64_t stride_b, stride_n, stride_h;
+} vp_rows;
+
+/* One float per cached token and kv-head: element (b, kv-head g, token j) lives
+ * at data + b*stride_b + g*stride_h + j (strides in elements). */
+typedef struct {
+  float* data;
+  int64_t stride_b, stride_h;
+} vp_weights;
+
+/*
+ * Allocates the workspace of vp_attend_new on a context, once: for calls of up
+ * to max_new new tokens per sequence, of which calls that accumulate weights
+ * pass at most max_weight_new (0: none does).  Waits for the device; call it
+ * outside stream capture.  A second call replaces the first one's workspace.
+ * VP_ERR_INVALID_ARG for max_new < 1, max_new > max_seq or a max_weight_new
+ * outside [0, max_new]; VP_ERR_UNSUPPORTED when max_weight_new * G > 128 (see
+ * vp_attend_new); VP_ERR_CUDA when the allocation fails (the context then has
+ * no such workspace).
+ */
+vp_status vp_reserve_new(vp_ctx* ctx, int32_t max_new, int32_t max_weight_new);
+
+/*
+ * Attention of the newest tokens of every sequence over its cache.  Sequence b
+ * holds seq_len[b] tokens, the last n_b of which are new (already appended);
+ * new token i stands at position t = seq_len[b] - n_b + i and attends to the
+ * tokens that vp_visible lets it see.
+ *   n_new        rows of q and out per sequence.
+ *   q, out       cfg.dtype rows; may be views of larger tensors.
+ *   k_cache, v_cache  caches of seq_len[b] live tokens, the new ones included.
+ *                Tokens that no new token sees (evicted pages, rows outside the
+ *                window or past the end) may hold anything, and the pages that
+ *                hold only such tokens need not be mapped.
+ *   seq_len      device int32 [batch], 0 <= seq_len <= max_seq.
+ *   new_len      device int32 [batch] or NULL: n_b, 0 <= n_b <= min(n_new,
+ *                seq_len[b]).  NULL: n_new in every sequence that is not empty.
+ *                Larger values are clamped and flagged (vp_check_errors).
+ *   lse          float [batch][n_new][H] or NULL: natural logarithm of the sum
+ *                of exp(logit) over the visible tokens.
+ *   weight_in,
+ *   weight_out   NULL, or for every live token j of every kv-head
+ *                weight_out[j] = weight_in[j] + the attention weight that j
+ *                received from the new tokens, summed over them and the G query
+ *                heads of the kv-head.  weight_in may be NULL (0 then) or the
+ *                same array as weight_out; entries at or past seq_len[b] are not
+ *                touched.  Needs n_new * G <= 128, else VP_ERR_UNSUPPORTED: after
+ *                a longer prompt, pass its last tokens once more as an
+ *                observation window.
+ * Rows that see nothing (i >= n_b, an empty sequence, a window of 0 without
+ * sinks) come out as 0 with lse = -infinity and add no weight.
+ * A page that a visible token needs but the block table does not map is left
+ * out of the attention and flagged.
+ * VP_ERR_CAPACITY when vp_reserve_new has not reserved for n_new (or the
+ * weights).  Allocates nothing and never synchronises; every kernel waits for
+ * the stream's previous work, so an input may be the output of the preceding
+ * call of this library.
+ */
+vp_status vp_attend_new(vp_ctx* ctx, int32_t batch, int32_t n_new, const vp_rows* q,
+                        const vp_kv* k_cache, const vp_kv* v_cache,
+                        const int32_t* seq_len, const int32_t* new_len, const vp_visible* visible,
+                        const vp_rows* out, float* lse,
+                        const vp_weights* weight_in, const vp_weights* weight_out, void* cuda_stream);
+
+/* What vp_evict keeps of a sequence of more than `keep` tokens: the first
+ * `sinks`, the last `recent`, and of the others the keep - sinks - recent with
+ * the largest accumulated weight, ties to the lower position (a NaN weight
+ * ranks below every other).  0 <= sinks, 0 <= recent, sinks + recent <= keep,
+ * keep >= 1. */
+typedef struct {
+  int32_t keep;
+  int32_t sinks;
+  int32_t recent;
+  int32_t granularity; /* 0: one kept set per sequence, weights summed over the kv-heads
+                          (in float, kv-head 0 first); 1: one kept set per kv-head          */
+} vp_evict_policy;
+
+/*
+ * Evicts tokens from the caches of one layer.  Sequences of at most
+ * policy->keep tokens keep all of them; of the others the kept rows move, in
+ * their order, to rows 0 .. keep - 1 of the destination.
+ *   k_src, v_src the caches to shrink.
+ *   k_dst, v_dst where the kept rows go: the source itself (same data, strides
+ *                and block table: in place), or caches that do not overlap it,
+ *                with rows for min(keep, seq_len[b]) tokens (paged when
+ *                block_table is set, with the context's page size).
+ *   weight       accumulated weights of the source (vp_attend_new).
+ *   weight_dst   NULL, or where the kept tokens' weights go.  The same array as
+ *                weight when in place; the freed entries keep .. seq_len - 1 are
+ *                then set to 0, so that tokens appended later start from 0.
+ *   seq_len      device int32 [batch], 0 <= seq_len <= max_seq.
+ *   kept_idx     int32 [batch][kept_cap] (granularity 1: [batch][Hkv][kept_cap]):
+ *                source positions of the kept tokens, ascending; unused slots
+ *                = -1.  kept_cap >= keep, else VP_ERR_CAPACITY.
+ *   new_len      int32 [batch]: min(seq_len, keep); may be seq_len itself.
+ * A kept row on an unmapped source page arrives as zeros, one whose destination
+ * page is unmapped is dropped; both are flagged (vp_check_errors).  Allocates
+ * nothing and never synchronises.
+ */
+vp_status vp_evict(vp_ctx* ctx, int32_t batch, const vp_kv* k_src, const vp_kv* v_src,
+                   const int32_t* seq_len, const vp_evict_policy* policy,
+                   const vp_kv* k_dst, const vp_kv* v_dst,
+                   const vp_weights* weight, const vp_weights* weight_dst,
+                   int32_t* kept_idx, int32_t kept_cap, int32_t* new_len, void* cuda_stream);
 
 /* Score kernel of later vp_decode_step calls on this context (an
  * implementation choice with no counterpart in the paper; results agree

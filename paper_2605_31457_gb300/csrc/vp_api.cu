@@ -9,62 +9,24 @@
 
 #include <algorithm>
 #include <string>
-#include <vector>
 
 #include "vp.h"
+#include "vp_ctx.h"
 #include "vp_internal.h"
 
-struct vp_ctx {
-  vp_config cfg;
-  int device = 0;
-  int num_sms = 0;
-  vp::WsLayout lay;
-  void* ws = nullptr;
-  size_t ws_bytes = 0;
-  float* z_ws = nullptr;
-  float* split_st = nullptr;
-  float* split_o = nullptr;
-  float* gpart_o = nullptr;
-  float* gpart_st = nullptr;
-  float* mt_o = nullptr;
-  float* mt_st = nullptr;
-  float* hmax = nullptr;
-  float diag_delta = 0.f;          // diagnostics (vp_set_diagnostics)
-  int32_t* diag_n_act = nullptr;
-  uint32_t* diag_bits = nullptr;
-  int32_t score_path = VP_SCORE_AUTO;  // vp_set_score_path
-  unsigned* tickets = nullptr;
-  unsigned* err = nullptr;
-  std::string last_error;
-  std::vector<cudaEvent_t> tev;  // stage-timing events, 4 per slot
-  int32_t tslots = 0;
-  int64_t tcalls = 0;
-  int32_t last_score_path = 0;  // vp_last_launch: score kernel and kernel count of the last call
-  int32_t last_kernels = 0;
-};
+using vp::aligned16;
+using vp::cuda_fail;
+using vp::fail;
+using vp::kv_ok;
 
 namespace {
-
 
 constexpr int64_t kPpm = 1000000;
 constexpr int kMaxVisual = 32768;  // score keys of one sequence fit in shared memory
 constexpr int kMaxHeads = 128;
 constexpr int kMaxGroup = 16;
 
-vp_status fail(vp_ctx* ctx, vp_status st, const std::string& msg) {
-  if (ctx) ctx->last_error = msg;
-  else vp::context_free_error() = msg;
-  return st;
-}
-
-vp_status cuda_fail(vp_ctx* ctx, const char* what, cudaError_t e) {
-  return fail(ctx, VP_ERR_CUDA, std::string(what) + ": " + cudaGetErrorString(e));
-}
-
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
 
 // Largest K_t the budget yields for n visual tokens (K_t is non-decreasing in
 // N_v in every mode, so the bound for max_visual covers every sequence).
@@ -100,28 +62,6 @@ bool budget_ok(const vp_budget& bd, std::string* why) {
   if (bd.fixed_k < 0) { *why = "budget.fixed_k must be >= 0"; return false; }
   if (bd.granularity != 0 && bd.granularity != 1) { *why = "budget.granularity must be 0 or 1"; return false; }
   if (bd.mode == VP_TOP_P && bd.granularity != 0) { *why = "the top-p budget needs granularity 0"; return false; }
-  return true;
-}
-
-bool kv_ok(const vp_ctx* ctx, const vp_kv* kv, const char* name, std::string* why) {
-  const size_t esz = ctx->cfg.dtype == VP_BF16 ? 2 : 4;
-  char buf[160];
-  if (!kv || !kv->data) { snprintf(buf, sizeof buf, "%s: NULL cache", name); *why = buf; return false; }
-  if (!aligned16(kv->data)) { snprintf(buf, sizeof buf, "%s: data must be 16-byte aligned", name); *why = buf; return false; }
-  const int64_t strides[3] = {kv->stride_b, kv->stride_h, kv->stride_t};
-  for (int64_t s : strides) {
-    if (s < 0 || ((uint64_t)s * esz) % 16 != 0) {
-      snprintf(buf, sizeof buf, "%s: strides must be >= 0 and multiples of 16 bytes", name); *why = buf; return false;
-    }
-  }
-  if (ctx->cfg.paged) {
-    if (!kv->block_table || kv->max_pages < 1 || kv->num_pages < 1) {
-      snprintf(buf, sizeof buf, "%s: paged cache needs block_table, max_pages >= 1, num_pages >= 1", name);
-      *why = buf; return false;
-    }
-  } else if (kv->block_table) {
-    snprintf(buf, sizeof buf, "%s: block_table given but the context is not paged", name); *why = buf; return false;
-  }
   return true;
 }
 
@@ -470,10 +410,11 @@ vp_status vp_check_errors(vp_ctx* ctx, void* cuda_stream) {
   std::string msg = "device checks failed:";
   if (word & vp::ERR_SPAN) msg += " visual span outside the live cache or above max_visual;";
   if (word & vp::ERR_TEXT) msg += " text_len < 1;";
-  if (word & vp::ERR_LEN) msg += " vis_len + text_len above max_seq;";
+  if (word & vp::ERR_LEN) msg += " vis_len + text_len above max_seq, or seq_len outside [0, max_seq];";
   if (word & vp::ERR_PAGE) msg += " block table entry outside the pool;";
   if (word & vp::ERR_KEPT) msg += " kept index outside the visual span;";
   if (word & vp::ERR_NONFINITE) msg += " non-finite importance score;";
+  if (word & vp::ERR_NEW) msg += " new_len outside [0, min(n_new, seq_len)];";
   if (word & vp::ERR_TIMEOUT) msg += " an asynchronous copy did not complete in time;";
   return fail(ctx, VP_ERR_DEVICE_PRECOND, msg);
 }
@@ -525,6 +466,7 @@ void vp_free(vp_ctx* ctx) {
     for (cudaEvent_t ev : ctx->tev) cudaEventDestroy(ev);
   }
   if (ctx->ws) cudaFree(ctx->ws);
+  if (ctx->new_ws) cudaFree(ctx->new_ws);
   delete ctx;
 }
 

@@ -1,0 +1,153 @@
+// Definitions of vp_attend_new and vp_evict shared by the host side
+// (vp_cache_api.cu) and the kernels (vp_attend.cu, vp_evict.cu).
+#pragma once
+
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "vp_internal.h"
+
+namespace vp {
+
+// Rows of query heads (vp_rows), strides in elements.
+struct RowView {
+  void* data;
+  int64_t sb, sn, sh;
+};
+// One float per cached token and kv-head (vp_weights).
+struct WeightView {
+  float* data;
+  int64_t sb, sh;
+};
+
+constexpr int kNewWeightRows = 128;  // n_new * G of a call that accumulates weights
+constexpr int kAnyTile = 32;         // cached tokens per tile of k_att_any
+constexpr int kAnyRows = 16;         // most query rows per CTA of k_att_any
+
+// The workspace of vp_attend_new (vp_reserve_new), offsets in bytes.
+struct NewLayout {
+  int max_new = 0, max_weight_new = 0;
+  int z_row = 0;              // floats per row of logits
+  size_t o_st = 0, o_o = 0, o_z = 0, total = 0;
+};
+
+// Query row r of a kv-head = new token r / G, query head g * G + r % G.
+struct AttendParams {
+  int dtype, B, H, Hkv, G, D, max_seq;
+  int paged, page_size, page_shift;
+  int n_new, R;               // R = n_new * G query rows per (sequence, kv-head)
+  RowView q, out;
+  KvView k, v;
+  const int32_t* seq_len;
+  const int32_t* new_len;     // or NULL
+  int window, sinks;
+  float c_log2;               // logit scale * log2(e)
+  float* lse;                 // [B][n_new][H] or NULL
+  int weigh;                  // weights asked for
+  WeightView w_in, w_out;     // w_in.data may be NULL
+  // workspace
+  float* part_o;              // partial outputs, unnormalised
+  float* part_st;             // their {maximum in log2 units, sum}
+  float* z;                   // [B * Hkv][R][z_row] logits in log2 units, of visible tokens, when weigh
+  int z_row;
+  unsigned* err;
+  int ns;                     // splits of k_att_any
+  int num_sms;
+};
+
+// The cached tokens that query rows with positions in [t0, t1] (t0 <= t1) see
+// between them: [0, s_end) and [lo, hi), s_end <= lo when both are non-empty
+// and apart; with window < 0 everything is in [lo, hi).
+struct SeenRange {
+  int s_end, lo, hi;
+};
+__host__ __device__ inline SeenRange seen_range(int t0, int t1, int window, int sinks) {
+  SeenRange r;
+  r.hi = t1 + 1;
+  if (window < 0) {
+    r.s_end = r.lo = 0;
+    return r;
+  }
+  r.lo = window > t0 ? 0 : t0 - window + 1;
+  if (window == 0) r.lo = r.hi;  // only the sinks
+  r.s_end = sinks < r.hi ? sinks : r.hi;
+  if (r.s_end >= r.lo) {         // one run
+    r.lo = 0;
+    r.s_end = 0;
+    if (window == 0) r.hi = sinks < r.hi ? sinks : r.hi;
+  }
+  return r;
+}
+// The same as a list of tiles of `rows` tokens: entry u is tile u for
+// u < na, else tile b0 + u - na; n entries, no tile twice.
+struct TileList {
+  int na, b0, n;
+  __host__ __device__ int tile(int u) const { return u < na ? u : b0 + u - na; }
+};
+__host__ __device__ inline TileList tile_list(const SeenRange& r, int rows) {
+  TileList l;
+  l.na = (r.s_end + rows - 1) / rows;
+  l.b0 = r.lo / rows;
+  const int b1 = (r.hi + rows - 1) / rows;
+  if (l.b0 < l.na) l.b0 = l.na;  // the two runs meet in one tile
+  l.n = l.na + (b1 > l.b0 && r.hi > r.lo ? b1 - l.b0 : 0);
+  return l;
+}
+__host__ __device__ inline bool sees(int j, int t, int window, int sinks) {
+  return j <= t && (window < 0 || j > t - window || j < sinks);
+}
+
+// Splits of k_att_any: enough CTAs for four per SM, at least two tiles each.
+inline int any_splits(int B, int Hkv, int R, int rows, int n_new, int window, int sinks, int max_seq, int num_sms) {
+  const int64_t units = (int64_t)B * Hkv * ((R + rows - 1) / rows);
+  int64_t span = max_seq;
+  if (window >= 0 && (int64_t)window + n_new + sinks + 2 * kAnyTile < span)
+    span = (int64_t)window + n_new + sinks + 2 * kAnyTile;
+  const int64_t most = span / (2 * kAnyTile);
+  int64_t ns = (4 * (int64_t)num_sms + units - 1) / units;
+  if (ns > most) ns = most;
+  return ns < 1 ? 1 : (int)ns;
+}
+inline int any_rows(int R) { return R <= 4 ? 4 : R <= 8 ? 8 : kAnyRows; }
+
+inline NewLayout new_layout(int max_batch, int H, int Hkv, int D, int max_seq, int max_new, int max_weight_new,
+                            int num_sms) {
+  NewLayout w;
+  w.max_new = max_new;
+  w.max_weight_new = max_weight_new;
+  const size_t G = (size_t)(H / Hkv);
+  // k_att_any splits only while there are fewer than four CTAs per SM before
+  // the split, so its partial rows stay below twice that; a call with weights
+  // goes through partials even unsplit.
+  size_t rows = (size_t)8 * num_sms * kAnyRows;
+  if (rows < (size_t)max_batch * Hkv * max_weight_new * G) rows = (size_t)max_batch * Hkv * max_weight_new * G;
+  size_t off = 0;
+  w.o_st = off; off = ws_round(off + rows * 2 * 4);
+  w.o_o = off; off = ws_round(off + rows * D * 4);
+  w.z_row = (max_seq + 127) / 128 * 128;
+  w.o_z = off; off = ws_round(off + (size_t)max_batch * Hkv * max_weight_new * G * w.z_row * 4);
+  w.total = off;
+  return w;
+}
+
+// Eviction (vp_evict).
+struct EvictParams {
+  int esz, B, Hkv, D, max_seq;
+  int page_size, page_shift;  // of whichever cache is paged
+  KvView ks, vs, kd, vd;
+  int in_place;
+  const int32_t* seq_len;
+  int keep, sinks, recent, granularity;
+  WeightView w, wd;           // wd.data may be NULL
+  int32_t* kept_idx;
+  int kept_cap;
+  int32_t* new_len;
+  unsigned* err;
+  int num_sms;
+};
+
+cudaError_t configure_attend();
+cudaError_t launch_attend(const AttendParams& p, cudaStream_t s);
+cudaError_t launch_evict(const EvictParams& p, cudaStream_t s);
+
+}  // namespace vp

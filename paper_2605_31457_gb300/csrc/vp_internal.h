@@ -18,11 +18,12 @@ std::string& context_free_error();
 enum : unsigned {
   ERR_SPAN = 1u,       // vis_start / vis_len outside the live cache or max_visual
   ERR_TEXT = 2u,       // text_len < 1 (no current token)
-  ERR_LEN = 4u,        // vis_len + text_len > max_seq
+  ERR_LEN = 4u,        // vis_len + text_len > max_seq, or seq_len outside [0, max_seq]
   ERR_PAGE = 8u,       // block-table entry outside [0, num_pages) or row past max_pages
   ERR_KEPT = 16u,      // a kept index outside [0, N_v)
   ERR_NONFINITE = 32u, // a non-finite score reached the selection
-  ERR_TIMEOUT = 64u    // a bounded wait for an asynchronous copy gave up
+  ERR_TIMEOUT = 64u,   // a bounded wait for an asynchronous copy gave up
+  ERR_NEW = 128u       // new_len outside [0, min(n_new, seq_len)]
 };
 
 // Split statistics written by the score kernel for every (sequence, query

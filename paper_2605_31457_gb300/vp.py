@@ -41,7 +41,9 @@ VP_SCORE_TC = 2
 
 EXPORTED = ("vp_init", "vp_decode_step", "vp_max_kept", "vp_last_error", "vp_check_errors",
             "vp_timing_enable", "vp_timing_read", "vp_free", "vp_decode_step_noalloc", "vp_decode_gather",
-            "vp_set_diagnostics", "vp_set_score_path", "vp_compact_kv", "vp_last_launch")
+            "vp_set_diagnostics", "vp_set_score_path", "vp_compact_kv", "vp_last_launch", "vp_reserve_new",
+            "vp_attend_new", "vp_evict")
+VP_NO_WINDOW = -1
 VP_NOALLOC_SCRATCH_BYTES = 16 << 20
 
 
@@ -69,6 +71,24 @@ class vp_budget(ctypes.Structure):
                 ("granularity", ctypes.c_int32)]
 
 
+class vp_visible(ctypes.Structure):
+    _fields_ = [("window", ctypes.c_int32), ("sinks", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+class vp_rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("stride_b", ctypes.c_int64), ("stride_n", ctypes.c_int64),
+                ("stride_h", ctypes.c_int64)]
+
+
+class vp_weights(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("stride_b", ctypes.c_int64), ("stride_h", ctypes.c_int64)]
+
+
+class vp_evict_policy(ctypes.Structure):
+    _fields_ = [("keep", ctypes.c_int32), ("sinks", ctypes.c_int32), ("recent", ctypes.c_int32),
+                ("granularity", ctypes.c_int32)]
+
+
 _P = ctypes.c_void_p
 lib.vp_init.argtypes = [ctypes.POINTER(vp_config), ctypes.POINTER(_P)]
 lib.vp_init.restype = ctypes.c_int
@@ -85,6 +105,16 @@ lib.vp_set_diagnostics.restype = ctypes.c_int
 lib.vp_compact_kv.argtypes = [_P, ctypes.c_int32, ctypes.POINTER(vp_kv), ctypes.POINTER(vp_kv),
                               ctypes.POINTER(vp_span), _P, _P, ctypes.c_int32, _P, _P]
 lib.vp_compact_kv.restype = ctypes.c_int
+lib.vp_reserve_new.argtypes = [_P, ctypes.c_int32, ctypes.c_int32]
+lib.vp_reserve_new.restype = ctypes.c_int
+lib.vp_attend_new.argtypes = [_P, ctypes.c_int32, ctypes.c_int32, ctypes.POINTER(vp_rows), ctypes.POINTER(vp_kv),
+                              ctypes.POINTER(vp_kv), _P, _P, ctypes.POINTER(vp_visible), ctypes.POINTER(vp_rows), _P,
+                              ctypes.POINTER(vp_weights), ctypes.POINTER(vp_weights), _P]
+lib.vp_attend_new.restype = ctypes.c_int
+lib.vp_evict.argtypes = [_P, ctypes.c_int32, ctypes.POINTER(vp_kv), ctypes.POINTER(vp_kv), _P,
+                         ctypes.POINTER(vp_evict_policy), ctypes.POINTER(vp_kv), ctypes.POINTER(vp_kv),
+                         ctypes.POINTER(vp_weights), ctypes.POINTER(vp_weights), _P, ctypes.c_int32, _P, _P]
+lib.vp_evict.restype = ctypes.c_int
 lib.vp_set_score_path.argtypes = [_P, ctypes.c_int32]
 lib.vp_set_score_path.restype = ctypes.c_int
 lib.vp_last_launch.argtypes = [_P, ctypes.POINTER(ctypes.c_int32), ctypes.POINTER(ctypes.c_int32)]
@@ -179,6 +209,45 @@ def vp_compact_kv(ctx, batch, src: vp_kv, dst: vp_kv, visual_span: vp_span, text
     return _check(st, ctx) if check else st
 
 
+def _stream(stream):
+    if stream is None:
+        import torch
+        stream = torch.cuda.current_stream().cuda_stream
+    elif hasattr(stream, "cuda_stream"):
+        stream = stream.cuda_stream
+    return ctypes.c_void_p(stream)
+
+
+def _ref(struct):
+    return None if struct is None else ctypes.byref(struct)
+
+
+def vp_reserve_new(ctx, max_new, max_weight_new=0):
+    """Allocates the workspace of vp_attend_new: up to ``max_new`` new tokens per
+    sequence, ``max_weight_new`` in calls that accumulate weights."""
+    return _check(lib.vp_reserve_new(ctx, int(max_new), int(max_weight_new)), ctx)
+
+
+def vp_attend_new(ctx, batch, n_new, q: vp_rows, k_cache: vp_kv, v_cache: vp_kv, seq_len, visible: vp_visible,
+                  out: vp_rows, new_len=None, lse=None, weight_in: vp_weights = None, weight_out: vp_weights = None,
+                  stream=None, check=True):
+    """Enqueues the attention of the ``n_new`` newest tokens of every sequence over
+    its cache.  q and out are ``rows(tensor)``, weight_in and weight_out
+    ``token_weights(tensor)`` or None; seq_len, new_len and lse are tensors."""
+    st = lib.vp_attend_new(ctx, batch, n_new, _ref(q), _ref(k_cache), _ref(v_cache), _ptr(seq_len), _ptr(new_len),
+                           _ref(visible), _ref(out), _ptr(lse), _ref(weight_in), _ref(weight_out), _stream(stream))
+    return _check(st, ctx) if check else st
+
+
+def vp_evict(ctx, batch, k_src: vp_kv, v_src: vp_kv, seq_len, policy: vp_evict_policy, k_dst: vp_kv, v_dst: vp_kv,
+             weight: vp_weights, weight_dst: vp_weights, kept_idx, kept_cap, new_len, stream=None, check=True):
+    """Enqueues the eviction of the least attended tokens: the kept rows of k_src
+    and v_src move to the front of k_dst and v_dst (the same caches: in place)."""
+    st = lib.vp_evict(ctx, batch, _ref(k_src), _ref(v_src), _ptr(seq_len), _ref(policy), _ref(k_dst), _ref(v_dst),
+                      _ref(weight), _ref(weight_dst), _ptr(kept_idx), kept_cap, _ptr(new_len), _stream(stream))
+    return _check(st, ctx) if check else st
+
+
 def vp_set_score_path(ctx, path):
     """Score kernel of later vp_decode_step calls: VP_SCORE_AUTO, VP_SCORE_MMA
     or VP_SCORE_TC."""
@@ -270,6 +339,27 @@ def kv_paged(pool, block_table) -> vp_kv:
     assert pool.dim() == 4 and pool.stride(3) == 1 and block_table.dim() == 2
     return vp_kv(pool.data_ptr(), pool.stride(0), pool.stride(1), pool.stride(2),
                  block_table.data_ptr(), block_table.shape[1], pool.shape[0])
+
+
+def rows(t) -> vp_rows:
+    """Query or output rows: a [B, n_new, H, D] tensor (any strides with a
+    contiguous last axis, e.g. a slice of a fused projection)."""
+    assert t.dim() == 4 and t.stride(3) == 1
+    return vp_rows(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2))
+
+
+def token_weights(t) -> vp_weights:
+    """Accumulated weights: a float32 [B, Hkv, T] tensor with a contiguous last axis."""
+    assert t.dim() == 3 and t.stride(2) == 1 and t.element_size() == 4 and t.is_floating_point()
+    return vp_weights(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def make_visible(window=VP_NO_WINDOW, sinks=0, scale=0.0) -> vp_visible:
+    return vp_visible(window, sinks, scale)
+
+
+def make_evict(keep, sinks=0, recent=0, granularity=1) -> vp_evict_policy:
+    return vp_evict_policy(keep, sinks, recent, granularity)
 
 
 def span(vis_start, vis_len) -> vp_span:
