@@ -12,36 +12,21 @@
 // parts of V_i join as m = max m_p, l = sum l_p e^(m_p - m), o likewise.
 // Logits are carried in log2 units (one exp2 each).
 //
+//   k_att_tc    (vp_attend_tc.cu) tensor-core kernel: bf16;
 //   k_att_any   FFMA kernel: fp32 caches, and bf16 caches of any layout;
-//   k_att_join  joins partials into out and lse, and adds the weights.
+//   k_att_join  joins partials into out and lse, and adds the weights;
+//   k_att_join_cut  joins the prompt items that k_att_tc cut between CTAs.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <math_constants.h>
 #include <stdint.h>
 
 #include "vp_attend.h"
+#include "vp_attend_device.h"
 #include "vp_device.h"
 
 namespace vp {
 namespace {
-
-constexpr float kLn2 = 0.6931471805599453f;
-
-// Live tokens of a sequence and how many of them are new.
-struct NewSeq {
-  int len, n;
-};
-__device__ __forceinline__ NewSeq load_new(const AttendParams& p, int b, bool report) {
-  NewSeq s;
-  s.len = __ldcg(p.seq_len + b);
-  unsigned e = 0;
-  if (s.len < 0 || s.len > p.max_seq) { e |= ERR_LEN; s.len = min(max(s.len, 0), p.max_seq); }
-  s.n = p.new_len ? __ldcg(p.new_len + b) : (s.len > 0 ? p.n_new : 0);
-  const int most = min(p.n_new, s.len);
-  if (s.n < 0 || s.n > most) { e |= ERR_NEW; s.n = min(max(s.n, 0), most); }
-  if (e && report) atomicOr(p.err, e);
-  return s;
-}
 
 // Row of (sequence b, kv-head g, token j); NULL where the block table maps it
 // to no page of the pool.
@@ -230,6 +215,50 @@ __global__ void __launch_bounds__(128) k_att_any(const __grid_constant__ AttendP
 }
 
 // ---------------------------------------------------------------------------
+// The partials of one query row: n records (those that are not live were never
+// written).  k_att_any leaves one per split; k_att_tc, in its one-row-block
+// form, one per part of the item and softmax group with tiles.
+// ---------------------------------------------------------------------------
+struct Partials {
+  int64_t first;     // record of entry 0
+  int n, stride;     // entries; records between them
+  int64_t W, p0, p1; // k_att_tc: total work, the item's tiles on it
+  int nc, c0;
+};
+__device__ __forceinline__ int part_tiles(const Partials& q, int c) {
+  const int64_t a = cut(q.W, q.nc, c), z = cut(q.W, q.nc, c + 1);
+  return (int)(min(z, q.p1) - max(a, q.p0));
+}
+__device__ __forceinline__ Partials partials_of(const AttendParams& p, int b, int g) {
+  Partials q;
+  q.stride = p.R;
+  if (p.kind == ATT_ANY) {
+    q.first = (int64_t)(b * p.Hkv + g) * p.ns * p.R;
+    q.n = p.ns;
+    return q;
+  }
+  const int total = __ldcg(p.prefix + p.B), at = __ldcg(p.prefix + b), next = __ldcg(p.prefix + b + 1);
+  q.W = (int64_t)total * p.Hkv;
+  q.nc = (int)min((int64_t)p.grid, q.W);
+  q.p0 = (int64_t)g * total + at + kItemCost;
+  q.p1 = (int64_t)g * total + next;
+  q.n = 0;
+  if (q.p1 > q.p0) {
+    q.c0 = owner(q.W, q.nc, q.p0);
+    q.n = 2 * (owner(q.W, q.nc, q.p1 - 1) - q.c0 + 1);
+    q.first = (int64_t)(g * p.B + b + q.c0) * 2 * p.R;
+  }
+  return q;
+}
+__device__ __forceinline__ bool partial_live(const AttendParams& p, const Partials& q, int i) {
+  return p.kind == ATT_ANY || part_tiles(q, q.c0 + (i >> 1)) > (i & 1);
+}
+__device__ __forceinline__ float2 partial_stat(const AttendParams& p, const Partials& q, int i, int row) {
+  if (!partial_live(p, q, i)) return make_float2(-CUDART_INF_F, 0.f);
+  return __ldcg(reinterpret_cast<const float2*>(p.part_st) + q.first + (int64_t)i * q.stride + row);
+}
+
+// ---------------------------------------------------------------------------
 // k_att_join: 128 threads.  Blocks below B * Hkv * R join the partials of one
 // query row into out and lse; the others (when weights are asked for) add the
 // weights of 512 cached tokens of one (sequence, kv-head), from the stored
@@ -250,10 +279,10 @@ __global__ void __launch_bounds__(128) k_att_join(const __grid_constant__ Attend
     const int row = blockIdx.x % p.R, bg = blockIdx.x / p.R, b = bg / p.Hkv, g = bg % p.Hkv;
     const NewSeq sq = load_new(p, b, false);
     const int n = row / p.G, h = g * p.G + row % p.G;
-    const int parts = n < sq.n ? p.ns : 0;
-    auto rec = [&](int i) { return ((int64_t)bg * p.ns + i) * p.R + row; };
+    const Partials q = partials_of(p, b, g);
+    const int parts = n < sq.n ? q.n : 0;
     float m = -CUDART_INF_F;
-    for (int i = tid; i < parts; i += 128) m = fmaxf(m, __ldcg(p.part_st + 2 * rec(i)));
+    for (int i = tid; i < parts; i += 128) m = fmaxf(m, partial_stat(p, q, i, row).x);
     m = warp_max(m);
     if (lane == 0) red[warp] = m;
     __syncthreads();
@@ -262,12 +291,13 @@ __global__ void __launch_bounds__(128) k_att_join(const __grid_constant__ Attend
 #pragma unroll
     for (int d = 0; d < DL; ++d) acc[d] = 0.f;
     for (int i = warp; i < parts; i += 4) {
-      const float2 st = __ldcg(reinterpret_cast<const float2*>(p.part_st + 2 * rec(i)));
+      const float2 st = partial_stat(p, q, i, row);
       if (st.x == -CUDART_INF_F) continue;
       const float f = exp2f(st.x - m);
+      const float* po = p.part_o + (q.first + (int64_t)i * q.stride + row) * D + lane;
       l = fmaf(st.y, f, l);
 #pragma unroll
-      for (int d = 0; d < DL; ++d) acc[d] = fmaf(f, __ldcg(p.part_o + rec(i) * D + 32 * d + lane), acc[d]);
+      for (int d = 0; d < DL; ++d) acc[d] = fmaf(f, __ldcg(po + 32 * d), acc[d]);
     }
     __syncthreads();
     if (lane == 0) red[warp] = l;
@@ -288,13 +318,13 @@ __global__ void __launch_bounds__(128) k_att_join(const __grid_constant__ Attend
   const NewSeq sq = load_new(p, b, false);
   if (j0 >= sq.len) return;
   const int rows = sq.n * p.G;
+  const Partials q = partials_of(p, b, g);
   for (int row = warp; row < rows; row += 4) {
-    auto rec = [&](int i) { return ((int64_t)bg * p.ns + i) * p.R + row; };
     float m = -CUDART_INF_F, l = 0.f;
-    for (int i = lane; i < p.ns; i += 32) m = fmaxf(m, __ldcg(p.part_st + 2 * rec(i)));
+    for (int i = lane; i < q.n; i += 32) m = fmaxf(m, partial_stat(p, q, i, row).x);
     m = warp_max(m);
-    for (int i = lane; i < p.ns; i += 32) {
-      const float2 st = __ldcg(reinterpret_cast<const float2*>(p.part_st + 2 * rec(i)));
+    for (int i = lane; i < q.n; i += 32) {
+      const float2 st = partial_stat(p, q, i, row);
       if (st.x != -CUDART_INF_F) l = fmaf(st.y, exp2f(st.x - m), l);
     }
     l = warp_sum(l);
@@ -313,44 +343,124 @@ __global__ void __launch_bounds__(128) k_att_join(const __grid_constant__ Attend
   }
 }
 
-cudaError_t launch_dep(void (*kernel)(AttendParams), dim3 grid, int threads, size_t smem, cudaStream_t st,
-                       const AttendParams& p) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = grid;
-  cfg.blockDim = dim3(threads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kernel, p);
+// ---------------------------------------------------------------------------
+// k_att_join_cut: the items of the two-group form of k_att_tc that were cut
+// between CTAs.  Blocks (c, x) with the cut before CTA c the first one inside
+// its item join 32 of its 256 query rows, a warp per row; the other blocks
+// leave at once.
+// ---------------------------------------------------------------------------
+template <int D>
+__global__ void __launch_bounds__(128) k_att_join_cut(const __grid_constant__ AttendParams p) {
+  constexpr int DL = D / 32, kRows = 32;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  pdl_wait();
+  const int pairs = p.B * p.nqt, c = blockIdx.y + 1;
+  const int total = __ldcg(p.prefix + pairs);
+  const int64_t W = (int64_t)total * p.Hkv;
+  const int nc = (int)min((int64_t)p.grid, W);
+  if (c >= nc) return;
+  const int64_t x = cut(W, nc, c);
+  const int g = (int)(x / total), at = (int)(x - (int64_t)g * total);
+  int lo = 0, hi = pairs;  // the pair that holds position `at`
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (__ldcg(p.prefix + mid) <= at) lo = mid;
+    else hi = mid;
+  }
+  const int64_t p0 = (int64_t)g * total + __ldcg(p.prefix + lo), p1 = (int64_t)g * total + __ldcg(p.prefix + lo + 1);
+  if (x == p0 || cut(W, nc, c - 1) > p0) return;  // no item is cut here, or it was cut before
+  const int b = lo / p.nqt, qt = lo % p.nqt, last = owner(W, nc, p1 - 1);
+  const NewSeq sq = load_new(p, b, false);
+  for (int r = blockIdx.x * kRows + warp; r < (blockIdx.x + 1) * kRows; r += 4) {
+    const int row = qt * 2 * kTcTile + r;
+    if (row >= p.R) return;
+    const int n = row / p.G, h = g * p.G + row % p.G;
+    // CTA c - 1 began the item (its second record); the later ones went on with it.
+    auto rec = [&](int k) { return (int64_t)(k < c ? 2 * k + 1 : 2 * k) * 2 * kTcTile + r; };
+    auto live = [&](int k) {
+      return min(cut(W, nc, k + 1), p1) > max(cut(W, nc, k), p0 + kItemCost);
+    };
+    float m = -CUDART_INF_F, l = 0.f, acc[DL];
+#pragma unroll
+    for (int d = 0; d < DL; ++d) acc[d] = 0.f;
+    if (n < sq.n) {
+      for (int k = c - 1; k <= last; ++k)
+        if (live(k)) m = fmaxf(m, __ldcg(p.part_st + 2 * rec(k)));
+      for (int k = c - 1; k <= last; ++k) {
+        if (!live(k)) continue;
+        const float2 st = __ldcg(reinterpret_cast<const float2*>(p.part_st) + rec(k));
+        if (st.x == -CUDART_INF_F) continue;
+        const float f = exp2f(st.x - m);
+        const float* po = p.part_o + rec(k) * D + lane;
+        l = fmaf(st.y, f, l);
+#pragma unroll
+        for (int d = 0; d < DL; ++d) acc[d] = fmaf(f, __ldcg(po + 32 * d), acc[d]);
+      }
+    }
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+    __nv_bfloat16* o = static_cast<__nv_bfloat16*>(p.out.data) + (int64_t)b * p.out.sb + (int64_t)n * p.out.sn +
+                       (int64_t)h * p.out.sh;
+#pragma unroll
+    for (int d = 0; d < DL; ++d) o[32 * d + lane] = __float2bfloat16_rn(acc[d] * inv);
+    if (p.lse && lane == 0)
+      p.lse[((int64_t)b * p.n_new + n) * p.H + h] = l > 0.f ? (m + log2f(l)) * kLn2 : -CUDART_INF_F;
+  }
+}
+
+template <typename T, int D>
+cudaError_t launch_join(const AttendParams& p, cudaStream_t st) {
+  const int64_t chunks = p.weigh ? (p.max_seq + kJoinTokens - 1) / kJoinTokens : 0;
+  const int64_t joins = (int64_t)p.B * p.Hkv * (p.R + chunks);
+  if (joins > INT32_MAX) return cudaErrorInvalidConfiguration;
+  return launch_dep(k_att_join<T, D>, dim3((unsigned)joins), 128, 0, st, p);
+}
+
+template <int D>
+cudaError_t launch_tensor(const AttendParams& p, cudaStream_t st) {
+  const cudaError_t e = launch_tc(p, st);
+  if (e != cudaSuccess) return e;
+  if (p.kind == ATT_TC1) return launch_join<__nv_bfloat16, D>(p, st);
+  return p.grid > 1 ? launch_dep(k_att_join_cut<D>, dim3(2 * kTcTile / 32, p.grid - 1), 128, 0, st, p) : cudaSuccess;
 }
 
 template <typename T, int D>
 cudaError_t launch_any(const AttendParams& p, cudaStream_t st) {
   const int rb = any_rows(p.R);
   const int64_t ctas = (int64_t)p.B * p.Hkv * ((p.R + rb - 1) / rb) * p.ns;
-  const int64_t chunks = p.weigh ? (p.max_seq + kJoinTokens - 1) / kJoinTokens : 0;
-  const int64_t joins = (int64_t)p.B * p.Hkv * (p.R + chunks);
-  if (ctas > INT32_MAX || joins > INT32_MAX) return cudaErrorInvalidConfiguration;
+  if (ctas > INT32_MAX) return cudaErrorInvalidConfiguration;
   const dim3 grid((unsigned)ctas);
   cudaError_t e;
   if (rb == 4) e = launch_dep(k_att_any<T, D, 1>, grid, 128, sizeof(AnySmem<D, 1>), st, p);
   else if (rb == 8) e = launch_dep(k_att_any<T, D, 2>, grid, 128, sizeof(AnySmem<D, 2>), st, p);
   else e = launch_dep(k_att_any<T, D, 4>, grid, 128, sizeof(AnySmem<D, 4>), st, p);
   if (e != cudaSuccess || (p.ns == 1 && !p.weigh)) return e;
-  return launch_dep(k_att_join<T, D>, dim3((unsigned)joins), 128, 0, st, p);
+  return launch_join<T, D>(p, st);
 }
 
 }  // namespace
 
-cudaError_t configure_attend() {
-  return cudaSuccess;
+cudaError_t configure_attend() { return configure_tc(); }
+
+void plan_attend(AttendParams& p) {
+  p.kind = ATT_ANY;
+  p.ns = any_splits(p.B, p.Hkv, p.R, any_rows(p.R), p.n_new, p.window, p.sinks, p.max_seq, p.num_sms);
+  // The tensor cores read bf16, and boxes of fewer than 8 rows would split the
+  // swizzle's 1024-byte atoms.
+  if (p.dtype != 0 || (p.paged && p.page_size < 8)) return;
+  const KvShape shape{p.D, p.Hkv, p.B, p.paged, p.page_size, p.max_seq};
+  const int rows = p.paged && p.page_size < kTcTile ? p.page_size : kTcTile;
+  int vt = 0, vg = 0, vb = 0;
+  if (!encode_kv_map(p.k, shape, &p.tmk, &p.tpos, &p.gpos, &p.bpos, rows) ||
+      !encode_kv_map(p.v, shape, &p.tmv, &vt, &vg, &vb, rows) || vt != p.tpos || vg != p.gpos || vb != p.bpos)
+    return;
+  p.kind = p.R <= kTcTile ? ATT_TC1 : ATT_TC2;
+  p.nqt = p.kind == ATT_TC1 ? 1 : (p.R + 2 * kTcTile - 1) / (2 * kTcTile);
+  p.grid = p.num_sms;
+  p.stream_once = p.kind == ATT_TC1;
 }
 
 cudaError_t launch_attend(const AttendParams& p, cudaStream_t st) {
+  if (p.kind != ATT_ANY) return p.D == 128 ? launch_tensor<128>(p, st) : launch_tensor<64>(p, st);
   if (p.dtype == 0)
     return p.D == 128 ? launch_any<__nv_bfloat16, 128>(p, st) : launch_any<__nv_bfloat16, 64>(p, st);
   return p.D == 128 ? launch_any<float, 128>(p, st) : launch_any<float, 64>(p, st);

@@ -135,7 +135,8 @@ vp_status attend_new(vp_ctx* ctx, int32_t batch, int32_t n_new, const vp_rows* q
   p.z_row = ctx->new_lay.z_row;
   p.err = ctx->err;
   p.num_sms = ctx->num_sms;
-  p.ns = vp::any_splits(batch, Hkv, p.R, vp::any_rows(p.R), n_new, p.window, p.sinks, c.max_seq, p.num_sms);
+  p.prefix = reinterpret_cast<int*>(ws + ctx->new_lay.o_pre);
+  vp::plan_attend(p);
   const cudaError_t e = vp::launch_attend(p, static_cast<cudaStream_t>(cuda_stream));
   if (e != cudaSuccess) return cuda_fail(ctx, "vp_attend_new: launch", e);
   return VP_OK;

@@ -296,6 +296,13 @@ cudaError_t configure_kernels(int max_visual, int H, int nsp_max);
 // With p.use_tc set on entry (a plan made for the tensor-core kernel) it also
 // fills p.tmk2 / p.tmv2 and keeps use_tc only if that kernel can run.
 void encode_kv_maps(StepParams& p);
+// The 4-D descriptor of one bf16 cache in boxes of R rows x 64 dimensions, and
+// the descriptor dimensions (1..3) of its token, kv-head and sequence / page
+// axes; false for a layout it cannot describe within the caller's memory.
+struct KvShape {
+  int D, Hkv, B, paged, page_size, max_seq;
+};
+bool encode_kv_map(const KvView& kv, const KvShape& p, CUtensorMap* map, int* tpos, int* gpos, int* bpos, int R);
 // The tensor-core score kernel's shape conditions (decode step, bf16, D = 128,
 // at most 16 query heads per kv-head, pages of at least 8 rows).
 inline bool tc_eligible(int dtype, int D, int G, int paged, int page_size) {

@@ -3912,12 +3912,13 @@ EncodeTiledFn encode_fn() {
   }();
   return fn;
 }
+}  // namespace
 
 // 4-D descriptor of one cache: dims {D, token, kv-head, sequence or page}, the
 // last three ordered by increasing stride, boxes of 64 dimensions x R rows.
 // Returns false for a layout whose extent along the token axis cannot be
 // bounded by the caller's memory.
-bool encode_one(const KvView& kv, const StepParams& p, CUtensorMap* map, int* tpos, int* gpos, int* bpos, int R) {
+bool encode_kv_map(const KvView& kv, const KvShape& p, CUtensorMap* map, int* tpos, int* gpos, int* bpos, int R) {
   EncodeTiledFn fn = encode_fn();
   if (!fn || !kv.data) return false;
   struct Ax { int64_t stride, size; int id; };  // id: 0 token, 1 kv-head, 2 sequence / page
@@ -3954,6 +3955,11 @@ bool encode_one(const KvView& kv, const StepParams& p, CUtensorMap* map, int* tp
                         CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS;
+}
+
+namespace {
+bool encode_one(const KvView& kv, const StepParams& p, CUtensorMap* map, int* tpos, int* gpos, int* bpos, int R) {
+  return encode_kv_map(kv, KvShape{p.D, p.Hkv, p.B, p.paged, p.page_size, p.max_seq}, map, tpos, gpos, bpos, R);
 }
 }  // namespace
 
