@@ -30,22 +30,24 @@ constexpr int kTcTile = 128;         // cached tokens per tile of k_att_tc; quer
 struct NewLayout {
   int max_new = 0, max_weight_new = 0;
   int z_row = 0;              // floats per row of logits
-  size_t o_pre = 0, o_st = 0, o_o = 0, o_z = 0, total = 0;
+  size_t o_tk = 0, o_lse = 0, o_st = 0, o_o = 0, o_z = 0, total = 0;
 };
 
-// Which kernel serves a call.  k_att_tc runs in two forms: up to 128 query
-// rows per (sequence, kv-head) are one accumulator, whose tiles alternate
-// between the two softmax groups; more rows go 256 at a time, both groups
-// reading every tile.
-enum { ATT_ANY = 0, ATT_TC1 = 1, ATT_TC2 = 2 };
+// Which kernel serves a call (plan_attend).  `block` query rows of one
+// (sequence, kv-head) are an item of the tensor-core kernels:
+//   ATT_DEC  k_att_dec: at most 32 query rows, all of them one item;
+//   ATT_TC1  k_att_tc: at most 128, one item whose tiles alternate between its
+//            two softmax groups;
+//   ATT_TC2  k_att_tc: 256 rows at a time, 128 for each group.
+enum { ATT_ANY = 0, ATT_DEC = 1, ATT_TC1 = 2, ATT_TC2 = 3 };
+constexpr int kDecRows = 32;
 
 // Query row r of a kv-head = new token r / G, query head g * G + r % G.
 struct AttendParams {
   CUtensorMap tmk, tmv;       // k_att_tc: the caches in boxes of up to 128 rows
   int tpos, gpos, bpos;       // descriptor dimensions of the token, kv-head and sequence / page axes
   int kind;                   // ATT_*
-  int nqt;                    // k_att_tc: row blocks per (sequence, kv-head)
-  int* prefix;                // k_att_tc: work before each (sequence, row block), of one kv-head; then its total
+  int block, nqt;             // tensor-core kernels: query rows of an item, items per (sequence, kv-head)
   int dtype, B, H, Hkv, G, D, max_seq;
   int paged, page_size, page_shift;
   int n_new, R;               // R = n_new * G query rows per (sequence, kv-head)
@@ -59,14 +61,15 @@ struct AttendParams {
   int weigh;                  // weights asked for
   WeightView w_in, w_out;     // w_in.data may be NULL
   // workspace
+  unsigned* tickets;          // [2 * grid] records written of the items cut between CTAs; 0 between calls
+  float* lse2;                // [B * Hkv][R] log-sum-exp in log2 units (+inf: an empty row), when weigh
   float* part_o;              // partial outputs, unnormalised
   float* part_st;             // their {maximum in log2 units, sum}
   float* z;                   // [B * Hkv][R][z_row] logits in log2 units, of visible tokens, when weigh
   int z_row;
   unsigned* err;
   int ns;                     // splits of k_att_any
-  int grid;                   // CTAs of k_att_tc
-  int stream_once;            // its tiles are read by one CTA each: evict-first in L2
+  int grid;                   // CTAs of the tensor-core kernels
   int num_sms;
 };
 
@@ -112,14 +115,14 @@ __host__ __device__ inline bool sees(int j, int t, int window, int sinks) {
   return j <= t && (window < 0 || j > t - window || j < sinks);
 }
 
-// ---- The work of k_att_tc.  An item is one block of query rows (256 in the
-// two-group form, else all) of one (sequence, kv-head); its cost is the tiles
-// it sees plus kItemCost, a fixed part for loading the queries, filling the
-// pipeline and writing the result.  Items follow one another kv-head by
-// kv-head, sequence by sequence, and the line of their costs is cut into equal
-// parts, one per CTA: a CTA owns tiles, not items, so ragged lengths leave no
-// CTA idle.
-constexpr int kItemCost = 2;
+// ---- The work of the tensor-core kernels.  The cost of an item is the tiles
+// it sees plus a fixed part for loading its queries and writing its result.
+// Items follow one another kv-head by kv-head, sequence by sequence, and the
+// line of their costs is cut into equal parts, one per CTA: a CTA owns tiles,
+// not items, so ragged lengths leave no CTA idle.  An item whose tiles lie with
+// several CTAs leaves a record (m, l, O) per CTA (and group); the last CTA to
+// finish joins them.
+constexpr int kItemCost = 1;
 struct AttItem {
   int row0, rows;  // query rows [row0, row0 + rows)
   SeenRange sr;
@@ -136,10 +139,22 @@ __host__ __device__ inline AttItem att_item(int len, int n, int G, int block, in
   it.tl = tile_list(it.sr, kTcTile);
   return it;
 }
-// CTA c of nc owns [cut(c), cut(c + 1)) of a line of `total`; owner(x) is the
-// CTA that owns position x.
-__host__ __device__ inline int64_t cut(int64_t total, int nc, int c) { return total * c / nc; }
-__host__ __device__ inline int owner(int64_t total, int nc, int64_t x) { return (int)(((x + 1) * nc - 1) / total); }
+// A line of `total` positions cut for at most `ctas` CTAs: CTA c owns
+// [start(c), start(c + 1)); the first `extra` of them own one position more.
+struct LineCut {
+  int nc, per, extra;
+  __host__ __device__ LineCut() {}
+  __host__ __device__ LineCut(int64_t total, int ctas) {
+    nc = total < ctas ? (int)total : ctas;
+    per = (int)(total / nc);
+    extra = (int)(total - (int64_t)per * nc);
+  }
+  __host__ __device__ int64_t start(int c) const { return (int64_t)c * per + (c < extra ? c : extra); }
+  __host__ __device__ int owner(int64_t x) const {
+    const int64_t big = (int64_t)extra * (per + 1);
+    return x < big ? (int)(x / (per + 1)) : extra + (int)((x - big) / per);
+  }
+};
 
 // Splits of k_att_any: enough CTAs for four per SM, at least two tiles each.
 inline int any_splits(int B, int Hkv, int R, int rows, int n_new, int window, int sinks, int max_seq, int num_sms) {
@@ -165,15 +180,12 @@ inline NewLayout new_layout(int max_batch, int H, int Hkv, int D, int max_seq, i
   // goes through partials even unsplit.
   size_t rows = (size_t)8 * num_sms * kAnyRows;
   if (rows < (size_t)max_batch * Hkv * max_weight_new * G) rows = (size_t)max_batch * Hkv * max_weight_new * G;
-  // k_att_tc: one partial per (part, group), a part being an item's share of a
-  // CTA; in the two-group form only for items cut between CTAs.
-  const size_t most = max_new * G < (size_t)kTcTile ? max_new * G : kTcTile;
-  const size_t rows1 = 2 * ((size_t)max_batch * Hkv + num_sms) * most, rows2 = (size_t)2 * num_sms * 2 * kTcTile;
-  if (rows < rows1) rows = rows1;
-  if (max_new * G > (size_t)kTcTile && rows < rows2) rows = rows2;
-  const size_t nqt = (max_new * G + 2 * kTcTile - 1) / (2 * kTcTile);
+  // The tensor-core kernels: two records per CTA (the item it goes on with and
+  // the one it begins), of 32 rows at two CTAs per SM or of 256 at one.
+  if (rows < (size_t)2 * num_sms * 2 * kTcTile) rows = (size_t)2 * num_sms * 2 * kTcTile;
   size_t off = 0;
-  w.o_pre = off; off = ws_round(off + ((size_t)max_batch * nqt + 1) * 4);
+  w.o_tk = off; off = ws_round(off + (size_t)4 * num_sms * 4);
+  w.o_lse = off; off = ws_round(off + (size_t)max_batch * Hkv * max_weight_new * G * 4);
   w.o_st = off; off = ws_round(off + rows * 2 * 4);
   w.o_o = off; off = ws_round(off + rows * D * 4);
   w.z_row = (max_seq + 127) / 128 * 128;
@@ -201,7 +213,9 @@ struct EvictParams {
 cudaError_t configure_attend();
 // Chooses the kernel (p.kind) and its launch shape; encodes the tensor maps.
 void plan_attend(AttendParams& p);
+cudaError_t configure_dec();
 cudaError_t configure_tc();
+cudaError_t launch_dec(const AttendParams& p, cudaStream_t s);
 cudaError_t launch_tc(const AttendParams& p, cudaStream_t s);
 cudaError_t launch_attend(const AttendParams& p, cudaStream_t s);
 cudaError_t launch_evict(const EvictParams& p, cudaStream_t s);

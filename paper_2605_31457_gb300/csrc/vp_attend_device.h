@@ -1,10 +1,13 @@
 // Device and launch helpers shared by the kernels of vp_attend_new.
 #pragma once
 
+#include <cuda_bf16.h>
 #include <cuda_runtime.h>
+#include <math_constants.h>
 #include <stdint.h>
 
 #include "vp_attend.h"
+#include "vp_device.h"
 
 namespace vp {
 
@@ -26,8 +29,179 @@ __device__ __forceinline__ NewSeq load_new(const AttendParams& p, int b, bool re
   return s;
 }
 
+// Output row (new token row / G, query head g * G + row % G) of sequence b.
+template <typename T>
+__device__ __forceinline__ T* out_row(const AttendParams& p, int b, int g, int row) {
+  return static_cast<T*>(p.out.data) + (int64_t)b * p.out.sb + (int64_t)(row / p.G) * p.out.sn +
+         (int64_t)(g * p.G + row % p.G) * p.out.sh;
+}
+// The log-sum-exp of a row from its maximum (log2 units) and sum.
+__device__ __forceinline__ void store_lse(const AttendParams& p, int b, int g, int row, float m, float l) {
+  const float x = l > 0.f ? m + log2f(l) : -CUDART_INF_F;
+  if (p.lse) p.lse[((int64_t)b * p.n_new + row / p.G) * p.H + g * p.G + row % p.G] = x * kLn2;
+  if (p.weigh) p.lse2[(int64_t)(b * p.Hkv + g) * p.R + row] = l > 0.f ? x : CUDART_INF_F;
+}
+
+// ---- The line of work of the tensor-core kernels (AttItem, LineCut).
+
+// A CTA's place on it: the item (kv-head g, pair = sequence * nqt + row block)
+// and the position within the item, its position on the line, positions left.
+struct Walk {
+  int g, pair, off;
+  int64_t pos;
+  int left;
+};
+// The next item a CTA does, or its share of it: tiles [u0, u1) of the list.
+struct Part {
+  int g, b, u0, u1;
+  bool owner;       // this CTA holds the item's first position: it answers for an item without tiles
+  int64_t first;    // the item's first tile on the line
+  NewSeq sq;
+  AttItem it;
+  __device__ bool whole() const { return u0 == 0 && u1 == it.tl.n; }
+};
+__device__ __forceinline__ bool next_part(const AttendParams& p, Walk& w, Part& q) {
+  if (w.left <= 0) return false;
+  q.g = w.g;
+  q.b = w.pair / p.nqt;
+  q.sq = load_new(p, q.b, false);
+  q.it = att_item(q.sq.len, q.sq.n, p.G, p.block, w.pair - q.b * p.nqt, p.window, p.sinks);
+  const int cost = q.it.tl.n + kItemCost, end = min(cost, w.off + w.left), done = end - w.off;
+  q.u0 = max(0, w.off - kItemCost);
+  q.u1 = max(0, end - kItemCost);
+  q.owner = w.off == 0;
+  q.first = w.pos - w.off + kItemCost;
+  w.left -= done;
+  w.pos += done;
+  w.off = 0;
+  if (++w.pair == p.B * p.nqt) { w.pair = 0; ++w.g; }
+  return true;
+}
+// Finds this CTA's start: each thread sums the costs of a run of pairs, a block
+// scan gives their places.  misc: NT / 32 + 2 ints of shared memory.
+template <int NT>
+__device__ __forceinline__ Walk line_start(const AttendParams& p, int* misc, LineCut& lc) {
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int pairs = p.B * p.nqt, run = (pairs + NT - 1) / NT;
+  const int i0 = min(pairs, tid * run), i1 = min(pairs, i0 + run);
+  auto pair_cost = [&](int i, bool report) {
+    const int b = i / p.nqt;
+    const NewSeq sq = load_new(p, b, report && blockIdx.x == 0 && i == b * p.nqt);
+    return att_item(sq.len, sq.n, p.G, p.block, i - b * p.nqt, p.window, p.sinks).tl.n + kItemCost;
+  };
+  int mine = 0;
+  for (int i = i0; i < i1; ++i) mine += pair_cost(i, true);
+  int incl = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += y;
+  }
+  if (lane == 31) misc[warp] = incl;
+  __syncthreads();
+  int before = incl - mine, total = 0;
+#pragma unroll
+  for (int w = 0; w < NT / 32; ++w) {
+    if (w < warp) before += misc[w];
+    total += misc[w];
+  }
+  lc = LineCut((int64_t)total * p.Hkv, gridDim.x);
+  Walk w{0, 0, 0, 0, 0};
+  if ((int)blockIdx.x < lc.nc) {
+    w.pos = lc.start(blockIdx.x);
+    w.left = (int)(lc.start(blockIdx.x + 1) - w.pos);
+    w.g = (int)(w.pos / total);
+  }
+  const int at = (int)(w.pos - (int64_t)w.g * total);
+  if (at >= before && at < before + mine) {
+    int sum = before, i = i0;
+    if (run > 1)
+      for (;; ++i) {
+        const int cost = pair_cost(i, false);
+        if (at < sum + cost) break;
+        sum += cost;
+      }
+    misc[NT / 32] = i;
+    misc[NT / 32 + 1] = at - sum;
+  }
+  __syncthreads();
+  w.pair = misc[NT / 32];
+  w.off = misc[NT / 32 + 1];
+  return w;
+}
+
+// ---- Joining records.  A record holds, for RS query rows, the maximum and sum
+// (part_st) and the unnormalised output (part_o) of one share of an item.
+
+// Called by the NT threads of `bar` after their record is written: true for the
+// group that is the last of `expected` to arrive at the ticket.
+template <typename Sync>
+__device__ __forceinline__ bool last_to_arrive(unsigned* ticket, unsigned expected, int tid, int* flag, Sync&& sync) {
+  __threadfence();
+  sync();
+  if (tid == 0) {
+    const bool last = atomicAdd(ticket, 1u) == expected - 1;
+    if (last) *ticket = 0;  // for the next call
+    *flag = last;
+  }
+  sync();
+  const bool last = *flag != 0;
+  if (last) __threadfence();
+  return last;
+}
+
+// Joins records rec(0) .. rec(n - 1) of rows [row0, row0 + rows) into out and
+// lse: a thread per row and four dimensions, records read eight at a time.
+template <typename T, int D, int NT, typename Rec>
+__device__ __forceinline__ void join_records(const AttendParams& p, int b, int g, int row0, int rows, int n, int RS,
+                                             Rec&& rec, int tid) {
+  constexpr int C4 = D / 4, U = 8;
+  for (int e = tid; e < rows * C4; e += NT) {
+    const int r = e / C4, d = 4 * (e % C4);
+    float m = -CUDART_INF_F, l = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int k0 = 0; k0 < n; k0 += U) {
+      float2 st[U];
+      float4 x[U];
+#pragma unroll
+      for (int k = 0; k < U; ++k) {
+        st[k] = make_float2(-CUDART_INF_F, 0.f);
+        x[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (k0 + k < n) {
+          const int64_t at = (int64_t)rec(k0 + k) * RS + r;
+          st[k] = __ldcg(reinterpret_cast<const float2*>(p.part_st) + at);
+          x[k] = __ldcg(reinterpret_cast<const float4*>(p.part_o + at * D + d));
+        }
+      }
+      float mn = m;
+#pragma unroll
+      for (int k = 0; k < U; ++k) mn = fmaxf(mn, st[k].x);
+      const float mu = mn == -CUDART_INF_F ? 0.f : mn;
+      const float f = exp2f(m - mu);
+      l *= f; o.x *= f; o.y *= f; o.z *= f; o.w *= f;
+#pragma unroll
+      for (int k = 0; k < U; ++k) {
+        const float w = exp2f(st[k].x - mu);
+        l = fmaf(w, st[k].y, l);
+        o.x = fmaf(w, x[k].x, o.x);
+        o.y = fmaf(w, x[k].y, o.y);
+        o.z = fmaf(w, x[k].z, o.z);
+        o.w = fmaf(w, x[k].w, o.w);
+      }
+      m = mn;
+    }
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+    T* out = out_row<T>(p, b, g, row0 + r) + d;
+    out[0] = from_f<T>(o.x * inv);
+    out[1] = from_f<T>(o.y * inv);
+    out[2] = from_f<T>(o.z * inv);
+    out[3] = from_f<T>(o.w * inv);
+    if (d == 0) store_lse(p, b, g, row0 + r, m, l);
+  }
+}
+
 inline cudaError_t launch_dep(void (*kernel)(AttendParams), dim3 grid, int threads, size_t smem, cudaStream_t st,
-                       const AttendParams& p) {
+                              const AttendParams& p) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = dim3(threads);

@@ -74,36 +74,6 @@ __host__ __device__ constexpr uint32_t att_idesc(int n, int b_mn) {
          ((uint32_t)(128 >> 4) << 24);
 }
 
-// A CTA's place on the line of work, and the part of an item it does next.
-struct Walk {
-  int g, pair, off, left;  // kv-head, (sequence, row block), position within the item, positions left
-};
-struct Part {
-  int g, b, pair, qt, u0, u1;  // tiles [u0, u1) of the item's list
-  bool cont, whole;            // begun by an earlier CTA; all of the item
-  NewSeq sq;
-  AttItem it;
-};
-template <int NQ>
-__device__ __forceinline__ bool next_part(const AttendParams& p, Walk& w, Part& q) {
-  if (w.left <= 0) return false;
-  q.g = w.g;
-  q.pair = w.pair;
-  q.b = w.pair / p.nqt;
-  q.qt = w.pair - q.b * p.nqt;
-  q.sq = load_new(p, q.b, false);
-  q.it = att_item(q.sq.len, q.sq.n, p.G, NQ * kTcTile, q.qt, p.window, p.sinks);
-  const int cost = q.it.tl.n + kItemCost, end = min(cost, w.off + w.left);
-  q.u0 = max(0, w.off - kItemCost);
-  q.u1 = max(0, end - kItemCost);
-  q.cont = w.off > 0;
-  q.whole = w.off == 0 && end == cost;
-  w.left -= end - w.off;
-  w.off = 0;
-  if (++w.pair == p.B * p.nqt) { w.pair = 0; ++w.g; }
-  return true;
-}
-
 template <int D, int NQ>
 __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant__ AttendParams p) {
   using C = TcCfg2<D, NQ>;
@@ -121,7 +91,7 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
   uint64_t* q_full = s_full + 8;                                     // [2] queries loaded (128; NQ = 1: [0], 256)
   uint64_t* done = s_full + 10;                                      // every tensor-core operation complete
   volatile uint32_t* bad_ring = reinterpret_cast<uint32_t*>(smem + C::OFF_BAD);
-  int* misc = reinterpret_cast<int*>(smem + C::OFF_MISC);            // [0..9] scan; [10..12] start; [15] TMEM
+  int* misc = reinterpret_cast<int*>(smem + C::OFF_MISC);            // [0..11] line_start; [12, 13] flags; [15] TMEM
 
   if (tid == 0) {
     for (int i = 0; i < S; ++i) {
@@ -147,51 +117,10 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
   }
   pdl_wait();
   pdl_trigger();
-  // ---- the line of work: each thread sums a run of (sequence, row block) pairs
-  const int pairs = p.B * p.nqt, run = (pairs + kAttThreads - 1) / kAttThreads;
-  auto pair_cost = [&](int i) {
-    const int b = i / p.nqt;
-    const NewSeq sq = load_new(p, b, blockIdx.x == 0 && i % p.nqt == 0);
-    return att_item(sq.len, sq.n, p.G, NQ * kTcTile, i % p.nqt, p.window, p.sinks).tl.n + kItemCost;
-  };
-  int mine = 0;
-  for (int i = tid * run; i < min(pairs, (tid + 1) * run); ++i) mine += pair_cost(i);
-  int incl = mine;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int y = __shfl_up_sync(0xffffffffu, incl, o);
-    if (lane >= o) incl += y;
-  }
-  if (lane == 31) misc[warp] = incl;
+  LineCut lc;
   tc_fence_before();
-  __syncthreads();
+  Walk walk = line_start<kAttThreads>(p, misc, lc);  // passes the CTA-wide barrier
   tc_fence_after();
-  int before = incl - mine, total = 0;
-#pragma unroll
-  for (int w = 0; w < kAttThreads / 32; ++w) {
-    if (w < warp) before += misc[w];
-    total += misc[w];
-  }
-  const int64_t W = (int64_t)total * p.Hkv;
-  const int nc = W < (int64_t)gridDim.x ? (int)W : (int)gridDim.x;
-  const bool idle = (int)blockIdx.x >= nc;
-  const int64_t x0 = idle ? 0 : cut(W, nc, blockIdx.x), x1 = idle ? 0 : cut(W, nc, blockIdx.x + 1);
-  const int g0 = (int)(x0 / total), at = (int)(x0 - (int64_t)g0 * total);
-  if (blockIdx.x == 0 && tid == 0) p.prefix[pairs] = total;
-  if (blockIdx.x == 0 || (at >= before && at < before + mine)) {
-    int sum = before;
-    for (int i = tid * run; i < min(pairs, (tid + 1) * run); ++i) {
-      const int cost = pair_cost(i);
-      if (blockIdx.x == 0) p.prefix[i] = sum;
-      if (at >= sum && at < sum + cost) {
-        misc[10] = i;
-        misc[11] = at - sum;
-      }
-      sum += cost;
-    }
-  }
-  __syncthreads();
-  Walk walk{g0, misc[10], misc[11], (int)(x1 - x0)};
   Part q;
   const unsigned tmem = (unsigned)misc[15];  // columns [0, 128), [128, 256): S / P; from 256: O of the groups
   const int R2 = p.paged ? min(kTcTile, p.page_size) : kTcTile;  // rows per copied box
@@ -206,7 +135,6 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
     // copies half hh of box x.
     const int x = lane / C::HALVES, hh = lane % C::HALVES;
     int pc = 0, tiles = 0;
-    const bool once = p.stream_once;
     auto lookup = [&](const Part& q, int u, int& kp, int& vp) {  // pages of this lane's box of tile u; -2: not needed
       kp = vp = -2;
       if (x >= nb) return;
@@ -234,13 +162,13 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
         const int row = p.paged ? j & (p.page_size - 1) : j;
         auto crd = [&](int axis) { return axis == p.tpos ? row : axis == p.gpos ? q.g : page; };
         const unsigned dst = smem_u32(smem + sl * C::SLOT) + hh * C::HALF + x * R2 * 128;
-        if (once) tma_load_4d(dst, map, 64 * hh, crd(1), crd(2), crd(3), full + sl);
+        if (NQ == 1) tma_load_4d(dst, map, 64 * hh, crd(1), crd(2), crd(3), full + sl);
         else tma_load_4d_keep(dst, map, 64 * hh, crd(1), crd(2), crd(3), full + sl);
       }
       ++pc;
       return true;
     };
-    while (!timed_out && next_part<NQ>(p, walk, q)) {
+    while (!timed_out && next_part(p, walk, q)) {
       const int n = q.u1 - q.u0;
       int kp = -2, vp = -2, kn, vn;   // pages of tile i, looked up one tile ahead
       int vq[LA];                     // V pages of the tiles whose V is due
@@ -276,7 +204,8 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
       tc_fence_after();
       return ok;
     };
-    int pc = 0, parts = 0, np[2] = {0, 0}, no[2] = {0, 0};  // pieces, parts with tiles; per group: P read, parts with tiles
+    int pc = 0, parts = 0, parts2 = 0;         // pieces; parts with tiles, of them with rows of the second group
+    int np[2] = {0, 0}, no[2] = {0, 0};        // per group: P read, parts with tiles
     auto qk = [&](int s, int sl) {
       if (lane == 0) {
         const unsigned kb = smem_u32(smem + sl * C::SLOT), qb = smem_u32(smem + C::OFF_Q + (NQ == 1 ? 0 : s) * C::SLOT);
@@ -311,12 +240,13 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
       if (lane == 0) umma_commit(empty + sl);
       __syncwarp();
     };
-    while (!timed_out && next_part<NQ>(p, walk, q)) {
+    while (!timed_out && next_part(p, walk, q)) {
       const int n = q.u1 - q.u0;
       if (n <= 0) continue;
       const bool two = NQ == 2 && q.it.rows > kTcTile;  // the second group has rows
-      if (!wait_all(q_full, parts & 1) || (NQ == 2 && !wait_all(q_full + 1, parts & 1))) { timed_out = true; break; }
+      if (!wait_all(q_full, parts & 1) || (two && !wait_all(q_full + 1, parts2 & 1))) { timed_out = true; break; }
       ++parts;
+      parts2 += two;
       for (int i = 0; i < n + LA; ++i) {
         int vs = 0, ks = 0;
         if (i >= LA) {
@@ -361,17 +291,20 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
       tc_fence_after();
       return !dead;
     };
-    while (next_part<NQ>(p, walk, q)) {
+    while (next_part(p, walk, q)) {
       const int n = q.u1 - q.u0;
       const SeenRange sr = q.it.sr;
-      const int row = q.it.row0 + (NQ == 2 ? s * kTcTile : 0) + r;  // query row of the kv-head
+      const int row_s = q.it.row0 + (NQ == 2 ? s * kTcTile : 0), row = row_s + r;  // query row of the kv-head
       const bool valid = row < q.it.row0 + q.it.rows;
       const bool rows_here = __any_sync(0xffffffffu, valid);
       const int t = valid ? q.sq.len - q.sq.n + row / p.G : -1;      // its position
       const int low = p.window < 0 ? -1 : t - p.window;              // the window sees j > low
       float m = -CUDART_INF_F, l = 0.f;
       bool have = false;  // O holds something
-      if (n > 0) {
+      // A group without rows takes no part: it must not arrive at q_full, whose
+      // phases nobody would wait for.
+      const bool group = NQ == 1 || s == 0 || q.it.rows > kTcTile;
+      if (n > 0 && group) {
         // Queries: in the one-row-block form both groups load half of the rows,
         // once neither reads the last part's S any more (its products with
         // the old queries are then complete).
@@ -389,7 +322,6 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
         fence_proxy_async();  // read by the tensor core
         mbar_arrive(q_full + (NQ == 1 ? 0 : s));
       }
-      const bool group = NQ == 1 || s == 0 || q.it.rows > kTcTile;  // this group takes part
       for (int i = NQ == 1 ? s : 0; i < n && group; i += NQ == 1 ? 2 : 1) {
         const int j0 = q.it.tl.tile(q.u0 + i) * kTcTile;
         wait(s_full + s, ns & 1);
@@ -484,26 +416,29 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
       }
       pc += 2 * max(0, n);
       tiles += max(0, n);
-      // ---- the part's result
-      const bool whole = NQ == 2 && q.whole;
+      // ---- rows that see nothing: padding, or all of an item without tiles
+      if (q.owner && (NQ == 2 || s == 0) && row < min(p.R, q.it.row0 + p.block) && (!valid || q.it.tl.n == 0)) {
+        uint4* o = reinterpret_cast<uint4*>(out_row<__nv_bfloat16>(p, q.b, q.g, row));
+#pragma unroll
+        for (int k = 0; k < D / 8; ++k) o[k] = make_uint4(0u, 0u, 0u, 0u);
+        store_lse(p, q.b, q.g, row, 0.f, 0.f);
+      }
+      if (n <= 0 || !group) continue;
+      // ---- the others' output, or this CTA's record of it
+      const bool direct = NQ == 2 && q.whole();
+      const int c0 = lc.owner(q.first);
+      auto rec_of = [&](int c, int grp) { return (2 * c + (c == c0 ? 1 : 0)) * 2 + grp; };
       if (have) wait(pv_done + s, (ns - 1) & 1);
-      if (!valid) l = 0.f;
-      if (rows_here || (whole && q.it.row0 + s * kTcTile < p.R)) {
+      if (rows_here) {
         float* po = nullptr;
         __nv_bfloat16* out = nullptr;
-        if (whole) {
-          if (row < p.R) {
-            const int i = row / p.G, h = q.g * p.G + row % p.G;
-            out = static_cast<__nv_bfloat16*>(p.out.data) + (int64_t)q.b * p.out.sb + (int64_t)i * p.out.sn +
-                  (int64_t)h * p.out.sh;
-            if (p.lse) p.lse[((int64_t)q.b * p.n_new + i) * p.H + h] = l > 0.f ? (m + log2f(l)) * kLn2 : -CUDART_INF_F;
-          }
-        } else if (have && valid) {
-          const int64_t rec = NQ == 1
-              ? ((int64_t)(q.g * pairs + q.pair + (int)blockIdx.x) * 2 + s) * p.R + row
-              : (int64_t)(2 * blockIdx.x + (q.cont ? 0 : 1)) * 2 * kTcTile + s * kTcTile + r;
-          *reinterpret_cast<float2*>(p.part_st + 2 * rec) = make_float2(m, l);
-          po = p.part_o + rec * D;
+        if (valid && direct) {
+          out = out_row<__nv_bfloat16>(p, q.b, q.g, row);
+          store_lse(p, q.b, q.g, row, m, l);
+        } else if (valid) {
+          const int64_t at = (int64_t)rec_of(blockIdx.x, s) * kTcTile + r;
+          *reinterpret_cast<float2*>(p.part_st + 2 * at) = make_float2(m, l);
+          po = p.part_o + at * D;
         }
         const float inv = l > 0.f ? 1.f / l : 0.f;
 #pragma unroll
@@ -512,10 +447,6 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
           if (have && !dead) {
             tmem_ld(oaddr + k, o);
           } else {
-#pragma unroll
-            for (int x = 0; x < 32; ++x) o[x] = 0.f;
-          }
-          if (l == 0.f) {  // nothing seen: O may hold anything
 #pragma unroll
             for (int x = 0; x < 32; ++x) o[x] = 0.f;
           }
@@ -540,6 +471,18 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
       if (have) {
         tc_fence_before();
         mbar_arrive(o_free + s);
+      }
+      if (direct) continue;
+      // NQ = 1: the records of both groups of every CTA; NQ = 2: this group's rows.
+      const int parts = lc.owner(q.first + q.it.tl.n - 1) - c0 + 1;
+      auto sync = [&] { asm volatile("barrier.cta.sync %0, 128;\n" ::"r"(2 + s) : "memory"); };
+      if (last_to_arrive(p.tickets + 2 * c0 + (NQ == 2 ? s : 0), NQ == 1 ? 2 * parts : parts, r, misc + 12 + s, sync)) {
+        if (NQ == 1)
+          join_records<__nv_bfloat16, D, 128>(p, q.b, q.g, 0, q.it.rows, 2 * parts, kTcTile,
+                                              [&](int k) { return rec_of(c0 + (k >> 1), k & 1); }, r);
+        else
+          join_records<__nv_bfloat16, D, 128>(p, q.b, q.g, row_s, min(kTcTile, q.it.rows - s * kTcTile), parts, kTcTile,
+                                              [&](int k) { return rec_of(c0 + k, s); }, r);
       }
     }
     if (dead) timed_out = true;

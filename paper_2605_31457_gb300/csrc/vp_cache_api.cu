@@ -73,6 +73,11 @@ vp_status reserve_new(vp_ctx* ctx, int32_t max_new, int32_t max_weight_new) {
                                            max_weight_new, ctx->num_sms);
   e = vp::configure_attend();
   if (e == cudaSuccess) e = cudaMalloc(&ctx->new_ws, lay.total);
+  if (e == cudaSuccess) {
+    e = cudaMemset(static_cast<char*>(ctx->new_ws) + lay.o_tk, 0, lay.o_lse - lay.o_tk);
+    if (e == cudaSuccess) e = cudaDeviceSynchronize();
+    if (e != cudaSuccess) cudaFree(ctx->new_ws);
+  }
   if (e != cudaSuccess) {
     ctx->new_ws = nullptr;
     cudaGetLastError();
@@ -135,7 +140,8 @@ vp_status attend_new(vp_ctx* ctx, int32_t batch, int32_t n_new, const vp_rows* q
   p.z_row = ctx->new_lay.z_row;
   p.err = ctx->err;
   p.num_sms = ctx->num_sms;
-  p.prefix = reinterpret_cast<int*>(ws + ctx->new_lay.o_pre);
+  p.tickets = reinterpret_cast<unsigned*>(ws + ctx->new_lay.o_tk);
+  p.lse2 = reinterpret_cast<float*>(ws + ctx->new_lay.o_lse);
   vp::plan_attend(p);
   const cudaError_t e = vp::launch_attend(p, static_cast<cudaStream_t>(cuda_stream));
   if (e != cudaSuccess) return cuda_fail(ctx, "vp_attend_new: launch", e);

@@ -544,3 +544,21 @@ def test_null_contexts(lib):
     assert lib.lib.vp_attend_new(None, 1, 1, *([None] * 11)) == lib.VP_ERR_NOT_INITIALIZED
     assert lib.lib.vp_evict(None, 1, *([None] * 9), 0, None, None) == lib.VP_ERR_NOT_INITIALIZED
     assert ctypes.sizeof(lib.vp_visible) == 12 and ctypes.sizeof(lib.vp_rows) == 32
+
+
+def test_prompt_blocks_with_few_rows_in_a_row(lib):
+    """Many short prompts whose last row block is small, several per CTA, over
+    and over: every call must give the first call's bits."""
+    n, B = 45, 40
+    lens = tuple(n + 13 * i for i in range(B))
+    c = Case(lib, (28, 4), 128, "bf16", lens=lens, n_new=n, seed=17)
+    c.call()
+    torch.cuda.synchronize()
+    c.check()
+    first = c.out.clone()
+    for _ in range(30):
+        c.out.fill_(float("nan"))
+        c.call()
+        assert torch.equal(c.out.view(torch.int16), first.view(torch.int16))
+    lib.vp_check_errors(c.ctx)
+    lib.vp_free(c.ctx)
