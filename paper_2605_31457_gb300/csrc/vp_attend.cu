@@ -285,6 +285,7 @@ void plan_attend(AttendParams& p) {
   p.kind = p.R <= kDecRows ? ATT_DEC : p.R <= kTcTile ? ATT_TC1 : ATT_TC2;
   p.block = p.kind == ATT_TC2 ? 2 * kTcTile : p.R;
   p.nqt = (p.R + p.block - 1) / p.block;
+  p.fixed = (p.kind == ATT_DEC ? 1 : 2) * kTileUnits;
   p.grid = p.kind == ATT_DEC && p.R <= kDecRows / 2 ? 2 * p.num_sms : p.num_sms;
 }
 

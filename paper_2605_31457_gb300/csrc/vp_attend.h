@@ -48,9 +48,11 @@ struct AttendParams {
   int tpos, gpos, bpos;       // descriptor dimensions of the token, kv-head and sequence / page axes
   int kind;                   // ATT_*
   int block, nqt;             // tensor-core kernels: query rows of an item, items per (sequence, kv-head)
+  int fixed;                  // the fixed part of an item's cost, in units
   int dtype, B, H, Hkv, G, D, max_seq;
   int paged, page_size, page_shift;
-  int n_new, R;               // R = n_new * G query rows per (sequence, kv-head)
+  int n_new, R;               // R = n_new * G query rows per (sequence, kv-head), below 2^28
+  uint32_t g_mul;             // floor(2^32 / G) + 1: row / G is its high product with the row; 0: G = 1
   RowView q, out;
   KvView k, v;
   const int32_t* seq_len;
@@ -115,37 +117,64 @@ __host__ __device__ inline bool sees(int j, int t, int window, int sinks) {
   return j <= t && (window < 0 || j > t - window || j < sinks);
 }
 
-// ---- The work of the tensor-core kernels.  The cost of an item is the tiles
-// it sees plus a fixed part for loading its queries and writing its result.
+// ---- The work of the tensor-core kernels.  The cost of an item is its tiles'
+// plus a fixed part for loading its queries and writing its result, in units:
+// measured, a tile of k_att_tc with P split in two terms takes 1.5 times one
+// without, an item's fixed part about as long as two tiles.
 // Items follow one another kv-head by kv-head, sequence by sequence, and the
 // line of their costs is cut into equal parts, one per CTA: a CTA owns tiles,
 // not items, so ragged lengths leave no CTA idle.  An item whose tiles lie with
 // several CTAs leaves a record (m, l, O) per CTA (and group); the last CTA to
 // finish joins them.
-constexpr int kItemCost = 1;
+constexpr int kTileUnits = 2, kSplitUnits = 3;
+
+// An item's P is split into two bf16 terms, hi + lo, unless it is one of many
+// rows each of which sees at least kSplitSeen tokens.  P's rounding to one term,
+// up to 2^-8 of each probability, shows in the output beside the output's own
+// where few tokens share the weight; over longer ranges it averages out, and the
+// second P.V product would cost a third of the tensor cores' time.
+constexpr int kSplitSeen = 2048;
+
 struct AttItem {
   int row0, rows;  // query rows [row0, row0 + rows)
+  int split;       // P in two terms
   SeenRange sr;
   TileList tl;
+  __host__ __device__ int unit() const { return split ? kSplitUnits : kTileUnits; }
+  __host__ __device__ int cost(int fixed) const { return fixed + tl.n * unit(); }
+  // Tiles that start in front of position x of the item.
+  __host__ __device__ int tiles_before(int x, int fixed) const {
+    const int u = (x - fixed + unit() - 1) / unit();
+    return x <= fixed ? 0 : u < tl.n ? u : tl.n;
+  }
 };
 __host__ __device__ inline AttItem att_item(int len, int n, int G, int block, int qt, int window, int sinks) {
   AttItem it;
   it.row0 = qt * block;
   const int left = n * G - it.row0;
   it.rows = left < 0 ? 0 : left < block ? left : block;
+  it.split = 1;
   it.sr = SeenRange{0, 0, 0};
-  if (it.rows > 0)
-    it.sr = seen_range(len - n + it.row0 / G, len - n + (it.row0 + it.rows - 1) / G, window, sinks);
+  if (it.rows > 0) {
+    const int t = len - n + it.row0 / G;
+    it.sr = seen_range(t, len - n + (it.row0 + it.rows - 1) / G, window, sinks);
+    const int in = window < 0 || window > t ? t + 1 : window;
+    const int seen = in + (sinks < t + 1 - in ? sinks : t + 1 - in);
+    it.split = block <= kTcTile || seen < kSplitSeen;
+  }
   it.tl = tile_list(it.sr, kTcTile);
   return it;
 }
 // A line of `total` positions cut for at most `ctas` CTAs: CTA c owns
-// [start(c), start(c + 1)); the first `extra` of them own one position more.
+// [start(c), start(c + 1)); the first `extra` of them own one position more.  A
+// CTA does the tiles that start in its part, which is at least a tile long, so
+// that every CTA between those of an item's first and last tile has one of them.
 struct LineCut {
   int nc, per, extra;
   __host__ __device__ LineCut() {}
   __host__ __device__ LineCut(int64_t total, int ctas) {
-    nc = total < ctas ? (int)total : ctas;
+    const int64_t most = total > kSplitUnits ? total / kSplitUnits : 1;
+    nc = most < ctas ? (int)most : ctas;
     per = (int)(total / nc);
     extra = (int)(total - (int64_t)per * nc);
   }

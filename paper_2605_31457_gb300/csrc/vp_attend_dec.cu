@@ -461,7 +461,7 @@ __global__ void __launch_bounds__(kDecThreads, DecCfg<D, GM>::CPS) k_att_dec(con
         }
       }
       if (direct) continue;
-      const int parts = lc.owner(q.first + q.it.tl.n - 1) - c0 + 1;
+      const int parts = lc.owner(q.last) - c0 + 1;
       if (last_to_arrive(p.tickets + c0, parts, st, misc + 8, sync))
         join_records<__nv_bfloat16, D, 128>(p, q.b, q.g, 0, rows, parts, GM, [&](int k) { return rec_of(c0 + k); }, st);
     }

@@ -29,6 +29,10 @@ __device__ __forceinline__ NewSeq load_new(const AttendParams& p, int b, bool re
   return s;
 }
 
+// The new token of a query row, row / G, by a multiplication (rows < 2^28).
+__device__ __forceinline__ int row_token(const AttendParams& p, int row) {
+  return p.g_mul ? (int)__umulhi((unsigned)row, p.g_mul) : row;
+}
 // Output row (new token row / G, query head g * G + row % G) of sequence b.
 template <typename T>
 __device__ __forceinline__ T* out_row(const AttendParams& p, int b, int g, int row) {
@@ -55,7 +59,8 @@ struct Walk {
 struct Part {
   int g, b, u0, u1;
   bool owner;       // this CTA holds the item's first position: it answers for an item without tiles
-  int64_t first;    // the item's first tile on the line
+  int64_t first;    // the item's first tile on the line, and its last
+  int64_t last;
   NewSeq sq;
   AttItem it;
   __device__ bool whole() const { return u0 == 0 && u1 == it.tl.n; }
@@ -66,11 +71,12 @@ __device__ __forceinline__ bool next_part(const AttendParams& p, Walk& w, Part& 
   q.b = w.pair / p.nqt;
   q.sq = load_new(p, q.b, false);
   q.it = att_item(q.sq.len, q.sq.n, p.G, p.block, w.pair - q.b * p.nqt, p.window, p.sinks);
-  const int cost = q.it.tl.n + kItemCost, end = min(cost, w.off + w.left), done = end - w.off;
-  q.u0 = max(0, w.off - kItemCost);
-  q.u1 = max(0, end - kItemCost);
+  const int cost = q.it.cost(p.fixed), end = min(cost, w.off + w.left), done = end - w.off;
+  q.u0 = q.it.tiles_before(w.off, p.fixed);
+  q.u1 = q.it.tiles_before(end, p.fixed);
   q.owner = w.off == 0;
-  q.first = w.pos - w.off + kItemCost;
+  q.first = w.pos - w.off + p.fixed;
+  q.last = q.first + (int64_t)(q.it.tl.n - 1) * q.it.unit();
   w.left -= done;
   w.pos += done;
   w.off = 0;
@@ -87,7 +93,7 @@ __device__ __forceinline__ Walk line_start(const AttendParams& p, int* misc, Lin
   auto pair_cost = [&](int i, bool report) {
     const int b = i / p.nqt;
     const NewSeq sq = load_new(p, b, report && blockIdx.x == 0 && i == b * p.nqt);
-    return att_item(sq.len, sq.n, p.G, p.block, i - b * p.nqt, p.window, p.sinks).tl.n + kItemCost;
+    return att_item(sq.len, sq.n, p.G, p.block, i - b * p.nqt, p.window, p.sinks).cost(p.fixed);
   };
   int mine = 0;
   for (int i = i0; i < i1; ++i) mine += pair_cost(i, true);

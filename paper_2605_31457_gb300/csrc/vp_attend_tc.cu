@@ -13,13 +13,14 @@ namespace vp {
 namespace {
 
 // ---------------------------------------------------------------------------
-// k_att_tc<D, NQ>: one CTA per SM, 320 threads in four roles.
+// k_att_tc<D, NQ>: one CTA per SM, 352 threads in four roles.
 //   warps 0-3, 4-7  two softmax groups, a thread per query row;
 //   warp 8          copies tiles of 128 K or V rows into a ring (4-D bulk-tensor
 //                   copies, 128-byte swizzle);
-//   warp 9          one lane issues tcgen05.mma: S = Q K^T (M = 128 query rows,
-//                   N = 128 tokens, K = D) and O += P V (M = 128, N = D, K =
-//                   128 tokens) with P in TMEM.
+//   warps 9, 10     one lane each issues tcgen05.mma for one of the groups: S =
+//                   Q K^T (M = 128 query rows, N = 128 tokens, K = D) and, half
+//                   a tile at a time, O += P V (M = 128, N = D, K = 64) with P
+//                   in TMEM.
 // Query rows are the (new token, head of the kv-head) pairs, so a group of G
 // heads shares every K and V row that is copied.  Each softmax group has its
 // own S and O in TMEM (4 x 128 columns = all 512 at D = 128); P, rounded to
@@ -35,10 +36,12 @@ namespace {
 // The work is a line of tiles cut evenly over the CTAs (vp_attend.h): an item
 // cut between CTAs leaves partials (m, l, O) that k_att_join merges.
 //
-// Softmax: a row's reference maximum is raised only when a logit passes it by
-// more than 8 (log2 units), when O is rescaled in TMEM; P then stays below 2^8
-// and the sums, in 32 bits, mean the same.  P is rounded to bf16 for the tensor
-// cores (the caches are bf16 themselves); l sums the unrounded values.
+// Softmax: a row's reference m is the largest logit of the first 32 tokens it
+// sees, and is raised only when a logit passes it by more than 64 (log2 units),
+// when O is rescaled in TMEM: P = exp2(z - m) <= 2^64 has bf16's and float's
+// full precision all the same, and no pass over S for a maximum is needed.  P goes to the tensor cores as bf16,
+// in two terms hi + lo where few tokens share the weight (AttItem::split); l sums the
+// unrounded values.
 //
 // Rows of a tile that nobody sees may hold anything: their logits are masked,
 // and their V rows are zeroed in shared memory before the product (0 x NaN is
@@ -47,7 +50,9 @@ namespace {
 // Waits are bounded: a role whose wait gives up stops working, still meets
 // every barrier of its group, and the error word reports it.
 // ---------------------------------------------------------------------------
-constexpr int kAttThreads = 320;
+constexpr int kAttThreads = 352;
+constexpr int kSub = 64;       // tokens of a softmax step: half a tile
+constexpr float kRaise = 64.f;
 constexpr int kMaskRing = 16;  // tiles between the copy warp and the softmax groups, at most
 
 template <int D, int NQ>
@@ -59,10 +64,10 @@ struct TcCfg2 {
   static constexpr int LA = NQ == 1 ? 2 : 1;            // tiles whose S is ahead of the P.V product
   static constexpr int OFF_Q = S * SLOT;
   static constexpr int OFF_BAR = OFF_Q + NQ * SLOT;
-  static constexpr int NBAR = 2 * S + 11;               // full, empty, s_full, p_full, pv_done, o_free, q_full, done
+  static constexpr int NBAR = 2 * S + 16;               // full, empty, s_full, p_full, pv_done, o_free, q_full, done
   static constexpr int OFF_BAD = OFF_BAR + NBAR * 8;    // unmapped boxes of a tile, one bit each
   static constexpr int OFF_MISC = OFF_BAD + kMaskRing * 4;  // int [16]: scan, start, TMEM base
-  static constexpr size_t SMEM = 1024 + (size_t)OFF_MISC + 16 * 4;
+  static constexpr size_t SMEM = 1024 + (size_t)OFF_MISC + 20 * 4;
   static_assert(SMEM <= 232448, "227 KB of shared memory");
   static_assert(S >= 2 * LA, "the K tiles ahead and a V tile fit the ring");
 };
@@ -74,38 +79,57 @@ __host__ __device__ constexpr uint32_t att_idesc(int n, int b_mn) {
          ((uint32_t)(128 >> 4) << 24);
 }
 
+// The first n of 32 bits.
+__device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
+// Which of the 32 tokens from jb on (columns k .. k + 31 of their tile) a row at
+// position t sees whose window begins after `low`; bad: the tile's unmapped boxes
+// of `box` rows.
+__device__ __forceinline__ uint32_t seen_bits(int jb, int t, int low, int sinks, uint32_t bad, int k, int box) {
+  uint32_t see = low_bits(t + 1 - jb) & (~low_bits(low + 1 - jb) | low_bits(sinks - jb));
+  if (bad)
+    for (int x = 0; x < 32; ++x)
+      if ((bad >> ((k + x) / box)) & 1u) see &= ~(1u << x);
+  return see;
+}
+// The 32 tokens' logits that `see` lacks become -infinity.
+__device__ __forceinline__ void mask_cols(float (&x)[32], uint32_t see) {
+#pragma unroll
+  for (int i = 0; i < 32; ++i) x[i] = (see >> i) & 1u ? x[i] : -CUDART_INF_F;
+}
 template <int D, int NQ>
 __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant__ AttendParams p) {
   using C = TcCfg2<D, NQ>;
   constexpr int S = C::S, LA = C::LA;
-  constexpr uint32_t kIdQK = att_idesc(128, 0), kIdPV = att_idesc(D, 1);
+  constexpr uint32_t kIdQK = att_idesc(kTcTile, 0), kIdPV = att_idesc(D, 1);
   extern __shared__ __align__(16) unsigned char smem_raw[];
   unsigned char* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + C::OFF_BAR);  // [S] a slot's copies landed
   uint64_t* empty = full + S;                                        // [S] a slot's tile was read
   uint64_t* s_full = full + 2 * S;                                   // [2] S of a group written
-  uint64_t* p_full = s_full + 2;                                     // [2] P written (128 arrivals)
-  uint64_t* pv_done = s_full + 4;                                    // [2] P.V complete
-  uint64_t* o_free = s_full + 6;                                     // [2] O of the last part read (128)
-  uint64_t* q_full = s_full + 8;                                     // [2] queries loaded (128; NQ = 1: [0], 256)
-  uint64_t* done = s_full + 10;                                      // every tensor-core operation complete
+  uint64_t* p_full = s_full + 2;                                     // [2][2] half a tile's P of a group written (an arrival per warp)
+  uint64_t* pv_done = s_full + 6;                                    // [2][2] P.V of that half complete
+  uint64_t* o_free = s_full + 10;                                    // [2] O of the last part read (128)
+  uint64_t* q_full = s_full + 12;                                    // [2] a group's queries loaded (128; NQ = 1: 256)
+  uint64_t* done = s_full + 14;                                      // [2] every product of a group complete
   volatile uint32_t* bad_ring = reinterpret_cast<uint32_t*>(smem + C::OFF_BAD);
-  int* misc = reinterpret_cast<int*>(smem + C::OFF_MISC);            // [0..11] line_start; [12, 13] flags; [15] TMEM
+  int* misc = reinterpret_cast<int*>(smem + C::OFF_MISC);            // [0, 13) line_start; [13, 14] flags; [15] TMEM
 
   if (tid == 0) {
     for (int i = 0; i < S; ++i) {
       mbar_init(full + i, 1);
-      mbar_init(empty + i, 1);
+      mbar_init(empty + i, 2);
+    }
+    for (int i = 0; i < 4; ++i) {
+      mbar_init(p_full + i, 4);
+      mbar_init(pv_done + i, 1);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(s_full + i, 1);
-      mbar_init(p_full + i, 128);
-      mbar_init(pv_done + i, 1);
       mbar_init(o_free + i, 128);
       mbar_init(q_full + i, NQ == 1 ? 256 : 128);
+      mbar_init(done + i, 1);
     }
-    mbar_init(done, 1);
     mbar_fence_init();
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&p.tmk)) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&p.tmv)) : "memory");
@@ -197,95 +221,132 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
     // Copies still in flight (only after a timeout can any be unread) land
     // before the CTA's shared memory is released.
     for (int k = max(0, pc - S); k < pc; ++k) mbar_wait(full + k % S, (k / S) & 1);
-  } else if (warp == 9) {
-    // -------------------------------------------------------- tensor cores
+  } else if (warp >= 9) {
+    // ------------------------------- tensor cores, a warp for each group s
+    // P.V takes half a tile at a time, so that the first half's runs while the
+    // softmax threads turn the second half of S into P.  One warp for both
+    // groups spent more time waiting at barriers than the products took.
     auto wait_all = [&](uint64_t* bar, unsigned parity) {
       const bool ok = __all_sync(0xffffffffu, mbar_wait(bar, parity));
       tc_fence_after();
       return ok;
     };
-    int pc = 0, parts = 0, parts2 = 0;         // pieces; parts with tiles, of them with rows of the second group
-    int np[2] = {0, 0}, no[2] = {0, 0};        // per group: P read, parts with tiles
-    auto qk = [&](int s, int sl) {
-      if (lane == 0) {
-        const unsigned kb = smem_u32(smem + sl * C::SLOT), qb = smem_u32(smem + C::OFF_Q + (NQ == 1 ? 0 : s) * C::SLOT);
-#pragma unroll
-        for (int ks = 0; ks < D / 16; ++ks)
-          umma(tmem + 128 * s, umma_desc(qb + (ks >> 2) * C::HALF + (ks & 3) * 32, 16, 1024),
-               umma_desc(kb + (ks >> 2) * C::HALF + (ks & 3) * 32, 16, 1024), kIdQK, ks > 0);
-        umma_commit(s_full + s);
-      }
-      __syncwarp();
-    };
-    auto pv = [&](int s, int sl, bool first) {
-      if (first && !wait_all(o_free + s, (no[s] & 1) ^ 1)) return false;
-      if (first) ++no[s];
-      if (!wait_all(p_full + s, np[s] & 1)) return false;
-      ++np[s];
-      if (lane == 0) {
-        const unsigned vb = smem_u32(smem + sl * C::SLOT);
-#pragma unroll
-        for (int ks = 0; ks < kTcTile / 16; ++ks)
-          umma_ts(tmem + 256 + D * s, tmem + 128 * s + 8 * ks, umma_desc(vb + ks * 2048, C::HALF, 1024), kIdPV,
-                  !first || ks > 0);
-#pragma unroll
-        for (int ks = 0; ks < kTcTile / 16; ++ks)
-          umma_ts(tmem + 256 + D * s, tmem + 128 * s + 64 + 8 * ks, umma_desc(vb + ks * 2048, C::HALF, 1024), kIdPV, true);
-        umma_commit(pv_done + s);
-      }
-      __syncwarp();
-      return true;
-    };
-    auto release = [&](int sl) {
-      if (lane == 0) umma_commit(empty + sl);
-      __syncwarp();
-    };
+    const int leader = elect_one();
+    // Warp-wide reductions leave these in uniform registers, which the
+    // products' operands must be in.
+    const unsigned tm = __reduce_max_sync(0xffffffffu, tmem);
+    const int s = __reduce_max_sync(0xffffffffu, warp - 9);
+    int pc = 0, tiles = 0;                     // pieces and tiles of the parts before
+    unsigned parts = 0, tp = 0;                // parts with tiles of this group, its tiles before
     while (!timed_out && next_part(p, walk, q)) {
-      const int n = q.u1 - q.u0;
+      const int n = __reduce_max_sync(0xffffffffu, q.u1 - q.u0);
       if (n <= 0) continue;
-      const bool two = NQ == 2 && q.it.rows > kTcTile;  // the second group has rows
-      if (!wait_all(q_full, parts & 1) || (two && !wait_all(q_full + 1, parts2 & 1))) { timed_out = true; break; }
-      ++parts;
-      parts2 += two;
-      for (int i = 0; i < n + LA; ++i) {
-        int vs = 0, ks = 0;
-        if (i >= LA) {
-          vs = pc % S;
-          if (!wait_all(full + vs, (pc / S) & 1)) { timed_out = true; break; }
-          ++pc;
-          const int j = i - LA;
-          if (!pv(NQ == 1 ? j & 1 : 0, vs, NQ == 1 ? j < 2 : j == 0)) { timed_out = true; break; }
-          if (!two) release(vs);
-        }
-        if (i < n) {
-          ks = pc % S;
-          if (!wait_all(full + ks, (pc / S) & 1)) { timed_out = true; break; }
-          ++pc;
-          qk(NQ == 1 ? i & 1 : 0, ks);
-          if (!two) release(ks);
-        }
-        if (two) {
-          if (i >= LA) {
-            if (!pv(1, vs, i == LA)) { timed_out = true; break; }
-            release(vs);
-          }
-          if (i < n) {
-            qk(1, ks);
-            release(ks);
-          }
-        }
+      const int two = __reduce_max_sync(0xffffffffu, NQ == 2 && q.it.rows > kTcTile);  // the second group has rows
+      const int split = __reduce_max_sync(0xffffffffu, q.it.split);
+      const int mine = NQ == 2 ? (s == 0 || two ? n : 0) : (n + 1 - s) / 2;  // tiles of this group
+      if (mine > 0) {
+        if (!wait_all(q_full + s, parts & 1)) { timed_out = true; break; }
+        ++parts;
       }
+      // Every piece of the ring is waited for, in order, and released by both
+      // warps, the group's own or not: a warp that left some out could take a
+      // later phase of a slot's barrier for the one it waits for.
+      int at = pc;
+      auto pass = [&](int to) {
+        for (; at < to && !timed_out; ++at) {
+          if (!wait_all(full + at % S, (at / S) & 1)) timed_out = true;
+          else umma_commit_on(leader, empty + at % S);
+        }
+      };
+      // P.V of the group's tile k (the part's tile `tile`), then QK of the next;
+      // a tile's K and V among the pieces in the copy warp's order.  What has
+      // landed is waited for before P is, so that nothing but products stands
+      // between a group's P and its next S.
+#pragma unroll 1
+      for (int k = -1; k < mine && !timed_out; ++k) {
+        const int tile = NQ == 1 ? 2 * k + s : k, next = NQ == 1 ? tile + 2 : tile + 1;
+        const unsigned o = tm + 256 + D * s, pa = tm + 128 * s;
+        const bool more = k + 1 < mine;
+        int vs = 0, ks = 0;
+        if (k >= 0) {
+          const int piece = pc + min(tile + LA, n) + tile;
+          vs = piece % S;
+          pass(piece);
+          if (timed_out || !wait_all(full + vs, (piece / S) & 1)) { timed_out = true; break; }
+          ++at;
+          // V rows that no row of the item sees, or of unmapped pages: zero them
+          // before the product reads them (both warps, where both do).
+          const int j0 = q.it.tl.tile(q.u0 + tile) * kTcTile;
+          const uint32_t bad = bad_ring[(tiles + tile) % kMaskRing];
+          const SeenRange& sr = q.it.sr;
+          if (bad || !((j0 >= sr.lo && j0 + kTcTile <= sr.hi) || j0 + kTcTile <= sr.s_end)) {
+#pragma unroll 1
+            for (int r = lane; r < kTcTile; r += 32) {
+              const int j = j0 + r;
+              if ((j < sr.s_end || (j >= sr.lo && j < sr.hi)) && !((bad >> (r / R2)) & 1u)) continue;
+              unsigned char* vr = smem + vs * C::SLOT + r * 128;
+#pragma unroll
+              for (int x = 0; x < C::HALVES * 8; ++x)
+                *reinterpret_cast<uint4*>(vr + (x >> 3) * C::HALF + (x & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+            }
+            fence_proxy_async();
+            __syncwarp();
+          }
+          if (k == 0 && !wait_all(o_free + s, parts & 1)) { timed_out = true; break; }
+        }
+        if (more) {
+          const int piece = pc + next + max(0, next - LA + 1);
+          ks = piece % S;
+          pass(piece);
+          if (timed_out || !wait_all(full + ks, (piece / S) & 1)) { timed_out = true; break; }
+          ++at;
+        }
+        if (k >= 0) {
+          const uint64_t vd = umma_desc(smem_u32(smem + vs * C::SLOT), C::HALF, 1024);
+#pragma unroll 1
+          for (int half = 0; half < 2; ++half) {
+            if (!wait_all(p_full + 2 * s + half, (tp + k) & 1)) { timed_out = true; break; }
+#pragma unroll
+            for (int x = 0; x < kSub / 16; ++x)  // 16 tokens: 2048 bytes of V, in the descriptor's 16-byte units
+              umma_ts_on(leader, o, pa + kSub * half + 32 * (x >> 1) + 8 * (x & 1), vd + half * kSub * 8 + x * 128, kIdPV,
+                         k > 0 || half > 0 || x > 0);
+            if (split) {
+#pragma unroll
+              for (int x = 0; x < kSub / 16; ++x)
+                umma_ts_on(leader, o, pa + kSub * half + 32 * (x >> 1) + 16 + 8 * (x & 1),
+                           vd + half * kSub * 8 + x * 128, kIdPV, true);
+            }
+            umma_commit_on(leader, pv_done + 2 * s + half);
+          }
+          if (timed_out) break;
+        }
+        if (more) {
+          const uint64_t kd = umma_desc(smem_u32(smem + ks * C::SLOT), 16, 1024);
+          const uint64_t qd = umma_desc(smem_u32(smem + C::OFF_Q + (NQ == 1 ? 0 : s) * C::SLOT), 16, 1024);
+#pragma unroll
+          for (int x = 0; x < D / 16; ++x)  // 16 dimensions: 32 bytes, every fourth step the next half
+            umma_on(leader, pa, qd + (x >> 2) * (C::HALF / 16) + (x & 3) * 2, kd + (x >> 2) * (C::HALF / 16) + (x & 3) * 2,
+                    kIdQK, x > 0);
+          umma_commit_on(leader, s_full + s);
+          umma_commit_on(leader, empty + ks);
+        }
+        if (k >= 0) umma_commit_on(leader, empty + vs);  // (arrives once the QK above is complete too)
+      }
+      pass(pc + 2 * n);
+      tp += mine;
+      pc += 2 * n;
+      tiles += n;
     }
-    if (lane == 0) umma_commit(done);  // after every operation issued above
+    umma_commit_on(leader, done + s);  // after every product issued above
     __syncwarp();
-    if (!mbar_wait(done, 0)) timed_out = true;
+    if (!mbar_wait(done + s, 0)) timed_out = true;
   } else {
     // ------------------------------------------- softmax, one row a thread
     const int s = warp >> 2, r = tid & 127;
     const unsigned taddr = tmem + ((unsigned)((warp & 3) * 32) << 16) + 128 * s, oaddr = taddr + 256 + (D - 128) * s;
     const float c = p.c_log2;
     bool dead = false;            // a wait of this thread gave up: skip the work, keep the barriers
-    int ns = 0, pc = 0, tiles = 0;  // S buffers of this group read; pieces and tiles of the parts before
+    int ns = 0, tiles = 0;        // steps of this group done, tiles of the parts before
     auto wait = [&](uint64_t* bar, unsigned parity) {
       if (!__all_sync(0xffffffffu, !dead && mbar_wait(bar, parity))) dead = true;
       tc_fence_after();
@@ -293,16 +354,16 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
     };
     while (next_part(p, walk, q)) {
       const int n = q.u1 - q.u0;
-      const SeenRange sr = q.it.sr;
       const int row_s = q.it.row0 + (NQ == 2 ? s * kTcTile : 0), row = row_s + r;  // query row of the kv-head
       const bool valid = row < q.it.row0 + q.it.rows;
       const bool rows_here = __any_sync(0xffffffffu, valid);
       const int t = valid ? q.sq.len - q.sq.n + row / p.G : -1;      // its position
       const int low = p.window < 0 ? -1 : t - p.window;              // the window sees j > low
       float m = -CUDART_INF_F, l = 0.f;
+      const bool split = q.it.split;
       bool have = false;  // O holds something
       // A group without rows takes no part: it must not arrive at q_full, whose
-      // phases nobody would wait for.
+      // phases nobody would wait for (nor, with NQ = 1, for one without tiles).
       const bool group = NQ == 1 || s == 0 || q.it.rows > kTcTile;
       if (n > 0 && group) {
         // Queries: in the one-row-block form both groups load half of the rows,
@@ -313,108 +374,134 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
         const int rows_q = NQ == 1 ? q.it.rows : min(kTcTile, max(0, q.it.rows - s * kTcTile));
         const __nv_bfloat16* qb = static_cast<const __nv_bfloat16*>(p.q.data) + (int64_t)q.b * p.q.sb;
         unsigned char* qs = smem + C::OFF_Q + (NQ == 1 ? 0 : s) * C::SLOT;
-        for (int i = NQ == 1 ? tid : r; i < rows_q * P16; i += NQ == 1 ? 256 : 128) {
-          const int rr = i / P16, cc = i % P16, qrow = q.it.row0 + (NQ == 2 ? s * kTcTile : 0) + rr;
-          const uint4 v = *reinterpret_cast<const uint4*>(qb + (int64_t)(qrow / p.G) * p.q.sn +
-                                                          (int64_t)(q.g * p.G + qrow % p.G) * p.q.sh + 8 * cc);
-          *reinterpret_cast<uint4*>(qs + (cc >> 3) * C::HALF + rr * 128 + (((cc & 7) ^ (rr & 7)) << 4)) = v;
+        constexpr int kStep = NQ == 1 ? 256 : 128, kBatch = D == 128 ? 16 : 8;  // loads in flight per thread
+        for (int i0 = NQ == 1 ? tid : r; i0 < rows_q * P16; i0 += kStep * kBatch) {
+          uint4 v[kBatch];
+#pragma unroll
+          for (int x = 0; x < kBatch; ++x) {
+            const int i = i0 + x * kStep, qrow = q.it.row0 + (NQ == 2 ? s * kTcTile : 0) + i / P16;
+            if (i < rows_q * P16)
+              v[x] = *reinterpret_cast<const uint4*>(qb + (int64_t)row_token(p, qrow) * p.q.sn +
+                                                     (int64_t)(q.g * p.G + qrow - row_token(p, qrow) * p.G) * p.q.sh +
+                                                     8 * (i % P16));
+          }
+#pragma unroll
+          for (int x = 0; x < kBatch; ++x) {
+            const int i = i0 + x * kStep, rr = i / P16, cc = i % P16;
+            if (i < rows_q * P16)
+              *reinterpret_cast<uint4*>(qs + (cc >> 3) * C::HALF + rr * 128 + (((cc & 7) ^ (rr & 7)) << 4)) = v[x];
+          }
         }
         fence_proxy_async();  // read by the tensor core
-        mbar_arrive(q_full + (NQ == 1 ? 0 : s));
+        if (NQ == 2) {
+          mbar_arrive(q_full + s);
+        } else {
+          mbar_arrive(q_full);
+          if (n > 1) mbar_arrive(q_full + 1);
+        }
       }
       for (int i = NQ == 1 ? s : 0; i < n && group; i += NQ == 1 ? 2 : 1) {
         const int j0 = q.it.tl.tile(q.u0 + i) * kTcTile;
-        wait(s_full + s, ns & 1);
+        bool all = !valid || (j0 + kTcTile - 1 <= t && (j0 > low || j0 + kTcTile <= p.sinks));
+        wait(s_full + s, (ns >> 1) & 1);
         const uint32_t bad = bad_ring[(tiles + i) % kMaskRing];
-        // Rows of the tile that no row of the item sees, or of unmapped pages:
-        // zero their V before the product reads it.
-        const bool clean = bad == 0 && ((j0 >= sr.lo && j0 + kTcTile <= sr.hi) || j0 + kTcTile <= sr.s_end);
-        if (!clean && (NQ == 1 || s == 0)) {
-          const int vp = pc + min(i + LA, n) + i, sl = vp % S;  // the tile's V among the pieces
-          if (wait(full + sl, (vp / S) & 1)) {
-            const int j = j0 + r;
-            if (!(j < sr.s_end || (j >= sr.lo && j < sr.hi)) || ((bad >> (r / R2)) & 1u)) {
-              unsigned char* vr = smem + sl * C::SLOT + r * 128;
-#pragma unroll
-              for (int k = 0; k < C::HALVES * 8; ++k)
-                *reinterpret_cast<uint4*>(vr + (k >> 3) * C::HALF + (k & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+        if (bad) all = false;
+        const bool masked = !__all_sync(0xffffffffu, all);
+        float* zr = p.weigh && valid ? p.z + ((int64_t)(q.b * p.Hkv + q.g) * p.R + row) * p.z_row + j0 : nullptr;
+#pragma unroll 1
+        for (int k0 = 0; k0 < kTcTile; k0 += kSub) {
+          const int half = k0 / kSub;
+          if (rows_here && !dead) {
+            // 64 columns of the row of S.  P = exp2(c z - m) goes over them:
+            // columns [k, k + 16), k = 0 and 32, take hi of tokens k .. k + 31
+            // and the next 16 lo (with split).  The exponentials are formed with
+            // the reference as it is, next to the maximum that says whether it
+            // must be raised, not after it.  In a rolled loop over the halves:
+            // eleven warps run different code at once, and unrolled over the
+            // whole row this outgrew the instruction cache (the warps that issue
+            // the products then waited for their next instructions, not for data).
+            float x[64];
+            float (&xa)[32] = *reinterpret_cast<float (*)[32]>(x), (&xb)[32] = *reinterpret_cast<float (*)[32]>(x + 32);
+            tmem_ld_start(taddr + k0, xa);
+            tmem_ld_start(taddr + k0 + 32, xb);
+            tmem_ld_wait(xa);
+            tmem_ld_wait(xb);
+            if (masked) {
+              mask_cols(xa, seen_bits(j0 + k0, t, low, p.sinks, bad, k0, R2));
+              mask_cols(xb, seen_bits(j0 + k0 + 32, t, low, p.sinks, bad, k0 + 32, R2));
             }
-            fence_proxy_async();
-          }
-        }
-        if (rows_here && !dead) {
-          float z[128];
-          tmem_ld(taddr, z);
-          const bool all = !valid || (bad == 0 && j0 + kTcTile - 1 <= t && (j0 > low || j0 + kTcTile <= p.sinks));
-          if (!__all_sync(0xffffffffu, all)) {
+            if (zr) {
 #pragma unroll
-            for (int k = 0; k < 128; ++k) {
-              const int j = j0 + k;
-              if (!(j <= t && (j > low || j < p.sinks))) z[k] = -CUDART_INF_F;
+              for (int k = 0; k < kSub; k += 4)
+                *reinterpret_cast<float4*>(zr + k0 + k) =
+                    make_float4(x[k] * c, x[k + 1] * c, x[k + 2] * c, x[k + 3] * c);
             }
-            if (bad) {
+            uint32_t hi[32];
+            float2 s0, s1;
+            auto exps = [&] {
+              const float mu = m == -CUDART_INF_F ? 0.f : m;
+              const float2 c2 = make_float2(c, c), mu2 = make_float2(-mu, -mu);
+              s0 = s1 = make_float2(0.f, 0.f);
 #pragma unroll
-              for (int k = 0; k < 128; ++k)
-                if ((bad >> (k / R2)) & 1u) z[k] = -CUDART_INF_F;
-            }
-          }
-          if (p.weigh && valid) {
-            float4* zr = reinterpret_cast<float4*>(
-                p.z + ((int64_t)(q.b * p.Hkv + q.g) * p.R + row) * p.z_row + j0);
-#pragma unroll
-            for (int k = 0; k < 32; ++k) zr[k] = make_float4(z[4 * k] * c, z[4 * k + 1] * c, z[4 * k + 2] * c, z[4 * k + 3] * c);
-          }
-          float mx = z[0];
-#pragma unroll
-          for (int k = 1; k < 128; ++k) mx = fmaxf(mx, z[k]);
-          mx *= c;
-          if (!have) {
-            m = mx;
-          } else if (__any_sync(0xffffffffu, valid && mx > m + 8.f)) {
-            // O holds the products of this group's tiles so far: rescale it
-            // once the last of them is complete.
-            const float mn = fmaxf(m, mx), f = m == -CUDART_INF_F ? 0.f : fexp2(m - mn);
-            m = mn;
-            l *= f;
-            if (wait(pv_done + s, (ns - 1) & 1)) {
-#pragma unroll
-              for (int k = 0; k < D; k += 32) {
-                float o[32];
-                tmem_ld(oaddr + k, o);
-#pragma unroll
-                for (int x = 0; x < 32; ++x) o[x] *= f;
-                tmem_st(oaddr + k, o);
+              for (int k = 0; k < 32; ++k) {
+                float2 e = fma2(make_float2(x[2 * k], x[2 * k + 1]), c2, mu2);
+                e.x = fexp2(e.x);
+                e.y = fexp2(e.y);
+                if (k & 1) s1 = add2(s1, e);
+                else s0 = add2(s0, e);
+                hi[k] = pack_bf16(e.x, e.y);
               }
-              tmem_st_wait();
-            }
-          }
-          const float mu = m == -CUDART_INF_F ? 0.f : m;
-          float l0 = 0.f, l1 = 0.f;
+            };
+            exps();
+            float mx[4];
 #pragma unroll
-          for (int k = 0; k < 128; k += 32) {
-            uint32_t hi[16], lo[16];
+            for (int k = 0; k < 4; ++k) {
+              mx[k] = x[k];
 #pragma unroll
-            for (int x = 0; x < 16; ++x) {
-              const float a = fexp2(fmaf(z[k + 2 * x], c, -mu)), b = fexp2(fmaf(z[k + 2 * x + 1], c, -mu));
-              l0 += a;
-              l1 += b;
-              hi[x] = pack_bf16(a, b);
-              float ah, bh;
-              bf2(hi[x], ah, bh);
-              lo[x] = pack_bf16(a - ah, b - bh);
+              for (int y = 4; y < kSub; y += 8) mx[k] = fmaxf(fmaxf(mx[k], x[y + k]), y + 4 < kSub ? x[y + 4 + k] : mx[k]);
             }
-            tmem_st(taddr + k / 2, hi);
-            tmem_st(taddr + 64 + k / 2, lo);
+            const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c;
+            if (__any_sync(0xffffffffu, valid && top > m + kRaise)) {
+              const float mn = fmaxf(m, top), f = m == -CUDART_INF_F ? 0.f : fexp2(m - mn);
+              m = mn;
+              l *= f;
+              // O holds the products of this group's steps so far: rescale it
+              // once the last of them is complete.
+              if (have && wait(pv_done + 2 * s + ((ns - 1) & 1), ((ns - 1) >> 1) & 1)) {
+#pragma unroll 1
+                for (int e = 0; e < D; e += 16) {
+                  float o[16];
+                  tmem_ld16(oaddr + e, o);
+#pragma unroll
+                  for (int i = 0; i < 16; ++i) o[i] *= f;
+                  tmem_st16(oaddr + e, o);
+                }
+              }
+              exps();
+            }
+            l += (s0.x + s0.y) + (s1.x + s1.y);
+            tmem_st(taddr + k0, *reinterpret_cast<uint32_t (*)[16]>(hi));
+            tmem_st(taddr + k0 + 32, *reinterpret_cast<uint32_t (*)[16]>(hi + 16));
+            if (split) {
+              const float mu = m == -CUDART_INF_F ? 0.f : m;
+#pragma unroll
+              for (int k = 0; k < 32; ++k) {
+                float2 h;
+                bf2(hi[k], h.x, h.y);
+                hi[k] = pack_bf16(fexp2(fmaf(x[2 * k], c, -mu)) - h.x, fexp2(fmaf(x[2 * k + 1], c, -mu)) - h.y);
+              }
+              tmem_st(taddr + k0 + 16, *reinterpret_cast<uint32_t (*)[16]>(hi));
+              tmem_st(taddr + k0 + 48, *reinterpret_cast<uint32_t (*)[16]>(hi + 16));
+            }
+            tmem_st_wait();
           }
-          l += l0 + l1;
-          tmem_st_wait();
+          have = true;
+          ++ns;
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(p_full + 2 * s + half);
         }
-        have = true;
-        ++ns;
-        tc_fence_before();
-        mbar_arrive(p_full + s);
       }
-      pc += 2 * max(0, n);
       tiles += max(0, n);
       // ---- rows that see nothing: padding, or all of an item without tiles
       if (q.owner && (NQ == 2 || s == 0) && row < min(p.R, q.it.row0 + p.block) && (!valid || q.it.tl.n == 0)) {
@@ -428,7 +515,7 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
       const bool direct = NQ == 2 && q.whole();
       const int c0 = lc.owner(q.first);
       auto rec_of = [&](int c, int grp) { return (2 * c + (c == c0 ? 1 : 0)) * 2 + grp; };
-      if (have) wait(pv_done + s, (ns - 1) & 1);
+      if (have) wait(pv_done + 2 * s + ((ns - 1) & 1), ((ns - 1) >> 1) & 1);
       if (rows_here) {
         float* po = nullptr;
         __nv_bfloat16* out = nullptr;
@@ -474,9 +561,9 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
       }
       if (direct) continue;
       // NQ = 1: the records of both groups of every CTA; NQ = 2: this group's rows.
-      const int parts = lc.owner(q.first + q.it.tl.n - 1) - c0 + 1;
+      const int parts = lc.owner(q.last) - c0 + 1;
       auto sync = [&] { asm volatile("barrier.cta.sync %0, 128;\n" ::"r"(2 + s) : "memory"); };
-      if (last_to_arrive(p.tickets + 2 * c0 + (NQ == 2 ? s : 0), NQ == 1 ? 2 * parts : parts, r, misc + 12 + s, sync)) {
+      if (last_to_arrive(p.tickets + 2 * c0 + (NQ == 2 ? s : 0), NQ == 1 ? 2 * parts : parts, r, misc + 13 + s, sync)) {
         if (NQ == 1)
           join_records<__nv_bfloat16, D, 128>(p, q.b, q.g, 0, q.it.rows, 2 * parts, kTcTile,
                                               [&](int k) { return rec_of(c0 + (k >> 1), k & 1); }, r);

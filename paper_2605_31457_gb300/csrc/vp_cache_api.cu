@@ -62,7 +62,7 @@ vp_status reserve_new(vp_ctx* ctx, int32_t max_new, int32_t max_weight_new) {
   const int G = c.num_q_heads / c.num_kv_heads;
   if ((int64_t)max_weight_new * G > vp::kNewWeightRows)
     return fail(ctx, VP_ERR_UNSUPPORTED, "vp_reserve_new: weights need max_weight_new * G <= 128");
-  if ((int64_t)max_new * G > INT32_MAX / 2)
+  if ((int64_t)max_new * G >= (1 << 28))
     return fail(ctx, VP_ERR_UNSUPPORTED, "vp_reserve_new: max_new * G is too large");
   cudaError_t e = cudaDeviceSynchronize();
   if (e != cudaSuccess) return cuda_fail(ctx, "vp_reserve_new", e);
@@ -123,6 +123,7 @@ vp_status attend_new(vp_ctx* ctx, int32_t batch, int32_t n_new, const vp_rows* q
   p.paged = c.paged; p.page_size = c.paged ? c.page_size : 1;
   while ((1 << p.page_shift) < p.page_size) ++p.page_shift;
   p.n_new = n_new; p.R = n_new * G;
+  p.g_mul = G == 1 ? 0u : (uint32_t)((1ull << 32) / (unsigned)G + 1);
   p.q = vp::RowView{q->data, q->stride_b, q->stride_n, q->stride_h};
   p.out = vp::RowView{out->data, out->stride_b, out->stride_n, out->stride_h};
   p.k = view(*k_cache); p.v = view(*v_cache);

@@ -562,3 +562,19 @@ def test_prompt_blocks_with_few_rows_in_a_row(lib):
         assert torch.equal(c.out.view(torch.int16), first.view(torch.int16))
     lib.vp_check_errors(c.ctx)
     lib.vp_free(c.ctx)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("n_new,heads", [(1, (28, 4)), (4, (28, 4)), (10, (28, 4)), (90, (8, 2))])
+def test_logits_that_jump_far(lib, dtype, n_new, heads):
+    """Logits that rise by hundreds along the cache: the running reference has to
+    follow, and what was summed before it has to vanish without a trace."""
+    c = Case(lib, heads, 128, dtype, lens=(700, 333), n_new=n_new, spread=30.0, seed=18, poison=False,
+             weigh=n_new * heads[0] // heads[1] <= 128)
+    ramp = torch.linspace(-3.0, 3.0, 700, device="cuda")[None, None, :, None]
+    k = (c.kt.float() * 0.05 + ramp * c.q[:, -1:, ::heads[0] // heads[1]].float().transpose(1, 2) / 30.0).to(c.kt.dtype)
+    c.kt.copy_(k)
+    c.ref = [O.attend_new(c.q[b].double().cpu().numpy(), c.kt[b].double().cpu().numpy(), c.vt[b].double().cpu().numpy(),
+                          c.lens[b], c.ns[b]) for b in range(2)]
+    assert max(r["lse"].max() for r in c.ref) > 200
+    c.run()
