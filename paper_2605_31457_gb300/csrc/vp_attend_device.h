@@ -55,7 +55,8 @@ struct Walk {
   int64_t pos;
   int left;
 };
-// The next item a CTA does, or its share of it: tiles [u0, u1) of the list.
+// The next item a CTA does, or its share of it (the same in every lane of a
+// converged warp, which calls it together): tiles [u0, u1) of the list.
 struct Part {
   int g, b, u0, u1;
   bool owner;       // this CTA holds the item's first position: it answers for an item without tiles
@@ -70,6 +71,8 @@ __device__ __forceinline__ bool next_part(const AttendParams& p, Walk& w, Part& 
   q.g = w.g;
   q.b = w.pair / p.nqt;
   q.sq = load_new(p, q.b, false);
+  q.sq.len = uniform(q.sq.len);
+  q.sq.n = uniform(q.sq.n);
   q.it = att_item(q.sq.len, q.sq.n, p.G, p.block, w.pair - q.b * p.nqt, p.window, p.sinks);
   const int cost = q.it.cost(p.fixed), end = min(cost, w.off + w.left), done = end - w.off;
   q.u0 = q.it.tiles_before(w.off, p.fixed);
@@ -111,6 +114,7 @@ __device__ __forceinline__ Walk line_start(const AttendParams& p, int* misc, Lin
     if (w < warp) before += misc[w];
     total += misc[w];
   }
+  total = uniform(total);
   lc = LineCut((int64_t)total * p.Hkv, gridDim.x);
   Walk w{0, 0, 0, 0, 0};
   if ((int)blockIdx.x < lc.nc) {
@@ -131,8 +135,8 @@ __device__ __forceinline__ Walk line_start(const AttendParams& p, int* misc, Lin
     misc[NT / 32 + 1] = at - sum;
   }
   __syncthreads();
-  w.pair = misc[NT / 32];
-  w.off = misc[NT / 32 + 1];
+  w.pair = uniform(misc[NT / 32]);
+  w.off = uniform(misc[NT / 32 + 1]);
   return w;
 }
 

@@ -64,7 +64,7 @@ struct TcCfg2 {
   static constexpr int LA = NQ == 1 ? 2 : 1;            // tiles whose S is ahead of the P.V product
   static constexpr int OFF_Q = S * SLOT;
   static constexpr int OFF_BAR = OFF_Q + NQ * SLOT;
-  static constexpr int NBAR = 2 * S + 16;               // full, empty, s_full, p_full, pv_done, o_free, q_full, done
+  static constexpr int NBAR = 2 * S + 18;               // full, empty, s_full, p_full, pv_done, o_free, q_full, done
   static constexpr int OFF_BAD = OFF_BAR + NBAR * 8;    // unmapped boxes of a tile, one bit each
   static constexpr int OFF_MISC = OFF_BAD + kMaskRing * 4;  // int [16]: scan, start, TMEM base
   static constexpr size_t SMEM = 1024 + (size_t)OFF_MISC + 20 * 4;
@@ -100,18 +100,18 @@ template <int D, int NQ>
 __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant__ AttendParams p) {
   using C = TcCfg2<D, NQ>;
   constexpr int S = C::S, LA = C::LA;
-  constexpr uint32_t kIdQK = att_idesc(kTcTile, 0), kIdPV = att_idesc(D, 1);
+  constexpr uint32_t kIdQK = att_idesc(kSub, 0), kIdPV = att_idesc(D, 1);
   extern __shared__ __align__(16) unsigned char smem_raw[];
   unsigned char* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + C::OFF_BAR);  // [S] a slot's copies landed
   uint64_t* empty = full + S;                                        // [S] a slot's tile was read
-  uint64_t* s_full = full + 2 * S;                                   // [2] S of a group written
-  uint64_t* p_full = s_full + 2;                                     // [2][2] half a tile's P of a group written (an arrival per warp)
-  uint64_t* pv_done = s_full + 6;                                    // [2][2] P.V of that half complete
-  uint64_t* o_free = s_full + 10;                                    // [2] O of the last part read (128)
-  uint64_t* q_full = s_full + 12;                                    // [2] a group's queries loaded (128; NQ = 1: 256)
-  uint64_t* done = s_full + 14;                                      // [2] every product of a group complete
+  uint64_t* s_full = full + 2 * S;                                   // [2][2] half a tile's S of a group written
+  uint64_t* p_full = s_full + 4;                                     // [2][2] its P written (an arrival per warp)
+  uint64_t* pv_done = s_full + 8;                                    // [2][2] its P.V complete
+  uint64_t* o_free = s_full + 12;                                    // [2] O of the last part read (128)
+  uint64_t* q_full = s_full + 14;                                    // [2] a group's queries loaded (128; NQ = 1: 256)
+  uint64_t* done = s_full + 16;                                      // [2] every product of a group complete
   volatile uint32_t* bad_ring = reinterpret_cast<uint32_t*>(smem + C::OFF_BAD);
   int* misc = reinterpret_cast<int*>(smem + C::OFF_MISC);            // [0, 13) line_start; [13, 14] flags; [15] TMEM
 
@@ -121,11 +121,11 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
       mbar_init(empty + i, 2);
     }
     for (int i = 0; i < 4; ++i) {
+      mbar_init(s_full + i, 1);
       mbar_init(p_full + i, 4);
       mbar_init(pv_done + i, 1);
     }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(s_full + i, 1);
       mbar_init(o_free + i, 128);
       mbar_init(q_full + i, NQ == 1 ? 256 : 128);
       mbar_init(done + i, 1);
@@ -146,7 +146,7 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
   Walk walk = line_start<kAttThreads>(p, misc, lc);  // passes the CTA-wide barrier
   tc_fence_after();
   Part q;
-  const unsigned tmem = (unsigned)misc[15];  // columns [0, 128), [128, 256): S / P; from 256: O of the groups
+  const unsigned tmem = (unsigned)uniform(misc[15]);  // columns [0, 128), [128, 256): S / P; from 256: O of the groups
   const int R2 = p.paged ? min(kTcTile, p.page_size) : kTcTile;  // rows per copied box
   const int nb = kTcTile / R2;
   unsigned err = 0;
@@ -223,8 +223,9 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
     for (int k = max(0, pc - S); k < pc; ++k) mbar_wait(full + k % S, (k / S) & 1);
   } else if (warp >= 9) {
     // ------------------------------- tensor cores, a warp for each group s
-    // P.V takes half a tile at a time, so that the first half's runs while the
-    // softmax threads turn the second half of S into P.  One warp for both
+    // Half a tile at a time: S of the next tile's half follows P.V of this
+    // tile's same half, whose columns it takes, so that the softmax threads have
+    // the next S while they form a P.  One warp for both
     // groups spent more time waiting at barriers than the products took.
     auto wait_all = [&](uint64_t* bar, unsigned parity) {
       const bool ok = __all_sync(0xffffffffu, mbar_wait(bar, parity));
@@ -232,17 +233,14 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
       return ok;
     };
     const int leader = elect_one();
-    // Warp-wide reductions leave these in uniform registers, which the
-    // products' operands must be in.
-    const unsigned tm = __reduce_max_sync(0xffffffffu, tmem);
-    const int s = __reduce_max_sync(0xffffffffu, warp - 9);
+    const int s = uniform(warp - 9);
     int pc = 0, tiles = 0;                     // pieces and tiles of the parts before
     unsigned parts = 0, tp = 0;                // parts with tiles of this group, its tiles before
     while (!timed_out && next_part(p, walk, q)) {
-      const int n = __reduce_max_sync(0xffffffffu, q.u1 - q.u0);
+      const int n = q.u1 - q.u0;
       if (n <= 0) continue;
-      const int two = __reduce_max_sync(0xffffffffu, NQ == 2 && q.it.rows > kTcTile);  // the second group has rows
-      const int split = __reduce_max_sync(0xffffffffu, q.it.split);
+      const int two = NQ == 2 && q.it.rows > kTcTile;  // the second group has rows
+      const int split = q.it.split;
       const int mine = NQ == 2 ? (s == 0 || two ? n : 0) : (n + 1 - s) / 2;  // tiles of this group
       if (mine > 0) {
         if (!wait_all(q_full + s, parts & 1)) { timed_out = true; break; }
@@ -265,7 +263,7 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
 #pragma unroll 1
       for (int k = -1; k < mine && !timed_out; ++k) {
         const int tile = NQ == 1 ? 2 * k + s : k, next = NQ == 1 ? tile + 2 : tile + 1;
-        const unsigned o = tm + 256 + D * s, pa = tm + 128 * s;
+        const unsigned o = tmem + 256 + D * s, pa = tmem + 128 * s;
         const bool more = k + 1 < mine;
         int vs = 0, ks = 0;
         if (k >= 0) {
@@ -301,36 +299,27 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
           if (timed_out || !wait_all(full + ks, (piece / S) & 1)) { timed_out = true; break; }
           ++at;
         }
-        if (k >= 0) {
-          const uint64_t vd = umma_desc(smem_u32(smem + vs * C::SLOT), C::HALF, 1024);
+        const uint64_t vd = umma_desc(smem_u32(smem + vs * C::SLOT), C::HALF, 1024);
+        const uint64_t kd = umma_desc(smem_u32(smem + ks * C::SLOT), 16, 1024);
+        const uint64_t qd = umma_desc(smem_u32(smem + C::OFF_Q + (NQ == 1 ? 0 : s) * C::SLOT), 16, 1024);
 #pragma unroll 1
-          for (int half = 0; half < 2; ++half) {
+        for (int half = 0; half < 2; ++half) {
+          if (k >= 0) {
             if (!wait_all(p_full + 2 * s + half, (tp + k) & 1)) { timed_out = true; break; }
-#pragma unroll
-            for (int x = 0; x < kSub / 16; ++x)  // 16 tokens: 2048 bytes of V, in the descriptor's 16-byte units
-              umma_ts_on(leader, o, pa + kSub * half + 32 * (x >> 1) + 8 * (x & 1), vd + half * kSub * 8 + x * 128, kIdPV,
-                         k > 0 || half > 0 || x > 0);
-            if (split) {
-#pragma unroll
-              for (int x = 0; x < kSub / 16; ++x)
-                umma_ts_on(leader, o, pa + kSub * half + 32 * (x >> 1) + 16 + 8 * (x & 1),
-                           vd + half * kSub * 8 + x * 128, kIdPV, true);
-            }
+            umma4_ts_on(leader, o, pa + kSub * half, vd + half * kSub * 8, kIdPV, k > 0 || half > 0);
+            if (split) umma4_ts_on(leader, o, pa + kSub * half + 16, vd + half * kSub * 8, kIdPV, 1);
             umma_commit_on(leader, pv_done + 2 * s + half);
           }
-          if (timed_out) break;
+          if (more) {
+            umma4_on(leader, pa + kSub * half, qd, kd + half * kSub * 8, kIdQK, 0);
+            if (D == 128)  // the other 64 dimensions
+              umma4_on(leader, pa + kSub * half, qd + C::HALF / 16, kd + half * kSub * 8 + C::HALF / 16, kIdQK, 1);
+            umma_commit_on(leader, s_full + 2 * s + half);
+          }
         }
-        if (more) {
-          const uint64_t kd = umma_desc(smem_u32(smem + ks * C::SLOT), 16, 1024);
-          const uint64_t qd = umma_desc(smem_u32(smem + C::OFF_Q + (NQ == 1 ? 0 : s) * C::SLOT), 16, 1024);
-#pragma unroll
-          for (int x = 0; x < D / 16; ++x)  // 16 dimensions: 32 bytes, every fourth step the next half
-            umma_on(leader, pa, qd + (x >> 2) * (C::HALF / 16) + (x & 3) * 2, kd + (x >> 2) * (C::HALF / 16) + (x & 3) * 2,
-                    kIdQK, x > 0);
-          umma_commit_on(leader, s_full + s);
-          umma_commit_on(leader, empty + ks);
-        }
-        if (k >= 0) umma_commit_on(leader, empty + vs);  // (arrives once the QK above is complete too)
+        if (timed_out) break;
+        if (more) umma_commit_on(leader, empty + ks);
+        if (k >= 0) umma_commit_on(leader, empty + vs);
       }
       pass(pc + 2 * n);
       tp += mine;
@@ -403,7 +392,7 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
       for (int i = NQ == 1 ? s : 0; i < n && group; i += NQ == 1 ? 2 : 1) {
         const int j0 = q.it.tl.tile(q.u0 + i) * kTcTile;
         bool all = !valid || (j0 + kTcTile - 1 <= t && (j0 > low || j0 + kTcTile <= p.sinks));
-        wait(s_full + s, (ns >> 1) & 1);
+        wait(s_full + 2 * s, (ns >> 1) & 1);
         const uint32_t bad = bad_ring[(tiles + i) % kMaskRing];
         if (bad) all = false;
         const bool masked = !__all_sync(0xffffffffu, all);
@@ -411,6 +400,7 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
 #pragma unroll 1
         for (int k0 = 0; k0 < kTcTile; k0 += kSub) {
           const int half = k0 / kSub;
+          if (half) wait(s_full + 2 * s + 1, (ns >> 1) & 1);
           if (rows_here && !dead) {
             // 64 columns of the row of S.  P = exp2(c z - m) goes over them:
             // columns [k, k + 16), k = 0 and 32, take hi of tokens k .. k + 31

@@ -243,19 +243,41 @@ __device__ __forceinline__ void umma(unsigned d, uint64_t a, uint64_t b, uint32_
   asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n"
                ::"r"(d), "l"(a), "l"(b), "r"(id), "r"((int)acc) : "memory");
 }
-// The same with the A operand in TMEM (lane = row, 32-bit column c holding K
-// elements 2c and 2c + 1), and the three forms issued by the lanes whose `on` is
-// non-zero: one lane of a warp that otherwise runs converged, so that operands
-// stay in the uniform registers the instructions read them from.
-__device__ __forceinline__ void umma_on(int on, unsigned d, uint64_t a, uint64_t b, uint32_t id, bool acc) {
-  asm volatile("{\n .reg .pred p, q;\n setp.ne.b32 p, %4, 0;\n setp.ne.b32 q, %5, 0;\n"
-               " @q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n"
-               ::"r"(d), "l"(a), "l"(b), "r"(id), "r"((int)acc), "r"(on) : "memory");
+// A value that is the same in every lane of a converged warp, as one that the
+// compiler knows to be: what is computed from such values stays in the uniform
+// registers that tensor-core instructions take their operands from.
+__device__ __forceinline__ int uniform(int x) { return __reduce_max_sync(0xffffffffu, x); }
+__device__ __forceinline__ int64_t uniform(int64_t x) {
+  return (int64_t)uniform((int)(x >> 32)) << 32 | (uint32_t)uniform((int)x);
 }
-__device__ __forceinline__ void umma_ts_on(int on, unsigned d, unsigned a, uint64_t b, uint32_t id, bool acc) {
-  asm volatile("{\n .reg .pred p, q;\n setp.ne.b32 p, %4, 0;\n setp.ne.b32 q, %5, 0;\n"
-               " @q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n"
-               ::"r"(d), "r"(a), "l"(b), "r"(id), "r"((int)acc), "r"(on) : "memory");
+// Four products in a row by the lane whose `on` is non-zero, in a warp that runs
+// converged: A and B in shared memory, K-major, 16 elements (32 bytes) a step ...
+__device__ __forceinline__ void umma4_on(int on, unsigned d, uint64_t a, uint64_t b, uint32_t id, int acc) {
+  asm volatile(
+      "{\n .reg .pred p, q, t;\n .reg .b64 a1, a2, a3, b1, b2, b3;\n"
+      " setp.ne.b32 p, %4, 0;\n setp.ne.b32 q, %5, 0;\n setp.eq.u32 t, 0, 0;\n"
+      " add.s64 a1, %1, 2;\n add.s64 b1, %2, 2;\n add.s64 a2, %1, 4;\n add.s64 b2, %2, 4;\n"
+      " add.s64 a3, %1, 6;\n add.s64 b3, %2, 6;\n"
+      " @q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n"
+      " @q tcgen05.mma.cta_group::1.kind::f16 [%0], a1, b1, %3, t;\n"
+      " @q tcgen05.mma.cta_group::1.kind::f16 [%0], a2, b2, %3, t;\n"
+      " @q tcgen05.mma.cta_group::1.kind::f16 [%0], a3, b3, %3, t;\n}\n"
+      ::"r"(d), "l"(a), "l"(b), "r"(id), "r"(acc), "r"(on) : "memory");
+}
+// ... and with A in TMEM (lane = row, 32-bit column c holding K elements 2c and
+// 2c + 1), at columns a, a + 8, a + 32, a + 40, and B MN-major in shared memory,
+// 16 rows of 128 bytes a step.
+__device__ __forceinline__ void umma4_ts_on(int on, unsigned d, unsigned a, uint64_t b, uint32_t id, int acc) {
+  asm volatile(
+      "{\n .reg .pred p, q, t;\n .reg .b32 a1, a2, a3;\n .reg .b64 b1, b2, b3;\n"
+      " setp.ne.b32 p, %4, 0;\n setp.ne.b32 q, %5, 0;\n setp.eq.u32 t, 0, 0;\n"
+      " add.u32 a1, %1, 8;\n add.s64 b1, %2, 128;\n add.u32 a2, %1, 32;\n add.s64 b2, %2, 256;\n"
+      " add.u32 a3, %1, 40;\n add.s64 b3, %2, 384;\n"
+      " @q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n"
+      " @q tcgen05.mma.cta_group::1.kind::f16 [%0], [a1], b1, %3, t;\n"
+      " @q tcgen05.mma.cta_group::1.kind::f16 [%0], [a2], b2, %3, t;\n"
+      " @q tcgen05.mma.cta_group::1.kind::f16 [%0], [a3], b3, %3, t;\n}\n"
+      ::"r"(d), "r"(a), "l"(b), "r"(id), "r"(acc), "r"(on) : "memory");
 }
 __device__ __forceinline__ void umma_commit_on(int on, uint64_t* bar) {
   asm volatile("{\n .reg .pred q;\n setp.ne.b32 q, %1, 0;\n"
