@@ -12,7 +12,7 @@
 // parts of V_i join as m = max m_p, l = sum l_p e^(m_p - m), o likewise.
 // Logits are carried in log2 units (one exp2 each).
 //
-//   k_att_dec   (vp_attend_dec.cu) bf16, up to 32 query rows per kv-head;
+//   k_att_dec   (vp_attend_dec.cu) bf16, up to 64 query rows per kv-head;
 //   k_att_tc    (vp_attend_tc.cu) bf16, more rows;
 //   k_att_any   fp32 caches, and bf16 caches of any layout;
 //   k_att_weights  the accumulated weights, from the logits the others stored.
@@ -286,7 +286,7 @@ void plan_attend(AttendParams& p) {
   p.block = p.kind == ATT_TC2 ? 2 * kTcTile : p.R;
   p.nqt = (p.R + p.block - 1) / p.block;
   p.fixed = (p.kind == ATT_DEC ? 1 : 2) * kTileUnits;
-  p.grid = p.kind == ATT_DEC && p.R <= kDecRows / 2 ? 2 * p.num_sms : p.num_sms;
+  p.grid = p.kind == ATT_DEC && p.R <= 16 ? 2 * p.num_sms : p.num_sms;  // CTAs per SM
 }
 
 cudaError_t launch_attend(const AttendParams& p, cudaStream_t st) {

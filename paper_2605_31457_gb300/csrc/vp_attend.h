@@ -35,12 +35,12 @@ struct NewLayout {
 
 // Which kernel serves a call (plan_attend).  `block` query rows of one
 // (sequence, kv-head) are an item of the tensor-core kernels:
-//   ATT_DEC  k_att_dec: at most 32 query rows, all of them one item;
+//   ATT_DEC  k_att_dec: at most 64 query rows, all of them one item;
 //   ATT_TC1  k_att_tc: at most 128, one item whose tiles alternate between its
 //            two softmax groups;
 //   ATT_TC2  k_att_tc: 256 rows at a time, 128 for each group.
 enum { ATT_ANY = 0, ATT_DEC = 1, ATT_TC1 = 2, ATT_TC2 = 3 };
-constexpr int kDecRows = 32;
+constexpr int kDecRows = 64;
 
 // Query row r of a kv-head = new token r / G, query head g * G + r % G.
 struct AttendParams {

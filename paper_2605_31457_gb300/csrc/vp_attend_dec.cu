@@ -1,5 +1,5 @@
 // k_att_dec: attention of one or a few new tokens over a long cache on the
-// fifth-generation tensor cores (vp_attend_new, bf16, up to 32 query rows).
+// fifth-generation tensor cores (vp_attend_new, bf16, up to 64 query rows).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <math_constants.h>
@@ -13,24 +13,26 @@ namespace vp {
 namespace {
 
 // ---------------------------------------------------------------------------
-// k_att_dec<D, GM>: up to GM (8, 16 or 32) query rows of a (sequence, kv-head),
-// 192 threads in three roles, two CTAs per SM (one for GM = 32):
+// k_att_dec<D, GM>: up to GM (8, 16, 32 or 64) query rows of a (sequence,
+// kv-head), in three roles, two CTAs per SM (one from GM = 32 on):
 //   warp 0     copies tiles of 128 K or V rows into a ring (4-D bulk-tensor
 //              copies, 128-byte swizzle, evict-first in L2: each is read once);
 //   warp 1     one lane issues tcgen05.mma with the cache as the M side, so
 //              that few query rows do not leave the accumulators empty:
 //              S = K Q^T (M = 128 tokens, N = query rows, K = D) and
 //              O += V^T P^T (M = D, N = 2 GM, K = 128 tokens);
-//   warps 2-5  one thread per token: reads its row of S, forms P and writes it,
-//              transposed, to shared memory.
+//   groups of four warps, one for every 16 query rows: a thread per token reads
+//              its 16 columns of S, forms P and writes it, transposed, to shared
+//              memory.
 // P enters the product as two bf16 terms, P = hi + lo, in columns [0, GM) and
 // [GM, 2 GM) of P^T; the two halves of O are added at the end.  P's rounding
 // (2^-17 of it) then vanishes beside the output's, at no cost: the kernel is
 // bound by HBM, 64 KB per tile at D = 128.
 //
-// A row's reference maximum is raised only when a logit passes it by more than
-// 8 (log2 units), when O and the sums are rescaled, so most tiles need no
-// exchange between the threads.  The work is a line of tiles cut evenly over
+// A row's reference is the largest logit of the first tile it sees and is raised
+// only when a logit passes it by more than 64 (log2 units), when O and the sums
+// are rescaled, so most tiles need no exchange between the threads; P <= 2^64
+// has bf16's and float's full precision all the same.  The work is a line of tiles cut evenly over
 // the CTAs (AttItem, LineCut): an item whose tiles lie with several CTAs leaves
 // a record per CTA, and the last CTA to finish joins them.
 //
@@ -40,7 +42,7 @@ namespace {
 // Waits are bounded: a thread whose wait gives up stops its work, still passes
 // every barrier of its group, and the error word reports it.
 // ---------------------------------------------------------------------------
-constexpr int kDecThreads = 192;
+constexpr float kDecRaise = 64.f;
 constexpr int kBadRing = 16;  // more than the tiles between the copy warp and the others
 
 template <int D, int GM>
@@ -48,8 +50,11 @@ struct DecCfg {
   static constexpr int HALF = kTcTile * 128;           // 128 rows x 64 dimensions, swizzled
   static constexpr int HALVES = D / 64;
   static constexpr int SLOT = HALVES * HALF;           // a tile of K or of V
-  static constexpr int CPS = GM == 32 ? 1 : 2;         // CTAs per SM
-  static constexpr int S = (D == 128 ? 6 : 10) / CPS;  // ring slots
+  static constexpr int CPS = GM >= 32 ? 1 : 2;         // CTAs per SM
+  static constexpr int S = GM == 64 ? (D == 128 ? 5 : 8) : (D == 128 ? 6 : 10) / CPS;  // ring slots
+  static constexpr int GR = GM < 16 ? GM : 16;         // query rows of a softmax group
+  static constexpr int SG = GM / GR;                   // softmax groups
+  static constexpr int THREADS = 64 + 128 * SG;
   static constexpr int NQ = GM < 16 ? 16 : GM;         // query rows of the QK product
   static constexpr int NP = 2 * GM;                    // columns of P^T: hi, lo
   static constexpr int PB = GM == 8 ? 2 : 1;           // P buffers
@@ -61,11 +66,12 @@ struct DecCfg {
   static constexpr int OFF_BAR = OFF_P + PB * PBUF;
   static constexpr int NBAR = 2 * S + 2 + 2 + PB + PB + 3;  // full, empty, s_full, s_free, p_full, pv_done, q_full, o_free, done
   static constexpr int OFF_BAD = OFF_BAR + NBAR * 8;   // unmapped boxes of a tile, one bit each
-  static constexpr int OFF_MISC = OFF_BAD + kBadRing * 4;     // int [12]: line_start, flag, TMEM base
-  static constexpr int OFF_RED = OFF_MISC + 12 * 4;    // float [4][GM]: maxima, then sums
+  static constexpr int LINE = THREADS / 32 + 4;        // ints of line_start
+  static constexpr int OFF_MISC = OFF_BAD + kBadRing * 4;     // int: line_start, flags, TMEM base
+  static constexpr int OFF_RED = OFF_MISC + (LINE + SG + 1) * 4;  // float [SG][4][GR]: maxima, then sums
   static constexpr size_t SMEM = 1024 + (size_t)OFF_RED + 4 * GM * 4;
   static constexpr int O_COL = 2 * NQ;                 // TMEM columns: two S buffers, then O
-  static constexpr int COLS = O_COL + NP <= 64 ? 64 : 128;
+  static constexpr int COLS = O_COL + NP <= 64 ? 64 : O_COL + NP <= 128 ? 128 : 256;
   static_assert(O_COL + NP <= COLS, "TMEM columns");
   static_assert(SMEM <= 232448 / CPS - (CPS > 1 ? 1024 : 0), "shared memory of the CTAs of an SM");
   static_assert(PHALF % 1024 == 0 && QHALF % 1024 == 0, "swizzle atoms stay aligned");
@@ -77,21 +83,10 @@ __host__ __device__ constexpr uint32_t dec_idesc(int m, int n, int a_mn) {
          ((uint32_t)(m >> 4) << 24);
 }
 
-// N consecutive TMEM columns of this thread's lane.
-template <int N>
-__device__ __forceinline__ void load_cols(unsigned taddr, float (&v)[N]) {
-  if constexpr (N == 32) {
-    tmem_ld(taddr, v);
-  } else {
-    static_assert(N == 16, "column count");
-    tmem_ld16(taddr, v);
-  }
-}
-
 template <int D, int GM>
-__global__ void __launch_bounds__(kDecThreads, DecCfg<D, GM>::CPS) k_att_dec(const __grid_constant__ AttendParams p) {
+__global__ void __launch_bounds__(DecCfg<D, GM>::THREADS, DecCfg<D, GM>::CPS) k_att_dec(const __grid_constant__ AttendParams p) {
   using C = DecCfg<D, GM>;
-  constexpr int S = C::S, PB = C::PB;
+  constexpr int S = C::S, PB = C::PB, GR = C::GR;
   constexpr uint32_t kIdQK = dec_idesc(128, C::NQ, 0), kIdPV = dec_idesc(D, C::NP, 1);
   extern __shared__ __align__(16) unsigned char smem_raw[];
   unsigned char* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
@@ -99,14 +94,14 @@ __global__ void __launch_bounds__(kDecThreads, DecCfg<D, GM>::CPS) k_att_dec(con
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + C::OFF_BAR);  // [S] a slot's copies landed
   uint64_t* empty = full + S;                                        // [S] a slot's tile was read
   uint64_t* s_full = full + 2 * S;                                   // [2] S buffer written
-  uint64_t* s_free = s_full + 2;                                     // [2] S buffer read (128 arrivals)
-  uint64_t* p_full = s_full + 4;                                     // [PB] P buffer written (128 arrivals)
+  uint64_t* s_free = s_full + 2;                                     // [2] S buffer read (an arrival per softmax warp)
+  uint64_t* p_full = s_full + 4;                                     // [PB] P buffer written (likewise)
   uint64_t* pv_done = p_full + PB;                                   // [PB] P.V of that buffer complete
-  uint64_t* q_full = pv_done + PB;                                   // queries loaded (128 arrivals)
-  uint64_t* o_free = q_full + 1;                                     // O of the last part read (128 arrivals)
+  uint64_t* q_full = pv_done + PB;                                   // queries loaded (likewise)
+  uint64_t* o_free = q_full + 1;                                     // O of the last part read (likewise)
   uint64_t* done = q_full + 2;                                       // every tensor-core operation complete
   volatile uint32_t* bad_ring = reinterpret_cast<uint32_t*>(smem + C::OFF_BAD);
-  int* misc = reinterpret_cast<int*>(smem + C::OFF_MISC);            // [0, 8) line_start; [8] flag; [9] TMEM
+  int* misc = reinterpret_cast<int*>(smem + C::OFF_MISC);            // [0, LINE) line_start; [LINE, LINE + SG) flags; then TMEM
   float* red = reinterpret_cast<float*>(smem + C::OFF_RED);
 
   if (tid == 0) {
@@ -116,21 +111,21 @@ __global__ void __launch_bounds__(kDecThreads, DecCfg<D, GM>::CPS) k_att_dec(con
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(s_full + i, 1);
-      mbar_init(s_free + i, 128);
+      mbar_init(s_free + i, 4 * C::SG);
     }
     for (int i = 0; i < PB; ++i) {
-      mbar_init(p_full + i, 128);
+      mbar_init(p_full + i, 4 * C::SG);
       mbar_init(pv_done + i, 1);
     }
-    mbar_init(q_full, 128);
-    mbar_init(o_free, 128);
+    mbar_init(q_full, 4 * C::SG);
+    mbar_init(o_free, 4 * C::SG);
     mbar_init(done, 1);
     mbar_fence_init();
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&p.tmk)) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&p.tmv)) : "memory");
   }
   if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(smem_u32(misc + 9)),
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(smem_u32(misc + C::LINE + C::SG)),
                  "n"(C::COLS)
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
@@ -139,10 +134,10 @@ __global__ void __launch_bounds__(kDecThreads, DecCfg<D, GM>::CPS) k_att_dec(con
   pdl_trigger();
   LineCut lc;
   tc_fence_before();
-  Walk walk = line_start<kDecThreads>(p, misc, lc);  // passes the CTA-wide barrier
+  Walk walk = line_start<C::THREADS>(p, misc, lc);  // passes the CTA-wide barrier
   tc_fence_after();
   Part q;
-  const unsigned tmem = (unsigned)misc[9];
+  const unsigned tmem = (unsigned)misc[C::LINE + C::SG];
   const int R2 = p.paged ? min(kTcTile, p.page_size) : kTcTile;  // rows per copied box
   const int nb = kTcTile / R2;
   unsigned err = 0;
@@ -289,12 +284,19 @@ __global__ void __launch_bounds__(kDecThreads, DecCfg<D, GM>::CPS) k_att_dec(con
     if (!mbar_wait(done, 0)) timed_out = true;
   } else {
     // ------------------------------------------- softmax, one token a thread
-    const int wq = warp & 3;                     // TMEM lanes [32 wq, 32 wq + 32)
-    const int r = wq * 32 + lane, st = tid - 64; // token row of a tile; index among these threads
+    const int sg = C::SG == 1 ? 0 : (tid - 64) >> 7, wq = warp & 3;  // group; its warp's TMEM lanes are [32 wq, 32 wq + 32)
+    const int r = wq * 32 + lane, st = (tid - 64) & 127;  // token row of a tile; index within the group
+    const int h0 = sg * GR;                         // the group's query rows are [h0, h0 + GR)
     const unsigned taddr = tmem + ((unsigned)(wq * 32) << 16);
+    const unsigned scol = taddr + h0, ocol = taddr + C::O_COL + h0;
+    float* redg = red + sg * 4 * GR;
     const float c = p.c_log2;
     const int G = p.G;
-    auto sync = [] { asm volatile("barrier.cta.sync 1, 128;\n" ::: "memory"); };
+    auto sync = [&] { asm volatile("barrier.cta.sync %0, 128;\n" ::"r"(1 + sg) : "memory"); };
+    auto arrive = [&](uint64_t* bar) {  // for this warp
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar);
+    };
     bool dead = false;  // a wait of this thread gave up: skip the work, keep the barriers
     auto wait = [&](uint64_t* bar, unsigned parity) {
       if (!__all_sync(0xffffffffu, !dead && mbar_wait(bar, parity))) dead = true;
@@ -303,167 +305,169 @@ __global__ void __launch_bounds__(kDecThreads, DecCfg<D, GM>::CPS) k_att_dec(con
     };
     int ks = 0, tiles = 0;  // tiles done by this CTA, of the parts before
     while (next_part(p, walk, q)) {
-      const int n = q.u1 - q.u0, rows = q.it.rows;
+      const int n = q.u1 - q.u0;
+      const int rows = min(GR, max(0, q.it.rows - h0));  // of the group
       // ---- rows that see nothing: padding, or all of an item without tiles
       if (q.owner) {
         const int first = q.it.tl.n == 0 ? 0 : rows;
-        for (int i = st; i < (p.R - first) * (D / 8); i += 128) {
-          const int row = first + i / (D / 8);
+        for (int i = st; i < (min(GR, p.R - h0) - first) * (D / 8); i += 128) {
+          const int row = h0 + first + i / (D / 8);
           reinterpret_cast<uint4*>(out_row<__nv_bfloat16>(p, q.b, q.g, row))[i % (D / 8)] = make_uint4(0u, 0u, 0u, 0u);
           if (i % (D / 8) == 0) store_lse(p, q.b, q.g, row, 0.f, 0.f);
         }
       }
       if (n <= 0) continue;
-      // ---- queries, K-major and swizzled.  The products with the last part's
-      // queries are complete: this thread has waited for their S; the barrier
-      // covers the others.
-      sync();
+      // ---- the group's queries, K-major and swizzled.  The products with the
+      // last part's are complete: this thread has waited for their S.
       for (int i = st; i < rows * (D / 8); i += 128) {
-        const int rr = i / (D / 8), cc = i % (D / 8);
+        const int rr = h0 + i / (D / 8), cc = i % (D / 8), tok = row_token(p, rr);
         const uint4 v = *reinterpret_cast<const uint4*>(
-            static_cast<const __nv_bfloat16*>(p.q.data) + (int64_t)q.b * p.q.sb + (int64_t)(rr / G) * p.q.sn +
-            (int64_t)(q.g * G + rr % G) * p.q.sh + 8 * cc);
+            static_cast<const __nv_bfloat16*>(p.q.data) + (int64_t)q.b * p.q.sb + (int64_t)tok * p.q.sn +
+            (int64_t)(q.g * G + rr - tok * G) * p.q.sh + 8 * cc);
         *reinterpret_cast<uint4*>(smem + C::OFF_Q + (cc >> 3) * C::QHALF + rr * 128 + (((cc & 7) ^ (rr & 7)) << 4)) = v;
       }
       fence_proxy_async();  // read by the tensor core
-      mbar_arrive(q_full);
-      const int t0 = q.sq.len - q.sq.n, t1 = t0 + (rows - 1) / G;  // positions of the first and last row
-      float mref[GM], l[GM];
+      arrive(q_full);
+      const int base = q.sq.len - q.sq.n;          // position of new token 0
+      const int t0 = base + row_token(p, h0), t1 = base + row_token(p, h0 + max(0, rows - 1));  // of the group's rows
+      float mref[GR], l[GR];
 #pragma unroll
-      for (int h = 0; h < GM; ++h) {
+      for (int h = 0; h < GR; ++h) {
         mref[h] = -CUDART_INF_F;
         l[h] = 0.f;
       }
       for (int i = 0; i < n; ++i, ++ks) {
         const int sb = ks & 1, pb = ks % PB;
-        float z[C::NQ];
-        if (wait(s_full + sb, (ks >> 1) & 1)) {
-          load_cols(taddr + C::NQ * sb, z);
+        const int j0 = q.it.tl.tile(q.u0 + i) * kTcTile, j = j0 + r;
+        // Which rows see this thread's token, a bit each.
+        uint32_t see = (1u << rows) - 1u;
+        const bool part = j0 + kTcTile - 1 > t0 || !(p.window < 0 || j0 > t1 - p.window || j0 + kTcTile <= p.sinks);
+        if (part) {
+          uint32_t seen = 0;
+          for (int h = 0; h < rows; ++h)
+            if (sees(j, base + row_token(p, h0 + h), p.window, p.sinks)) seen |= 1u << h;
+          see = seen;
+        }
+        float z[16];
+        if (wait(s_full + sb, (ks >> 1) & 1) && rows > 0) {
+          tmem_ld16(scol + C::NQ * sb, z);
         } else {
 #pragma unroll
-          for (int h = 0; h < C::NQ; ++h) z[h] = 0.f;
+          for (int h = 0; h < 16; ++h) z[h] = 0.f;
         }
         tc_fence_before();
-        mbar_arrive(s_free + sb);
-        const int j0 = q.it.tl.tile(q.u0 + i) * kTcTile, j = j0 + r;
+        arrive(s_free + sb);
         const uint32_t bad = bad_ring[(tiles + i) % kBadRing];
-        // Which rows see this thread's token, a bit each.
-        uint32_t see = rows >= 32 ? 0xffffffffu : (1u << rows) - 1u;
-        if (bad || j0 + kTcTile - 1 > t0 || !(p.window < 0 || j0 > t1 - p.window || j0 + kTcTile <= p.sinks)) {
-          uint32_t seen = 0;
-          if (!((bad >> (r / R2)) & 1u))
-            for (int k = 0, bit = 0; bit < rows; ++k, bit += G)
-              if (sees(j, t0 + k, p.window, p.sinks)) seen |= (G >= 32 ? 0xffffffffu : (1u << G) - 1u) << bit;
-          see &= seen;
-        }
-#pragma unroll
-        for (int h = 0; h < GM; ++h) z[h] *= c;
+        if ((bad >> (r / R2)) & 1u) see = 0;
         if (p.weigh && !dead) {
-          float* zr = p.z + (int64_t)(q.b * p.Hkv + q.g) * p.R * p.z_row + j;
+          float* zr = p.z + ((int64_t)(q.b * p.Hkv + q.g) * p.R + h0) * p.z_row + j;
 #pragma unroll
-          for (int h = 0; h < GM; ++h)
-            if (h < rows) zr[(int64_t)h * p.z_row] = (see >> h) & 1u ? z[h] : -CUDART_INF_F;
+          for (int h = 0; h < GR; ++h)
+            if (h < rows) zr[(int64_t)h * p.z_row] = (see >> h) & 1u ? z[h] * c : -CUDART_INF_F;
         }
         bool need = false;
 #pragma unroll
-        for (int h = 0; h < GM; ++h) {
-          if (!((see >> h) & 1u)) z[h] = -CUDART_INF_F;
-          need |= z[h] > mref[h] + 8.f;
+        for (int h = 0; h < GR; ++h) {
+          z[h] = (see >> h) & 1u ? z[h] * c : -CUDART_INF_F;
+          need |= z[h] > mref[h] + kDecRaise;
         }
         int raise;
-        asm volatile("{\n .reg .pred p, q;\n setp.ne.b32 p, %1, 0;\n barrier.cta.red.or.pred q, 1, 128, p;\n selp.s32 %0, 1, 0, q;\n}\n"
-                     : "=r"(raise) : "r"((int)need) : "memory");
+        asm volatile("{\n .reg .pred p, q;\n setp.ne.b32 p, %1, 0;\n barrier.cta.red.or.pred q, %2, 128, p;\n selp.s32 %0, 1, 0, q;\n}\n"
+                     : "=r"(raise) : "r"((int)need), "r"(1 + sg) : "memory");
         if (raise) {
 #pragma unroll
-          for (int h = 0; h < GM; ++h) {
+          for (int h = 0; h < GR; ++h) {
             const float m = warp_max(z[h]);
-            if (lane == 0) red[wq * GM + h] = m;
+            if (lane == 0) redg[wq * GR + h] = m;
           }
           sync();
           // O holds the products of this part's tiles so far: rescale it once
           // the last of them is complete.
           const bool fix = i > 0 && wait(pv_done + (ks - 1) % PB, ((ks - 1) / PB) & 1);
-          float f[GM];
+          float f[GR];
 #pragma unroll
-          for (int h = 0; h < GM; ++h) {
-            const float mn = fmaxf(fmaxf(mref[h], fmaxf(red[h], red[GM + h])), fmaxf(red[2 * GM + h], red[3 * GM + h]));
+          for (int h = 0; h < GR; ++h) {
+            const float mn = fmaxf(fmaxf(mref[h], fmaxf(redg[h], redg[GR + h])), fmaxf(redg[2 * GR + h], redg[3 * GR + h]));
             f[h] = mref[h] == -CUDART_INF_F ? 0.f : fexp2(mref[h] - mn);
             l[h] *= f[h];
             mref[h] = mn;
           }
           if (fix) {
 #pragma unroll
-            for (int k = 0; k < C::NP; k += 16) {
+            for (int k = 0; k < 2 * GR; k += 16) {  // GR = 8: hi and lo side by side
               float o[16];
-              tmem_ld16(taddr + C::O_COL + k, o);
+              tmem_ld16(ocol + (k / GR) * GM, o);
 #pragma unroll
-              for (int h = 0; h < 16; ++h) o[h] *= f[(k + h) % GM];
-              tmem_st16(taddr + C::O_COL + k, o);
+              for (int h = 0; h < 16; ++h) o[h] *= f[h % GR];
+              tmem_st16(ocol + (k / GR) * GM, o);
             }
           }
-          sync();  // red is read before its next use
+          sync();  // redg is read before its next use
         }
         if (ks >= PB && !dead) wait(pv_done + pb, ((ks / PB) & 1) ^ 1);  // P buffer free
-        unsigned char* pt = smem + C::OFF_P + pb * C::PBUF + (r >> 6) * C::PHALF + (r & 7) * 2;
+        if (rows > 0) {
+          unsigned char* pt = smem + C::OFF_P + pb * C::PBUF + (r >> 6) * C::PHALF + h0 * 128 + (r & 7) * 2;
 #pragma unroll
-        for (int h = 0; h < GM; ++h) {
-          const float mu = mref[h] == -CUDART_INF_F ? 0.f : mref[h];
-          const float pe = fexp2(z[h] - mu);
-          l[h] += pe;
-          const __nv_bfloat16 hi = __float2bfloat16_rn(pe), lo = __float2bfloat16_rn(pe - __bfloat162float(hi));
-          const unsigned col = (((r & 63) >> 3) ^ (h & 7)) << 4;
-          *reinterpret_cast<__nv_bfloat16*>(pt + h * 128 + col) = hi;
-          *reinterpret_cast<__nv_bfloat16*>(pt + (GM + h) * 128 + col) = lo;
+          for (int h = 0; h < GR; ++h) {
+            const float mu = mref[h] == -CUDART_INF_F ? 0.f : mref[h];
+            const float pe = fexp2(z[h] - mu);
+            l[h] += pe;
+            const __nv_bfloat16 hi = __float2bfloat16_rn(pe), lo = __float2bfloat16_rn(pe - __bfloat162float(hi));
+            const unsigned col = (((r & 63) >> 3) ^ (h & 7)) << 4;
+            *reinterpret_cast<__nv_bfloat16*>(pt + h * 128 + col) = hi;
+            *reinterpret_cast<__nv_bfloat16*>(pt + (GM + h) * 128 + col) = lo;
+          }
         }
         fence_proxy_async();
         tc_fence_before();
-        mbar_arrive(p_full + pb);
+        arrive(p_full + pb);
       }
       tiles += n;
       // ---- the rows' sums over the threads, then their output or this CTA's
       // record of it.  A thread holds dimension d of O.
       sync();
 #pragma unroll
-      for (int h = 0; h < GM; ++h) {
+      for (int h = 0; h < GR; ++h) {
         const float s = warp_sum(l[h]);
-        if (lane == 0) red[wq * GM + h] = s;
+        if (lane == 0) redg[wq * GR + h] = s;
       }
-      float o[C::NP];
+      float o[2 * GR];  // hi, lo
       if (wait(pv_done + (ks - 1) % PB, ((ks - 1) / PB) & 1)) {
 #pragma unroll
-        for (int k = 0; k < C::NP; k += 16) tmem_ld16(taddr + C::O_COL + k, *reinterpret_cast<float (*)[16]>(o + k));
+        for (int k = 0; k < 2 * GR; k += 16) tmem_ld16(ocol + (k / GR) * GM, *reinterpret_cast<float (*)[16]>(o + k));
       } else {
 #pragma unroll
-        for (int k = 0; k < C::NP; ++k) o[k] = 0.f;
+        for (int k = 0; k < 2 * GR; ++k) o[k] = 0.f;
       }
       tc_fence_before();
-      mbar_arrive(o_free);
+      arrive(o_free);
       sync();
+      if (rows <= 0) continue;
       const bool direct = q.whole();
       const int c0 = lc.owner(q.first);
-      auto rec_of = [&](int cta) { return 2 * cta + (cta == c0 ? 1 : 0); };
+      auto rec_of = [&](int cta) { return (2 * cta + (cta == c0 ? 1 : 0)) * C::SG + sg; };
       // D = 64: an M = 64 accumulator holds rows 16 w .. 16 w + 15 in the first
       // 16 lanes of warp w.
       const int d = D == 128 ? r : 16 * wq + (lane & 15);
       const bool mine = D == 128 || lane < 16;
 #pragma unroll
-      for (int h = 0; h < GM; ++h) {
+      for (int h = 0; h < GR; ++h) {
         if (h >= rows) continue;
-        const float sum = (red[h] + red[GM + h]) + (red[2 * GM + h] + red[3 * GM + h]);
-        const float x = o[h] + o[GM + h];
+        const float sum = (redg[h] + redg[GR + h]) + (redg[2 * GR + h] + redg[3 * GR + h]);
+        const float x = o[h] + o[GR + h];
         if (direct) {
-          if (mine) out_row<__nv_bfloat16>(p, q.b, q.g, h)[d] = __float2bfloat16_rn(sum > 0.f ? x / sum : 0.f);
-          if (st == 0) store_lse(p, q.b, q.g, h, mref[h], sum);
+          if (mine) out_row<__nv_bfloat16>(p, q.b, q.g, h0 + h)[d] = __float2bfloat16_rn(sum > 0.f ? x / sum : 0.f);
+          if (st == 0) store_lse(p, q.b, q.g, h0 + h, mref[h], sum);
         } else {
-          const int64_t at = (int64_t)rec_of(blockIdx.x) * GM + h;
+          const int64_t at = (int64_t)rec_of(blockIdx.x) * GR + h;
           if (mine) p.part_o[at * D + d] = x;
           if (st == 0) *reinterpret_cast<float2*>(p.part_st + 2 * at) = make_float2(mref[h], sum);
         }
       }
       if (direct) continue;
       const int parts = lc.owner(q.last) - c0 + 1;
-      if (last_to_arrive(p.tickets + c0, parts, st, misc + 8, sync))
-        join_records<__nv_bfloat16, D, 128>(p, q.b, q.g, 0, rows, parts, GM, [&](int k) { return rec_of(c0 + k); }, st);
+      if (last_to_arrive(p.tickets + c0 * C::SG + sg, parts, st, misc + C::LINE + sg, sync))
+        join_records<__nv_bfloat16, D, 128>(p, q.b, q.g, h0, rows, parts, GR, [&](int k) { return rec_of(c0 + k); }, st);
     }
     if (dead) timed_out = true;
   }
@@ -481,14 +485,15 @@ __global__ void __launch_bounds__(kDecThreads, DecCfg<D, GM>::CPS) k_att_dec(con
 
 template <int D, int GM>
 cudaError_t launch_dec_d(const AttendParams& p, cudaStream_t st) {
-  return launch_dep(k_att_dec<D, GM>, dim3(p.grid), kDecThreads, DecCfg<D, GM>::SMEM, st, p);
+  return launch_dep(k_att_dec<D, GM>, dim3(p.grid), DecCfg<D, GM>::THREADS, DecCfg<D, GM>::SMEM, st, p);
 }
 
 template <int D>
 cudaError_t launch_dec_r(const AttendParams& p, cudaStream_t st) {
   if (p.R <= 8) return launch_dec_d<D, 8>(p, st);
   if (p.R <= 16) return launch_dec_d<D, 16>(p, st);
-  return launch_dec_d<D, 32>(p, st);
+  if (p.R <= 32) return launch_dec_d<D, 32>(p, st);
+  return launch_dec_d<D, 64>(p, st);
 }
 
 template <int D, int GM>
@@ -502,6 +507,8 @@ cudaError_t configure_dec() {
   cudaError_t e = set_dec_smem<128, 8>();
   if (e == cudaSuccess) e = set_dec_smem<128, 16>();
   if (e == cudaSuccess) e = set_dec_smem<128, 32>();
+  if (e == cudaSuccess) e = set_dec_smem<128, 64>();
+  if (e == cudaSuccess) e = set_dec_smem<64, 64>();
   if (e == cudaSuccess) e = set_dec_smem<64, 8>();
   if (e == cudaSuccess) e = set_dec_smem<64, 16>();
   if (e == cudaSuccess) e = set_dec_smem<64, 32>();

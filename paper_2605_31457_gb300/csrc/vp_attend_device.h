@@ -54,6 +54,8 @@ struct Walk {
   int g, pair, off;
   int64_t pos;
   int left;
+  NewSeq sq;        // of the first item
+  bool known;
 };
 // The next item a CTA does, or its share of it (the same in every lane of a
 // converged warp, which calls it together): tiles [u0, u1) of the list.
@@ -70,9 +72,10 @@ __device__ __forceinline__ bool next_part(const AttendParams& p, Walk& w, Part& 
   if (w.left <= 0) return false;
   q.g = w.g;
   q.b = w.pair / p.nqt;
-  q.sq = load_new(p, q.b, false);
-  q.sq.len = uniform(q.sq.len);
-  q.sq.n = uniform(q.sq.n);
+  if (!w.known) w.sq = load_new(p, q.b, false);
+  w.known = false;
+  q.sq.len = uniform(w.sq.len);
+  q.sq.n = uniform(w.sq.n);
   q.it = att_item(q.sq.len, q.sq.n, p.G, p.block, w.pair - q.b * p.nqt, p.window, p.sinks);
   const int cost = q.it.cost(p.fixed), end = min(cost, w.off + w.left), done = end - w.off;
   q.u0 = q.it.tiles_before(w.off, p.fixed);
@@ -87,15 +90,16 @@ __device__ __forceinline__ bool next_part(const AttendParams& p, Walk& w, Part& 
   return true;
 }
 // Finds this CTA's start: each thread sums the costs of a run of pairs, a block
-// scan gives their places.  misc: NT / 32 + 2 ints of shared memory.
+// scan gives their places.  misc: NT / 32 + 4 ints of shared memory.
 template <int NT>
 __device__ __forceinline__ Walk line_start(const AttendParams& p, int* misc, LineCut& lc) {
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int pairs = p.B * p.nqt, run = (pairs + NT - 1) / NT;
   const int i0 = min(pairs, tid * run), i1 = min(pairs, i0 + run);
+  NewSeq sq{0, 0};  // of the last pair looked at
   auto pair_cost = [&](int i, bool report) {
     const int b = i / p.nqt;
-    const NewSeq sq = load_new(p, b, report && blockIdx.x == 0 && i == b * p.nqt);
+    sq = load_new(p, b, report && blockIdx.x == 0 && i == b * p.nqt);
     return att_item(sq.len, sq.n, p.G, p.block, i - b * p.nqt, p.window, p.sinks).cost(p.fixed);
   };
   int mine = 0;
@@ -116,7 +120,7 @@ __device__ __forceinline__ Walk line_start(const AttendParams& p, int* misc, Lin
   }
   total = uniform(total);
   lc = LineCut((int64_t)total * p.Hkv, gridDim.x);
-  Walk w{0, 0, 0, 0, 0};
+  Walk w{0, 0, 0, 0, 0, {0, 0}, true};
   if ((int)blockIdx.x < lc.nc) {
     w.pos = lc.start(blockIdx.x);
     w.left = (int)(lc.start(blockIdx.x + 1) - w.pos);
@@ -133,10 +137,14 @@ __device__ __forceinline__ Walk line_start(const AttendParams& p, int* misc, Lin
       }
     misc[NT / 32] = i;
     misc[NT / 32 + 1] = at - sum;
+    if (run > 1) sq = load_new(p, i / p.nqt, false);
+    misc[NT / 32 + 2] = sq.len;
+    misc[NT / 32 + 3] = sq.n;
   }
   __syncthreads();
   w.pair = uniform(misc[NT / 32]);
   w.off = uniform(misc[NT / 32 + 1]);
+  w.sq = NewSeq{misc[NT / 32 + 2], misc[NT / 32 + 3]};
   return w;
 }
 

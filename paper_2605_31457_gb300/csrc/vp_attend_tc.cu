@@ -113,7 +113,7 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
   uint64_t* q_full = s_full + 14;                                    // [2] a group's queries loaded (128; NQ = 1: 256)
   uint64_t* done = s_full + 16;                                      // [2] every product of a group complete
   volatile uint32_t* bad_ring = reinterpret_cast<uint32_t*>(smem + C::OFF_BAD);
-  int* misc = reinterpret_cast<int*>(smem + C::OFF_MISC);            // [0, 13) line_start; [13, 14] flags; [15] TMEM
+  int* misc = reinterpret_cast<int*>(smem + C::OFF_MISC);            // [0, 15) line_start; [15, 16] flags; [17] TMEM
 
   if (tid == 0) {
     for (int i = 0; i < S; ++i) {
@@ -135,7 +135,7 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&p.tmv)) : "memory");
   }
   if (warp == 9) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;\n" ::"r"(smem_u32(misc + 15))
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;\n" ::"r"(smem_u32(misc + 17))
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
   }
@@ -146,7 +146,7 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
   Walk walk = line_start<kAttThreads>(p, misc, lc);  // passes the CTA-wide barrier
   tc_fence_after();
   Part q;
-  const unsigned tmem = (unsigned)uniform(misc[15]);  // columns [0, 128), [128, 256): S / P; from 256: O of the groups
+  const unsigned tmem = (unsigned)uniform(misc[17]);  // columns [0, 128), [128, 256): S / P; from 256: O of the groups
   const int R2 = p.paged ? min(kTcTile, p.page_size) : kTcTile;  // rows per copied box
   const int nb = kTcTile / R2;
   unsigned err = 0;
@@ -553,7 +553,7 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
       // NQ = 1: the records of both groups of every CTA; NQ = 2: this group's rows.
       const int parts = lc.owner(q.last) - c0 + 1;
       auto sync = [&] { asm volatile("barrier.cta.sync %0, 128;\n" ::"r"(2 + s) : "memory"); };
-      if (last_to_arrive(p.tickets + 2 * c0 + (NQ == 2 ? s : 0), NQ == 1 ? 2 * parts : parts, r, misc + 13 + s, sync)) {
+      if (last_to_arrive(p.tickets + 2 * c0 + (NQ == 2 ? s : 0), NQ == 1 ? 2 * parts : parts, r, misc + 15 + s, sync)) {
         if (NQ == 1)
           join_records<__nv_bfloat16, D, 128>(p, q.b, q.g, 0, q.it.rows, 2 * parts, kTcTile,
                                               [&](int k) { return rec_of(c0 + (k >> 1), k & 1); }, r);

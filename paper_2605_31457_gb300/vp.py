@@ -212,7 +212,9 @@ def vp_compact_kv(ctx, batch, src: vp_kv, dst: vp_kv, visual_span: vp_span, text
 def _stream(stream):
     if stream is None:
         import torch
-        stream = torch.cuda.current_stream().cuda_stream
+        # The handle of torch.cuda.current_stream(), without making the object:
+        # a decode step calls this once per layer.
+        stream = torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     elif hasattr(stream, "cuda_stream"):
         stream = stream.cuda_stream
     return ctypes.c_void_p(stream)
