@@ -286,6 +286,10 @@ void plan_attend(AttendParams& p) {
   p.block = p.kind == ATT_TC2 ? 2 * kTcTile : p.R;
   p.nqt = (p.R + p.block - 1) / p.block;
   p.fixed = (p.kind == ATT_DEC ? 1 : 2) * kTileUnits;
+  if (line_bound((int64_t)p.B * p.Hkv * p.nqt, p.max_seq, p.fixed) > INT32_MAX) {
+    p.kind = ATT_ANY;
+    return;
+  }
   p.grid = p.kind == ATT_DEC && p.R <= 16 ? 2 * p.num_sms : p.num_sms;  // CTAs per SM
 }
 

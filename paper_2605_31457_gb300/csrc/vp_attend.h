@@ -167,23 +167,37 @@ __host__ __device__ inline AttItem att_item(int len, int n, int G, int block, in
 }
 // A line of `total` positions cut for at most `ctas` CTAs: CTA c owns
 // [start(c), start(c + 1)); the first `extra` of them own one position more.  A
-// CTA does the tiles that start in its part, which is at least a tile long, so
-// that every CTA between those of an item's first and last tile has one of them.
+// CTA does the tiles that start in its part.  Parts are longer than a tile, so
+// every CTA between those of an item's first and last tile has one of them.
 struct LineCut {
   int nc, per, extra;
   __host__ __device__ LineCut() {}
-  __host__ __device__ LineCut(int64_t total, int ctas) {
-    const int64_t most = total > kSplitUnits ? total / kSplitUnits : 1;
-    nc = most < ctas ? (int)most : ctas;
-    per = (int)(total / nc);
-    extra = (int)(total - (int64_t)per * nc);
+  __host__ __device__ LineCut(int total, int ctas) {
+    const int most = total > kSplitUnits ? total / kSplitUnits : 1;
+    nc = most < ctas ? most : ctas;
+    per = total / nc;
+    extra = total - per * nc;
   }
-  __host__ __device__ int64_t start(int c) const { return (int64_t)c * per + (c < extra ? c : extra); }
-  __host__ __device__ int owner(int64_t x) const {
-    const int64_t big = (int64_t)extra * (per + 1);
-    return x < big ? (int)(x / (per + 1)) : extra + (int)((x - big) / per);
+  __host__ __device__ int start(int c) const { return c * per + (c < extra ? c : extra); }
+  __host__ __device__ int owner(int x) const {
+    const int big = extra * (per + 1);
+    return x < big ? (int)((unsigned)x / (unsigned)(per + 1)) : extra + (int)((unsigned)(x - big) / (unsigned)per);
   }
 };
+// Few items (at most a quarter as many as CTAs) are not cut as one line: each
+// gets CTAs of its own, share_count of them, so that no CTA does the end of one
+// item and then the beginning of another while the rest wait (one sequence of
+// 3857 tokens, 28/4 heads: 17.1 -> 15.4 us a call; with up to half as many items
+// as CTAs, 32 sequences of 2816 to 6400 tokens went from 66 to 73 us).  Share k of m is [cost * k / m,
+// cost * (k + 1) / m): at least half of `per` >= min_share(fixed), which covers
+// the fixed part and a tile, so every share has a tile.
+__host__ __device__ inline int min_share(int fixed) { return 2 * (fixed > kSplitUnits ? fixed + 1 : kSplitUnits); }
+__host__ __device__ inline int share_count(int cost, int per) { return (cost + per - 1) / per; }
+
+// The longest line a call can have (it is kept below 2^31).
+inline int64_t line_bound(int64_t items, int max_seq, int fixed) {
+  return items * (fixed + (int64_t)kSplitUnits * ((max_seq + kTcTile - 1) / kTcTile + 1));
+}
 
 // Splits of k_att_any: enough CTAs for four per SM, at least two tiles each.
 inline int any_splits(int B, int Hkv, int R, int rows, int n_new, int window, int sinks, int max_seq, int num_sms) {

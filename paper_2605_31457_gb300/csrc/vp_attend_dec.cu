@@ -66,7 +66,7 @@ struct DecCfg {
   static constexpr int OFF_BAR = OFF_P + PB * PBUF;
   static constexpr int NBAR = 2 * S + 2 + 2 + PB + PB + 3;  // full, empty, s_full, s_free, p_full, pv_done, q_full, o_free, done
   static constexpr int OFF_BAD = OFF_BAR + NBAR * 8;   // unmapped boxes of a tile, one bit each
-  static constexpr int LINE = THREADS / 32 + 4;        // ints of line_start
+  static constexpr int LINE = THREADS / 32 + 7;        // ints of line_start
   static constexpr int OFF_MISC = OFF_BAD + kBadRing * 4;     // int: line_start, flags, TMEM base
   static constexpr int OFF_RED = OFF_MISC + (LINE + SG + 1) * 4;  // float [SG][4][GR]: maxima, then sums
   static constexpr size_t SMEM = 1024 + (size_t)OFF_RED + 4 * GM * 4;
@@ -132,9 +132,8 @@ __global__ void __launch_bounds__(DecCfg<D, GM>::THREADS, DecCfg<D, GM>::CPS) k_
   }
   pdl_wait();
   pdl_trigger();
-  LineCut lc;
   tc_fence_before();
-  Walk walk = line_start<C::THREADS>(p, misc, lc);  // passes the CTA-wide barrier
+  Walk walk = line_start<C::THREADS>(p, misc);  // passes the CTA-wide barrier
   tc_fence_after();
   Part q;
   const unsigned tmem = (unsigned)misc[C::LINE + C::SG];
@@ -444,7 +443,7 @@ __global__ void __launch_bounds__(DecCfg<D, GM>::THREADS, DecCfg<D, GM>::CPS) k_
       sync();
       if (rows <= 0) continue;
       const bool direct = q.whole();
-      const int c0 = lc.owner(q.first);
+      const int c0 = q.c0;
       auto rec_of = [&](int cta) { return (2 * cta + (cta == c0 ? 1 : 0)) * C::SG + sg; };
       // D = 64: an M = 64 accumulator holds rows 16 w .. 16 w + 15 in the first
       // 16 lanes of warp w.
@@ -465,9 +464,8 @@ __global__ void __launch_bounds__(DecCfg<D, GM>::THREADS, DecCfg<D, GM>::CPS) k_
         }
       }
       if (direct) continue;
-      const int parts = lc.owner(q.last) - c0 + 1;
-      if (last_to_arrive(p.tickets + c0 * C::SG + sg, parts, st, misc + C::LINE + sg, sync))
-        join_records<__nv_bfloat16, D, 128>(p, q.b, q.g, h0, rows, parts, GR, [&](int k) { return rec_of(c0 + k); }, st);
+      if (last_to_arrive(p.tickets + c0 * C::SG + sg, q.parts, st, misc + C::LINE + sg, sync))
+        join_records<__nv_bfloat16, D, 128>(p, q.b, q.g, h0, rows, q.parts, GR, [&](int k) { return rec_of(c0 + k); }, st);
     }
     if (dead) timed_out = true;
   }

@@ -36,13 +36,15 @@ __device__ __forceinline__ int row_token(const AttendParams& p, int row) {
 // Output row (new token row / G, query head g * G + row % G) of sequence b.
 template <typename T>
 __device__ __forceinline__ T* out_row(const AttendParams& p, int b, int g, int row) {
-  return static_cast<T*>(p.out.data) + (int64_t)b * p.out.sb + (int64_t)(row / p.G) * p.out.sn +
-         (int64_t)(g * p.G + row % p.G) * p.out.sh;
+  const int tok = row_token(p, row);
+  return static_cast<T*>(p.out.data) + (int64_t)b * p.out.sb + (int64_t)tok * p.out.sn +
+         (int64_t)(g * p.G + row - tok * p.G) * p.out.sh;
 }
 // The log-sum-exp of a row from its maximum (log2 units) and sum.
 __device__ __forceinline__ void store_lse(const AttendParams& p, int b, int g, int row, float m, float l) {
   const float x = l > 0.f ? m + log2f(l) : -CUDART_INF_F;
-  if (p.lse) p.lse[((int64_t)b * p.n_new + row / p.G) * p.H + g * p.G + row % p.G] = x * kLn2;
+  const int tok = row_token(p, row);
+  if (p.lse) p.lse[((int64_t)b * p.n_new + tok) * p.H + g * p.G + row - tok * p.G] = x * kLn2;
   if (p.weigh) p.lse2[(int64_t)(b * p.Hkv + g) * p.R + row] = l > 0.f ? x : CUDART_INF_F;
 }
 
@@ -50,20 +52,21 @@ __device__ __forceinline__ void store_lse(const AttendParams& p, int b, int g, i
 
 // A CTA's place on it: the item (kv-head g, pair = sequence * nqt + row block)
 // and the position within the item, its position on the line, positions left.
+// With `shares` set the CTA has one part, share_at of an item's `shares`.
 struct Walk {
   int g, pair, off;
-  int64_t pos;
-  int left;
+  int pos, left;
+  int shares, share_at;
   NewSeq sq;        // of the first item
   bool known;
+  LineCut lc;
 };
 // The next item a CTA does, or its share of it (the same in every lane of a
 // converged warp, which calls it together): tiles [u0, u1) of the list.
 struct Part {
   int g, b, u0, u1;
   bool owner;       // this CTA holds the item's first position: it answers for an item without tiles
-  int64_t first;    // the item's first tile on the line, and its last
-  int64_t last;
+  int c0, parts;    // the item's tiles lie with CTAs [c0, c0 + parts)
   NewSeq sq;
   AttItem it;
   __device__ bool whole() const { return u0 == 0 && u1 == it.tl.n; }
@@ -71,7 +74,7 @@ struct Part {
 __device__ __forceinline__ bool next_part(const AttendParams& p, Walk& w, Part& q) {
   if (w.left <= 0) return false;
   q.g = w.g;
-  q.b = w.pair / p.nqt;
+  q.b = p.nqt == 1 ? w.pair : w.pair / p.nqt;
   if (!w.known) w.sq = load_new(p, q.b, false);
   w.known = false;
   q.sq.len = uniform(w.sq.len);
@@ -81,70 +84,121 @@ __device__ __forceinline__ bool next_part(const AttendParams& p, Walk& w, Part& 
   q.u0 = q.it.tiles_before(w.off, p.fixed);
   q.u1 = q.it.tiles_before(end, p.fixed);
   q.owner = w.off == 0;
-  q.first = w.pos - w.off + p.fixed;
-  q.last = q.first + (int64_t)(q.it.tl.n - 1) * q.it.unit();
+  if (w.shares) {
+    q.c0 = blockIdx.x - w.share_at;
+    q.parts = w.shares;
+  } else if (q.whole()) {
+    q.c0 = blockIdx.x;
+    q.parts = 1;
+  } else {
+    const int first = w.pos - w.off + p.fixed;
+    q.c0 = w.lc.owner(first);
+    q.parts = w.lc.owner(first + (q.it.tl.n - 1) * q.it.unit()) - q.c0 + 1;
+  }
   w.left -= done;
   w.pos += done;
   w.off = 0;
   if (++w.pair == p.B * p.nqt) { w.pair = 0; ++w.g; }
   return true;
 }
-// Finds this CTA's start: each thread sums the costs of a run of pairs, a block
-// scan gives their places.  misc: NT / 32 + 4 ints of shared memory.
+// The sum over the block's NT threads before this one, and over all of them.
 template <int NT>
-__device__ __forceinline__ Walk line_start(const AttendParams& p, int* misc, LineCut& lc) {
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int pairs = p.B * p.nqt, run = (pairs + NT - 1) / NT;
-  const int i0 = min(pairs, tid * run), i1 = min(pairs, i0 + run);
-  NewSeq sq{0, 0};  // of the last pair looked at
-  auto pair_cost = [&](int i, bool report) {
-    const int b = i / p.nqt;
-    sq = load_new(p, b, report && blockIdx.x == 0 && i == b * p.nqt);
-    return att_item(sq.len, sq.n, p.G, p.block, i - b * p.nqt, p.window, p.sinks).cost(p.fixed);
-  };
-  int mine = 0;
-  for (int i = i0; i < i1; ++i) mine += pair_cost(i, true);
-  int incl = mine;
+__device__ __forceinline__ int block_scan(int x, int* warps, int& total) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  int incl = x;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
     const int y = __shfl_up_sync(0xffffffffu, incl, o);
     if (lane >= o) incl += y;
   }
-  if (lane == 31) misc[warp] = incl;
   __syncthreads();
-  int before = incl - mine, total = 0;
-#pragma unroll
+  if (lane == 31) warps[warp] = incl;
+  __syncthreads();
+  int before = incl - x;
+  total = 0;
   for (int w = 0; w < NT / 32; ++w) {
-    if (w < warp) before += misc[w];
-    total += misc[w];
+    if (w < warp) before += warps[w];
+    total += warps[w];
   }
-  total = uniform(total);
-  lc = LineCut((int64_t)total * p.Hkv, gridDim.x);
-  Walk w{0, 0, 0, 0, 0, {0, 0}, true};
-  if ((int)blockIdx.x < lc.nc) {
-    w.pos = lc.start(blockIdx.x);
-    w.left = (int)(lc.start(blockIdx.x + 1) - w.pos);
-    w.g = (int)(w.pos / total);
-  }
-  const int at = (int)(w.pos - (int64_t)w.g * total);
-  if (at >= before && at < before + mine) {
-    int sum = before, i = i0;
-    if (run > 1)
-      for (;; ++i) {
-        const int cost = pair_cost(i, false);
-        if (at < sum + cost) break;
-        sum += cost;
+  return before;
+}
+// Finds this CTA's start: each thread sums the costs of a run of pairs, a block
+// scan gives their places.  misc: NT / 32 + 7 ints of shared memory.
+template <int NT>
+__device__ __forceinline__ Walk line_start(const AttendParams& p, int* misc) {
+  const int tid = threadIdx.x, ctas = gridDim.x;
+  const int pairs = p.B * p.nqt, run = (pairs + NT - 1) / NT;
+  const int i0 = min(pairs, tid * run), i1 = min(pairs, i0 + run);
+  int* found = misc + NT / 32;
+  NewSeq sq{0, 0};  // of the last pair looked at
+  auto pair_cost = [&](int i, bool report) {
+    const int b = p.nqt == 1 ? i : i / p.nqt;
+    sq = load_new(p, b, report && blockIdx.x == 0 && i == b * p.nqt);
+    return att_item(sq.len, sq.n, p.G, p.block, i - b * p.nqt, p.window, p.sinks).cost(p.fixed);
+  };
+  int mine = 0;
+  for (int i = i0; i < i1; ++i) mine += pair_cost(i, true);
+  int total;
+  int before = block_scan<NT>(mine, misc, total);
+  Walk w{0, 0, 0, 0, 0, 0, 0, {0, 0}, true, LineCut()};
+  if (pairs * p.Hkv <= ctas / 4 && run == 1) {
+    // Few items: the smallest share that leaves no more shares than CTAs, found
+    // in a few tries between the even share and one that surely does.
+    const int all = total * p.Hkv, low = (all + ctas - 1) / ctas;
+    const int high = (all + ctas - pairs * p.Hkv - 1) / (ctas - pairs * p.Hkv);
+    int per, m = 0, heads;
+    for (int t = 0; t < 4; ++t) {
+      per = max(min_share(p.fixed), low + (high - low) * t / 3);
+      m = tid < pairs ? share_count(mine, per) : 0;
+      before = block_scan<NT>(m, misc, heads);
+      if (heads * p.Hkv <= ctas) break;
+    }
+    w.g = blockIdx.x / heads;
+    const int at = blockIdx.x - w.g * heads;
+    if (tid < pairs && at >= before && at < before + m) {
+      const int k = at - before;
+      found[0] = tid;
+      found[1] = mine * k / m;
+      found[2] = sq.len;
+      found[3] = sq.n;
+      found[4] = m;
+      found[5] = mine * (k + 1) / m - mine * k / m;
+      found[6] = k;
+    }
+    __syncthreads();
+    if (w.g < p.Hkv) {
+      w.left = uniform(found[5]);
+      w.shares = uniform(found[4]);
+      w.share_at = uniform(found[6]);
+    }
+  } else {
+    total = uniform(total);
+    w.lc = LineCut(total * p.Hkv, ctas);
+    if ((int)blockIdx.x < w.lc.nc) {
+      w.pos = w.lc.start(blockIdx.x);
+      w.left = w.lc.start(blockIdx.x + 1) - w.pos;
+      w.g = w.pos / total;
+    }
+    const int at = w.pos - w.g * total;
+    if (at >= before && at < before + mine) {
+      int sum = before, i = i0;
+      if (run > 1) {
+        for (;; ++i) {
+          const int cost = pair_cost(i, false);
+          if (at < sum + cost) break;
+          sum += cost;
+        }
       }
-    misc[NT / 32] = i;
-    misc[NT / 32 + 1] = at - sum;
-    if (run > 1) sq = load_new(p, i / p.nqt, false);
-    misc[NT / 32 + 2] = sq.len;
-    misc[NT / 32 + 3] = sq.n;
+      found[0] = i;
+      found[1] = at - sum;
+      found[2] = sq.len;
+      found[3] = sq.n;
+    }
+    __syncthreads();
   }
-  __syncthreads();
-  w.pair = uniform(misc[NT / 32]);
-  w.off = uniform(misc[NT / 32 + 1]);
-  w.sq = NewSeq{misc[NT / 32 + 2], misc[NT / 32 + 3]};
+  w.pair = uniform(found[0]);
+  w.off = uniform(found[1]);
+  w.sq = NewSeq{found[2], found[3]};
   return w;
 }
 
@@ -155,9 +209,9 @@ __device__ __forceinline__ Walk line_start(const AttendParams& p, int* misc, Lin
 // group that is the last of `expected` to arrive at the ticket.
 template <typename Sync>
 __device__ __forceinline__ bool last_to_arrive(unsigned* ticket, unsigned expected, int tid, int* flag, Sync&& sync) {
-  __threadfence();
   sync();
   if (tid == 0) {
+    __threadfence();  // orders what the barrier made this thread see, too
     const bool last = atomicAdd(ticket, 1u) == expected - 1;
     if (last) *ticket = 0;  // for the next call
     *flag = last;
@@ -169,11 +223,12 @@ __device__ __forceinline__ bool last_to_arrive(unsigned* ticket, unsigned expect
 }
 
 // Joins records rec(0) .. rec(n - 1) of rows [row0, row0 + rows) into out and
-// lse: a thread per row and four dimensions, records read eight at a time.
+// lse: a thread per row and four dimensions, sixteen records in flight (a round
+// trip to L2 each: the join is bound by their number).
 template <typename T, int D, int NT, typename Rec>
 __device__ __forceinline__ void join_records(const AttendParams& p, int b, int g, int row0, int rows, int n, int RS,
                                              Rec&& rec, int tid) {
-  constexpr int C4 = D / 4, U = 8;
+  constexpr int C4 = D / 4, U = 16;
   for (int e = tid; e < rows * C4; e += NT) {
     const int r = e / C4, d = 4 * (e % C4);
     float m = -CUDART_INF_F, l = 0.f;

@@ -67,7 +67,7 @@ struct TcCfg2 {
   static constexpr int NBAR = 2 * S + 18;               // full, empty, s_full, p_full, pv_done, o_free, q_full, done
   static constexpr int OFF_BAD = OFF_BAR + NBAR * 8;    // unmapped boxes of a tile, one bit each
   static constexpr int OFF_MISC = OFF_BAD + kMaskRing * 4;  // int [16]: scan, start, TMEM base
-  static constexpr size_t SMEM = 1024 + (size_t)OFF_MISC + 20 * 4;
+  static constexpr size_t SMEM = 1024 + (size_t)OFF_MISC + 24 * 4;
   static_assert(SMEM <= 232448, "227 KB of shared memory");
   static_assert(S >= 2 * LA, "the K tiles ahead and a V tile fit the ring");
 };
@@ -113,7 +113,7 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
   uint64_t* q_full = s_full + 14;                                    // [2] a group's queries loaded (128; NQ = 1: 256)
   uint64_t* done = s_full + 16;                                      // [2] every product of a group complete
   volatile uint32_t* bad_ring = reinterpret_cast<uint32_t*>(smem + C::OFF_BAD);
-  int* misc = reinterpret_cast<int*>(smem + C::OFF_MISC);            // [0, 15) line_start; [15, 16] flags; [17] TMEM
+  int* misc = reinterpret_cast<int*>(smem + C::OFF_MISC);            // [0, 18) line_start; [18, 19] flags; [20] TMEM
 
   if (tid == 0) {
     for (int i = 0; i < S; ++i) {
@@ -135,18 +135,17 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&p.tmv)) : "memory");
   }
   if (warp == 9) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;\n" ::"r"(smem_u32(misc + 17))
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;\n" ::"r"(smem_u32(misc + 20))
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
   }
   pdl_wait();
   pdl_trigger();
-  LineCut lc;
   tc_fence_before();
-  Walk walk = line_start<kAttThreads>(p, misc, lc);  // passes the CTA-wide barrier
+  Walk walk = line_start<kAttThreads>(p, misc);  // passes the CTA-wide barrier
   tc_fence_after();
   Part q;
-  const unsigned tmem = (unsigned)uniform(misc[17]);  // columns [0, 128), [128, 256): S / P; from 256: O of the groups
+  const unsigned tmem = (unsigned)uniform(misc[20]);  // columns [0, 128), [128, 256): S / P; from 256: O of the groups
   const int R2 = p.paged ? min(kTcTile, p.page_size) : kTcTile;  // rows per copied box
   const int nb = kTcTile / R2;
   unsigned err = 0;
@@ -503,7 +502,7 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
       if (n <= 0 || !group) continue;
       // ---- the others' output, or this CTA's record of it
       const bool direct = NQ == 2 && q.whole();
-      const int c0 = lc.owner(q.first);
+      const int c0 = q.c0;
       auto rec_of = [&](int c, int grp) { return (2 * c + (c == c0 ? 1 : 0)) * 2 + grp; };
       if (have) wait(pv_done + 2 * s + ((ns - 1) & 1), ((ns - 1) >> 1) & 1);
       if (rows_here) {
@@ -551,9 +550,9 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
       }
       if (direct) continue;
       // NQ = 1: the records of both groups of every CTA; NQ = 2: this group's rows.
-      const int parts = lc.owner(q.last) - c0 + 1;
+      const int parts = q.parts;
       auto sync = [&] { asm volatile("barrier.cta.sync %0, 128;\n" ::"r"(2 + s) : "memory"); };
-      if (last_to_arrive(p.tickets + 2 * c0 + (NQ == 2 ? s : 0), NQ == 1 ? 2 * parts : parts, r, misc + 15 + s, sync)) {
+      if (last_to_arrive(p.tickets + 2 * c0 + (NQ == 2 ? s : 0), NQ == 1 ? 2 * parts : parts, r, misc + 18 + s, sync)) {
         if (NQ == 1)
           join_records<__nv_bfloat16, D, 128>(p, q.b, q.g, 0, q.it.rows, 2 * parts, kTcTile,
                                               [&](int k) { return rec_of(c0 + (k >> 1), k & 1); }, r);
