@@ -137,6 +137,7 @@ vp_status vp_init(const vp_config* cfg, vp_ctx** out_ctx) {
   ctx->err = reinterpret_cast<unsigned*>(base + L.o_err);
   e = cudaMemset(ctx->ws, 0, ctx->ws_bytes);
   if (e == cudaSuccess) e = vp::configure_kernels(c.max_visual, c.num_q_heads, L.nsp_max);
+  if (e == cudaSuccess) e = vp::configure_evict();
   if (e == cudaSuccess) e = cudaDeviceSynchronize();
   if (e != cudaSuccess) {
     vp_status st = cuda_fail(nullptr, "vp_init: workspace set-up failed", e);

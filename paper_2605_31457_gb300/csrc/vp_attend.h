@@ -261,6 +261,7 @@ cudaError_t configure_tc();
 cudaError_t launch_dec(const AttendParams& p, cudaStream_t s);
 cudaError_t launch_tc(const AttendParams& p, cudaStream_t s);
 cudaError_t launch_attend(const AttendParams& p, cudaStream_t s);
+cudaError_t configure_evict();
 cudaError_t launch_evict(const EvictParams& p, cudaStream_t s);
 
 }  // namespace vp

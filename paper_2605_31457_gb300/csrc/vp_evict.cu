@@ -15,8 +15,8 @@ namespace vp {
 namespace {
 
 constexpr int kSelThreads = 1024, kSelWarps = kSelThreads / 32;
-constexpr int kMoveThreads = 256;
-constexpr int kMoveRows = 64;       // destination rows per CTA of k_evict_move, out of place
+constexpr int kMoveThreads = 128;   // and four rows a thread: the best of 1 to 8 rows and 128 to 512 threads
+constexpr int kMoveLoads = 4;       // rows a thread of k_evict_move has in flight, out of place
 constexpr int kInPlaceRows = 8;     // rows a thread of it holds at a time, in place
 constexpr int kBins = 2048;         // 11-bit digits
 
@@ -34,26 +34,28 @@ __device__ __forceinline__ int live_len(const EvictParams& p, int b, bool report
   return min(max(t, 0), p.max_seq);
 }
 
-// Sum over the block; every thread gets it.  red: one int per warp.
-__device__ __forceinline__ int block_sum(int x, int* red) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  x = __reduce_add_sync(0xffffffffu, x);
-  __syncthreads();
-  if (lane == 0) red[warp] = x;
-  __syncthreads();
-  return __reduce_add_sync(0xffffffffu, red[lane]);
-}
-
 // ---------------------------------------------------------------------------
-// k_evict_select: one CTA of 1024 threads per (kept set, sequence).  The m-th
-// largest key of the middle is found by radix select, three passes of 11, 11
-// and 10 bits over the weights (in L2 after the first), a histogram of 2048
-// bins in shared memory each; keys above it stay, and of the equal ones the
+// k_evict_select<KR>: one CTA of 1024 threads per (kept set, sequence).  Each
+// warp owns a contiguous segment of the tokens, each thread every 32nd token of
+// it; their keys are formed once and held, KR per thread in registers or (KR =
+// 0) in shared memory, up to kSelShared of them (KR < 0, longer caches: formed
+// again in every pass).  The m-th largest key of the middle is found by radix
+// select in three passes of 11, 11 and 10 bits, a histogram of 2048 bins each.
+// After the first one a thread holds, a bit per token, which stay for sure and
+// which are in the threshold's bin; only the latter, a few in a hundred, are
+// looked at again.  Keys above the threshold stay, and of the equal ones the
 // first in position, so the result does not depend on any order of atomics.
-// Two passes over contiguous warp segments then count and write the kept
-// positions.  Bound by latency: five passes over T weights by one SM.
+// Bound by instructions and barriers on one SM.  Slower were: 256 bins with a
+// column per lane against queues at one address and four passes (3857 tokens:
+// 10.0 against 7.6 us), one addition per bin and warp after matching the lanes
+// (10.4 us), clusters of eight CTAs that share their histograms through
+// distributed shared memory (20480 tokens: 44 us).
 // ---------------------------------------------------------------------------
+constexpr int kSelShared = 32 * kSelThreads;  // keys held in shared memory, at most: a bit of a word each
+
+template <int KR>
 __global__ void __launch_bounds__(kSelThreads) k_evict_select(const __grid_constant__ EvictParams p) {
+  extern __shared__ uint32_t keys_s[];
   __shared__ int hist[kBins];
   __shared__ int red[kSelWarps];
   __shared__ int seg_kept[kSelWarps], seg_eq[kSelWarps];
@@ -65,101 +67,172 @@ __global__ void __launch_bounds__(kSelThreads) k_evict_select(const __grid_const
   const int T = live_len(p, b, blockIdx.x == 0);
   int32_t* kept = p.kept_idx + ((int64_t)b * (p.granularity ? p.Hkv : 1) + g0) * p.kept_cap;
   const int K = min(T, p.keep);
-  for (int i = K + tid; i < p.kept_cap; i += kSelThreads) kept[i] = -1;
   const float* w0 = p.w.data + (int64_t)b * p.w.sb + (int64_t)g0 * p.w.sh;
-  auto key_of = [&](int j) {
+  float* wd0 = p.wd.data + (int64_t)b * p.wd.sb + (int64_t)g0 * p.wd.sh;
+  for (int i = K + tid; i < p.kept_cap; i += kSelThreads) kept[i] = -1;
+  if (T <= p.keep) {  // every token stays where it is
+    for (int j = tid; j < T; j += kSelThreads) kept[j] = j;
+    if (p.wd.data && !p.in_place)
+      for (int g = 0; g < (p.granularity ? 1 : p.Hkv); ++g)
+        for (int j = tid; j < T; j += kSelThreads) wd0[(int64_t)g * p.wd.sh + j] = w0[(int64_t)g * p.w.sh + j];
+    return;
+  }
+  const int steps = KR > 0 ? KR : (T + kSelThreads - 1) / kSelThreads;
+  const int a = warp * steps * 32 + lane;  // the thread's first token
+  const int lo = p.sinks, hi = T - p.recent;  // the middle to choose from
+  auto weight_at = [&](int j) {
     float w = w0[j];
     if (!p.granularity)
       for (int g = 1; g < p.Hkv; ++g) w += w0[(int64_t)g * p.w.sh + j];
-    return order_key(w);
+    return w;
   };
-  if (T <= p.keep) {
-    for (int i = tid; i < T; i += kSelThreads) kept[i] = i;
-  } else {
-    const int lo = p.sinks, hi = T - p.recent;
-    int m = p.keep - p.sinks - p.recent;  // to choose of the hi - lo > m tokens between
-    uint32_t prefix = 0, mask = 0;        // digits of the threshold found so far
-    int equal = 0;                        // of the keys equal to the threshold, how many stay
-    if (m > 0) {
-      for (int pass = 0; pass < 3; ++pass) {
-        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
-        const uint32_t digits = pass == 2 ? 1023u : 2047u;
-        for (int i = tid; i < kBins; i += kSelThreads) hist[i] = 0;
-        __syncthreads();
-        for (int j = lo + tid; j < hi; j += kSelThreads) {
-          const uint32_t k = key_of(j);
-          if ((k & mask) == prefix) atomicAdd(&hist[(k >> shift) & digits], 1);
-        }
-        __syncthreads();
-        // The bin that holds the m-th largest: thread i owns bins 2i, 2i + 1
-        // counted from the top.
-        const int top = kBins - 1 - 2 * tid;
-        const int h1 = hist[top], h0 = hist[top - 1];
-        int incl = h1 + h0;
+  float held[KR > 0 ? KR : 1];
+  if constexpr (KR > 0) {
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const int y = __shfl_up_sync(0xffffffffu, incl, o);
-          if (lane >= o) incl += y;
+    for (int i = 0; i < KR; ++i) held[i] = a + 32 * i < T ? weight_at(a + 32 * i) : 0.f;
+  } else if constexpr (KR == 0) {  // a thread reads back only what it wrote
+#pragma unroll 8
+    for (int j = a; j < min(T, a + 32 * steps); j += 32) keys_s[j] = order_key(weight_at(j));
+  }
+  // Calls f(step, key) for this thread's tokens of the middle, of those in `bits` where there is one.
+  auto each = [&](uint32_t bits, auto&& f) {
+    if constexpr (KR > 0) {
+#pragma unroll
+      for (int i = 0; i < KR; ++i)
+        if (((bits >> i) & 1u) && a + 32 * i >= lo && a + 32 * i < hi) f(i, order_key(held[i]));
+    } else if constexpr (KR == 0) {
+      if (bits == 0xffffffffu) {
+#pragma unroll 4
+        for (int i = 0; i < steps; ++i) {
+          const int j = a + 32 * i;
+          if (j >= lo && j < hi) f(i, keys_s[j]);
         }
-        if (lane == 31) red[warp] = incl;
-        __syncthreads();
-        const int before = __reduce_add_sync(0xffffffffu, lane < warp ? red[lane] : 0);
-        const int ex = before + incl - h1 - h0;  // keys in higher bins
-        if (ex < m && m <= ex + h1) { bin_s = top; above_s = ex; }
-        else if (ex + h1 < m && m <= ex + h1 + h0) { bin_s = top - 1; above_s = ex + h1; }
-        __syncthreads();
-        m -= above_s;
-        prefix |= (uint32_t)bin_s << shift;
-        mask |= digits << shift;
-        __syncthreads();
+      } else {
+        for (uint32_t c = bits; c; c &= c - 1) {
+          const int i = __ffs(c) - 1;
+          f(i, keys_s[a + 32 * i]);
+        }
       }
-      equal = m;
+    } else {
+      for (int i = 0; i < steps; ++i) {
+        const int j = a + 32 * i;
+        if (j >= lo && j < hi) f(i, order_key(weight_at(j)));
+      }
     }
-    // Each warp takes a contiguous segment: counts, block scan, then writes.
-    const int seg = ((T + kSelThreads - 1) / kSelThreads) * 32;
-    const int a = min(T, warp * seg), z = min(T, a + seg);
-    const bool any = p.keep > p.sinks + p.recent;
-    auto classify = [&](int j, bool& above, bool& eq) {
-      above = eq = false;
-      if (j >= z) return;
-      if (j < lo || j >= hi) { above = true; return; }
-      if (!any) return;
-      const uint32_t k = key_of(j);
-      above = k > prefix;
-      eq = k == prefix;
-    };
-    int ng = 0, ne = 0;
-    for (int j = a + lane; j - lane < z; j += 32) {
-      bool above, eq;
-      classify(j, above, eq);
-      ng += __popc(__ballot_sync(0xffffffffu, above));
-      ne += __popc(__ballot_sync(0xffffffffu, eq));
+  };
+  int m = p.keep - p.sinks - p.recent;  // how many of the middle stay
+  uint32_t prefix = 0, mask = 0;        // digits of the threshold found so far
+  uint32_t up = 0, cand = 0xffffffffu;  // a bit per step: stays for sure; may be equal to the threshold
+  const bool any = m > 0;
+  if (any) {
+    for (int pass = 0; pass < 3; ++pass) {
+      const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
+      const uint32_t digits = pass == 2 ? 1023u : 2047u;
+      for (int i = tid; i < kBins; i += kSelThreads) hist[i] = 0;
+      __syncthreads();
+      each(cand, [&](int, uint32_t k) {
+        if ((k & mask) == prefix) atomicAdd(&hist[(k >> shift) & digits], 1);
+      });
+      __syncthreads();
+      // The bin that holds the m-th largest: thread i owns bins 2i, 2i + 1
+      // counted from the top.
+      const int top = kBins - 1 - 2 * tid;
+      const int h1 = hist[top], h0 = hist[top - 1];
+      int incl = h1 + h0;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += y;
+      }
+      if (lane == 31) red[warp] = incl;
+      __syncthreads();
+      const int before = __reduce_add_sync(0xffffffffu, lane < warp ? red[lane] : 0);
+      const int ex = before + incl - h1 - h0;  // keys in higher bins
+      if (ex < m && m <= ex + h1) { bin_s = top; above_s = ex; }
+      else if (ex + h1 < m && m <= ex + h1 + h0) { bin_s = top - 1; above_s = ex + h1; }
+      __syncthreads();
+      m -= above_s;
+      prefix |= (uint32_t)bin_s << shift;
+      mask |= digits << shift;
+      if constexpr (KR >= 0) {
+        uint32_t in = 0;
+        each(cand, [&](int i, uint32_t k) {
+          const uint32_t d = k & mask;
+          if (d > prefix) up |= 1u << i;
+          if (d == prefix) in |= 1u << i;
+        });
+        cand = in;
+      }
     }
-    if (lane == 0) { seg_kept[warp] = ng; seg_eq[warp] = ne; }
-    __syncthreads();
-    int eq_before = __reduce_add_sync(0xffffffffu, lane < warp ? seg_eq[lane] : 0);
-    int at = __reduce_add_sync(0xffffffffu, lane < warp ? seg_kept[lane] : 0) + min(eq_before, equal);
-    for (int j = a + lane; j - lane < z; j += 32) {
-      bool above, eq;
-      classify(j, above, eq);
-      const unsigned me = __ballot_sync(0xffffffffu, eq), below = (1u << lane) - 1u;
-      const bool stay = above || (eq && eq_before + __popc(me & below) < equal);
-      const unsigned ms = __ballot_sync(0xffffffffu, stay);
-      if (stay) kept[at + __popc(ms & below)] = j;
-      at += __popc(ms);
-      eq_before += __popc(me);
+  } else {
+    cand = 0;
+  }
+  const int equal = any ? m : 0;  // of the keys equal to the threshold, how many stay
+  // Counts per segment, their scan, then the kept positions in order.
+  auto stays = [&](int i, int j, bool& eq) {  // without ties; eq: equal to the threshold
+    const bool mid = j >= lo && j < hi;
+    if constexpr (KR >= 0) {
+      eq = (cand >> i) & 1u;
+      return (bool)((up >> i) & 1u) || (j < T && !mid);
+    } else {
+      const uint32_t k = mid && any ? order_key(weight_at(j)) : 0u;
+      eq = mid && any && k == prefix;
+      return (mid && any && k > prefix) || (j < T && !mid);
+    }
+  };
+  int ng = 0, ne = 0;
+#pragma unroll 4
+  for (int i = 0; i < steps; ++i) {
+    bool eq;
+    ng += stays(i, a + 32 * i, eq);
+    ne += eq;
+  }
+  ng = __reduce_add_sync(0xffffffffu, ng);
+  ne = __reduce_add_sync(0xffffffffu, ne);
+  if (lane == 0) { seg_kept[warp] = ng; seg_eq[warp] = ne; }
+  __syncthreads();
+  int eq_before = __reduce_add_sync(0xffffffffu, lane < warp ? seg_eq[lane] : 0);
+  int at = __reduce_add_sync(0xffffffffu, lane < warp ? seg_kept[lane] : 0) + min(eq_before, equal);
+  // One kept set per kv-head: the weights go along, from registers (every one
+  // has been read, so also in place) or, out of place, read again.
+  const bool along = p.granularity && p.wd.data && (KR > 0 || !p.in_place);
+  auto emit = [&](int i, int j, float w) {
+    bool eq;
+    const bool sure = stays(i, j, eq);
+    const unsigned me = __ballot_sync(0xffffffffu, eq), below = (1u << lane) - 1u;
+    const bool stay = sure || (eq && eq_before + __popc(me & below) < equal);
+    const unsigned ms = __ballot_sync(0xffffffffu, stay);
+    const int to = at + __popc(ms & below);
+    if (stay && to < K) {
+      kept[to] = j;
+      if (along) wd0[to] = w;
+    }
+    at += __popc(ms);
+    eq_before += __popc(me);
+  };
+  if constexpr (KR > 0) {
+#pragma unroll
+    for (int i = 0; i < KR; ++i) emit(i, a + 32 * i, held[i]);
+  } else {
+    for (int i0 = 0; i0 < steps; i0 += 4) {
+      float w[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) w[k] = along && i0 + k < steps && a + 32 * (i0 + k) < T ? w0[a + 32 * (i0 + k)] : 0.f;
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (i0 + k < steps) emit(i0 + k, a + 32 * (i0 + k), w[k]);
     }
   }
   if (!p.wd.data) return;
-  // The kept weights, moved towards the front: a round's reads come before its
-  // writes, and later rounds read beyond them (kept[i] >= i), so it may be in
-  // place.
+  // Other forms: the kept weights move towards the front; a round's reads come
+  // before its writes, and later rounds read beyond them (kept[i] >= i), so it
+  // may be in place.
   __syncthreads();
-  const int ng = p.granularity ? 1 : p.Hkv;
-  for (int g = 0; g < ng; ++g) {
+  const int heads = p.granularity ? 1 : p.Hkv;
+  for (int g = 0; g < heads; ++g) {
     const float* src = w0 + (int64_t)g * p.w.sh;
-    float* dst = p.wd.data + (int64_t)b * p.wd.sb + (int64_t)(g0 + g) * p.wd.sh;
-    for (int i0 = 0; i0 < K; i0 += kSelThreads) {
+    float* dst = wd0 + (int64_t)g * p.wd.sh;
+    for (int i0 = 0; i0 < (along ? 0 : K); i0 += kSelThreads) {
       const int i = i0 + tid;
       float x = 0.f;
       if (i < K) x = src[kept[i]];
@@ -171,28 +244,34 @@ __global__ void __launch_bounds__(kSelThreads) k_evict_select(const __grid_const
   }
 }
 
-// Bytes of row (b, g, j) of a cache; NULL where its page is unmapped.
-__device__ __forceinline__ char* row_bytes(const EvictParams& p, const KvView& kv, int b, int g, int j) {
-  char* base = static_cast<char*>(const_cast<void*>(kv.data));
-  int64_t off;
-  if (!kv.block_table) {
-    off = (int64_t)b * kv.sb + (int64_t)g * kv.sh + (int64_t)j * kv.st;
-  } else {
-    const int lp = j >> p.page_shift;
-    const int page = lp < kv.max_pages ? __ldg(kv.block_table + (int64_t)b * kv.max_pages + lp) : -1;
-    if (page < 0 || page >= kv.num_pages) return nullptr;
-    off = (int64_t)page * kv.sb + (int64_t)g * kv.sh + (int64_t)(j & (p.page_size - 1)) * kv.st;
-  }
-  return base + off * p.esz;
+// The page of token j of sequence b, -1 where the block table maps it to none;
+// 0 in a contiguous cache.
+__device__ __forceinline__ int page_of(const EvictParams& p, const KvView& kv, int b, int j) {
+  if ((unsigned)j >= (unsigned)p.max_seq) return -1;  // no position of a kept list lies there
+  if (!kv.block_table) return 0;
+  const int lp = j >> p.page_shift;
+  const int page = lp < kv.max_pages ? __ldg(kv.block_table + (int64_t)b * kv.max_pages + lp) : -1;
+  return page < kv.num_pages ? page : -1;
+}
+// Bytes of row (b, g, j) of a cache, its page known; NULL for page -1.
+__device__ __forceinline__ char* row_bytes(const EvictParams& p, const KvView& kv, int b, int g, int j, int page) {
+  if (page < 0) return nullptr;
+  const int64_t off = kv.block_table
+      ? (int64_t)page * kv.sb + (int64_t)g * kv.sh + (int64_t)(j & (p.page_size - 1)) * kv.st
+      : (int64_t)b * kv.sb + (int64_t)g * kv.sh + (int64_t)j * kv.st;
+  return static_cast<char*>(const_cast<void*>(kv.data)) + off * p.esz;
 }
 
 // ---------------------------------------------------------------------------
 // k_evict_move: one (sequence, kv-head, K or V) per group of CTAs; each thread
-// copies 16-byte pieces.  Out of place a CTA takes 64 destination rows.  In
-// place a CTA takes a column slice of every row, in rounds of destination rows
-// in ascending order: a round's reads come before its writes (a barrier
-// between), and kept[i] >= i, so no row is overwritten before it is read.
-// Bound by HBM: each kept row is read and written once.
+// copies 16-byte pieces.  Out of place a CTA takes a run of destination rows, a
+// thread the same piece of four of them, all four in flight (a form with sixteen
+// rows per thread, lists and pages read ahead, had too few CTAs per SM: 150
+// against 118 us for 512 MB).  In place a CTA takes a column slice of every
+// row, in rounds of destination rows in ascending order: a round's reads come
+// before its writes (a barrier between), and kept[i] >= i, so no row is
+// overwritten before it is read.  Bound by HBM: each kept row is read and written
+// once.
 // ---------------------------------------------------------------------------
 template <bool IN_PLACE>
 __global__ void __launch_bounds__(kMoveThreads) k_evict_move(const __grid_constant__ EvictParams p, int slices,
@@ -215,14 +294,31 @@ __global__ void __launch_bounds__(kMoveThreads) k_evict_move(const __grid_consta
   const int pieces = p.D * p.esz / 16;
   unsigned err = 0;
   if (!IN_PLACE) {
-    const int step = kMoveThreads / pieces, r1 = min(K, (part + 1) * kMoveRows);
-    for (int i = part * kMoveRows + tid / pieces; i < r1; i += step) {
-      const char* s = row_bytes(p, src, b, g, __ldcg(kept + i));
-      char* d = row_bytes(p, dst, b, g, i);
-      uint4 x = make_uint4(0u, 0u, 0u, 0u);
-      if (s) x = *(reinterpret_cast<const uint4*>(s) + tid % pieces);
-      if (d) *(reinterpret_cast<uint4*>(d) + tid % pieces) = x;
-      if (!s || !d) err |= ERR_PAGE;
+    const int step = kMoveThreads / pieces, piece = tid % pieces;
+    const int i0 = part * step * kMoveLoads + tid / pieces;
+    const char* s[kMoveLoads];
+    uint4 x[kMoveLoads];
+#pragma unroll
+    for (int k = 0; k < kMoveLoads; ++k) {
+      const int i = i0 + k * step;
+      s[k] = nullptr;
+      if (i >= K) continue;
+      const int j = __ldcg(kept + i);
+      s[k] = row_bytes(p, src, b, g, j, page_of(p, src, b, j));
+      if (!s[k]) err |= ERR_PAGE;
+    }
+#pragma unroll
+    for (int k = 0; k < kMoveLoads; ++k) {
+      x[k] = make_uint4(0u, 0u, 0u, 0u);
+      if (s[k]) x[k] = __ldcs(reinterpret_cast<const uint4*>(s[k]) + piece);
+    }
+#pragma unroll
+    for (int k = 0; k < kMoveLoads; ++k) {
+      const int i = i0 + k * step;
+      if (i >= K) continue;
+      char* d = row_bytes(p, dst, b, g, i, page_of(p, dst, b, i));
+      if (d) __stcs(reinterpret_cast<uint4*>(d) + piece, x[k]);
+      else err |= ERR_PAGE;
     }
   } else if (K > 0 && __ldcg(kept + K - 1) != K - 1) {  // else every row stays where it is
     const int mine = pieces / slices, step = kMoveThreads / mine;
@@ -237,7 +333,7 @@ __global__ void __launch_bounds__(kMoveThreads) k_evict_move(const __grid_consta
         x[k] = make_uint4(0u, 0u, 0u, 0u);
         moved[k] = j != i;
         if (!moved[k]) continue;
-        const char* s = row_bytes(p, src, b, g, j);
+        const char* s = row_bytes(p, src, b, g, j, page_of(p, src, b, j));
         if (s) x[k] = *(reinterpret_cast<const uint4*>(s) + piece);
         else err |= ERR_PAGE;
       }
@@ -245,7 +341,8 @@ __global__ void __launch_bounds__(kMoveThreads) k_evict_move(const __grid_consta
 #pragma unroll
       for (int k = 0; k < kInPlaceRows; ++k) {
         if (!moved[k]) continue;
-        char* d = row_bytes(p, dst, b, g, i0 + k * step + r);
+        const int i = i0 + k * step + r;
+        char* d = row_bytes(p, dst, b, g, i, page_of(p, dst, b, i));
         if (d) *(reinterpret_cast<uint4*>(d) + piece) = x[k];
         else err |= ERR_PAGE;
       }
@@ -256,10 +353,11 @@ __global__ void __launch_bounds__(kMoveThreads) k_evict_move(const __grid_consta
 }
 
 template <typename... Args>
-cudaError_t launch_dep(void (*kernel)(Args...), dim3 grid, int threads, cudaStream_t st, Args... args) {
+cudaError_t launch_dep(void (*kernel)(Args...), dim3 grid, int threads, size_t smem, cudaStream_t st, Args... args) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -271,8 +369,17 @@ cudaError_t launch_dep(void (*kernel)(Args...), dim3 grid, int threads, cudaStre
 
 }  // namespace
 
+cudaError_t configure_evict() {
+  return cudaFuncSetAttribute(k_evict_select<0>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSelShared * 4);
+}
+
 cudaError_t launch_evict(const EvictParams& p, cudaStream_t st) {
-  cudaError_t e = launch_dep(k_evict_select, dim3(p.granularity ? p.Hkv : 1, p.B), kSelThreads, st, p);
+  const dim3 sets(p.granularity ? p.Hkv : 1, p.B);
+  cudaError_t e;
+  if (p.max_seq <= 4 * kSelThreads) e = launch_dep(k_evict_select<4>, sets, kSelThreads, 0, st, p);
+  else if (p.max_seq <= 8 * kSelThreads) e = launch_dep(k_evict_select<8>, sets, kSelThreads, 0, st, p);
+  else if (p.max_seq <= kSelShared) e = launch_dep(k_evict_select<0>, sets, kSelThreads, (size_t)p.max_seq * 4, st, p);
+  else e = launch_dep(k_evict_select<-1>, sets, kSelThreads, 0, st, p);
   if (e != cudaSuccess) return e;
   const int64_t units = (int64_t)p.B * p.Hkv * 2;
   // In place: column slices of at least 32 bytes (a sector), as many as it
@@ -281,11 +388,12 @@ cudaError_t launch_evict(const EvictParams& p, cudaStream_t st) {
   int slices = 1;
   while (slices * 2 <= pieces / 2 && units * slices < 2 * p.num_sms) slices *= 2;
   const int rows = p.keep < p.max_seq ? p.keep : p.max_seq;
-  const int chunks = (rows + kMoveRows - 1) / kMoveRows;
-  const int64_t ctas = units * (p.in_place ? slices : chunks);
-  if (ctas > INT32_MAX) return cudaErrorInvalidConfiguration;
-  if (ctas == 0) return cudaSuccess;
-  return launch_dep(p.in_place ? k_evict_move<true> : k_evict_move<false>, dim3((unsigned)ctas), kMoveThreads, st, p,
+  const int run = kMoveThreads / pieces * kMoveLoads;
+  const int chunks = (rows + run - 1) / run;
+  const int64_t grid = units * (p.in_place ? slices : chunks);
+  if (grid > INT32_MAX) return cudaErrorInvalidConfiguration;
+  if (grid == 0) return cudaSuccess;
+  return launch_dep(p.in_place ? k_evict_move<true> : k_evict_move<false>, dim3((unsigned)grid), kMoveThreads, 0, st, p,
                     slices, chunks);
 }
 

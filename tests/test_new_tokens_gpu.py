@@ -578,3 +578,11 @@ def test_logits_that_jump_far(lib, dtype, n_new, heads):
                           c.lens[b], c.ns[b]) for b in range(2)]
     assert max(r["lse"].max() for r in c.ref) > 200
     c.run()
+
+
+@pytest.mark.parametrize("longest", [4096, 4097, 8192, 8193, 32768, 32769])
+@pytest.mark.parametrize("granularity,in_place", [(1, False), (1, True), (0, True)])
+def test_evict_cache_lengths(lib, longest, granularity, in_place):
+    """Either side of every length at which the selection changes its form."""
+    _evict(lib, (4, 2), 64, lens=(longest, 3000, 31), keep=2500, sinks=4, recent=100, granularity=granularity,
+           in_place=in_place, weights="whole" if granularity == 0 else "ties")
