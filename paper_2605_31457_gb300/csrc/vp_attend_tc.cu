@@ -36,12 +36,12 @@ namespace {
 // The work is a line of tiles cut evenly over the CTAs (vp_attend.h): an item
 // cut between CTAs leaves partials (m, l, O) that k_att_join merges.
 //
-// Softmax: a row's reference m is the largest logit of the first 32 tokens it
-// sees, and is raised only when a logit passes it by more than 64 (log2 units),
-// when O is rescaled in TMEM: P = exp2(z - m) <= 2^64 has bf16's and float's
-// full precision all the same, and no pass over S for a maximum is needed.  P goes to the tensor cores as bf16,
-// in two terms hi + lo where few tokens share the weight (AttItem::split); l sums the
-// unrounded values.
+// Softmax: a row's reference m is the largest logit of the first 64 tokens it
+// sees, and is raised, O rescaled in TMEM, only when P = exp2(z - m) passes 2^64:
+// up to there P has bf16's and float's full precision all the same, and S is
+// read once.  P goes to the tensor cores as bf16, in two terms hi + lo where few
+// tokens share the weight (AttItem::split); l sums the unrounded values in 32
+// bits.
 //
 // Rows of a tile that nobody sees may hold anything: their logits are masked,
 // and their V rows are zeroed in shared memory before the product (0 x NaN is
@@ -52,7 +52,7 @@ namespace {
 // ---------------------------------------------------------------------------
 constexpr int kAttThreads = 352;
 constexpr int kSub = 64;       // tokens of a softmax step: half a tile
-constexpr float kRaise = 64.f;
+constexpr float kPMost = 18446744073709551616.f;  // 2^64
 constexpr int kMaskRing = 16;  // tiles between the copy warp and the softmax groups, at most
 
 template <int D, int NQ>
@@ -226,106 +226,122 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
     // tile's same half, whose columns it takes, so that the softmax threads have
     // the next S while they form a P.  One warp for both
     // groups spent more time waiting at barriers than the products took.
-    auto wait_all = [&](uint64_t* bar, unsigned parity) {
-      const bool ok = __all_sync(0xffffffffu, mbar_wait(bar, parity));
-      tc_fence_after();
-      return ok;
-    };
+    auto wait = [&](uint64_t* bar, unsigned parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity)); };
     const int leader = elect_one();
     const int s = uniform(warp - 9);
-    int pc = 0, tiles = 0;                     // pieces and tiles of the parts before
-    unsigned parts = 0, tp = 0;                // parts with tiles of this group, its tiles before
+    const unsigned o = tmem + 256 + D * s, pa = tmem + 128 * s;
+    int slot = 0, tiles = 0;                   // the ring's next piece; tiles of the parts before
+    unsigned phase = 0, parts = 0, tp = 0;     // of the ring; parts with tiles of this group, its tiles before
+    // The next piece of the ring.  Every one is waited for, in order, and released
+    // by both warps, the group's own or not: a warp that left some out could take
+    // a later phase of a slot's barrier for the one it waits for.
+    auto take = [&](int& sl) {
+      sl = slot;
+      const bool ok = wait(full + slot, phase);
+      if (++slot == S) { slot = 0; phase ^= 1; }
+      return ok;
+    };
+    auto qk = [&](int half, int ks) {  // by the leader: S of half a tile
+      const uint32_t kd = umma_desc_lo(smem_u32(smem + ks * C::SLOT) + half * kSub * 128, 16);
+      const uint32_t qd = umma_desc_lo(smem_u32(smem + C::OFF_Q + (NQ == 1 ? 0 : s) * C::SLOT), 16);
+      umma_ss<kIdQK, 0>(pa + kSub * half, qd, kd);
+#pragma unroll
+      for (int x = 1; x < D / 16; ++x) {  // 16 dimensions: 32 bytes, every fourth step the next half
+        const uint32_t at = (x >> 2) * (C::HALF / 16) + (x & 3) * 2;
+        umma_ss<kIdQK, 1>(pa + kSub * half, qd + at, kd + at);
+      }
+      umma_commit(s_full + 2 * s + half);
+    };
     while (!timed_out && next_part(p, walk, q)) {
       const int n = q.u1 - q.u0;
       if (n <= 0) continue;
       const int two = NQ == 2 && q.it.rows > kTcTile;  // the second group has rows
       const int split = q.it.split;
-      const int mine = NQ == 2 ? (s == 0 || two ? n : 0) : (n + 1 - s) / 2;  // tiles of this group
-      if (mine > 0) {
-        if (!wait_all(q_full + s, parts & 1)) { timed_out = true; break; }
+      auto own = [&](int t) { return NQ == 2 ? s == 0 || two : (t & 1) == s; };  // tile t is this group's
+      if (NQ == 2 ? s == 0 || two : n > s) {  // it has tiles in this part
+        if (!wait(q_full + s, parts & 1)) { timed_out = true; break; }
         ++parts;
       }
-      // Every piece of the ring is waited for, in order, and released by both
-      // warps, the group's own or not: a warp that left some out could take a
-      // later phase of a slot's barrier for the one it waits for.
-      int at = pc;
-      auto pass = [&](int to) {
-        for (; at < to && !timed_out; ++at) {
-          if (!wait_all(full + at % S, (at / S) & 1)) timed_out = true;
-          else umma_commit_on(leader, empty + at % S);
-        }
-      };
-      // P.V of the group's tile k (the part's tile `tile`), then QK of the next;
-      // a tile's K and V among the pieces in the copy warp's order.  What has
-      // landed is waited for before P is, so that nothing but products stands
-      // between a group's P and its next S.
-#pragma unroll 1
-      for (int k = -1; k < mine && !timed_out; ++k) {
-        const int tile = NQ == 1 ? 2 * k + s : k, next = NQ == 1 ? tile + 2 : tile + 1;
-        const unsigned o = tmem + 256 + D * s, pa = tmem + 128 * s;
-        const bool more = k + 1 < mine;
-        int vs = 0, ks = 0;
-        if (k >= 0) {
-          const int piece = pc + min(tile + LA, n) + tile;
-          vs = piece % S;
-          pass(piece);
-          if (timed_out || !wait_all(full + vs, (piece / S) & 1)) { timed_out = true; break; }
-          ++at;
-          // V rows that no row of the item sees, or of unmapped pages: zero them
-          // before the product reads them (both warps, where both do).
-          const int j0 = q.it.tl.tile(q.u0 + tile) * kTcTile;
-          const uint32_t bad = bad_ring[(tiles + tile) % kMaskRing];
-          const SeenRange& sr = q.it.sr;
-          if (bad || !((j0 >= sr.lo && j0 + kTcTile <= sr.hi) || j0 + kTcTile <= sr.s_end)) {
-#pragma unroll 1
-            for (int r = lane; r < kTcTile; r += 32) {
-              const int j = j0 + r;
-              if ((j < sr.s_end || (j >= sr.lo && j < sr.hi)) && !((bad >> (r / R2)) & 1u)) continue;
-              unsigned char* vr = smem + vs * C::SLOT + r * 128;
-#pragma unroll
-              for (int x = 0; x < C::HALVES * 8; ++x)
-                *reinterpret_cast<uint4*>(vr + (x >> 3) * C::HALF + (x & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
-            }
-            fence_proxy_async();
-            __syncwarp();
+      // The copy warp's order: K of the first LA tiles, then V of a tile and K of
+      // the tile LA later.
+      for (int t = 0; t < min(LA, n); ++t) {
+        int ks;
+        if (!take(ks)) { timed_out = true; break; }
+        if (leader) {
+          if (own(t)) {
+            qk(0, ks);
+            qk(1, ks);
           }
-          if (k == 0 && !wait_all(o_free + s, parts & 1)) { timed_out = true; break; }
+          umma_commit(empty + ks);
         }
-        if (more) {
-          const int piece = pc + next + max(0, next - LA + 1);
-          ks = piece % S;
-          pass(piece);
-          if (timed_out || !wait_all(full + ks, (piece / S) & 1)) { timed_out = true; break; }
-          ++at;
+        __syncwarp();
+      }
+      int mine = 0;  // tiles of this group so far
+#pragma unroll 1
+      for (int t = 0; t < n && !timed_out; ++t) {
+        int vs, ks = -1;
+        if (!take(vs) || (t + LA < n && !take(ks))) { timed_out = true; break; }
+        if (!own(t)) {
+          if (leader) {
+            umma_commit(empty + vs);
+            if (ks >= 0) umma_commit(empty + ks);
+          }
+          __syncwarp();
+          continue;
         }
-        const uint64_t vd = umma_desc(smem_u32(smem + vs * C::SLOT), C::HALF, 1024);
-        const uint64_t kd = umma_desc(smem_u32(smem + ks * C::SLOT), 16, 1024);
-        const uint64_t qd = umma_desc(smem_u32(smem + C::OFF_Q + (NQ == 1 ? 0 : s) * C::SLOT), 16, 1024);
+        // V rows that no row of the item sees, or of unmapped pages: zero them
+        // before the product reads them (both warps, where both do).
+        const int j0 = q.it.tl.tile(q.u0 + t) * kTcTile;
+        const uint32_t bad = bad_ring[(tiles + t) % kMaskRing];
+        const SeenRange& sr = q.it.sr;
+        if (bad || !((j0 >= sr.lo && j0 + kTcTile <= sr.hi) || j0 + kTcTile <= sr.s_end)) {
+#pragma unroll 1
+          for (int r = lane; r < kTcTile; r += 32) {
+            const int j = j0 + r;
+            if ((j < sr.s_end || (j >= sr.lo && j < sr.hi)) && !((bad >> (r / R2)) & 1u)) continue;
+            unsigned char* vr = smem + vs * C::SLOT + r * 128;
+#pragma unroll
+            for (int x = 0; x < C::HALVES * 8; ++x)
+              *reinterpret_cast<uint4*>(vr + (x >> 3) * C::HALF + (x & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+          }
+          fence_proxy_async();
+          __syncwarp();
+        }
+        if (mine == 0 && !wait(o_free + s, parts & 1)) { timed_out = true; break; }
 #pragma unroll 1
         for (int half = 0; half < 2; ++half) {
-          if (k >= 0) {
-            if (!wait_all(p_full + 2 * s + half, (tp + k) & 1)) { timed_out = true; break; }
-            umma4_ts_on(leader, o, pa + kSub * half, vd + half * kSub * 8, kIdPV, k > 0 || half > 0);
-            if (split) umma4_ts_on(leader, o, pa + kSub * half + 16, vd + half * kSub * 8, kIdPV, 1);
-            umma_commit_on(leader, pv_done + 2 * s + half);
+          if (!wait(p_full + 2 * s + half, tp & 1)) { timed_out = true; break; }
+          tc_fence_after();
+          if (leader) {
+            const uint32_t vd = umma_desc_lo(smem_u32(smem + vs * C::SLOT) + half * kSub * 128, C::HALF);
+            const unsigned ph = pa + kSub * half;
+            // 16 tokens a product: 2048 bytes of V
+            if (mine == 0 && half == 0) umma_ts<kIdPV, 0>(o, ph, vd);
+            else umma_ts<kIdPV, 1>(o, ph, vd);
+            umma_ts<kIdPV, 1>(o, ph + 8, vd + 128);
+            umma_ts<kIdPV, 1>(o, ph + 32, vd + 256);
+            umma_ts<kIdPV, 1>(o, ph + 40, vd + 384);
+            if (split) {
+              umma_ts<kIdPV, 1>(o, ph + 16, vd);
+              umma_ts<kIdPV, 1>(o, ph + 24, vd + 128);
+              umma_ts<kIdPV, 1>(o, ph + 48, vd + 256);
+              umma_ts<kIdPV, 1>(o, ph + 56, vd + 384);
+            }
+            umma_commit(pv_done + 2 * s + half);
+            if (ks >= 0) qk(half, ks);
+            if (half) {
+              umma_commit(empty + vs);
+              if (ks >= 0) umma_commit(empty + ks);
+            }
           }
-          if (more) {
-            umma4_on(leader, pa + kSub * half, qd, kd + half * kSub * 8, kIdQK, 0);
-            if (D == 128)  // the other 64 dimensions
-              umma4_on(leader, pa + kSub * half, qd + C::HALF / 16, kd + half * kSub * 8 + C::HALF / 16, kIdQK, 1);
-            umma_commit_on(leader, s_full + 2 * s + half);
-          }
+          __syncwarp();
         }
-        if (timed_out) break;
-        if (more) umma_commit_on(leader, empty + ks);
-        if (k >= 0) umma_commit_on(leader, empty + vs);
+        ++mine;
+        ++tp;
       }
-      pass(pc + 2 * n);
-      tp += mine;
-      pc += 2 * n;
       tiles += n;
     }
-    umma_commit_on(leader, done + s);  // after every product issued above
+    if (leader) umma_commit(done + s);  // after every product issued above
     __syncwarp();
     if (!mbar_wait(done + s, 0)) timed_out = true;
   } else {
@@ -403,28 +419,23 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
           if (rows_here && !dead) {
             // 64 columns of the row of S.  P = exp2(c z - m) goes over them:
             // columns [k, k + 16), k = 0 and 32, take hi of tokens k .. k + 31
-            // and the next 16 lo (with split).  The exponentials are formed with
-            // the reference as it is, next to the maximum that says whether it
-            // must be raised, not after it.  In a rolled loop over the halves:
-            // eleven warps run different code at once, and unrolled over the
-            // whole row this outgrew the instruction cache (the warps that issue
-            // the products then waited for their next instructions, not for data).
+            // and the next 16 lo (with split).  A P past 2^64 shows in their sum,
+            // so no maximum is formed unless the reference must be set or raised;
+            // S is then read again.  In a rolled loop over the halves: eleven
+            // warps run different code at once, and unrolled over the whole row
+            // this outgrew the instruction cache.
             float x[64];
             float (&xa)[32] = *reinterpret_cast<float (*)[32]>(x), (&xb)[32] = *reinterpret_cast<float (*)[32]>(x + 32);
-            tmem_ld_start(taddr + k0, xa);
-            tmem_ld_start(taddr + k0 + 32, xb);
-            tmem_ld_wait(xa);
-            tmem_ld_wait(xb);
-            if (masked) {
-              mask_cols(xa, seen_bits(j0 + k0, t, low, p.sinks, bad, k0, R2));
-              mask_cols(xb, seen_bits(j0 + k0 + 32, t, low, p.sinks, bad, k0 + 32, R2));
-            }
-            if (zr) {
-#pragma unroll
-              for (int k = 0; k < kSub; k += 4)
-                *reinterpret_cast<float4*>(zr + k0 + k) =
-                    make_float4(x[k] * c, x[k + 1] * c, x[k + 2] * c, x[k + 3] * c);
-            }
+            auto load = [&] {
+              tmem_ld_start(taddr + k0, xa);
+              tmem_ld_start(taddr + k0 + 32, xb);
+              tmem_ld_wait(xa);
+              tmem_ld_wait(xb);
+              if (masked) {
+                mask_cols(xa, seen_bits(j0 + k0, t, low, p.sinks, bad, k0, R2));
+                mask_cols(xb, seen_bits(j0 + k0 + 32, t, low, p.sinks, bad, k0 + 32, R2));
+              }
+            };
             uint32_t hi[32];
             float2 s0, s1;
             auto exps = [&] {
@@ -439,19 +450,25 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
                 if (k & 1) s1 = add2(s1, e);
                 else s0 = add2(s0, e);
                 hi[k] = pack_bf16(e.x, e.y);
+                x[2 * k] = e.x;
+                x[2 * k + 1] = e.y;
               }
+              return (s0.x + s0.y) + (s1.x + s1.y);
             };
-            exps();
-            float mx[4];
+            load();
+            if (zr) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              mx[k] = x[k];
-#pragma unroll
-              for (int y = 4; y < kSub; y += 8) mx[k] = fmaxf(fmaxf(mx[k], x[y + k]), y + 4 < kSub ? x[y + 4 + k] : mx[k]);
+              for (int k = 0; k < kSub; k += 4)
+                *reinterpret_cast<float4*>(zr + k0 + k) =
+                    make_float4(x[k] * c, x[k + 1] * c, x[k + 2] * c, x[k + 3] * c);
             }
-            const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c;
-            if (__any_sync(0xffffffffu, valid && top > m + kRaise)) {
-              const float mn = fmaxf(m, top), f = m == -CUDART_INF_F ? 0.f : fexp2(m - mn);
+            float sum = exps();
+            if (__any_sync(0xffffffffu, valid && (m == -CUDART_INF_F || sum > kPMost))) {
+              load();
+              float top = x[0];
+#pragma unroll
+              for (int k = 1; k < kSub; ++k) top = fmaxf(top, x[k]);
+              const float mn = fmaxf(m, top * c), f = m == -CUDART_INF_F ? 0.f : fexp2(m - mn);
               m = mn;
               l *= f;
               // O holds the products of this group's steps so far: rescale it
@@ -466,18 +483,18 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
                   tmem_st16(oaddr + e, o);
                 }
               }
-              exps();
+              sum = exps();
             }
-            l += (s0.x + s0.y) + (s1.x + s1.y);
+            l += sum;
             tmem_st(taddr + k0, *reinterpret_cast<uint32_t (*)[16]>(hi));
             tmem_st(taddr + k0 + 32, *reinterpret_cast<uint32_t (*)[16]>(hi + 16));
             if (split) {
-              const float mu = m == -CUDART_INF_F ? 0.f : m;
 #pragma unroll
               for (int k = 0; k < 32; ++k) {
                 float2 h;
                 bf2(hi[k], h.x, h.y);
-                hi[k] = pack_bf16(fexp2(fmaf(x[2 * k], c, -mu)) - h.x, fexp2(fmaf(x[2 * k + 1], c, -mu)) - h.y);
+                const float2 d = add2(make_float2(x[2 * k], x[2 * k + 1]), make_float2(-h.x, -h.y));
+                hi[k] = pack_bf16(d.x, d.y);
               }
               tmem_st(taddr + k0 + 16, *reinterpret_cast<uint32_t (*)[16]>(hi));
               tmem_st(taddr + k0 + 48, *reinterpret_cast<uint32_t (*)[16]>(hi + 16));

@@ -250,39 +250,26 @@ __device__ __forceinline__ int uniform(int x) { return __reduce_max_sync(0xfffff
 __device__ __forceinline__ int64_t uniform(int64_t x) {
   return (int64_t)uniform((int)(x >> 32)) << 32 | (uint32_t)uniform((int)x);
 }
-// Four products in a row by the lane whose `on` is non-zero, in a warp that runs
-// converged: A and B in shared memory, K-major, 16 elements (32 bytes) a step ...
-__device__ __forceinline__ void umma4_on(int on, unsigned d, uint64_t a, uint64_t b, uint32_t id, int acc) {
-  asm volatile(
-      "{\n .reg .pred p, q, t;\n .reg .b64 a1, a2, a3, b1, b2, b3;\n"
-      " setp.ne.b32 p, %4, 0;\n setp.ne.b32 q, %5, 0;\n setp.eq.u32 t, 0, 0;\n"
-      " add.s64 a1, %1, 2;\n add.s64 b1, %2, 2;\n add.s64 a2, %1, 4;\n add.s64 b2, %2, 4;\n"
-      " add.s64 a3, %1, 6;\n add.s64 b3, %2, 6;\n"
-      " @q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n"
-      " @q tcgen05.mma.cta_group::1.kind::f16 [%0], a1, b1, %3, t;\n"
-      " @q tcgen05.mma.cta_group::1.kind::f16 [%0], a2, b2, %3, t;\n"
-      " @q tcgen05.mma.cta_group::1.kind::f16 [%0], a3, b3, %3, t;\n}\n"
-      ::"r"(d), "l"(a), "l"(b), "r"(id), "r"(acc), "r"(on) : "memory");
+// The low word of umma_desc's descriptor for a stride of 1024 bytes, as the
+// products below take it: their high word is a constant.
+__device__ __forceinline__ uint32_t umma_desc_lo(unsigned addr, unsigned lbo) {
+  return ((addr >> 4) & 0x3fffu) | (((lbo >> 4) & 0x3fffu) << 16);
 }
-// ... and with A in TMEM (lane = row, 32-bit column c holding K elements 2c and
-// 2c + 1), at columns a, a + 8, a + 32, a + 40, and B MN-major in shared memory,
-// 16 rows of 128 bytes a step.
-__device__ __forceinline__ void umma4_ts_on(int on, unsigned d, unsigned a, uint64_t b, uint32_t id, int acc) {
-  asm volatile(
-      "{\n .reg .pred p, q, t;\n .reg .b32 a1, a2, a3;\n .reg .b64 b1, b2, b3;\n"
-      " setp.ne.b32 p, %4, 0;\n setp.ne.b32 q, %5, 0;\n setp.eq.u32 t, 0, 0;\n"
-      " add.u32 a1, %1, 8;\n add.s64 b1, %2, 128;\n add.u32 a2, %1, 32;\n add.s64 b2, %2, 256;\n"
-      " add.u32 a3, %1, 40;\n add.s64 b3, %2, 384;\n"
-      " @q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n"
-      " @q tcgen05.mma.cta_group::1.kind::f16 [%0], [a1], b1, %3, t;\n"
-      " @q tcgen05.mma.cta_group::1.kind::f16 [%0], [a2], b2, %3, t;\n"
-      " @q tcgen05.mma.cta_group::1.kind::f16 [%0], [a3], b3, %3, t;\n}\n"
-      ::"r"(d), "r"(a), "l"(b), "r"(id), "r"(acc), "r"(on) : "memory");
+constexpr uint32_t kDescHi = (1024u >> 4) | (1u << 14) | (2u << 29);
+// One product, its instruction descriptor ID and whether it accumulates known
+// at compile time: both operands in shared memory, or (ts) A in TMEM (lane =
+// row, 32-bit column c holding K elements 2c and 2c + 1).
+template <uint32_t ID, int ACC>
+__device__ __forceinline__ void umma_ss(unsigned d, uint32_t a, uint32_t b) {
+  asm volatile("{\n .reg .pred p;\n .reg .b64 a, b;\n setp.ne.b32 p, %4, 0;\n mov.b64 a, {%1, %5};\n mov.b64 b, {%2, %5};\n"
+               " tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n}\n"
+               ::"r"(d), "r"(a), "r"(b), "n"(ID), "n"(ACC), "n"(kDescHi) : "memory");
 }
-__device__ __forceinline__ void umma_commit_on(int on, uint64_t* bar) {
-  asm volatile("{\n .reg .pred q;\n setp.ne.b32 q, %1, 0;\n"
-               " @q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}\n"
-               ::"r"(smem_u32(bar)), "r"(on) : "memory");
+template <uint32_t ID, int ACC>
+__device__ __forceinline__ void umma_ts(unsigned d, unsigned a, uint32_t b) {
+  asm volatile("{\n .reg .pred p;\n .reg .b64 b;\n setp.ne.b32 p, %4, 0;\n mov.b64 b, {%2, %5};\n"
+               " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n}\n"
+               ::"r"(d), "r"(a), "r"(b), "n"(ID), "n"(ACC), "n"(kDescHi) : "memory");
 }
 // True in one lane of a converged warp.
 __device__ __forceinline__ bool elect_one() {
