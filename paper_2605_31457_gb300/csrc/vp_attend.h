@@ -199,16 +199,22 @@ inline int64_t line_bound(int64_t items, int max_seq, int fixed) {
   return items * (fixed + (int64_t)kSplitUnits * ((max_seq + kTcTile - 1) / kTcTile + 1));
 }
 
-// Splits of k_att_any: enough CTAs for four per SM, at least two tiles each.
+// Splits of k_att_any: those with the least tiles on the longest way through
+// the SMs, a wave being the CTAs that run at once and a CTA's start and end
+// about as long as kAnyFixed tiles; at most 8 CTAs per SM, at least a tile each.
+constexpr int kAnyFixed = 4;
 inline int any_splits(int B, int Hkv, int R, int rows, int n_new, int window, int sinks, int max_seq, int num_sms) {
   const int64_t units = (int64_t)B * Hkv * ((R + rows - 1) / rows);
   int64_t span = max_seq;
   if (window >= 0 && (int64_t)window + n_new + sinks + 2 * kAnyTile < span)
     span = (int64_t)window + n_new + sinks + 2 * kAnyTile;
-  const int64_t most = span / (2 * kAnyTile);
-  int64_t ns = (4 * (int64_t)num_sms + units - 1) / units;
-  if (ns > most) ns = most;
-  return ns < 1 ? 1 : (int)ns;
+  const int64_t tiles = (span + kAnyTile - 1) / kAnyTile, wave = (int64_t)(rows <= 8 ? 3 : 2) * num_sms;
+  int64_t best = 1, least = INT64_MAX;
+  for (int64_t ns = 1; ns == 1 || (ns <= tiles && units * ns <= 8 * num_sms); ++ns) {
+    const int64_t way = (units * ns + wave - 1) / wave * ((tiles + ns - 1) / ns + kAnyFixed);
+    if (way < least) { least = way; best = ns; }
+  }
+  return (int)best;
 }
 inline int any_rows(int R) { return R <= 4 ? 4 : R <= 8 ? 8 : kAnyRows; }
 
