@@ -306,7 +306,9 @@ vp_status vp_reserve_new(vp_ctx* ctx, int32_t max_new, int32_t max_weight_new);
  *   k_cache, v_cache  caches of seq_len[b] live tokens, the new ones included.
  *                Tokens that no new token sees (evicted pages, rows outside the
  *                window or past the end) may hold anything, and the pages that
- *                hold only such tokens need not be mapped.
+ *                hold only such tokens need not be mapped.  A value of V that is
+ *                not finite, at a token that some new token sees, can reach the
+ *                rows of the call's other new tokens (0 times infinity).
  *   seq_len      device int32 [batch], 0 <= seq_len <= max_seq.
  *   new_len      device int32 [batch] or NULL: n_b, 0 <= n_b <= min(n_new,
  *                seq_len[b]).  NULL: n_new in every sequence that is not empty.
