@@ -147,6 +147,7 @@ __device__ __forceinline__ Walk line_start(const AttendParams& p, int* misc) {
     const int all = total * p.Hkv, low = (all + ctas - 1) / ctas;
     const int high = (all + ctas - pairs * p.Hkv - 1) / (ctas - pairs * p.Hkv);
     int per, m = 0, heads;
+#pragma unroll 1
     for (int t = 0; t < 4; ++t) {
       per = max(min_share(p.fixed), low + (high - low) * t / 3);
       m = tid < pairs ? share_count(mine, per) : 0;

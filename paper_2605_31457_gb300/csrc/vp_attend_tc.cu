@@ -86,15 +86,34 @@ __device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 
 // of `box` rows.
 __device__ __forceinline__ uint32_t seen_bits(int jb, int t, int low, int sinks, uint32_t bad, int k, int box) {
   uint32_t see = low_bits(t + 1 - jb) & (~low_bits(low + 1 - jb) | low_bits(sinks - jb));
-  if (bad)
+  if (bad) {
+#pragma unroll 1
     for (int x = 0; x < 32; ++x)
       if ((bad >> ((k + x) / box)) & 1u) see &= ~(1u << x);
+  }
   return see;
 }
 // The 32 tokens' logits that `see` lacks become -infinity.
 __device__ __forceinline__ void mask_cols(float (&x)[32], uint32_t see) {
 #pragma unroll
   for (int i = 0; i < 32; ++i) x[i] = (see >> i) & 1u ? x[i] : -CUDART_INF_F;
+}
+// Four 16-byte pieces per lane: piece j of lane i of a quad goes to piece i of lane j.
+__device__ __forceinline__ void quad_transpose(uint4 (&v)[4], int lane) {
+  auto swap = [](uint4& a, uint4& b, bool upper, int x) {  // a of the upper lane and b of the lower one
+    const uint4 send = upper ? a : b;
+    uint4 got;
+    got.x = __shfl_xor_sync(0xffffffffu, send.x, x);
+    got.y = __shfl_xor_sync(0xffffffffu, send.y, x);
+    got.z = __shfl_xor_sync(0xffffffffu, send.z, x);
+    got.w = __shfl_xor_sync(0xffffffffu, send.w, x);
+    if (upper) a = got;
+    else b = got;
+  };
+  swap(v[0], v[1], lane & 1, 1);
+  swap(v[2], v[3], lane & 1, 1);
+  swap(v[0], v[2], lane & 2, 2);
+  swap(v[1], v[3], lane & 2, 2);
 }
 template <int D, int NQ>
 __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant__ AttendParams p) {
@@ -356,54 +375,57 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
       tc_fence_after();
       return !dead;
     };
-    while (next_part(p, walk, q)) {
+    // A group without rows takes no part: it must not arrive at q_full, whose
+    // phases nobody would wait for (nor, with NQ = 1, for a part without tiles).
+    auto takes_part = [&](const Part& q) { return q.u1 > q.u0 && (NQ == 1 || s == 0 || q.it.rows > kTcTile); };
+    // Queries of a part into shared memory, asynchronously: once S of the last
+    // tile of the part before is there, its products no longer read them.  In the
+    // one-row-block form both groups load half of the rows, when neither waits
+    // for an S any more.
+    auto load_queries = [&](const Part& q) {
+      if (!takes_part(q)) return;
+      if (NQ == 1) asm volatile("barrier.cta.sync 1, 256;\n" ::: "memory");
+      constexpr int P16 = D / 8, kStep = NQ == 1 ? 256 : 128;  // 16-byte pieces of a row; threads
+      const int first = q.it.row0 + (NQ == 1 ? 0 : s * kTcTile), rows_q = min(kTcTile, q.it.row0 + q.it.rows - first);
+      const __nv_bfloat16* qb = static_cast<const __nv_bfloat16*>(p.q.data) + (int64_t)q.b * p.q.sb;
+      const unsigned qs = smem_u32(smem + C::OFF_Q + (NQ == 1 ? 0 : s) * C::SLOT);
+      const int cc = tid % P16;
+#pragma unroll 4
+      for (int rr = (NQ == 1 ? tid : r) / P16; rr < rows_q; rr += kStep / P16) {
+        const int tok = row_token(p, first + rr);
+        const __nv_bfloat16* src = qb + (int64_t)tok * p.q.sn + (int64_t)(q.g * p.G + first + rr - tok * p.G) * p.q.sh + 8 * cc;
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(
+                         qs + (cc >> 3) * C::HALF + rr * 128 + (((cc & 7) ^ (rr & 7)) << 4)),
+                     "l"(src)
+                     : "memory");
+      }
+    };
+    auto queries_there = [&](const Part& q) {
+      if (!takes_part(q)) return;
+      asm volatile("cp.async.wait_all;" ::: "memory");
+      fence_proxy_async();  // read by the tensor core
+      if (NQ == 2) {
+        mbar_arrive(q_full + s);
+      } else {
+        mbar_arrive(q_full);
+        if (q.u1 - q.u0 > 1) mbar_arrive(q_full + 1);
+      }
+    };
+    // Each turn does part q and gets the queries of the next; in the first turn q
+    // is empty.  (One copy of the code for both: cold instructions cost more than
+    // the empty turn.)
+    q = Part();
+    for (;;) {
       const int n = q.u1 - q.u0;
       const int row_s = q.it.row0 + (NQ == 2 ? s * kTcTile : 0), row = row_s + r;  // query row of the kv-head
       const bool valid = row < q.it.row0 + q.it.rows;
       const bool rows_here = __any_sync(0xffffffffu, valid);
-      const int t = valid ? q.sq.len - q.sq.n + row / p.G : -1;      // its position
-      const int low = p.window < 0 ? -1 : t - p.window;              // the window sees j > low
+      const int t = valid ? q.sq.len - q.sq.n + row_token(p, row) : -1;  // its position
+      const int low = p.window < 0 ? -1 : t - p.window;                  // the window sees j > low
       float m = -CUDART_INF_F, l = 0.f;
       const bool split = q.it.split;
       bool have = false;  // O holds something
-      // A group without rows takes no part: it must not arrive at q_full, whose
-      // phases nobody would wait for (nor, with NQ = 1, for one without tiles).
       const bool group = NQ == 1 || s == 0 || q.it.rows > kTcTile;
-      if (n > 0 && group) {
-        // Queries: in the one-row-block form both groups load half of the rows,
-        // once neither reads the last part's S any more (its products with
-        // the old queries are then complete).
-        if (NQ == 1) asm volatile("barrier.cta.sync 1, 256;\n" ::: "memory");
-        constexpr int P16 = D / 8;  // 16-byte pieces of a row
-        const int rows_q = NQ == 1 ? q.it.rows : min(kTcTile, max(0, q.it.rows - s * kTcTile));
-        const __nv_bfloat16* qb = static_cast<const __nv_bfloat16*>(p.q.data) + (int64_t)q.b * p.q.sb;
-        unsigned char* qs = smem + C::OFF_Q + (NQ == 1 ? 0 : s) * C::SLOT;
-        constexpr int kStep = NQ == 1 ? 256 : 128, kBatch = D == 128 ? 16 : 8;  // loads in flight per thread
-        for (int i0 = NQ == 1 ? tid : r; i0 < rows_q * P16; i0 += kStep * kBatch) {
-          uint4 v[kBatch];
-#pragma unroll
-          for (int x = 0; x < kBatch; ++x) {
-            const int i = i0 + x * kStep, qrow = q.it.row0 + (NQ == 2 ? s * kTcTile : 0) + i / P16;
-            if (i < rows_q * P16)
-              v[x] = *reinterpret_cast<const uint4*>(qb + (int64_t)row_token(p, qrow) * p.q.sn +
-                                                     (int64_t)(q.g * p.G + qrow - row_token(p, qrow) * p.G) * p.q.sh +
-                                                     8 * (i % P16));
-          }
-#pragma unroll
-          for (int x = 0; x < kBatch; ++x) {
-            const int i = i0 + x * kStep, rr = i / P16, cc = i % P16;
-            if (i < rows_q * P16)
-              *reinterpret_cast<uint4*>(qs + (cc >> 3) * C::HALF + rr * 128 + (((cc & 7) ^ (rr & 7)) << 4)) = v[x];
-          }
-        }
-        fence_proxy_async();  // read by the tensor core
-        if (NQ == 2) {
-          mbar_arrive(q_full + s);
-        } else {
-          mbar_arrive(q_full);
-          if (n > 1) mbar_arrive(q_full + 1);
-        }
-      }
       for (int i = NQ == 1 ? s : 0; i < n && group; i += NQ == 1 ? 2 : 1) {
         const int j0 = q.it.tl.tile(q.u0 + i) * kTcTile;
         bool all = !valid || (j0 + kTcTile - 1 <= t && (j0 > low || j0 + kTcTile <= p.sinks));
@@ -426,7 +448,9 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
             // this outgrew the instruction cache.
             float x[64];
             float (&xa)[32] = *reinterpret_cast<float (*)[32]>(x), (&xb)[32] = *reinterpret_cast<float (*)[32]>(x + 32);
-            auto load = [&] {
+            uint32_t hi[32];
+            float sum;
+            for (bool again = false;; again = true) {
               tmem_ld_start(taddr + k0, xa);
               tmem_ld_start(taddr + k0 + 32, xb);
               tmem_ld_wait(xa);
@@ -435,13 +459,34 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
                 mask_cols(xa, seen_bits(j0 + k0, t, low, p.sinks, bad, k0, R2));
                 mask_cols(xb, seen_bits(j0 + k0 + 32, t, low, p.sinks, bad, k0 + 32, R2));
               }
-            };
-            uint32_t hi[32];
-            float2 s0, s1;
-            auto exps = [&] {
+              if (again) {
+                float top = x[0];
+#pragma unroll
+                for (int k = 1; k < kSub; ++k) top = fmaxf(top, x[k]);
+                const float mn = fmaxf(m, top * c), f = m == -CUDART_INF_F ? 0.f : fexp2(m - mn);
+                m = mn;
+                l *= f;
+                // O holds the products of this group's steps so far: rescale it
+                // once the last of them is complete.
+                if (have && wait(pv_done + 2 * s + ((ns - 1) & 1), ((ns - 1) >> 1) & 1)) {
+#pragma unroll 1
+                  for (int e = 0; e < D; e += 16) {
+                    float o[16];
+                    tmem_ld16(oaddr + e, o);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[i] *= f;
+                    tmem_st16(oaddr + e, o);
+                  }
+                }
+              } else if (zr) {
+#pragma unroll
+                for (int k = 0; k < kSub; k += 4)
+                  *reinterpret_cast<float4*>(zr + k0 + k) =
+                      make_float4(x[k] * c, x[k + 1] * c, x[k + 2] * c, x[k + 3] * c);
+              }
               const float mu = m == -CUDART_INF_F ? 0.f : m;
               const float2 c2 = make_float2(c, c), mu2 = make_float2(-mu, -mu);
-              s0 = s1 = make_float2(0.f, 0.f);
+              float2 s0 = make_float2(0.f, 0.f), s1 = s0;
 #pragma unroll
               for (int k = 0; k < 32; ++k) {
                 float2 e = fma2(make_float2(x[2 * k], x[2 * k + 1]), c2, mu2);
@@ -453,37 +498,8 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
                 x[2 * k] = e.x;
                 x[2 * k + 1] = e.y;
               }
-              return (s0.x + s0.y) + (s1.x + s1.y);
-            };
-            load();
-            if (zr) {
-#pragma unroll
-              for (int k = 0; k < kSub; k += 4)
-                *reinterpret_cast<float4*>(zr + k0 + k) =
-                    make_float4(x[k] * c, x[k + 1] * c, x[k + 2] * c, x[k + 3] * c);
-            }
-            float sum = exps();
-            if (__any_sync(0xffffffffu, valid && (m == -CUDART_INF_F || sum > kPMost))) {
-              load();
-              float top = x[0];
-#pragma unroll
-              for (int k = 1; k < kSub; ++k) top = fmaxf(top, x[k]);
-              const float mn = fmaxf(m, top * c), f = m == -CUDART_INF_F ? 0.f : fexp2(m - mn);
-              m = mn;
-              l *= f;
-              // O holds the products of this group's steps so far: rescale it
-              // once the last of them is complete.
-              if (have && wait(pv_done + 2 * s + ((ns - 1) & 1), ((ns - 1) >> 1) & 1)) {
-#pragma unroll 1
-                for (int e = 0; e < D; e += 16) {
-                  float o[16];
-                  tmem_ld16(oaddr + e, o);
-#pragma unroll
-                  for (int i = 0; i < 16; ++i) o[i] *= f;
-                  tmem_st16(oaddr + e, o);
-                }
-              }
-              sum = exps();
+              sum = (s0.x + s0.y) + (s1.x + s1.y);
+              if (again || !__any_sync(0xffffffffu, valid && (m == -CUDART_INF_F || sum > kPMost))) break;
             }
             l += sum;
             tmem_st(taddr + k0, *reinterpret_cast<uint32_t (*)[16]>(hi));
@@ -509,6 +525,9 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
         }
       }
       tiles += max(0, n);
+      Part next;
+      const bool more = next_part(p, walk, next);
+      if (more) load_queries(next);
       // ---- rows that see nothing: padding, or all of an item without tiles
       if (q.owner && (NQ == 2 || s == 0) && row < min(p.R, q.it.row0 + p.block) && (!valid || q.it.tl.n == 0)) {
         uint4* o = reinterpret_cast<uint4*>(out_row<__nv_bfloat16>(p, q.b, q.g, row));
@@ -516,13 +535,12 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
         for (int k = 0; k < D / 8; ++k) o[k] = make_uint4(0u, 0u, 0u, 0u);
         store_lse(p, q.b, q.g, row, 0.f, 0.f);
       }
-      if (n <= 0 || !group) continue;
       // ---- the others' output, or this CTA's record of it
       const bool direct = NQ == 2 && q.whole();
       const int c0 = q.c0;
       auto rec_of = [&](int c, int grp) { return (2 * c + (c == c0 ? 1 : 0)) * 2 + grp; };
       if (have) wait(pv_done + 2 * s + ((ns - 1) & 1), ((ns - 1) >> 1) & 1);
-      if (rows_here) {
+      if (rows_here && n > 0 && group) {
         float* po = nullptr;
         __nv_bfloat16* out = nullptr;
         if (valid && direct) {
@@ -534,7 +552,12 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
           po = p.part_o + at * D;
         }
         const float inv = l > 0.f ? 1.f / l : 0.f;
+        __nv_bfloat16* outs[4];  // the rows of this lane's quad
 #pragma unroll
+        for (int x = 0; x < 4; ++x)
+          outs[x] = reinterpret_cast<__nv_bfloat16*>(
+              __shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(out), (lane & ~3) + x));
+#pragma unroll 1
         for (int k = 0; k < D; k += 32) {
           float o[32];
           if (have && !dead) {
@@ -548,16 +571,18 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
             for (int x = 0; x < 32; x += 4)
               *reinterpret_cast<float4*>(po + k + x) = make_float4(o[x], o[x + 1], o[x + 2], o[x + 3]);
           }
-          if (out) {
+          if (direct) {
+            // A quad's lanes write 64 bytes of a row together.
+            uint4 v[4];
 #pragma unroll
-            for (int x = 0; x < 32; x += 8) {
-              uint4 v;
-              v.x = pack_bf16(o[x] * inv, o[x + 1] * inv);
-              v.y = pack_bf16(o[x + 2] * inv, o[x + 3] * inv);
-              v.z = pack_bf16(o[x + 4] * inv, o[x + 5] * inv);
-              v.w = pack_bf16(o[x + 6] * inv, o[x + 7] * inv);
-              *reinterpret_cast<uint4*>(out + k + x) = v;
-            }
+            for (int x = 0; x < 4; ++x)
+              v[x] = make_uint4(pack_bf16(o[8 * x] * inv, o[8 * x + 1] * inv), pack_bf16(o[8 * x + 2] * inv, o[8 * x + 3] * inv),
+                                pack_bf16(o[8 * x + 4] * inv, o[8 * x + 5] * inv),
+                                pack_bf16(o[8 * x + 6] * inv, o[8 * x + 7] * inv));
+            quad_transpose(v, lane);
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+              if (outs[x]) *reinterpret_cast<uint4*>(outs[x] + k + 8 * (lane & 3)) = v[x];
           }
         }
       }
@@ -565,11 +590,12 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
         tc_fence_before();
         mbar_arrive(o_free + s);
       }
-      if (direct) continue;
+      if (more) queries_there(next);
       // NQ = 1: the records of both groups of every CTA; NQ = 2: this group's rows.
       const int parts = q.parts;
       auto sync = [&] { asm volatile("barrier.cta.sync %0, 128;\n" ::"r"(2 + s) : "memory"); };
-      if (last_to_arrive(p.tickets + 2 * c0 + (NQ == 2 ? s : 0), NQ == 1 ? 2 * parts : parts, r, misc + 18 + s, sync)) {
+      if (!direct && n > 0 && group &&
+          last_to_arrive(p.tickets + 2 * c0 + (NQ == 2 ? s : 0), NQ == 1 ? 2 * parts : parts, r, misc + 18 + s, sync)) {
         if (NQ == 1)
           join_records<__nv_bfloat16, D, 128>(p, q.b, q.g, 0, q.it.rows, 2 * parts, kTcTile,
                                               [&](int k) { return rec_of(c0 + (k >> 1), k & 1); }, r);
@@ -577,6 +603,8 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
           join_records<__nv_bfloat16, D, 128>(p, q.b, q.g, row_s, min(kTcTile, q.it.rows - s * kTcTile), parts, kTcTile,
                                               [&](int k) { return rec_of(c0 + k, s); }, r);
       }
+      if (!more) break;
+      q = next;
     }
     if (dead) timed_out = true;
   }
