@@ -68,8 +68,8 @@ struct DecCfg {
   static constexpr int OFF_BAD = OFF_BAR + NBAR * 8;   // unmapped boxes of a tile, one bit each
   static constexpr int LINE = THREADS / 32 + 7;        // ints of line_start
   static constexpr int OFF_MISC = OFF_BAD + kBadRing * 4;     // int: line_start, flags, TMEM base
-  static constexpr int OFF_RED = OFF_MISC + (LINE + SG + 1) * 4;  // float [SG][4][GR]: maxima, then sums
-  static constexpr size_t SMEM = 1024 + (size_t)OFF_RED + 4 * GM * 4;
+  static constexpr int OFF_RED = OFF_MISC + (LINE + SG + 1) * 4;  // float [SG][5][GR]: maxima, then sums, of 4 warps; references
+  static constexpr size_t SMEM = 1024 + (size_t)OFF_RED + 5 * GM * 4;
   static constexpr int O_COL = 2 * NQ;                 // TMEM columns: two S buffers, then O
   static constexpr int COLS = O_COL + NP <= 64 ? 64 : O_COL + NP <= 128 ? 128 : 256;
   static_assert(O_COL + NP <= COLS, "TMEM columns");
@@ -185,6 +185,7 @@ __global__ void __launch_bounds__(DecCfg<D, GM>::THREADS, DecCfg<D, GM>::CPS) k_
       if (n <= 0) continue;
       int kp, vp, kn = -2, vn = -2, vd = -2;  // pages of tile i, of tile i + 1 (looked up ahead), V page due
       lookup(q, q.u0, kp, vp);
+#pragma unroll 1
       for (int i = 0; i <= n; ++i) {
         if (i + 1 < n) lookup(q, q.u0 + i + 1, kn, vn);
         if (i < n) {
@@ -205,6 +206,7 @@ __global__ void __launch_bounds__(DecCfg<D, GM>::THREADS, DecCfg<D, GM>::CPS) k_
     }
     // Copies still in flight (only after a timeout can any be unread) land
     // before the CTA's shared memory is released.
+#pragma unroll 1
     for (int k = max(0, pc - S); k < pc; ++k) mbar_wait(full + k % S, (k / S) & 1);
   } else if (warp == 1) {
     // -------------------------------------------------------- tensor cores
@@ -215,11 +217,13 @@ __global__ void __launch_bounds__(DecCfg<D, GM>::THREADS, DecCfg<D, GM>::CPS) k_
       tc_fence_after();
       return ok;
     };
+    const int leader = elect_one();
     int pc = 0, parts = 0, ks = 0, ps = 0, tiles = 0;  // pieces, parts with tiles, QK and P.V products, tiles before
     while (!timed_out && next_part(p, walk, q)) {
       const int n = q.u1 - q.u0;
       if (n <= 0) continue;
       if (!wait_all(q_full, parts & 1)) { timed_out = true; break; }
+#pragma unroll 1
       for (int i = 0; i <= n; ++i) {
         if (i < n) {
           const int sl = pc % S, sb = ks & 1;
@@ -227,12 +231,14 @@ __global__ void __launch_bounds__(DecCfg<D, GM>::THREADS, DecCfg<D, GM>::CPS) k_
             timed_out = true;
             break;
           }
-          if (lane == 0) {
-            const unsigned kb = smem_u32(smem + sl * C::SLOT), qb = smem_u32(smem + C::OFF_Q);
+          if (leader) {
+            const uint32_t kd = umma_desc_lo(smem_u32(smem + sl * C::SLOT), 16);
+            const uint32_t qd = umma_desc_lo(smem_u32(smem + C::OFF_Q), 16);
+            umma_ss<kIdQK, 0>(tmem + C::NQ * sb, kd, qd);
 #pragma unroll
-            for (int k = 0; k < D / 16; ++k)
-              umma(tmem + C::NQ * sb, umma_desc(kb + (k >> 2) * C::HALF + (k & 3) * 32, 16, 1024),
-                   umma_desc(qb + (k >> 2) * C::QHALF + (k & 3) * 32, 16, 1024), kIdQK, k > 0);
+            for (int k = 1; k < D / 16; ++k)  // 16 dimensions: 32 bytes, every fourth step the next half
+              umma_ss<kIdQK, 1>(tmem + C::NQ * sb, kd + (k >> 2) * (C::HALF / 16) + (k & 3) * 2,
+                                qd + (k >> 2) * (C::QHALF / 16) + (k & 3) * 2);
             umma_commit(s_full + sb);
             umma_commit(empty + sl);
           }
@@ -248,6 +254,7 @@ __global__ void __launch_bounds__(DecCfg<D, GM>::THREADS, DecCfg<D, GM>::CPS) k_
           const uint32_t bad = bad_ring[(tiles + i - 1) % kBadRing];
           const SeenRange& sr = q.it.sr;
           if (bad || !((j0 >= sr.lo && j0 + kTcTile <= sr.hi) || j0 + kTcTile <= sr.s_end)) {
+#pragma unroll 1
             for (int r = lane; r < kTcTile; r += 32) {
               const int j = j0 + r;
               if ((j < sr.s_end || (j >= sr.lo && j < sr.hi)) && !((bad >> (r / R2)) & 1u)) continue;
@@ -261,12 +268,14 @@ __global__ void __launch_bounds__(DecCfg<D, GM>::THREADS, DecCfg<D, GM>::CPS) k_
           __syncwarp();
           if (i == 1 && !wait_all(o_free, (parts & 1) ^ 1)) { timed_out = true; break; }
           if (!wait_all(p_full + pb, (ps / PB) & 1)) { timed_out = true; break; }
-          if (lane == 0) {
-            const unsigned vb = smem_u32(smem + sl * C::SLOT), pbs = smem_u32(smem + C::OFF_P + pb * C::PBUF);
+          if (leader) {
+            const uint32_t vd = umma_desc_lo(smem_u32(smem + sl * C::SLOT), C::HALF);
+            const uint32_t pd = umma_desc_lo(smem_u32(smem + C::OFF_P + pb * C::PBUF), 16);
+            if (i == 1) umma_ss<kIdPV, 0>(tmem + C::O_COL, vd, pd);
+            else umma_ss<kIdPV, 1>(tmem + C::O_COL, vd, pd);
 #pragma unroll
-            for (int k = 0; k < kTcTile / 16; ++k)
-              umma(tmem + C::O_COL, umma_desc(vb + k * 2048, C::HALF, 1024),
-                   umma_desc(pbs + (k >> 2) * C::PHALF + (k & 3) * 32, 16, 1024), kIdPV, i > 1 || k > 0);
+            for (int k = 1; k < kTcTile / 16; ++k)  // 16 tokens: 2048 bytes of V
+              umma_ss<kIdPV, 1>(tmem + C::O_COL, vd + k * 128, pd + (k >> 2) * (C::PHALF / 16) + (k & 3) * 2);
             umma_commit(pv_done + pb);
             umma_commit(empty + sl);
           }
@@ -278,7 +287,7 @@ __global__ void __launch_bounds__(DecCfg<D, GM>::THREADS, DecCfg<D, GM>::CPS) k_
       ++parts;
       tiles += n;
     }
-    if (lane == 0) umma_commit(done);  // after every operation issued above
+    if (leader) umma_commit(done);  // after every operation issued above
     __syncwarp();
     if (!mbar_wait(done, 0)) timed_out = true;
   } else {
@@ -288,7 +297,7 @@ __global__ void __launch_bounds__(DecCfg<D, GM>::THREADS, DecCfg<D, GM>::CPS) k_
     const int h0 = sg * GR;                         // the group's query rows are [h0, h0 + GR)
     const unsigned taddr = tmem + ((unsigned)(wq * 32) << 16);
     const unsigned scol = taddr + h0, ocol = taddr + C::O_COL + h0;
-    float* redg = red + sg * 4 * GR;
+    float* redg = red + sg * 5 * GR;
     const float c = p.c_log2;
     const int G = p.G;
     auto sync = [&] { asm volatile("barrier.cta.sync %0, 128;\n" ::"r"(1 + sg) : "memory"); };
@@ -309,6 +318,7 @@ __global__ void __launch_bounds__(DecCfg<D, GM>::THREADS, DecCfg<D, GM>::CPS) k_
       // ---- rows that see nothing: padding, or all of an item without tiles
       if (q.owner) {
         const int first = q.it.tl.n == 0 ? 0 : rows;
+#pragma unroll 1
         for (int i = st; i < (min(GR, p.R - h0) - first) * (D / 8); i += 128) {
           const int row = h0 + first + i / (D / 8);
           reinterpret_cast<uint4*>(out_row<__nv_bfloat16>(p, q.b, q.g, row))[i % (D / 8)] = make_uint4(0u, 0u, 0u, 0u);
@@ -318,6 +328,7 @@ __global__ void __launch_bounds__(DecCfg<D, GM>::THREADS, DecCfg<D, GM>::CPS) k_
       if (n <= 0) continue;
       // ---- the group's queries, K-major and swizzled.  The products with the
       // last part's are complete: this thread has waited for their S.
+#pragma unroll 1
       for (int i = st; i < rows * (D / 8); i += 128) {
         const int rr = h0 + i / (D / 8), cc = i % (D / 8), tok = row_token(p, rr);
         const uint4 v = *reinterpret_cast<const uint4*>(
@@ -335,6 +346,7 @@ __global__ void __launch_bounds__(DecCfg<D, GM>::THREADS, DecCfg<D, GM>::CPS) k_
         mref[h] = -CUDART_INF_F;
         l[h] = 0.f;
       }
+#pragma unroll 1
       for (int i = 0; i < n; ++i, ++ks) {
         const int sb = ks & 1, pb = ks % PB;
         const int j0 = q.it.tl.tile(q.u0 + i) * kTcTile, j = j0 + r;
@@ -343,6 +355,7 @@ __global__ void __launch_bounds__(DecCfg<D, GM>::THREADS, DecCfg<D, GM>::CPS) k_
         const bool part = j0 + kTcTile - 1 > t0 || !(p.window < 0 || j0 > t1 - p.window || j0 + kTcTile <= p.sinks);
         if (part) {
           uint32_t seen = 0;
+#pragma unroll 1
           for (int h = 0; h < rows; ++h)
             if (sees(j, base + row_token(p, h0 + h), p.window, p.sinks)) seen |= 1u << h;
           see = seen;
@@ -376,7 +389,7 @@ __global__ void __launch_bounds__(DecCfg<D, GM>::THREADS, DecCfg<D, GM>::CPS) k_
         if (raise) {
 #pragma unroll
           for (int h = 0; h < GR; ++h) {
-            const float m = warp_max(z[h]);
+            const float m = warp_max_now(z[h]);
             if (lane == 0) redg[wq * GR + h] = m;
           }
           sync();
@@ -430,13 +443,34 @@ __global__ void __launch_bounds__(DecCfg<D, GM>::THREADS, DecCfg<D, GM>::CPS) k_
         const float s = warp_sum(l[h]);
         if (lane == 0) redg[wq * GR + h] = s;
       }
-      float o[2 * GR];  // hi, lo
-      if (wait(pv_done + (ks - 1) % PB, ((ks - 1) / PB) & 1)) {
+      // They go through the group's rows of a P buffer, which no product reads any
+      // more, so that a thread writes 16 bytes: dimensions 32 x to 32 x + 31 of a
+      // row take the 128 bytes of its hi (x < 2) or lo values of half x & 1.
+      auto staged = [&](int h, int d) {
+        return reinterpret_cast<float*>(smem + C::OFF_P + ((d >> 5) & 1) * C::PHALF + ((d >> 6) * GM + h0 + h) * 128 +
+                                        (d & 31) * 4);
+      };
+      // D = 64: an M = 64 accumulator holds rows 16 w .. 16 w + 15 in the first
+      // 16 lanes of warp w.
+      const int dim = D == 128 ? r : 16 * wq + (lane & 15);
+      if (st == 0) {
 #pragma unroll
-        for (int k = 0; k < 2 * GR; k += 16) tmem_ld16(ocol + (k / GR) * GM, *reinterpret_cast<float (*)[16]>(o + k));
-      } else {
+        for (int h = 0; h < GR; ++h) redg[4 * GR + h] = mref[h];
+      }
+      const bool there = wait(pv_done + (ks - 1) % PB, ((ks - 1) / PB) & 1);
+      if (rows > 0) {
+        float o[2 * GR];  // hi, lo
+        if (there) {
 #pragma unroll
-        for (int k = 0; k < 2 * GR; ++k) o[k] = 0.f;
+          for (int k = 0; k < 2 * GR; k += 16) tmem_ld16(ocol + (k / GR) * GM, *reinterpret_cast<float (*)[16]>(o + k));
+        } else {
+#pragma unroll
+          for (int k = 0; k < 2 * GR; ++k) o[k] = 0.f;
+        }
+        if (D == 128 || lane < 16) {
+#pragma unroll
+          for (int h = 0; h < GR; ++h) *staged(h, dim) = o[h] + o[GR + h];
+        }
       }
       tc_fence_before();
       arrive(o_free);
@@ -445,22 +479,22 @@ __global__ void __launch_bounds__(DecCfg<D, GM>::THREADS, DecCfg<D, GM>::CPS) k_
       const bool direct = q.whole();
       const int c0 = q.c0;
       auto rec_of = [&](int cta) { return (2 * cta + (cta == c0 ? 1 : 0)) * C::SG + sg; };
-      // D = 64: an M = 64 accumulator holds rows 16 w .. 16 w + 15 in the first
-      // 16 lanes of warp w.
-      const int d = D == 128 ? r : 16 * wq + (lane & 15);
-      const bool mine = D == 128 || lane < 16;
-#pragma unroll
-      for (int h = 0; h < GR; ++h) {
-        if (h >= rows) continue;
+#pragma unroll 1
+      for (int i = st; i < rows * (D / 8); i += 128) {
+        const int h = i / (D / 8), d = 8 * (i % (D / 8));
         const float sum = (redg[h] + redg[GR + h]) + (redg[2 * GR + h] + redg[3 * GR + h]);
-        const float x = o[h] + o[GR + h];
+        const float4 x = *reinterpret_cast<const float4*>(staged(h, d)), y = *reinterpret_cast<const float4*>(staged(h, d + 4));
         if (direct) {
-          if (mine) out_row<__nv_bfloat16>(p, q.b, q.g, h0 + h)[d] = __float2bfloat16_rn(sum > 0.f ? x / sum : 0.f);
-          if (st == 0) store_lse(p, q.b, q.g, h0 + h, mref[h], sum);
+          const float inv = sum > 0.f ? 1.f / sum : 0.f;
+          *reinterpret_cast<uint4*>(out_row<__nv_bfloat16>(p, q.b, q.g, h0 + h) + d) =
+              make_uint4(pack_bf16(x.x * inv, x.y * inv), pack_bf16(x.z * inv, x.w * inv),
+                         pack_bf16(y.x * inv, y.y * inv), pack_bf16(y.z * inv, y.w * inv));
+          if (d == 0) store_lse(p, q.b, q.g, h0 + h, redg[4 * GR + h], sum);
         } else {
-          const int64_t at = (int64_t)rec_of(blockIdx.x) * GR + h;
-          if (mine) p.part_o[at * D + d] = x;
-          if (st == 0) *reinterpret_cast<float2*>(p.part_st + 2 * at) = make_float2(mref[h], sum);
+          const int at = rec_of(blockIdx.x) * GR + h;
+          *reinterpret_cast<float4*>(p.part_o + at * D + d) = x;
+          *reinterpret_cast<float4*>(p.part_o + at * D + d + 4) = y;
+          if (d == 0) *reinterpret_cast<float2*>(p.part_st + 2 * at) = make_float2(redg[4 * GR + h], sum);
         }
       }
       if (direct) continue;

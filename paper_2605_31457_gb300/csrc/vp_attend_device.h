@@ -114,13 +114,9 @@ __device__ __forceinline__ int block_scan(int x, int* warps, int& total) {
   __syncthreads();
   if (lane == 31) warps[warp] = incl;
   __syncthreads();
-  int before = incl - x;
-  total = 0;
-  for (int w = 0; w < NT / 32; ++w) {
-    if (w < warp) before += warps[w];
-    total += warps[w];
-  }
-  return before;
+  const int w = lane < NT / 32 ? warps[lane] : 0;
+  total = __reduce_add_sync(0xffffffffu, w);
+  return incl - x + __reduce_add_sync(0xffffffffu, lane < warp ? w : 0);
 }
 // Finds this CTA's start: each thread sums the costs of a run of pairs, a block
 // scan gives their places.  misc: NT / 32 + 7 ints of shared memory.
@@ -137,6 +133,7 @@ __device__ __forceinline__ Walk line_start(const AttendParams& p, int* misc) {
     return att_item(sq.len, sq.n, p.G, p.block, i - b * p.nqt, p.window, p.sinks).cost(p.fixed);
   };
   int mine = 0;
+#pragma unroll 1
   for (int i = i0; i < i1; ++i) mine += pair_cost(i, true);
   int total;
   int before = block_scan<NT>(mine, misc, total);
@@ -184,6 +181,7 @@ __device__ __forceinline__ Walk line_start(const AttendParams& p, int* misc) {
     if (at >= before && at < before + mine) {
       int sum = before, i = i0;
       if (run > 1) {
+#pragma unroll 1
         for (;; ++i) {
           const int cost = pair_cost(i, false);
           if (at < sum + cost) break;
@@ -230,10 +228,12 @@ template <typename T, int D, int NT, typename Rec>
 __device__ __forceinline__ void join_records(const AttendParams& p, int b, int g, int row0, int rows, int n, int RS,
                                              Rec&& rec, int tid) {
   constexpr int C4 = D / 4, U = 16;
+#pragma unroll 1
   for (int e = tid; e < rows * C4; e += NT) {
     const int r = e / C4, d = 4 * (e % C4);
     float m = -CUDART_INF_F, l = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
     for (int k0 = 0; k0 < n; k0 += U) {
       float2 st[U];
       float4 x[U];
@@ -242,7 +242,7 @@ __device__ __forceinline__ void join_records(const AttendParams& p, int b, int g
         st[k] = make_float2(-CUDART_INF_F, 0.f);
         x[k] = make_float4(0.f, 0.f, 0.f, 0.f);
         if (k0 + k < n) {
-          const int64_t at = (int64_t)rec(k0 + k) * RS + r;
+          const int at = rec(k0 + k) * RS + r;  // at most 4 records per SM of up to 128 rows
           st[k] = __ldcg(reinterpret_cast<const float2*>(p.part_st) + at);
           x[k] = __ldcg(reinterpret_cast<const float4*>(p.part_o + at * D + d));
         }

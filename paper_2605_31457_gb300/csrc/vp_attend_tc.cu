@@ -215,6 +215,7 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
       int kp = -2, vp = -2, kn, vn;   // pages of tile i, looked up one tile ahead
       int vq[LA];                     // V pages of the tiles whose V is due
       if (n > 0) lookup(q, q.u0, kp, vp);
+#pragma unroll 1
       for (int i = 0; i < n + LA && n > 0; ++i) {
         kn = vn = -2;
         if (i + 1 < n) lookup(q, q.u0 + i + 1, kn, vn);
@@ -238,6 +239,7 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
     }
     // Copies still in flight (only after a timeout can any be unread) land
     // before the CTA's shared memory is released.
+#pragma unroll 1
     for (int k = max(0, pc - S); k < pc; ++k) mbar_wait(full + k % S, (k / S) & 1);
   } else if (warp >= 9) {
     // ------------------------------- tensor cores, a warp for each group s
@@ -283,6 +285,7 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
       }
       // The copy warp's order: K of the first LA tiles, then V of a tile and K of
       // the tile LA later.
+#pragma unroll 1
       for (int t = 0; t < min(LA, n); ++t) {
         int ks;
         if (!take(ks)) { timed_out = true; break; }
@@ -426,6 +429,7 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
       const bool split = q.it.split;
       bool have = false;  // O holds something
       const bool group = NQ == 1 || s == 0 || q.it.rows > kTcTile;
+#pragma unroll 1
       for (int i = NQ == 1 ? s : 0; i < n && group; i += NQ == 1 ? 2 : 1) {
         const int j0 = q.it.tl.tile(q.u0 + i) * kTcTile;
         bool all = !valid || (j0 + kTcTile - 1 <= t && (j0 > low || j0 + kTcTile <= p.sinks));

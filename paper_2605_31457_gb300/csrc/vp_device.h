@@ -26,6 +26,12 @@ __device__ __forceinline__ float warp_sum(float x) {
   for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
   return x;
 }
+// The maximum over the warp by one instruction.
+__device__ __forceinline__ float warp_max_now(float x) {
+  float y;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;\n" : "=f"(y) : "f"(x));
+  return y;
+}
 // Reductions over the 8 lanes that share lane % 4 (the mma "group" axis).
 __device__ __forceinline__ float group_max(float x) {
   x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
