@@ -69,30 +69,52 @@ __global__ void __launch_bounds__(kSelThreads) k_evict_select(const __grid_const
   const int K = min(T, p.keep);
   const float* w0 = p.w.data + (int64_t)b * p.w.sb + (int64_t)g0 * p.w.sh;
   float* wd0 = p.wd.data + (int64_t)b * p.wd.sb + (int64_t)g0 * p.wd.sh;
+#pragma unroll 1
   for (int i = K + tid; i < p.kept_cap; i += kSelThreads) kept[i] = -1;
   if (T <= p.keep) {  // every token stays where it is
+#pragma unroll 1
     for (int j = tid; j < T; j += kSelThreads) kept[j] = j;
     if (p.wd.data && !p.in_place)
       for (int g = 0; g < (p.granularity ? 1 : p.Hkv); ++g)
+#pragma unroll 1
         for (int j = tid; j < T; j += kSelThreads) wd0[(int64_t)g * p.wd.sh + j] = w0[(int64_t)g * p.w.sh + j];
     return;
   }
   const int steps = KR > 0 ? KR : (T + kSelThreads - 1) / kSelThreads;
   const int a = warp * steps * 32 + lane;  // the thread's first token
   const int lo = p.sinks, hi = T - p.recent;  // the middle to choose from
+  const int heads = p.granularity ? 1 : p.Hkv;
+  // The weights of tokens j, j + 32, ..., summed over the heads of the set; 0 past the end.
+  auto weights_at = [&](int j, auto& w) {
+    constexpr int N = sizeof(w) / sizeof(float);
+#pragma unroll
+    for (int i = 0; i < N; ++i) w[i] = j + 32 * i < T ? w0[j + 32 * i] : 0.f;
+#pragma unroll 1
+    for (int g = 1; g < heads; ++g) {
+      float x[N];
+#pragma unroll
+      for (int i = 0; i < N; ++i) x[i] = j + 32 * i < T ? w0[(int64_t)g * p.w.sh + j + 32 * i] : 0.f;
+#pragma unroll
+      for (int i = 0; i < N; ++i) w[i] += x[i];
+    }
+  };
   auto weight_at = [&](int j) {
-    float w = w0[j];
-    if (!p.granularity)
-      for (int g = 1; g < p.Hkv; ++g) w += w0[(int64_t)g * p.w.sh + j];
-    return w;
+    float w[1];
+    weights_at(j, w);
+    return w[0];
   };
   float held[KR > 0 ? KR : 1];
   if constexpr (KR > 0) {
-#pragma unroll
-    for (int i = 0; i < KR; ++i) held[i] = a + 32 * i < T ? weight_at(a + 32 * i) : 0.f;
+    weights_at(a, held);
   } else if constexpr (KR == 0) {  // a thread reads back only what it wrote
-#pragma unroll 8
-    for (int j = a; j < min(T, a + 32 * steps); j += 32) keys_s[j] = order_key(weight_at(j));
+#pragma unroll 1
+    for (int i0 = 0; i0 < steps; i0 += 8) {
+      float w[8];
+      weights_at(a + 32 * i0, w);
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (i0 + k < steps && a + 32 * (i0 + k) < T) keys_s[a + 32 * (i0 + k)] = order_key(w[k]);
+    }
   }
   // Calls f(step, key) for this thread's tokens of the middle, of those in `bits` where there is one.
   auto each = [&](uint32_t bits, auto&& f) {
@@ -108,6 +130,7 @@ __global__ void __launch_bounds__(kSelThreads) k_evict_select(const __grid_const
           if (j >= lo && j < hi) f(i, keys_s[j]);
         }
       } else {
+#pragma unroll 1
         for (uint32_t c = bits; c; c &= c - 1) {
           const int i = __ffs(c) - 1;
           f(i, keys_s[a + 32 * i]);
@@ -125,6 +148,7 @@ __global__ void __launch_bounds__(kSelThreads) k_evict_select(const __grid_const
   uint32_t up = 0, cand = 0xffffffffu;  // a bit per step: stays for sure; may be equal to the threshold
   const bool any = m > 0;
   if (any) {
+#pragma unroll 1
     for (int pass = 0; pass < 3; ++pass) {
       const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
       const uint32_t digits = pass == 2 ? 1023u : 2047u;
@@ -214,6 +238,7 @@ __global__ void __launch_bounds__(kSelThreads) k_evict_select(const __grid_const
 #pragma unroll
     for (int i = 0; i < KR; ++i) emit(i, a + 32 * i, held[i]);
   } else {
+#pragma unroll 1
     for (int i0 = 0; i0 < steps; i0 += 4) {
       float w[4];
 #pragma unroll
@@ -228,10 +253,11 @@ __global__ void __launch_bounds__(kSelThreads) k_evict_select(const __grid_const
   // before its writes, and later rounds read beyond them (kept[i] >= i), so it
   // may be in place.
   __syncthreads();
-  const int heads = p.granularity ? 1 : p.Hkv;
+#pragma unroll 1
   for (int g = 0; g < heads; ++g) {
     const float* src = w0 + (int64_t)g * p.w.sh;
     float* dst = wd0 + (int64_t)g * p.wd.sh;
+#pragma unroll 1
     for (int i0 = 0; i0 < (along ? 0 : K); i0 += kSelThreads) {
       const int i = i0 + tid;
       float x = 0.f;
@@ -240,6 +266,7 @@ __global__ void __launch_bounds__(kSelThreads) k_evict_select(const __grid_const
       if (i < K) dst[i] = x;
     }
     if (p.in_place)
+#pragma unroll 1
       for (int i = K + tid; i < T; i += kSelThreads) dst[i] = 0.f;
   }
 }
