@@ -425,6 +425,11 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
       const bool rows_here = __any_sync(0xffffffffu, valid);
       const int t = valid ? q.sq.len - q.sq.n + row_token(p, row) : -1;  // its position
       const int low = p.window < 0 ? -1 : t - p.window;                  // the window sees j > low
+      // Tiles inside [all_lo, all_hi), or below both all_hi and the sinks' end, are
+      // seen whole by every row of the group.
+      const int last = min(row_s + kTcTile, q.it.row0 + q.it.rows) - 1;
+      const int all_hi = q.sq.len - q.sq.n + row_token(p, row_s) + 1;
+      const int all_lo = p.window < 0 ? 0 : q.sq.len - q.sq.n + row_token(p, max(last, 0)) - p.window + 1;
       float m = -CUDART_INF_F, l = 0.f;
       const bool split = q.it.split;
       bool have = false;  // O holds something
@@ -432,12 +437,10 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
 #pragma unroll 1
       for (int i = NQ == 1 ? s : 0; i < n && group; i += NQ == 1 ? 2 : 1) {
         const int j0 = q.it.tl.tile(q.u0 + i) * kTcTile;
-        bool all = !valid || (j0 + kTcTile - 1 <= t && (j0 > low || j0 + kTcTile <= p.sinks));
         wait(s_full + 2 * s, (ns >> 1) & 1);
-        const uint32_t bad = bad_ring[(tiles + i) % kMaskRing];
-        if (bad) all = false;
-        const bool masked = !__all_sync(0xffffffffu, all);
-        float* zr = p.weigh && valid ? p.z + ((int64_t)(q.b * p.Hkv + q.g) * p.R + row) * p.z_row + j0 : nullptr;
+        const uint32_t bad = p.paged ? bad_ring[(tiles + i) % kMaskRing] : 0u;
+        const bool masked = bad || j0 + kTcTile > all_hi || (j0 < all_lo && j0 + kTcTile > p.sinks);
+        float* zr = NQ == 1 && p.weigh && valid ? p.z + ((int64_t)(q.b * p.Hkv + q.g) * p.R + row) * p.z_row + j0 : nullptr;
 #pragma unroll 1
         for (int k0 = 0; k0 < kTcTile; k0 += kSub) {
           const int half = k0 / kSub;
