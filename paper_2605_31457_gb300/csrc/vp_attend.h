@@ -144,11 +144,21 @@ struct AttItem {
   __host__ __device__ int cost(int fixed) const { return fixed + tl.n * unit(); }
   // Tiles that start in front of position x of the item.
   __host__ __device__ int tiles_before(int x, int fixed) const {
-    const int u = (x - fixed + unit() - 1) / unit();
+    const int u = split ? (x - fixed + kSplitUnits - 1) / kSplitUnits : (x - fixed + kTileUnits - 1) / kTileUnits;
     return x <= fixed ? 0 : u < tl.n ? u : tl.n;
   }
 };
-__host__ __device__ inline AttItem att_item(int len, int n, int G, int block, int qt, int window, int sinks) {
+// row / G; on the device by AttendParams::g_mul.
+__host__ __device__ inline int token_of_row(int row, int G, uint32_t g_mul) {
+#ifdef __CUDA_ARCH__
+  return g_mul ? (int)__umulhi((unsigned)row, g_mul) : row;
+#else
+  (void)g_mul;
+  return row / G;
+#endif
+}
+__host__ __device__ inline AttItem att_item(int len, int n, int G, int block, int qt, int window, int sinks,
+                                            uint32_t g_mul = 0) {
   AttItem it;
   it.row0 = qt * block;
   const int left = n * G - it.row0;
@@ -156,8 +166,8 @@ __host__ __device__ inline AttItem att_item(int len, int n, int G, int block, in
   it.split = 1;
   it.sr = SeenRange{0, 0, 0};
   if (it.rows > 0) {
-    const int t = len - n + it.row0 / G;
-    it.sr = seen_range(t, len - n + (it.row0 + it.rows - 1) / G, window, sinks);
+    const int t = len - n + token_of_row(it.row0, G, g_mul);
+    it.sr = seen_range(t, len - n + token_of_row(it.row0 + it.rows - 1, G, g_mul), window, sinks);
     const int in = window < 0 || window > t ? t + 1 : window;
     const int seen = in + (sinks < t + 1 - in ? sinks : t + 1 - in);
     it.split = block <= kTcTile || seen < kSplitSeen;

@@ -251,7 +251,7 @@ __global__ void __launch_bounds__(DecCfg<D, GM>::THREADS, DecCfg<D, GM>::CPS) k_
           if (!wait_all(full + sl, (pc / S) & 1)) { timed_out = true; break; }
           // V rows that nobody sees, or of unmapped pages: zero them.
           const int j0 = q.it.tl.tile(q.u0 + i - 1) * kTcTile;
-          const uint32_t bad = bad_ring[(tiles + i - 1) % kBadRing];
+          const uint32_t bad = p.paged ? bad_ring[(tiles + i - 1) % kBadRing] : 0u;
           const SeenRange& sr = q.it.sr;
           if (bad || !((j0 >= sr.lo && j0 + kTcTile <= sr.hi) || j0 + kTcTile <= sr.s_end)) {
 #pragma unroll 1
@@ -369,8 +369,7 @@ __global__ void __launch_bounds__(DecCfg<D, GM>::THREADS, DecCfg<D, GM>::CPS) k_
         }
         tc_fence_before();
         arrive(s_free + sb);
-        const uint32_t bad = bad_ring[(tiles + i) % kBadRing];
-        if ((bad >> (r / R2)) & 1u) see = 0;
+        if (p.paged && ((bad_ring[(tiles + i) % kBadRing] >> (r / R2)) & 1u)) see = 0;
         if (p.weigh && !dead) {
           float* zr = p.z + ((int64_t)(q.b * p.Hkv + q.g) * p.R + h0) * p.z_row + j;
 #pragma unroll

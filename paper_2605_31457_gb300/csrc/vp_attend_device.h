@@ -30,9 +30,7 @@ __device__ __forceinline__ NewSeq load_new(const AttendParams& p, int b, bool re
 }
 
 // The new token of a query row, row / G, by a multiplication (rows < 2^28).
-__device__ __forceinline__ int row_token(const AttendParams& p, int row) {
-  return p.g_mul ? (int)__umulhi((unsigned)row, p.g_mul) : row;
-}
+__device__ __forceinline__ int row_token(const AttendParams& p, int row) { return token_of_row(row, p.G, p.g_mul); }
 // Output row (new token row / G, query head g * G + row % G) of sequence b.
 template <typename T>
 __device__ __forceinline__ T* out_row(const AttendParams& p, int b, int g, int row) {
@@ -79,7 +77,7 @@ __device__ __forceinline__ bool next_part(const AttendParams& p, Walk& w, Part& 
   w.known = false;
   q.sq.len = uniform(w.sq.len);
   q.sq.n = uniform(w.sq.n);
-  q.it = att_item(q.sq.len, q.sq.n, p.G, p.block, w.pair - q.b * p.nqt, p.window, p.sinks);
+  q.it = att_item(q.sq.len, q.sq.n, p.G, p.block, w.pair - q.b * p.nqt, p.window, p.sinks, p.g_mul);
   const int cost = q.it.cost(p.fixed), end = min(cost, w.off + w.left), done = end - w.off;
   q.u0 = q.it.tiles_before(w.off, p.fixed);
   q.u1 = q.it.tiles_before(end, p.fixed);
@@ -130,7 +128,7 @@ __device__ __forceinline__ Walk line_start(const AttendParams& p, int* misc) {
   auto pair_cost = [&](int i, bool report) {
     const int b = p.nqt == 1 ? i : i / p.nqt;
     sq = load_new(p, b, report && blockIdx.x == 0 && i == b * p.nqt);
-    return att_item(sq.len, sq.n, p.G, p.block, i - b * p.nqt, p.window, p.sinks).cost(p.fixed);
+    return att_item(sq.len, sq.n, p.G, p.block, i - b * p.nqt, p.window, p.sinks, p.g_mul).cost(p.fixed);
   };
   int mine = 0;
 #pragma unroll 1

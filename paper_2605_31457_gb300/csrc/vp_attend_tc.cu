@@ -83,13 +83,13 @@ __host__ __device__ constexpr uint32_t att_idesc(int n, int b_mn) {
 __device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
 // Which of the 32 tokens from jb on (columns k .. k + 31 of their tile) a row at
 // position t sees whose window begins after `low`; bad: the tile's unmapped boxes
-// of `box` rows.
+// of 1 << box rows.
 __device__ __forceinline__ uint32_t seen_bits(int jb, int t, int low, int sinks, uint32_t bad, int k, int box) {
   uint32_t see = low_bits(t + 1 - jb) & (~low_bits(low + 1 - jb) | low_bits(sinks - jb));
   if (bad) {
 #pragma unroll 1
     for (int x = 0; x < 32; ++x)
-      if ((bad >> ((k + x) / box)) & 1u) see &= ~(1u << x);
+      if ((bad >> ((k + x) >> box)) & 1u) see &= ~(1u << x);
   }
   return see;
 }
@@ -166,7 +166,7 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
   Part q;
   const unsigned tmem = (unsigned)uniform(misc[20]);  // columns [0, 128), [128, 256): S / P; from 256: O of the groups
   const int R2 = p.paged ? min(kTcTile, p.page_size) : kTcTile;  // rows per copied box
-  const int nb = kTcTile / R2;
+  const int box = 31 - __clz(R2), nb = kTcTile / R2;
   unsigned err = 0;
   bool timed_out = false;
 
@@ -314,13 +314,13 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
         // V rows that no row of the item sees, or of unmapped pages: zero them
         // before the product reads them (both warps, where both do).
         const int j0 = q.it.tl.tile(q.u0 + t) * kTcTile;
-        const uint32_t bad = bad_ring[(tiles + t) % kMaskRing];
+        const uint32_t bad = p.paged ? bad_ring[(tiles + t) % kMaskRing] : 0u;
         const SeenRange& sr = q.it.sr;
         if (bad || !((j0 >= sr.lo && j0 + kTcTile <= sr.hi) || j0 + kTcTile <= sr.s_end)) {
 #pragma unroll 1
           for (int r = lane; r < kTcTile; r += 32) {
             const int j = j0 + r;
-            if ((j < sr.s_end || (j >= sr.lo && j < sr.hi)) && !((bad >> (r / R2)) & 1u)) continue;
+            if ((j < sr.s_end || (j >= sr.lo && j < sr.hi)) && !((bad >> (r >> box)) & 1u)) continue;
             unsigned char* vr = smem + vs * C::SLOT + r * 128;
 #pragma unroll
             for (int x = 0; x < C::HALVES * 8; ++x)
@@ -463,8 +463,8 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
               tmem_ld_wait(xa);
               tmem_ld_wait(xb);
               if (masked) {
-                mask_cols(xa, seen_bits(j0 + k0, t, low, p.sinks, bad, k0, R2));
-                mask_cols(xb, seen_bits(j0 + k0 + 32, t, low, p.sinks, bad, k0 + 32, R2));
+                mask_cols(xa, seen_bits(j0 + k0, t, low, p.sinks, bad, k0, box));
+                mask_cols(xb, seen_bits(j0 + k0 + 32, t, low, p.sinks, bad, k0 + 32, box));
               }
               if (again) {
                 float top = x[0];
