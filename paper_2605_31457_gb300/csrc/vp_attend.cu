@@ -328,7 +328,8 @@ __global__ void __launch_bounds__(128) k_att_any(const __grid_constant__ AttendP
 // k_att_weights: weight_out = weight_in + sum over the query rows of
 // exp2(z - lse), from the logits that the attention kernel stored; a thread per
 // four cached tokens of one (sequence, kv-head).  Bound by reading the logits
-// (4 R bytes per token and kv-head, from L2 where they fit).
+// (4 R bytes per token and kv-head, from L2 where they fit): 9.5 us for 8 sequences
+// of 20480 tokens and 7 rows (18 MB).
 // ---------------------------------------------------------------------------
 constexpr int kWeightThreads = 128, kWeightTokens = 4 * kWeightThreads;
 

@@ -36,7 +36,7 @@ struct NewLayout {
 // Which kernel serves a call (plan_attend).  `block` query rows of one
 // (sequence, kv-head) are an item of the tensor-core kernels:
 //   ATT_DEC  k_att_dec: at most 64 query rows, all of them one item;
-//   ATT_TC1  k_att_tc: at most 128, one item whose tiles alternate between its
+//   ATT_TC1  k_att_tc: 65 to 128, one item whose tiles alternate between its
 //            two softmax groups;
 //   ATT_TC2  k_att_tc: 256 rows at a time, 128 for each group.
 enum { ATT_ANY = 0, ATT_DEC = 1, ATT_TC1 = 2, ATT_TC2 = 3 };
@@ -197,10 +197,11 @@ struct LineCut {
 // Few items (at most a quarter as many as CTAs) are not cut as one line: each
 // gets CTAs of its own, share_count of them, so that no CTA does the end of one
 // item and then the beginning of another while the rest wait (one sequence of
-// 3857 tokens, 28/4 heads: 17.1 -> 15.4 us a call; with up to half as many items
-// as CTAs, 32 sequences of 2816 to 6400 tokens went from 66 to 73 us).  Share k of m is [cost * k / m,
-// cost * (k + 1) / m): at least half of `per` >= min_share(fixed), which covers
-// the fixed part and a tile, so every share has a tile.
+// 3857 tokens, 28/4 heads: 17.1 -> 15.4 us a call when it was made; with up to
+// half as many items as CTAs, 32 sequences of 2816 to 6400 tokens went from 66 to
+// 73 us).  Share k of m is [cost * k / m, cost * (k + 1) / m): at least half of
+// `per` >= min_share(fixed), which covers the fixed part and a tile, so every share
+// has a tile.
 __host__ __device__ inline int min_share(int fixed) { return 2 * (fixed > kSplitUnits ? fixed + 1 : kSplitUnits); }
 __host__ __device__ inline int share_count(int cost, int per) { return (cost + per - 1) / per; }
 

@@ -27,14 +27,20 @@ namespace {
 // P enters the product as two bf16 terms, P = hi + lo, in columns [0, GM) and
 // [GM, 2 GM) of P^T; the two halves of O are added at the end.  P's rounding
 // (2^-17 of it) then vanishes beside the output's, at no cost: the kernel is
-// bound by HBM, 64 KB per tile at D = 128.
+// bound by HBM, 64 KB per tile at D = 128, and for few or short sequences by its
+// start and end (about 10 us: the line's cut, the first tiles, the records and
+// their join).  D = 128: 64 sequences of 17408 tokens, 32/8 heads, in 627 us (7.3
+// TB/s); 16 of 2305 to 9001 tokens with five new tokens each in 68 us (5.4 TB/s);
+// one of 3857 tokens, 28/4 heads, in 13.3 us.  With the queries as the M side and
+// a join kernel of its own (k_att_tc's first form, which served these calls before)
+// the first took 904 us against 639 and the last 28 us against 16.
 //
 // A row's reference is the largest logit of the first tile it sees and is raised
 // only when a logit passes it by more than 64 (log2 units), when O and the sums
 // are rescaled, so most tiles need no exchange between the threads; P <= 2^64
-// has bf16's and float's full precision all the same.  The work is a line of tiles cut evenly over
-// the CTAs (AttItem, LineCut): an item whose tiles lie with several CTAs leaves
-// a record per CTA, and the last CTA to finish joins them.
+// has bf16's and float's full precision all the same.  The work is a line of
+// tiles cut evenly over the CTAs (AttItem, LineCut): an item whose tiles lie with
+// several CTAs leaves a record per CTA, and the last CTA to finish joins them.
 //
 // Rows of a tile that nobody sees may hold anything: their logits are masked,
 // and their V rows are zeroed in shared memory before the product (0 x NaN is

@@ -23,24 +23,36 @@ namespace {
 //                   in TMEM.
 // Query rows are the (new token, head of the kv-head) pairs, so a group of G
 // heads shares every K and V row that is copied.  Each softmax group has its
-// own S and O in TMEM (4 x 128 columns = all 512 at D = 128); P, rounded to
-// bf16, overwrites S.  The groups take turns: while one turns its S into P the
-// tensor cores work for the other.
-//   NQ = 1 (decode, drafted tokens: at most 128 rows): both groups hold the
-//          same queries and take alternate tiles; each writes its own partial.
-//          Bound by HBM: 64 KB per tile at D = 128 against 0.25 us of tensor
-//          work, which is why M = 128 may stand mostly empty at G = 7 rows.
+// own S and O in TMEM (4 x 128 columns = all 512 at D = 128); P overwrites S.
+// The groups take turns: while one turns its S into P the tensor cores work for
+// the other.
+//   NQ = 1 (65 to 128 rows): both groups hold the same queries and take alternate
+//          tiles; each writes its own record.
 //   NQ = 2 (prompts): the groups hold 128 query rows each and both read every
-//          tile.  Bound by the tensor cores and, close behind, by the
-//          exponentials: 128 x 128 of them per 2 x 128 x 128 x D MACs.
+//          tile.
 // The work is a line of tiles cut evenly over the CTAs (vp_attend.h): an item
-// cut between CTAs leaves partials (m, l, O) that k_att_join merges.
+// cut between CTAs leaves a record (m, l, O) per CTA, and the last CTA to finish
+// joins them.
+//
+// Prompts are bound by two chains of about the same length that take turns, not
+// by a pipe: per half tile a softmax thread spends about 1000 clocks on 64
+// exponentials and as much on waits, TMEM loads and arrivals, and a product warp
+// as much on issuing 12 products (S from 64 tokens reads 6 KB of shared memory
+// for 32 clocks of tensor work).  28/4 heads of 128: 3857 tokens in 154 us (690
+// TFLOP/s); 32/8 heads, 12289 tokens with a window of 2048 and 4 sinks in 419 us
+// (900 TFLOP/s, tensor pipe 48% busy).  Slower were: two warps for every 32 rows,
+// 32 columns each (16 softmax warps of 96 registers; 533 against 447 us at the
+// time); S's second half loaded during the first's exponentials (461 against 420);
+// the next step's S fetched before a P is announced (491 against 419).  What
+// helped most was less code: instructions fetched from L2 cost more than the
+// work outside the tile loop (211 -> 90 KB of code, 526 -> 420 us with the next
+// part's queries loaded during this one's output).
 //
 // Softmax: a row's reference m is the largest logit of the first 64 tokens it
 // sees, and is raised, O rescaled in TMEM, only when P = exp2(z - m) passes 2^64:
 // up to there P has bf16's and float's full precision all the same, and S is
-// read once.  P goes to the tensor cores as bf16, in two terms hi + lo where few
-// tokens share the weight (AttItem::split); l sums the unrounded values in 32
+// read once.  P goes to the tensor cores as bf16, in two terms hi + lo unless
+// every row sees many tokens (AttItem::split); l sums the unrounded values in 32
 // bits.
 //
 // Rows of a tile that nobody sees may hold anything: their logits are masked,
@@ -450,9 +462,8 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
             // columns [k, k + 16), k = 0 and 32, take hi of tokens k .. k + 31
             // and the next 16 lo (with split).  A P past 2^64 shows in their sum,
             // so no maximum is formed unless the reference must be set or raised;
-            // S is then read again.  In a rolled loop over the halves: eleven
-            // warps run different code at once, and unrolled over the whole row
-            // this outgrew the instruction cache.
+            // S is then read again.  Loops stay rolled and each piece of code
+            // single: eleven warps run different code at once.
             float x[64];
             float (&xa)[32] = *reinterpret_cast<float (*)[32]>(x), (&xb)[32] = *reinterpret_cast<float (*)[32]>(x + 32);
             uint32_t hi[32];
@@ -618,7 +629,7 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
   if (timed_out) err |= ERR_TIMEOUT;
   if (err) atomicOr(p.err, err);
   // Every copy has landed and every tensor-core operation is complete (warps 8
-  // and 9 waited for them, bounded); free the columns.
+  // to 10 waited for them, bounded); free the columns.
   tc_fence_before();
   __syncthreads();
   if (warp == 9) {

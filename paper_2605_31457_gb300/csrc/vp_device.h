@@ -254,9 +254,6 @@ __device__ __forceinline__ void umma(unsigned d, uint64_t a, uint64_t b, uint32_
 // compiler knows to be: what is computed from such values stays in the uniform
 // registers that tensor-core instructions take their operands from.
 __device__ __forceinline__ int uniform(int x) { return __reduce_max_sync(0xffffffffu, x); }
-__device__ __forceinline__ int64_t uniform(int64_t x) {
-  return (int64_t)uniform((int)(x >> 32)) << 32 | (uint32_t)uniform((int)x);
-}
 // The low word of umma_desc's descriptor for a stride of 1024 bytes, as the
 // products below take it: their high word is a constant.
 __device__ __forceinline__ uint32_t umma_desc_lo(unsigned addr, unsigned lbo) {
