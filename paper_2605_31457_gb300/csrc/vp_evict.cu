@@ -15,8 +15,8 @@ namespace vp {
 namespace {
 
 constexpr int kSelThreads = 1024, kSelWarps = kSelThreads / 32;
-constexpr int kMoveThreads = 128;   // and four rows a thread: the best of 1 to 8 rows and 128 to 512 threads
-constexpr int kMoveLoads = 4;       // rows a thread of k_evict_move has in flight, out of place
+constexpr int kMoveThreads = 128, kMoveWarps = kMoveThreads / 32;
+constexpr int kMoveLoads = 4;       // 16-byte pieces a lane of k_evict_move has in flight, out of place
 constexpr int kInPlaceRows = 8;     // rows a thread of it holds at a time, in place
 constexpr int kBins = 2048;         // 11-bit digits
 
@@ -291,20 +291,21 @@ __device__ __forceinline__ char* row_bytes(const EvictParams& p, const KvView& k
 }
 
 // ---------------------------------------------------------------------------
-// k_evict_move: one (sequence, kv-head, K or V) per group of CTAs; each thread
-// copies 16-byte pieces.  Out of place a CTA takes a run of destination rows, a
-// thread the same piece of four of them, all four in flight (a form with sixteen
-// rows per thread, lists and pages read ahead, had too few CTAs per SM: 150
-// against 118 us for 512 MB).  In place a CTA takes a column slice of every
-// row, in rounds of destination rows in ascending order: a round's reads come
-// before its writes (a barrier between), and kept[i] >= i, so no row is
+// k_evict_move: one (sequence, kv-head, K or V) per group of CTAs.  Out of place
+// a warp takes a run of up to 32 destination rows: lane i looks up where row i
+// comes from and goes to, then the rows are moved 16 bytes a lane, their addresses
+// passed by shuffles (every lane finding its own rows' addresses, four rows each,
+// it was bound by those instructions: 119 against 91 us a call with 512 MB to move).
+// In place a CTA takes a column slice of every row, in rounds of destination rows
+// in ascending order: a round's reads come before its writes (a barrier between),
+// and kept[i] >= i, so no row is
 // overwritten before it is read.  Bound by HBM: each kept row is read and written
-// once (512 MB of kept 256-byte rows from pages of 16 in 111 us, 4.6 TB/s; longer
-// runs of rows per CTA, more rows in flight and plain cache hints were slower).
+// once (a call with 512 MB of 256-byte rows in pages of 16: 91 us, 5.6 TB/s with the
+// selection).
 // ---------------------------------------------------------------------------
 template <bool IN_PLACE>
 __global__ void __launch_bounds__(kMoveThreads) k_evict_move(const __grid_constant__ EvictParams p, int slices,
-                                                             int chunks) {
+                                                             int chunks, int run) {
   // No early trigger: the next call may read these caches before its own wait.
   pdl_wait();
   const int tid = threadIdx.x;
@@ -323,31 +324,35 @@ __global__ void __launch_bounds__(kMoveThreads) k_evict_move(const __grid_consta
   const int pieces = p.D * p.esz / 16;
   unsigned err = 0;
   if (!IN_PLACE) {
-    const int step = kMoveThreads / pieces, piece = tid % pieces;
-    const int i0 = part * step * kMoveLoads + tid / pieces;
-    const char* s[kMoveLoads];
-    uint4 x[kMoveLoads];
-#pragma unroll
-    for (int k = 0; k < kMoveLoads; ++k) {
-      const int i = i0 + k * step;
-      s[k] = nullptr;
-      if (i >= K) continue;
+    // Lane i of a warp finds where row i of its `run` rows comes from and goes to;
+    // then `pieces` lanes move a row together.
+    const int lane = tid & 31, i = (part * kMoveWarps + (tid >> 5)) * run + lane;
+    const char* from = nullptr;
+    char* to = nullptr;
+    if (lane < run && i < K) {
       const int j = __ldcg(kept + i);
-      s[k] = row_bytes(p, src, b, g, j, page_of(p, src, b, j));
-      if (!s[k]) err |= ERR_PAGE;
+      from = row_bytes(p, src, b, g, j, page_of(p, src, b, j));
+      to = row_bytes(p, dst, b, g, i, page_of(p, dst, b, i));
+      if (!from || !to) err |= ERR_PAGE;
     }
+    const int step = 32 / pieces, r = lane / pieces, at = lane % pieces * 16;
+    auto pointer = [](const char* x, int lane) {
+      return reinterpret_cast<char*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(x), lane));
+    };
+#pragma unroll 1
+    for (int r0 = r; r0 - r < run; r0 += kMoveLoads * step) {
+      uint4 x[kMoveLoads];
 #pragma unroll
-    for (int k = 0; k < kMoveLoads; ++k) {
-      x[k] = make_uint4(0u, 0u, 0u, 0u);
-      if (s[k]) x[k] = __ldcs(reinterpret_cast<const uint4*>(s[k]) + piece);
-    }
+      for (int k = 0; k < kMoveLoads; ++k) {
+        const char* s = pointer(from, r0 + k * step);
+        x[k] = make_uint4(0u, 0u, 0u, 0u);
+        if (s && r0 + k * step < run) x[k] = __ldcs(reinterpret_cast<const uint4*>(s + at));
+      }
 #pragma unroll
-    for (int k = 0; k < kMoveLoads; ++k) {
-      const int i = i0 + k * step;
-      if (i >= K) continue;
-      char* d = row_bytes(p, dst, b, g, i, page_of(p, dst, b, i));
-      if (d) __stcs(reinterpret_cast<uint4*>(d) + piece, x[k]);
-      else err |= ERR_PAGE;
+      for (int k = 0; k < kMoveLoads; ++k) {
+        char* d = pointer(to, r0 + k * step);
+        if (d && r0 + k * step < run) __stcs(reinterpret_cast<uint4*>(d + at), x[k]);
+      }
     }
   } else if (K > 0 && __ldcg(kept + K - 1) != K - 1) {  // else every row stays where it is
     const int mine = pieces / slices, step = kMoveThreads / mine;
@@ -417,13 +422,17 @@ cudaError_t launch_evict(const EvictParams& p, cudaStream_t st) {
   int slices = 1;
   while (slices * 2 <= pieces / 2 && units * slices < 2 * p.num_sms) slices *= 2;
   const int rows = p.keep < p.max_seq ? p.keep : p.max_seq;
-  const int run = kMoveThreads / pieces * kMoveLoads;
-  const int chunks = (rows + run - 1) / run;
+  // Rows of a warp, out of place: 16, or 8 where that leaves fewer than four CTAs
+  // per SM (one sequence, 2048 rows kept: 9.4 us a call against 10.0; 32 sequences,
+  // 4096 rows: 97 against 91).
+  const int64_t wide = units * ((rows + 16 * kMoveWarps - 1) / (16 * kMoveWarps));
+  const int run = wide >= 4 * p.num_sms ? 16 : 8, per_cta = kMoveWarps * run;
+  const int chunks = (rows + per_cta - 1) / per_cta;
   const int64_t grid = units * (p.in_place ? slices : chunks);
   if (grid > INT32_MAX) return cudaErrorInvalidConfiguration;
   if (grid == 0) return cudaSuccess;
   return launch_dep(p.in_place ? k_evict_move<true> : k_evict_move<false>, dim3((unsigned)grid), kMoveThreads, 0, st, p,
-                    slices, chunks);
+                    slices, chunks, run);
 }
 
 }  // namespace vp
