@@ -45,8 +45,8 @@ __device__ __forceinline__ int live_len(const EvictParams& p, int b, bool report
 // which are in the threshold's bin; only the latter, a few in a hundred, are
 // looked at again.  Keys above the threshold stay, and of the equal ones the
 // first in position, so the result does not depend on any order of atomics.
-// Bound by instructions and barriers on one SM: with the move's start 10.5 us for
-// a call on 3857 tokens, about 20 us of a call on 8 sequences of 20480 tokens.  Slower were: 256 bins with a
+// Bound by instructions and barriers on one SM: a call on one sequence of 3857
+// tokens takes 9.2 us with the move, on 8 of 20480 tokens 38 us.  Slower were: 256 bins with a
 // column per lane against queues at one address and four passes (3857 tokens:
 // 10.0 against 7.6 us), one addition per bin and warp after matching the lanes
 // (10.4 us), clusters of eight CTAs that share their histograms through
@@ -117,19 +117,24 @@ __global__ void __launch_bounds__(kSelThreads) k_evict_select(const __grid_const
         if (i0 + k < steps && a + 32 * (i0 + k) < T) keys_s[a + 32 * (i0 + k)] = order_key(w[k]);
     }
   }
-  // Calls f(step, key) for this thread's tokens of the middle, of those in `bits` where there is one.
-  auto each = [&](uint32_t bits, auto&& f) {
+  // This thread's steps, a bit each, whose token lies in front of x (KR >= 0: at most
+  // 32 steps).
+  auto in_front = [&](int x) {
+    const int n = min((x - a + 31) >> 5, steps);
+    return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u;
+  };
+  // Calls f(step, key) for this thread's tokens of the middle; KR >= 0: for those in
+  // `bits`, most of them or (few) a few.
+  auto each = [&](uint32_t bits, bool few, auto&& f) {
     if constexpr (KR > 0) {
 #pragma unroll
       for (int i = 0; i < KR; ++i)
-        if (((bits >> i) & 1u) && a + 32 * i >= lo && a + 32 * i < hi) f(i, order_key(held[i]));
+        if ((bits >> i) & 1u) f(i, order_key(held[i]));
     } else if constexpr (KR == 0) {
-      if (bits == 0xffffffffu) {
+      if (!few) {
 #pragma unroll 4
-        for (int i = 0; i < steps; ++i) {
-          const int j = a + 32 * i;
-          if (j >= lo && j < hi) f(i, keys_s[j]);
-        }
+        for (int i = 0; i < steps; ++i)
+          if ((bits >> i) & 1u) f(i, keys_s[a + 32 * i]);
       } else {
 #pragma unroll 1
         for (uint32_t c = bits; c; c &= c - 1) {
@@ -146,7 +151,8 @@ __global__ void __launch_bounds__(kSelThreads) k_evict_select(const __grid_const
   };
   int m = p.keep - p.sinks - p.recent;  // how many of the middle stay
   uint32_t prefix = 0, mask = 0;        // digits of the threshold found so far
-  uint32_t up = 0, cand = 0xffffffffu;  // a bit per step: stays for sure; may be equal to the threshold
+  // A bit per step: stays for sure; may be equal to the threshold.
+  uint32_t up = 0, cand = in_front(hi) & ~in_front(lo);
   const bool any = m > 0;
   if (any) {
 #pragma unroll 1
@@ -155,7 +161,7 @@ __global__ void __launch_bounds__(kSelThreads) k_evict_select(const __grid_const
       const uint32_t digits = pass == 2 ? 1023u : 2047u;
       for (int i = tid; i < kBins; i += kSelThreads) hist[i] = 0;
       __syncthreads();
-      each(cand, [&](int, uint32_t k) {
+      each(cand, pass > 0, [&](int, uint32_t k) {
         if ((k & mask) == prefix) atomicAdd(&hist[(k >> shift) & digits], 1);
       });
       __syncthreads();
@@ -181,7 +187,7 @@ __global__ void __launch_bounds__(kSelThreads) k_evict_select(const __grid_const
       mask |= digits << shift;
       if constexpr (KR >= 0) {
         uint32_t in = 0;
-        each(cand, [&](int i, uint32_t k) {
+        each(cand, pass > 0, [&](int i, uint32_t k) {
           const uint32_t d = k & mask;
           if (d > prefix) up |= 1u << i;
           if (d == prefix) in |= 1u << i;
@@ -194,23 +200,21 @@ __global__ void __launch_bounds__(kSelThreads) k_evict_select(const __grid_const
   }
   const int equal = any ? m : 0;  // of the keys equal to the threshold, how many stay
   // Counts per segment, their scan, then the kept positions in order.
-  auto stays = [&](int i, int j, bool& eq) {  // without ties; eq: equal to the threshold
+  auto stays = [&](int j, bool& eq) {  // KR < 0: without ties; eq: equal to the threshold
     const bool mid = j >= lo && j < hi;
-    if constexpr (KR >= 0) {
-      eq = (cand >> i) & 1u;
-      return (bool)((up >> i) & 1u) || (j < T && !mid);
-    } else {
-      const uint32_t k = mid && any ? order_key(weight_at(j)) : 0u;
-      eq = mid && any && k == prefix;
-      return (mid && any && k > prefix) || (j < T && !mid);
-    }
+    const uint32_t k = mid && any ? order_key(weight_at(j)) : 0u;
+    eq = mid && any && k == prefix;
+    return (mid && any && k > prefix) || (j < T && !mid);
   };
-  int ng = 0, ne = 0;
-#pragma unroll 4
-  for (int i = 0; i < steps; ++i) {
-    bool eq;
-    ng += stays(i, a + 32 * i, eq);
-    ne += eq;
+  if constexpr (KR >= 0) up |= (in_front(lo) | ~in_front(hi)) & in_front(T);
+  int ng = __popc(up), ne = __popc(cand);
+  if constexpr (KR < 0) {
+    ng = ne = 0;
+    for (int i = 0; i < steps; ++i) {
+      bool eq;
+      ng += stays(a + 32 * i, eq);
+      ne += eq;
+    }
   }
   ng = __reduce_add_sync(0xffffffffu, ng);
   ne = __reduce_add_sync(0xffffffffu, ne);
@@ -218,14 +222,22 @@ __global__ void __launch_bounds__(kSelThreads) k_evict_select(const __grid_const
   __syncthreads();
   int eq_before = __reduce_add_sync(0xffffffffu, lane < warp ? seg_eq[lane] : 0);
   int at = __reduce_add_sync(0xffffffffu, lane < warp ? seg_kept[lane] : 0) + min(eq_before, equal);
+  // Usually the equal ones all stay; only a tie that is split asks for their order.
+  const bool tie = KR < 0 || __reduce_add_sync(0xffffffffu, seg_eq[lane]) != equal;
+  if (!tie) up |= cand;
   // One kept set per kv-head: the weights go along, from registers (every one
   // has been read, so also in place) or, out of place, read again.
   const bool along = p.granularity && p.wd.data && (KR > 0 || !p.in_place);
   auto emit = [&](int i, int j, float w) {
-    bool eq;
-    const bool sure = stays(i, j, eq);
-    const unsigned me = __ballot_sync(0xffffffffu, eq), below = (1u << lane) - 1u;
-    const bool stay = sure || (eq && eq_before + __popc(me & below) < equal);
+    const unsigned below = (1u << lane) - 1u;
+    bool stay = (up >> i) & 1u;
+    if (tie) {
+      bool eq = (cand >> i) & 1u;
+      if constexpr (KR < 0) stay = stays(j, eq);
+      const unsigned me = __ballot_sync(0xffffffffu, eq);
+      stay = stay || (eq && eq_before + __popc(me & below) < equal);
+      eq_before += __popc(me);
+    }
     const unsigned ms = __ballot_sync(0xffffffffu, stay);
     const int to = at + __popc(ms & below);
     if (stay && to < K) {
@@ -233,7 +245,6 @@ __global__ void __launch_bounds__(kSelThreads) k_evict_select(const __grid_const
       if (along) wd0[to] = w;
     }
     at += __popc(ms);
-    eq_before += __popc(me);
   };
   if constexpr (KR > 0) {
 #pragma unroll
@@ -423,8 +434,8 @@ cudaError_t launch_evict(const EvictParams& p, cudaStream_t st) {
   while (slices * 2 <= pieces / 2 && units * slices < 2 * p.num_sms) slices *= 2;
   const int rows = p.keep < p.max_seq ? p.keep : p.max_seq;
   // Rows of a warp, out of place: 16, or 8 where that leaves fewer than four CTAs
-  // per SM (one sequence, 2048 rows kept: 9.4 us a call against 10.0; 32 sequences,
-  // 4096 rows: 97 against 91).
+  // per SM (one sequence, 2048 rows kept: 9.4 us a call with 8, 10.0 with 16; 32
+  // sequences, 4096 rows: 97 with 8, 91 with 16).
   const int64_t wide = units * ((rows + 16 * kMoveWarps - 1) / (16 * kMoveWarps));
   const int run = wide >= 4 * p.num_sms ? 16 : 8, per_cta = kMoveWarps * run;
   const int chunks = (rows + per_cta - 1) / per_cta;
