@@ -312,16 +312,12 @@ __global__ void __launch_bounds__(128) k_att_any(const __grid_constant__ AttendP
       if (d == 0) *reinterpret_cast<float2*>(p.part_st + 2 * (rec + r)) = make_float2(sm.m[r], sm.l[r]);
     } else if (r0 + r < p.R) {
       const float inv = sm.l[r] > 0.f ? 1.f / sm.l[r] : 0.f;
-      T* out = out_row<T>(p, b, g, r0 + r) + d;
-      out[0] = from_f<T>(o.x * inv);
-      out[1] = from_f<T>(o.y * inv);
-      out[2] = from_f<T>(o.z * inv);
-      out[3] = from_f<T>(o.w * inv);
+      store4(out_row<T>(p, b, g, r0 + r) + d, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
       if (d == 0) store_lse(p, b, g, r0 + r, sm.m[r], sm.l[r]);
     }
   }
   if (p.ns > 1 && last_to_arrive(p.tickets + unit, p.ns, tid, &sm.flag, [] { __syncthreads(); }))
-    join_records<T, D, 128>(p, b, g, r0, min(RB, p.R - r0), p.ns, RB, [&](int k) { return unit * p.ns + k; }, tid);
+    join_records<T, D, 128, 1, 16>(p, b, g, r0, min(RB, p.R - r0), p.ns, RB, [&](int k) { return unit * p.ns + k; }, tid);
 }
 
 // ---------------------------------------------------------------------------

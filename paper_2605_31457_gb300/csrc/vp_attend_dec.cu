@@ -504,7 +504,7 @@ __global__ void __launch_bounds__(DecCfg<D, GM>::THREADS, DecCfg<D, GM>::CPS) k_
       }
       if (direct) continue;
       if (last_to_arrive(p.tickets + c0 * C::SG + sg, q.parts, st, misc + C::LINE + sg, sync))
-        join_records<__nv_bfloat16, D, 128>(p, q.b, q.g, h0, rows, q.parts, GR, [&](int k) { return rec_of(c0 + k); }, st);
+        join_records<__nv_bfloat16, D, 128, 1, 16>(p, q.b, q.g, h0, rows, q.parts, GR, [&](int k) { return rec_of(c0 + k); }, st);
     }
     if (dead) timed_out = true;
   }

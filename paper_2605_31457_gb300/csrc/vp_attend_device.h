@@ -219,55 +219,72 @@ __device__ __forceinline__ bool last_to_arrive(unsigned* ticket, unsigned expect
   return last;
 }
 
+// Four values of a row, 8 or 16 bytes at once.
+__device__ __forceinline__ void store4(float* p, float4 x) { *reinterpret_cast<float4*>(p) = x; }
+__device__ __forceinline__ void store4(__nv_bfloat16* p, float4 x) {
+  *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(x.x, x.y), pack_bf16(x.z, x.w));
+}
 // Joins records rec(0) .. rec(n - 1) of rows [row0, row0 + rows) into out and
-// lse: a thread per row and four dimensions, sixteen records in flight (a round
-// trip to L2 each: the join is bound by their number).
-template <typename T, int D, int NT, typename Rec>
+// lse.  A thread takes EU groups of four dimensions of a row and has KU records in
+// flight (a round trip to L2 each time: the join is bound by their number): many
+// records of few rows want EU = 1 and KU = 16, few records of many rows EU = KU = 4
+// (two sequences, 400 new tokens of 1000, 28/4 heads of 128: 49 us a call against
+// 100).
+template <typename T, int D, int NT, int EU, int KU, typename Rec>
 __device__ __forceinline__ void join_records(const AttendParams& p, int b, int g, int row0, int rows, int n, int RS,
                                              Rec&& rec, int tid) {
-  constexpr int C4 = D / 4, U = 16;
+  constexpr int C = D / 4 / EU;  // threads per row, their groups C apart
 #pragma unroll 1
-  for (int e = tid; e < rows * C4; e += NT) {
-    const int r = e / C4, d = 4 * (e % C4);
+  for (int e = tid; e < rows * C; e += NT) {
+    const int r = e / C, d = 4 * (e % C);
     float m = -CUDART_INF_F, l = 0.f;
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 1
-    for (int k0 = 0; k0 < n; k0 += U) {
-      float2 st[U];
-      float4 x[U];
+    float4 o[EU];
 #pragma unroll
-      for (int k = 0; k < U; ++k) {
+    for (int i = 0; i < EU; ++i) o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+    for (int k0 = 0; k0 < n; k0 += KU) {
+      float2 st[KU];
+      float4 x[KU][EU];
+#pragma unroll
+      for (int k = 0; k < KU; ++k) {
         st[k] = make_float2(-CUDART_INF_F, 0.f);
-        x[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int i = 0; i < EU; ++i) x[k][i] = make_float4(0.f, 0.f, 0.f, 0.f);
         if (k0 + k < n) {
           const int at = rec(k0 + k) * RS + r;  // at most 4 records per SM of up to 128 rows
           st[k] = __ldcg(reinterpret_cast<const float2*>(p.part_st) + at);
-          x[k] = __ldcg(reinterpret_cast<const float4*>(p.part_o + at * D + d));
+#pragma unroll
+          for (int i = 0; i < EU; ++i)
+            x[k][i] = __ldcg(reinterpret_cast<const float4*>(p.part_o + at * D + d + 4 * C * i));
         }
       }
       float mn = m;
 #pragma unroll
-      for (int k = 0; k < U; ++k) mn = fmaxf(mn, st[k].x);
+      for (int k = 0; k < KU; ++k) mn = fmaxf(mn, st[k].x);
       const float mu = mn == -CUDART_INF_F ? 0.f : mn;
       const float f = exp2f(m - mu);
-      l *= f; o.x *= f; o.y *= f; o.z *= f; o.w *= f;
+      l *= f;
 #pragma unroll
-      for (int k = 0; k < U; ++k) {
+      for (int i = 0; i < EU; ++i) { o[i].x *= f; o[i].y *= f; o[i].z *= f; o[i].w *= f; }
+#pragma unroll
+      for (int k = 0; k < KU; ++k) {
         const float w = exp2f(st[k].x - mu);
         l = fmaf(w, st[k].y, l);
-        o.x = fmaf(w, x[k].x, o.x);
-        o.y = fmaf(w, x[k].y, o.y);
-        o.z = fmaf(w, x[k].z, o.z);
-        o.w = fmaf(w, x[k].w, o.w);
+#pragma unroll
+        for (int i = 0; i < EU; ++i) {
+          o[i].x = fmaf(w, x[k][i].x, o[i].x);
+          o[i].y = fmaf(w, x[k][i].y, o[i].y);
+          o[i].z = fmaf(w, x[k][i].z, o[i].z);
+          o[i].w = fmaf(w, x[k][i].w, o[i].w);
+        }
       }
       m = mn;
     }
     const float inv = l > 0.f ? 1.f / l : 0.f;
     T* out = out_row<T>(p, b, g, row0 + r) + d;
-    out[0] = from_f<T>(o.x * inv);
-    out[1] = from_f<T>(o.y * inv);
-    out[2] = from_f<T>(o.z * inv);
-    out[3] = from_f<T>(o.w * inv);
+#pragma unroll
+    for (int i = 0; i < EU; ++i)
+      store4(out + 4 * C * i, make_float4(o[i].x * inv, o[i].y * inv, o[i].z * inv, o[i].w * inv));
     if (d == 0) store_lse(p, b, g, row0 + r, m, l);
   }
 }

@@ -615,10 +615,10 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
       if (!direct && n > 0 && group &&
           last_to_arrive(p.tickets + 2 * c0 + (NQ == 2 ? s : 0), NQ == 1 ? 2 * parts : parts, r, misc + 18 + s, sync)) {
         if (NQ == 1)
-          join_records<__nv_bfloat16, D, 128>(p, q.b, q.g, 0, q.it.rows, 2 * parts, kTcTile,
+          join_records<__nv_bfloat16, D, 128, 4, 4>(p, q.b, q.g, 0, q.it.rows, 2 * parts, kTcTile,
                                               [&](int k) { return rec_of(c0 + (k >> 1), k & 1); }, r);
         else
-          join_records<__nv_bfloat16, D, 128>(p, q.b, q.g, row_s, min(kTcTile, q.it.rows - s * kTcTile), parts, kTcTile,
+          join_records<__nv_bfloat16, D, 128, 4, 4>(p, q.b, q.g, row_s, min(kTcTile, q.it.rows - s * kTcTile), parts, kTcTile,
                                               [&](int k) { return rec_of(c0 + k, s); }, r);
       }
       if (!more) break;
