@@ -38,15 +38,16 @@ namespace {
 // by a pipe: per half tile a softmax thread spends about 1000 clocks on 64
 // exponentials and as much on waits, TMEM loads and arrivals, and a product warp
 // as much on issuing 12 products (S from 64 tokens reads 6 KB of shared memory
-// for 32 clocks of tensor work).  28/4 heads of 128: 3857 tokens in 154 us (690
-// TFLOP/s); 32/8 heads, 12289 tokens with a window of 2048 and 4 sinks in 419 us
-// (900 TFLOP/s, tensor pipe 48% busy).  Slower were: two warps for every 32 rows,
+// for 32 clocks of tensor work).  28/4 heads of 128: 3857 tokens in 126 us (850
+// TFLOP/s); 32/8 heads, 12289 tokens with a window of 2048 and 4 sinks in 388 us
+// (976 TFLOP/s).  Slower were: two warps for every 32 rows,
 // 32 columns each (16 softmax warps of 96 registers; 533 against 447 us at the
 // time); S's second half loaded during the first's exponentials (461 against 420);
 // the next step's S fetched before a P is announced (491 against 419).  What
 // helped most was less code: instructions fetched from L2 cost more than the
 // work outside the tile loop (211 -> 90 KB of code, 526 -> 420 us with the next
-// part's queries loaded during this one's output).
+// part's queries loaded during this one's output), and joins with more loads in
+// flight (419 -> 388).
 //
 // Softmax: a row's reference m is the largest logit of the first 64 tokens it
 // sees, and is raised, O rescaled in TMEM, only when P = exp2(z - m) passes 2^64:
