@@ -205,6 +205,15 @@ struct LineCut {
 __host__ __device__ inline int min_share(int fixed) { return 2 * (fixed > kSplitUnits ? fixed + 1 : kSplitUnits); }
 __host__ __device__ inline int share_count(int cost, int per) { return (cost + per - 1) / per; }
 
+// Records and tickets of the tensor-core kernels.  Of the items whose tiles lie
+// with several CTAs a CTA does at most two: the one it goes on with (c0 < cta) and
+// the one it begins (c0 == cta).  Each has a record of its own there, and the CTA
+// it begins at has its ticket, so none of those is used twice in a call.  An item
+// whose tiles are one CTA's alone may be any of many: it must use no ticket, and
+// what it writes to a record is read before the CTA's next item.
+__host__ __device__ inline int record_of(int cta, int c0) { return 2 * cta + (cta == c0 ? 1 : 0); }
+__host__ __device__ inline bool by_ticket(int parts) { return parts > 1; }
+
 // The longest line a call can have (it is kept below 2^31).
 inline int64_t line_bound(int64_t items, int max_seq, int fixed) {
   return items * (fixed + (int64_t)kSplitUnits * ((max_seq + kTcTile - 1) / kTcTile + 1));

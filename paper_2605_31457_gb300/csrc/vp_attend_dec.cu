@@ -481,9 +481,9 @@ __global__ void __launch_bounds__(DecCfg<D, GM>::THREADS, DecCfg<D, GM>::CPS) k_
       arrive(o_free);
       sync();
       if (rows <= 0) continue;
-      const bool direct = q.whole();
+      const bool direct = !by_ticket(q.parts);
       const int c0 = q.c0;
-      auto rec_of = [&](int cta) { return (2 * cta + (cta == c0 ? 1 : 0)) * C::SG + sg; };
+      auto rec_of = [&](int cta) { return record_of(cta, c0) * C::SG + sg; };
 #pragma unroll 1
       for (int i = st; i < rows * (D / 8); i += 128) {
         const int h = i / (D / 8), d = 8 * (i % (D / 8));

@@ -27,12 +27,14 @@ namespace {
 // The groups take turns: while one turns its S into P the tensor cores work for
 // the other.
 //   NQ = 1 (65 to 128 rows): both groups hold the same queries and take alternate
-//          tiles; each writes its own record.
+//          tiles; each writes its own record, also of an item that the CTA does
+//          alone.
 //   NQ = 2 (prompts): the groups hold 128 query rows each and both read every
 //          tile.
 // The work is a line of tiles cut evenly over the CTAs (vp_attend.h): an item
 // cut between CTAs leaves a record (m, l, O) per CTA, and the last CTA to finish
-// joins them.
+// joins them; the two records of an item that one CTA has alone (NQ = 1) are
+// joined in it, between two barriers of the groups.
 //
 // Prompts are bound by two chains of about the same length that take turns, not
 // by a pipe: per half tile a softmax thread spends about 1000 clocks on 64
@@ -555,9 +557,9 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
         store_lse(p, q.b, q.g, row, 0.f, 0.f);
       }
       // ---- the others' output, or this CTA's record of it
-      const bool direct = NQ == 2 && q.whole();
+      const bool direct = NQ == 2 && !by_ticket(q.parts);
       const int c0 = q.c0;
-      auto rec_of = [&](int c, int grp) { return (2 * c + (c == c0 ? 1 : 0)) * 2 + grp; };
+      auto rec_of = [&](int c, int grp) { return record_of(c, c0) * 2 + grp; };
       if (have) wait(pv_done + 2 * s + ((ns - 1) & 1), ((ns - 1) >> 1) & 1);
       if (rows_here && n > 0 && group) {
         float* po = nullptr;
@@ -613,8 +615,18 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
       // NQ = 1: the records of both groups of every CTA; NQ = 2: this group's rows.
       const int parts = q.parts;
       auto sync = [&] { asm volatile("barrier.cta.sync %0, 128;\n" ::"r"(2 + s) : "memory"); };
-      if (!direct && n > 0 && group &&
-          last_to_arrive(p.tickets + 2 * c0 + (NQ == 2 ? s : 0), NQ == 1 ? 2 * parts : parts, r, misc + 18 + s, sync)) {
+      // NQ = 1, an item of this CTA alone: its groups' records meet at a barrier
+      // of the two, the first group joins them, and at a second one both know that
+      // the records may be written again (for the CTA's next item).
+      const bool meet = NQ == 1 && n > 0 && !by_ticket(parts);
+      bool join = false;
+      if (meet) {
+        asm volatile("barrier.cta.sync 1, 256;\n" ::: "memory");
+        join = s == 0;
+      } else if (!direct && n > 0 && group) {
+        join = last_to_arrive(p.tickets + 2 * c0 + (NQ == 2 ? s : 0), NQ == 1 ? 2 * parts : parts, r, misc + 18 + s, sync);
+      }
+      if (join) {
         if (NQ == 1)
           join_records<__nv_bfloat16, D, 128, 4, 4>(p, q.b, q.g, 0, q.it.rows, 2 * parts, kTcTile,
                                               [&](int k) { return rec_of(c0 + (k >> 1), k & 1); }, r);
@@ -622,6 +634,7 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
           join_records<__nv_bfloat16, D, 128, 4, 4>(p, q.b, q.g, row_s, min(kTcTile, q.it.rows - s * kTcTile), parts, kTcTile,
                                               [&](int k) { return rec_of(c0 + k, s); }, r);
       }
+      if (meet) asm volatile("barrier.cta.sync 1, 256;\n" ::: "memory");
       if (!more) break;
       q = next;
     }
