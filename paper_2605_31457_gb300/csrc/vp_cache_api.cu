@@ -187,10 +187,13 @@ vp_status evict(vp_ctx* ctx, int32_t batch, const vp_kv* k_src, const vp_kv* v_s
   if (in_place != same_cache(*v_src, *v_dst) ||
       (!in_place && (k_src->data == k_dst->data || v_src->data == v_dst->data)))
     return fail(ctx, VP_ERR_INVALID_ARG, "vp_evict: the destinations must be the sources themselves or not overlap them");
-  if (weight_dst && (weight_dst->data == weight->data) !=
-                        (in_place && weight_dst->stride_b == weight->stride_b && weight_dst->stride_h == weight->stride_h))
-    return fail(ctx, VP_ERR_INVALID_ARG, "vp_evict: weight_dst must be weight itself in place, and must not overlap it "
-                "otherwise");
+  if (weight_dst) {
+    // In place the freed entries up to seq_len are cleared, which only weight itself has room for.
+    const bool same = weight_dst->data == weight->data;
+    if (in_place ? !same || weight_dst->stride_b != weight->stride_b || weight_dst->stride_h != weight->stride_h : same)
+      return fail(ctx, VP_ERR_INVALID_ARG, "vp_evict: weight_dst must be weight itself in place, and must not overlap it "
+                  "otherwise");
+  }
   vp::EvictParams p;
   memset(&p, 0, sizeof p);
   p.esz = (int)esz;
