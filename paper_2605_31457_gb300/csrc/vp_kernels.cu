@@ -3924,6 +3924,16 @@ bool encode_kv_map(const KvView& kv, const KvShape& p, CUtensorMap* map, int* tp
   struct Ax { int64_t stride, size; int id; };  // id: 0 token, 1 kv-head, 2 sequence / page
   Ax ax[3] = {{kv.st, 0, 0}, {kv.sh, p.Hkv, 1}, {kv.sb, p.paged ? kv.num_pages : p.B, 2}};
   if (p.paged) ax[0].size = p.page_size;
+  // An axis of one element may have any stride (a [B, T, 1, D] tensor seen as
+  // [B, 1, T, D] has the token's): where it does not lie beyond the token axis, or
+  // another axis that does bounds it, it goes outermost.
+  constexpr int64_t kAnywhere = INT64_MAX;
+  if (!p.paged) {
+    bool bounded = false;
+    for (const Ax& a : ax) bounded |= a.id != 0 && a.size > 1 && a.stride > kv.st;
+    for (Ax& a : ax)
+      if (a.id != 0 && a.size == 1 && (bounded || a.stride <= kv.st)) a.stride = kAnywhere;
+  }
   for (int i = 0; i < 3; ++i)
     for (int j = i + 1; j < 3; ++j)
       if (ax[j].stride < ax[i].stride) { Ax t = ax[i]; ax[i] = ax[j]; ax[j] = t; }
@@ -3932,9 +3942,11 @@ bool encode_kv_map(const KvView& kv, const KvShape& p, CUtensorMap* map, int* tp
     // The token extent is the room its stride leaves before the next axis.
     int k = 0;
     while (ax[k].id != 0) ++k;
-    if (k == 2 || ax[k].stride <= 0) return false;
+    if (k == 2 || ax[k].stride <= 0 || ax[k + 1].stride == kAnywhere) return false;
     ax[k].size = ax[k + 1].stride / ax[k].stride;
   }
+  for (int i = 1; i < 3; ++i)
+    if (ax[i].stride == kAnywhere) ax[i].stride = ax[i - 1].stride * ax[i - 1].size;
   for (int i = 0; i < 3; ++i) {
     if (ax[i].size < 1 || ax[i].stride <= 0) return false;
     if (i < 2 && ax[i + 1].stride < ax[i].stride * ax[i].size) return false;  // axes must nest
