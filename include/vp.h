@@ -366,7 +366,9 @@ typedef struct {
  *   k_dst, v_dst where the kept rows go: the source itself (same data, strides
  *                and block table: in place), or caches that do not overlap it,
  *                with rows for min(keep, seq_len[b]) tokens (paged when
- *                block_table is set, with the context's page size).
+ *                block_table is set, with the context's page size; source and
+ *                destination may be pages of one pool, each with a table of its
+ *                own and no page in both).
  *   weight       accumulated weights of the source (vp_attend_new).
  *   weight_dst   NULL, or where the kept tokens' weights go.  The same array as
  *                weight when in place; the freed entries keep .. seq_len - 1 are

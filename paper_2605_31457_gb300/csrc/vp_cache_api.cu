@@ -53,6 +53,11 @@ bool same_cache(const vp_kv& a, const vp_kv& b) {
          a.block_table == b.block_table && a.max_pages == b.max_pages && a.num_pages == b.num_pages;
 }
 
+// Two caches in one pool whose pages the caller keeps apart (a block table each).
+bool other_pages(const vp_kv& a, const vp_kv& b) {
+  return a.block_table && b.block_table && a.block_table != b.block_table;
+}
+
 vp_status reserve_new(vp_ctx* ctx, int32_t max_new, int32_t max_weight_new) {
   const vp_config& c = ctx->cfg;
   if (max_new < 1 || max_new > c.max_seq)
@@ -185,7 +190,8 @@ vp_status evict(vp_ctx* ctx, int32_t batch, const vp_kv* k_src, const vp_kv* v_s
   }
   const bool in_place = same_cache(*k_src, *k_dst);
   if (in_place != same_cache(*v_src, *v_dst) ||
-      (!in_place && (k_src->data == k_dst->data || v_src->data == v_dst->data)))
+      (!in_place && ((k_src->data == k_dst->data && !other_pages(*k_src, *k_dst)) ||
+                     (v_src->data == v_dst->data && !other_pages(*v_src, *v_dst)))))
     return fail(ctx, VP_ERR_INVALID_ARG, "vp_evict: the destinations must be the sources themselves or not overlap them");
   if (weight_dst) {
     // In place the freed entries up to seq_len are cleared, which only weight itself has room for.
