@@ -259,7 +259,8 @@ vp_status vp_compact_kv(vp_ctx* ctx, int32_t batch, const vp_kv* src, const vp_k
  * an optional sliding window and sink tokens, a running sum of the attention
  * weight that every cached token received, and eviction of the tokens with
  * the smallest such sums.  They use the same contexts, caches (vp_kv), error
- * codes and device checks as vp_decode_step.
+ * codes and device checks as vp_decode_step, and return VP_ERR_INVALID_ARG when
+ * the current CUDA device is not the context's.
  */
 
 /* Which cached tokens a new token at position t sees: those at j <= t with

@@ -220,12 +220,19 @@ vp_status evict(vp_ctx* ctx, int32_t batch, const vp_kv* k_src, const vp_kv* v_s
   return VP_OK;
 }
 
-// No exception may cross the C ABI (a failed allocation of an error text).
+// No exception may cross the C ABI (a failed allocation of an error text), and
+// nothing is allocated or launched on another device than the context's.
 template <typename F>
-vp_status guarded(vp_ctx* ctx, F&& f) {
+vp_status guarded(vp_ctx* ctx, const char* name, F&& f) {
   if (!ctx) return VP_ERR_NOT_INITIALIZED;
   try {
     ctx->last_error.clear();
+    int device = 0;
+    const cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess) return cuda_fail(ctx, name, e);
+    if (device != ctx->device)
+      return fail(ctx, VP_ERR_INVALID_ARG, std::string(name) + ": the current device is " + std::to_string(device) +
+                  ", the context's is " + std::to_string(ctx->device));
     return f();
   } catch (const std::exception&) {
     return VP_ERR_CUDA;
@@ -237,7 +244,7 @@ vp_status guarded(vp_ctx* ctx, F&& f) {
 extern "C" {
 
 vp_status vp_reserve_new(vp_ctx* ctx, int32_t max_new, int32_t max_weight_new) {
-  return guarded(ctx, [&] { return reserve_new(ctx, max_new, max_weight_new); });
+  return guarded(ctx, "vp_reserve_new", [&] { return reserve_new(ctx, max_new, max_weight_new); });
 }
 
 vp_status vp_attend_new(vp_ctx* ctx, int32_t batch, int32_t n_new, const vp_rows* q,
@@ -245,7 +252,7 @@ vp_status vp_attend_new(vp_ctx* ctx, int32_t batch, int32_t n_new, const vp_rows
                         const int32_t* seq_len, const int32_t* new_len, const vp_visible* visible,
                         const vp_rows* out, float* lse,
                         const vp_weights* weight_in, const vp_weights* weight_out, void* cuda_stream) {
-  return guarded(ctx, [&] {
+  return guarded(ctx, "vp_attend_new", [&] {
     return attend_new(ctx, batch, n_new, q, k_cache, v_cache, seq_len, new_len, visible, out, lse, weight_in,
                       weight_out, cuda_stream);
   });
@@ -256,7 +263,7 @@ vp_status vp_evict(vp_ctx* ctx, int32_t batch, const vp_kv* k_src, const vp_kv* 
                    const vp_kv* k_dst, const vp_kv* v_dst,
                    const vp_weights* weight, const vp_weights* weight_dst,
                    int32_t* kept_idx, int32_t kept_cap, int32_t* new_len, void* cuda_stream) {
-  return guarded(ctx, [&] {
+  return guarded(ctx, "vp_evict", [&] {
     return evict(ctx, batch, k_src, v_src, seq_len, policy, k_dst, v_dst, weight, weight_dst, kept_idx, kept_cap,
                  new_len, cuda_stream);
   });
