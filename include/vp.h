@@ -317,7 +317,8 @@ vp_status vp_reserve_new(vp_ctx* ctx, int32_t max_new, int32_t max_weight_new);
  *                seq_len[b]).  NULL: n_new in every sequence that is not empty.
  *                Larger values are clamped and flagged (vp_check_errors).
  *   lse          float [batch][n_new][H] or NULL: natural logarithm of the sum
- *                of exp(logit) over the visible tokens.
+ *                of exp(logit) over the visible tokens.  A visible logit that is
+ *                not a number makes the row's lse, output and weights that too.
  *   weight_in,
  *   weight_out   NULL, or for every live token j of every kv-head
  *                weight_out[j] = weight_in[j] + the attention weight that j

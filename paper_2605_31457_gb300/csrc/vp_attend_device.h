@@ -38,12 +38,13 @@ __device__ __forceinline__ T* out_row(const AttendParams& p, int b, int g, int r
   return static_cast<T*>(p.out.data) + (int64_t)b * p.out.sb + (int64_t)tok * p.out.sn +
          (int64_t)(g * p.G + row - tok * p.G) * p.out.sh;
 }
-// The log-sum-exp of a row from its maximum (log2 units) and sum.
+// The log-sum-exp of a row from its maximum (log2 units) and sum: a sum of 0 is a
+// row that sees nothing, one that is not a number stays that.
 __device__ __forceinline__ void store_lse(const AttendParams& p, int b, int g, int row, float m, float l) {
-  const float x = l > 0.f ? m + log2f(l) : -CUDART_INF_F;
+  const float x = l == 0.f ? -CUDART_INF_F : m + log2f(l);
   const int tok = row_token(p, row);
   if (p.lse) p.lse[((int64_t)b * p.n_new + tok) * p.H + g * p.G + row - tok * p.G] = x * kLn2;
-  if (p.weigh) p.lse2[(int64_t)(b * p.Hkv + g) * p.R + row] = l > 0.f ? x : CUDART_INF_F;
+  if (p.weigh) p.lse2[(int64_t)(b * p.Hkv + g) * p.R + row] = l == 0.f ? CUDART_INF_F : x;
 }
 
 // ---- The line of work of the tensor-core kernels (AttItem, LineCut).
