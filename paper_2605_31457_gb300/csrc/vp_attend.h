@@ -63,7 +63,9 @@ struct AttendParams {
   int weigh;                  // weights asked for
   WeightView w_in, w_out;     // w_in.data may be NULL
   // workspace
-  unsigned* tickets;          // [2 * grid] records written of the items cut between CTAs; 0 between calls
+  unsigned* tickets;          // [4 * num_sms] records written of the items cut between CTAs; 0 between calls:
+                              // a CTA's (two of them per SM) or one for each 16 or 128 of its rows, or k_att_any's
+                              // for its row blocks, which it splits where there are at most four per SM
   float* lse2;                // [B * Hkv][R] log-sum-exp in log2 units (+inf: an empty row), when weigh
   float* part_o;              // partial outputs, unnormalised
   float* part_st;             // their {maximum in log2 units, sum}
@@ -244,14 +246,12 @@ inline NewLayout new_layout(int max_batch, int H, int Hkv, int D, int max_seq, i
   w.max_new = max_new;
   w.max_weight_new = max_weight_new;
   const size_t G = (size_t)(H / Hkv);
-  // k_att_any splits only while there are fewer than four CTAs per SM before
-  // the split, so its partial rows stay below twice that; a call with weights
-  // goes through partials even unsplit.
-  size_t rows = (size_t)8 * num_sms * kAnyRows;
-  if (rows < (size_t)max_batch * Hkv * max_weight_new * G) rows = (size_t)max_batch * Hkv * max_weight_new * G;
-  // The tensor-core kernels: two records per CTA (the item it goes on with and
-  // the one it begins), of 32 rows at two CTAs per SM or of 256 at one.
-  if (rows < (size_t)2 * num_sms * 2 * kTcTile) rows = (size_t)2 * num_sms * 2 * kTcTile;
+  // Partial rows.  The tensor-core kernels leave up to two records per CTA (the
+  // item it goes on with and the one it begins), of 16 rows at two CTAs per SM, of
+  // 64 or of 256 at one; k_att_any, whose CTAs number at most 8 per SM where it
+  // splits (any_splits), one of up to kAnyRows rows each.
+  const size_t rows = (size_t)2 * num_sms * 2 * kTcTile;
+  static_assert(8 * kAnyRows <= 4 * kTcTile, "k_att_any's partial rows fit");
   size_t off = 0;
   w.o_tk = off; off = ws_round(off + (size_t)4 * num_sms * 4);
   w.o_lse = off; off = ws_round(off + (size_t)max_batch * Hkv * max_weight_new * G * 4);

@@ -1,6 +1,7 @@
 // Host-only check of the records and tickets of vp_attend_new's tensor-core
 // kernels (vp_attend.h): over every line of items cut for any number of CTAs, an
-// item joined by ticket has its ticket, and each CTA's record of it, for itself.
+// item joined by ticket has its ticket, and each CTA's record of it, for itself;
+// the workspace has room for all of them and for no more.
 // Prints one line per violation and exits non-zero if there was any.
 #include <cstdio>
 #include <random>
@@ -45,6 +46,19 @@ int main() {
         begin += it.cost(fixed);
       }
   }
+  // The workspace holds every kernel's records and tickets, and grows with the
+  // batch and the weights by the logits and the log-sum-exps alone.
+  for (int sms : {1, 148, 152})
+    for (int D : {64, 128}) {
+      const NewLayout one = new_layout(1, 32, 4, D, 4096, 256, 0, sms), many = new_layout(64, 32, 4, D, 4096, 256, 16, sms);
+      const size_t rows = (many.o_z - many.o_o) / (D * sizeof(float)), tickets = (many.o_lse - many.o_tk) / sizeof(unsigned);
+      if (many.o_z - many.o_o != one.o_z - one.o_o || many.o_o - many.o_st != one.o_o - one.o_st)
+        ++fails, std::printf("FAIL records that grow: %zu, %zu bytes\n", one.o_z - one.o_o, many.o_z - many.o_o);
+      const size_t most = 4u * sms * kTcTile;  // 2 per CTA, 2 groups of 128 rows, a CTA per SM
+      if (rows < most || rows < 2u * 2 * sms * 16 || rows < 2u * sms * kDecRows || rows < 8u * sms * kAnyRows ||
+          tickets < 2u * sms * kDecRows / 32 || tickets < 4u * sms || (many.o_o - many.o_st) / 8 < rows)
+        ++fails, std::printf("FAIL room for records and tickets: %zu %zu\n", rows, tickets);
+    }
   std::printf("%d violations\n", fails);
   return fails != 0;
 }
