@@ -333,9 +333,8 @@ vp_status vp_reserve_new(vp_ctx* ctx, int32_t max_new, int32_t max_weight_new);
  * A page that a visible token needs but the block table does not map is left
  * out of the attention and flagged.
  * Logits, sums and outputs are accumulated in float.  bf16 caches: the
- * probabilities enter the product with V as two bf16 terms, or as one where
- * n_new * G > 128 and every row of a block of 256 sees at least 2048 tokens (an
- * error of up to 2^-8 of sum_j p_j |v_j|, next to the output's own rounding).
+ * probabilities enter the product with V as two bf16 terms (an error of up to
+ * 2^-16 of sum_j p_j |v_j|).
  * VP_ERR_CAPACITY when vp_reserve_new has not reserved for n_new (or the
  * weights).  Allocates nothing and never synchronises; every kernel waits for
  * the stream's previous work, so an input may be the output of the preceding

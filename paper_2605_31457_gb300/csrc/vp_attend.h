@@ -120,9 +120,10 @@ __host__ __device__ inline bool sees(int j, int t, int window, int sinks) {
 }
 
 // ---- The work of the tensor-core kernels.  The cost of an item is its tiles'
-// plus a fixed part for loading its queries and writing its result, in units:
-// measured, a tile of k_att_tc with P split in two terms takes 1.5 times one
-// without, an item's fixed part about as long as two tiles.
+// plus a fixed part for loading its queries and writing its result, in thirds of
+// a tile: measured, a tile takes 1.5 times as long as it would with P in one bf16
+// term, and an item's fixed part as long as one (k_att_dec) or two (k_att_tc) of
+// those.
 // Items follow one another kv-head by kv-head, sequence by sequence, and the
 // line of their costs is cut into equal parts, one per CTA: a CTA owns tiles,
 // not items, so ragged lengths leave no CTA idle.  An item whose tiles lie with
@@ -130,23 +131,15 @@ __host__ __device__ inline bool sees(int j, int t, int window, int sinks) {
 // finish joins them.
 constexpr int kTileUnits = 2, kSplitUnits = 3;
 
-// An item's P is split into two bf16 terms, hi + lo, unless it is one of many
-// rows each of which sees at least kSplitSeen tokens.  P's rounding to one term,
-// up to 2^-8 of each probability, shows in the output beside the output's own
-// where few tokens share the weight; over longer ranges it averages out, and the
-// second P.V product would cost a third of the tensor cores' time.
-constexpr int kSplitSeen = 2048;
-
 struct AttItem {
   int row0, rows;  // query rows [row0, row0 + rows)
-  int split;       // P in two terms
   SeenRange sr;
   TileList tl;
-  __host__ __device__ int unit() const { return split ? kSplitUnits : kTileUnits; }
+  __host__ __device__ int unit() const { return kSplitUnits; }
   __host__ __device__ int cost(int fixed) const { return fixed + tl.n * unit(); }
   // Tiles that start in front of position x of the item.
   __host__ __device__ int tiles_before(int x, int fixed) const {
-    const int u = split ? (x - fixed + kSplitUnits - 1) / kSplitUnits : (x - fixed + kTileUnits - 1) / kTileUnits;
+    const int u = (x - fixed + unit() - 1) / unit();
     return x <= fixed ? 0 : u < tl.n ? u : tl.n;
   }
 };
@@ -165,14 +158,11 @@ __host__ __device__ inline AttItem att_item(int len, int n, int G, int block, in
   it.row0 = qt * block;
   const int left = n * G - it.row0;
   it.rows = left < 0 ? 0 : left < block ? left : block;
-  it.split = 1;
   it.sr = SeenRange{0, 0, 0};
   if (it.rows > 0) {
-    const int t = len - n + token_of_row(it.row0, G, g_mul);
-    it.sr = seen_range(t, len - n + token_of_row(it.row0 + it.rows - 1, G, g_mul), window, sinks);
-    const int in = window < 0 || window > t ? t + 1 : window;
-    const int seen = in + (sinks < t + 1 - in ? sinks : t + 1 - in);
-    it.split = block <= kTcTile || seen < kSplitSeen;
+    const int first = len - n;
+    it.sr = seen_range(first + token_of_row(it.row0, G, g_mul), first + token_of_row(it.row0 + it.rows - 1, G, g_mul),
+                       window, sinks);
   }
   it.tl = tile_list(it.sr, kTcTile);
   return it;

@@ -26,7 +26,7 @@ namespace {
 //              memory.
 // P enters the product as two bf16 terms, P = hi + lo, in columns [0, GM) and
 // [GM, 2 GM) of P^T; the two halves of O are added at the end.  P's rounding
-// (2^-17 of it) then vanishes beside the output's, at no cost: the kernel is
+// (2^-16 of it) then vanishes beside the output's, at no cost: the kernel is
 // bound by HBM, 64 KB per tile at D = 128, and for few or short sequences by its
 // start and end (about 10 us: the line's cut, the first tiles, the records and
 // their join).  D = 128: 64 sequences of 17408 tokens, 32/8 heads, in 627 us (7.3

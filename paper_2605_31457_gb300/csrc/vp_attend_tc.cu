@@ -36,13 +36,13 @@ namespace {
 // joins them; the two records of an item that one CTA has alone (NQ = 1) are
 // joined in it, between two barriers of the groups.
 //
-// Prompts are bound by two chains of about the same length that take turns, not
-// by a pipe: per half tile a softmax thread spends about 1000 clocks on 64
-// exponentials and as much on waits, TMEM loads and arrivals, and a product warp
-// as much on issuing 12 products (S from 64 tokens reads 6 KB of shared memory
-// for 32 clocks of tensor work).  28/4 heads of 128: 3857 tokens in 126 us (850
-// TFLOP/s); 32/8 heads, 12289 tokens with a window of 2048 and 4 sinks in 388 us
-// (976 TFLOP/s).  Slower were: two warps for every 32 rows,
+// Prompts are bound by two chains that take turns, not by a pipe: per half tile
+// a softmax thread spends its time on 64 exponentials, the two terms of P, and
+// waits, TMEM loads and arrivals, and a product warp on issuing 16 products (S
+// from 64 tokens reads 6 KB of shared memory for 32 clocks of tensor work).  28/4
+// heads of 128: 3857 tokens in 147 us (725 TFLOP/s); 32/8 heads, 12289 tokens with
+// a window of 2048 and 4 sinks in 463 us (818 TFLOP/s).  When long ranges had P in
+// one term (see below), slower were: two warps for every 32 rows,
 // 32 columns each (16 softmax warps of 96 registers; 533 against 447 us at the
 // time); S's second half loaded during the first's exponentials (461 against 420);
 // the next step's S fetched before a P is announced (491 against 419).  What
@@ -54,9 +54,12 @@ namespace {
 // Softmax: a row's reference m is the largest logit of the first 64 tokens it
 // sees, and is raised, O rescaled in TMEM, only when P = exp2(z - m) passes 2^64:
 // up to there P has bf16's and float's full precision all the same, and S is
-// read once.  P goes to the tensor cores as bf16, in two terms hi + lo unless
-// every row sees many tokens (AttItem::split); l sums the unrounded values in 32
-// bits.
+// read once.  P goes to the tensor cores as two bf16 terms, hi + lo (2^-16 of it
+// at most is lost); l sums the unrounded values in 32 bits.  With one term the two
+// prompts above take 123 and 380 us, but its error does not average out: over 4096 to 16384 tokens it is 1.4 times that of a rounded
+// exact result where the weight is spread (2.3e-3 of the output's rms against
+// 1.7e-3) and 7 to 18 times where one token has nearly all of it (1.5e-3 against
+// 0.8e-4 to 2e-4), whatever the range.
 //
 // Rows of a tile that nobody sees may hold anything: their logits are masked,
 // and their V rows are zeroed in shared memory before the product (0 x NaN is
@@ -292,7 +295,6 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
       const int n = q.u1 - q.u0;
       if (n <= 0) continue;
       const int two = NQ == 2 && q.it.rows > kTcTile;  // the second group has rows
-      const int split = q.it.split;
       auto own = [&](int t) { return NQ == 2 ? s == 0 || two : (t & 1) == s; };  // tile t is this group's
       if (NQ == 2 ? s == 0 || two : n > s) {  // it has tiles in this part
         if (!wait(q_full + s, parts & 1)) { timed_out = true; break; }
@@ -358,12 +360,10 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
             umma_ts<kIdPV, 1>(o, ph + 8, vd + 128);
             umma_ts<kIdPV, 1>(o, ph + 32, vd + 256);
             umma_ts<kIdPV, 1>(o, ph + 40, vd + 384);
-            if (split) {
-              umma_ts<kIdPV, 1>(o, ph + 16, vd);
-              umma_ts<kIdPV, 1>(o, ph + 24, vd + 128);
-              umma_ts<kIdPV, 1>(o, ph + 48, vd + 256);
-              umma_ts<kIdPV, 1>(o, ph + 56, vd + 384);
-            }
+            umma_ts<kIdPV, 1>(o, ph + 16, vd);
+            umma_ts<kIdPV, 1>(o, ph + 24, vd + 128);
+            umma_ts<kIdPV, 1>(o, ph + 48, vd + 256);
+            umma_ts<kIdPV, 1>(o, ph + 56, vd + 384);
             umma_commit(pv_done + 2 * s + half);
             if (ks >= 0) qk(half, ks);
             if (half) {
@@ -446,7 +446,6 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
       const int all_hi = q.sq.len - q.sq.n + row_token(p, row_s) + 1;
       const int all_lo = p.window < 0 ? 0 : q.sq.len - q.sq.n + row_token(p, max(last, 0)) - p.window + 1;
       float m = -CUDART_INF_F, l = 0.f;
-      const bool split = q.it.split;
       bool have = false;  // O holds something
       const bool group = NQ == 1 || s == 0 || q.it.rows > kTcTile;
 #pragma unroll 1
@@ -463,7 +462,7 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
           if (rows_here && !dead) {
             // 64 columns of the row of S.  P = exp2(c z - m) goes over them:
             // columns [k, k + 16), k = 0 and 32, take hi of tokens k .. k + 31
-            // and the next 16 lo (with split).  A P past 2^64 shows in their sum,
+            // and the next 16 lo.  A P past 2^64 shows in their sum,
             // so no maximum is formed unless the reference must be set or raised;
             // S is then read again.  Loops stay rolled and each piece of code
             // single: eleven warps run different code at once.
@@ -525,17 +524,16 @@ __global__ void __launch_bounds__(kAttThreads, 1) k_att_tc(const __grid_constant
             l += sum;
             tmem_st(taddr + k0, *reinterpret_cast<uint32_t (*)[16]>(hi));
             tmem_st(taddr + k0 + 32, *reinterpret_cast<uint32_t (*)[16]>(hi + 16));
-            if (split) {
+            __syncwarp();  // no lo before the last hi is stored: both at once do not fit the registers
 #pragma unroll
-              for (int k = 0; k < 32; ++k) {
-                float2 h;
-                bf2(hi[k], h.x, h.y);
-                const float2 d = add2(make_float2(x[2 * k], x[2 * k + 1]), make_float2(-h.x, -h.y));
-                hi[k] = pack_bf16(d.x, d.y);
-              }
-              tmem_st(taddr + k0 + 16, *reinterpret_cast<uint32_t (*)[16]>(hi));
-              tmem_st(taddr + k0 + 48, *reinterpret_cast<uint32_t (*)[16]>(hi + 16));
+            for (int k = 0; k < 32; ++k) {
+              float2 h;
+              bf2(hi[k], h.x, h.y);
+              const float2 d = add2(make_float2(x[2 * k], x[2 * k + 1]), make_float2(-h.x, -h.y));
+              hi[k] = pack_bf16(d.x, d.y);
             }
+            tmem_st(taddr + k0 + 16, *reinterpret_cast<uint32_t (*)[16]>(hi));
+            tmem_st(taddr + k0 + 48, *reinterpret_cast<uint32_t (*)[16]>(hi + 16));
             tmem_st_wait();
           }
           have = true;
