@@ -156,9 +156,9 @@ vp_status vp_init(const vp_config* cfg, vp_ctx** out_ctx);
  * and page table before it waits for that call (it waits before its first
  * workspace write).  So no input of vp_decode_step may be written by the
  * immediately preceding call of this library on the stream; any other kernel
- * or copy in between removes the overlap.  vp_compact_kv's output caches are
- * exempt (its kernel completes before the next call starts), and
- * vp_decode_gather waits for the previous call before reading its kept set.
+ * or copy in between removes the overlap.  The outputs of vp_compact_kv and
+ * vp_evict are exempt (their last kernel completes before the next call starts),
+ * and vp_decode_gather waits for the previous call before reading its kept set.
  */
 vp_status vp_decode_step(vp_ctx* ctx, int32_t batch, const void* q,
                          const vp_kv* k_cache, const vp_kv* v_cache,
@@ -380,8 +380,10 @@ typedef struct {
  *                = -1.  kept_cap >= keep, else VP_ERR_CAPACITY.
  *   new_len      int32 [batch]: min(seq_len, keep); may be seq_len itself.
  * A kept row on an unmapped source page arrives as zeros, one whose destination
- * page is unmapped is dropped; both are flagged (vp_check_errors).  Allocates
- * nothing and never synchronises.
+ * page is unmapped is dropped; both are flagged (vp_check_errors).  In place, no
+ * page may be shared between sequences.  Allocates nothing and never
+ * synchronises; every kernel waits for the stream's previous work, and a call
+ * behind it, vp_decode_step included, may use its outputs.
  */
 vp_status vp_evict(vp_ctx* ctx, int32_t batch, const vp_kv* k_src, const vp_kv* v_src,
                    const int32_t* seq_len, const vp_evict_policy* policy,
