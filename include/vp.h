@@ -258,7 +258,9 @@ vp_status vp_compact_kv(vp_ctx* ctx, int32_t batch, const vp_kv* src, const vp_k
  * the cache (a decode step, drafted tokens, a prompt or a chunk of one) with
  * an optional sliding window and sink tokens, a running sum of the attention
  * weight that every cached token received, and eviction of the tokens with
- * the smallest such sums.  They use the same contexts, caches (vp_kv), error
+ * the smallest such sums.  One token over a whole cache is also what
+ * vp_decode_step computes with VP_DENSE; vp_attend_new takes less time for it and
+ * needs no visual span, vp_decode_step adds the visual masses and the kept list.  They use the same contexts, caches (vp_kv), error
  * codes and device checks as vp_decode_step, and return VP_ERR_INVALID_ARG when
  * the current CUDA device is not the context's.
  */
@@ -291,7 +293,10 @@ typedef struct {
  * Allocates the workspace of vp_attend_new on a context, once: for calls of up
  * to max_new new tokens per sequence, of which calls that accumulate weights
  * pass at most max_weight_new (0: none does).  Waits for the device; call it
- * outside stream capture.  A second call replaces the first one's workspace.
+ * outside stream capture.  A second call replaces the first one's workspace:
+ * graphs that captured vp_attend_new before it must not be replayed.  The logits
+ * of calls with weights take 4 * max_batch * H * max_weight_new * max_seq bytes
+ * of it, and tens of MB serve everything else.
  * VP_ERR_INVALID_ARG for max_new < 1, max_new > max_seq or a max_weight_new
  * outside [0, max_new]; VP_ERR_UNSUPPORTED when max_weight_new * G > 128 (see
  * vp_attend_new); VP_ERR_CUDA when the allocation fails (the context then has
@@ -332,6 +337,11 @@ vp_status vp_reserve_new(vp_ctx* ctx, int32_t max_new, int32_t max_weight_new);
  * sinks) come out as 0 with lse = -infinity and add no weight.
  * A page that a visible token needs but the block table does not map is left
  * out of the attention and flagged.
+ * Speed: bf16 caches run on the tensor cores when a tensor map describes both
+ * (the token axis not outermost, K's and V's axes in one order, pages of at least
+ * 8 tokens); other bf16 caches and fp32 caches go through a kernel of FMA
+ * instructions, which keeps up with memory for up to 8 query rows per kv-head
+ * and takes many times as long for prompts.
  * Logits, sums and outputs are accumulated in float.  bf16 caches: the
  * probabilities enter the product with V as two bf16 terms (an error of up to
  * 2^-16 of sum_j p_j |v_j|).

@@ -76,7 +76,8 @@ __device__ __forceinline__ void copy16(void* dst, const void* src, bool live) {
 // Up to 8 rows it is bound by the cache's bytes, above by the FMA pipes and the
 // latency of two warps per scheduler.  fp32, D = 128: 64 sequences of 1500 to
 // 5000 tokens, 32/8 heads, with weights 325 us (5.3 TB/s); 8 sequences of 5000
-// to 12000 tokens, 64 query rows 135 us (16 TFLOP/s).  The form before it, a
+// to 12000 tokens, one kv-head, 64 query rows 135 us (16 TFLOP/s); a prompt of
+// 3857 tokens, 28/4 heads, 4.26 ms (25 TFLOP/s).  The form before it, a
 // token per lane with all of K's row and loads between barriers, took 1076 and
 // 210 us.
 // ---------------------------------------------------------------------------

@@ -41,7 +41,10 @@ namespace {
 // waits, TMEM loads and arrivals, and a product warp on issuing 16 products (S
 // from 64 tokens reads 6 KB of shared memory for 32 clocks of tensor work).  28/4
 // heads of 128: 3857 tokens in 147 us (725 TFLOP/s); 32/8 heads, 12289 tokens with
-// a window of 2048 and 4 sinks in 463 us (818 TFLOP/s).  When long ranges had P in
+// a window of 2048 and 4 sinks in 463 us (818 TFLOP/s).  112 rows (NQ = 1): 64
+// sequences of 700 to 6400 tokens, 28/4 heads, 16 new tokens each in 126 us (3.7
+// TB/s of cache), or 400 us with weights, when it writes 407 MB of logits that their
+// kernel reads.  When long ranges had P in
 // one term (see below), slower were: two warps for every 32 rows,
 // 32 columns each (16 softmax warps of 96 registers; 533 against 447 us at the
 // time); S's second half loaded during the first's exponentials (461 against 420);
