@@ -13,7 +13,9 @@
  *
  * Beside it: vp_attend_new (attention of newly appended tokens: decode steps,
  * drafted tokens, prompts; sliding window, sinks, accumulated weights) and
- * vp_evict (eviction of cached tokens by accumulated weight).
+ * vp_evict (eviction of cached tokens by accumulated weight), vp_append and
+ * vp_append4 (position rotation and appending, to caches of the context's type or
+ * held in 4 bits) and vp_attend4 (attention over a cache held in 4 bits).
  *
  * Conventions shared by every entry point:
  *   - Tensors are caller-owned DEVICE memory unless stated otherwise; the
@@ -156,8 +158,9 @@ vp_status vp_init(const vp_config* cfg, vp_ctx** out_ctx);
  * and page table before it waits for that call (it waits before its first
  * workspace write).  So no input of vp_decode_step may be written by the
  * immediately preceding call of this library on the stream; any other kernel
- * or copy in between removes the overlap.  The outputs of vp_compact_kv and
- * vp_evict are exempt (their last kernel completes before the next call starts),
+ * or copy in between removes the overlap.  The outputs of vp_compact_kv,
+ * vp_evict, vp_append and vp_append4 are exempt (their last kernel completes
+ * before the next call starts),
  * and vp_decode_gather waits for the previous call before reading its kept set.
  */
 vp_status vp_decode_step(vp_ctx* ctx, int32_t batch, const void* q,
@@ -400,6 +403,129 @@ vp_status vp_evict(vp_ctx* ctx, int32_t batch, const vp_kv* k_src, const vp_kv* 
                    const vp_kv* k_dst, const vp_kv* v_dst,
                    const vp_weights* weight, const vp_weights* weight_dst,
                    int32_t* kept_idx, int32_t kept_cap, int32_t* new_len, void* cuda_stream);
+
+/*
+ * ---- Appending to the caches, and caches held in 4 bits ----
+ *
+ * vp_append takes a layer's new queries, keys and values as the projections leave
+ * them, rotates queries and keys by their positions and writes keys and values to
+ * their places in the caches, in one kernel.  vp_append4 writes them to caches held
+ * in 4 bits, which vp_attend4 attends over: a fifth more than a quarter of the
+ * memory, and of the time where that is what bounds it.  The entry points use the
+ * contexts, error codes and device checks of those above and return
+ * VP_ERR_INVALID_ARG when the current CUDA device is not the context's.
+ */
+
+/* Rotation of queries and keys.  Pair f, 0 <= f < rot_dim / 2, of a row at position
+ * x turns by an angle whose cosine is cos_sin[x][f] and whose sine
+ * cos_sin[x][rot_dim / 2 + f]: (a, b) becomes (a cos - b sin, b cos + a sin), in
+ * float with every operation rounded, then rounded once to cfg.dtype.  Dimensions
+ * from rot_dim on stay as they are. */
+typedef struct {
+  const float* cos_sin; /* device [max_pos][rot_dim], 16-byte aligned                */
+  int32_t max_pos;      /* positions of the table, >= 1                              */
+  int32_t rot_dim;      /* rotated dimensions of a row: a multiple of 16, <= D       */
+  int32_t interleaved;  /* pair f is 0: dimensions (f, f + rot_dim / 2); 1: (2f, 2f + 1) */
+  const int32_t* pos;   /* device [axes][batch][n_new], or NULL: a token's position is
+                           its place in its sequence.  A position outside
+                           [0, max_pos) is clamped and flagged                       */
+  int32_t axes;         /* 1 to 3 positions of a token (visual tokens: frame, row,
+                           column); without pos: 1                                   */
+  int32_t sections[3];  /* axes > 1: pairs that turn by each axis' position, in this
+                           order; their sum is rot_dim / 2                           */
+} vp_rotation;
+
+/*
+ * Appends the newest tokens of every sequence: new token i of sequence b, 0 <= i <
+ * n_b, goes to place seq_len[b] - n_b + i of its sequence.
+ *   q, k, v      rows of H query heads and Hkv keys and values of the new tokens,
+ *                cfg.dtype (stride_h steps from head to kv-head in k and v); may be
+ *                views of one projection's output.  q may be NULL: keys and values
+ *                only.
+ *   seq_len      device int32 [batch], 0 <= seq_len <= max_seq: tokens of the
+ *                sequence, the new ones included (as vp_attend_new takes it).
+ *   new_len      device int32 [batch] or NULL: n_b, 0 <= n_b <= min(n_new, seq_len);
+ *                NULL: n_new in every sequence that is not empty.
+ *   rotation     NULL: rows are copied as they are.
+ *   q_out        the rotated queries; may be q itself (same data and strides), must
+ *                not overlap the inputs otherwise.  NULL when q is.
+ *   k_cache, v_cache  where the keys and values go.
+ * Rows i >= n_b of q_out and every other row of the caches are left as they were.  A
+ * sequence whose seq_len or new_len is out of range is skipped, and flagged; a row
+ * whose page the block table does not map is not written (its query is), and
+ * flagged (vp_check_errors).  VP_ERR_CAPACITY for n_new > max_seq.
+ * Uses no workspace, allocates nothing and never synchronises; waits for the
+ * stream's previous work, and a call behind it, vp_decode_step included, may use
+ * its outputs.
+ */
+vp_status vp_append(vp_ctx* ctx, int32_t batch, int32_t n_new, const vp_rows* q, const vp_rows* k, const vp_rows* v,
+                    const int32_t* seq_len, const int32_t* new_len, const vp_rotation* rotation,
+                    const vp_rows* q_out, const vp_kv* k_cache, const vp_kv* v_cache, void* cuda_stream);
+
+/*
+ * One key or value cache held in 4 bits: D / 2 bytes of codes and D / 32 scales a
+ * row, one scale for 32 dimensions.  Dimension d of (b, kv-head g, token t) is held
+ * as (code - 8) * scale, its code the low (d even) or high (d odd) half of byte
+ *   contiguous: codes + b*code_stride_b + g*code_stride_h + t*code_stride_t + d/2
+ * and its scale the fp16 number
+ *   contiguous: scales + b*scale_stride_b + g*scale_stride_h + t*scale_stride_t + d/32
+ * (code strides in bytes, scale strides in scales); paged as in vp_kv, the page id
+ * in place of b and t % page_size in place of t, one block table for both arrays.
+ * Code rows start on 16-byte boundaries, scale rows on D / 16-byte ones, and the
+ * strides are multiples of these.  Only rows that are written or seen are touched.
+ */
+typedef struct {
+  void* codes;
+  void* scales;
+  int64_t code_stride_b, code_stride_h, code_stride_t;
+  int64_t scale_stride_b, scale_stride_h, scale_stride_t;
+  const int32_t* block_table;
+  int32_t max_pages;
+  int32_t num_pages;
+} vp_kv4;
+
+/*
+ * vp_append into caches held in 4 bits.  Rows are rotated and rounded to cfg.dtype
+ * as vp_append does; of each 32 values x the scale is the least number of four
+ * significant bits that is not below the float product of max |x| and 1/7.5, at
+ * least 2^-14 and at most 61440, and a code is rint(x * (1 / scale)) + 8, with the
+ * reciprocal and the product in float, cut to [0, 15].  A held value has at most 8
+ * significant bits: it is exact in bf16.  Infinities saturate; where one of the 32
+ * is not a number, all of them are held as that (scale 0x7fff).
+ *   k_held, v_held  NULL, or [batch][n_new][Hkv] rows of cfg.dtype: the values that
+ *                   the cache now holds for the new tokens (of a page that is not
+ *                   mapped: would hold).  Rows i >= n_b are left as they were.
+ * Everything else as for vp_append.
+ */
+vp_status vp_append4(vp_ctx* ctx, int32_t batch, int32_t n_new, const vp_rows* q, const vp_rows* k, const vp_rows* v,
+                     const int32_t* seq_len, const int32_t* new_len, const vp_rotation* rotation,
+                     const vp_rows* q_out, const vp_kv4* k_cache, const vp_kv4* v_cache,
+                     const vp_rows* k_held, const vp_rows* v_held, void* cuda_stream);
+
+/* Allocates the workspace of vp_attend4 on a context, once, for calls of up to
+ * max_new new tokens per sequence: some MB.  Waits for the device; call it outside
+ * stream capture.  A second call replaces the first one's workspace: graphs that
+ * captured vp_attend4 before it must not be replayed.  VP_ERR_INVALID_ARG for
+ * max_new < 1 or max_new > max_seq; VP_ERR_CUDA when the allocation fails (the
+ * context then has no such workspace). */
+vp_status vp_reserve4(vp_ctx* ctx, int32_t max_new);
+
+/*
+ * vp_attend_new over caches held in 4 bits: the arguments mean what they mean
+ * there, without accumulated weights.  Scales need not be vp_append4's: any finite
+ * fp16 number is served, and a group whose scale is not finite is as a cache row
+ * that is not.  Logits are exact products of queries and codes, scaled and summed
+ * in float.  bf16 contexts: the probabilities, and their products with the values'
+ * scales, are rounded to fp16 (2^-11 of each; the output's own rounding is 2^-8);
+ * fp32 contexts: both are two fp16 terms.  VP_ERR_CAPACITY when vp_reserve4 has not
+ * reserved for n_new.  Allocates nothing and never synchronises; every kernel waits
+ * for the stream's previous work, so an input may be the output of the preceding
+ * call of this library.
+ */
+vp_status vp_attend4(vp_ctx* ctx, int32_t batch, int32_t n_new, const vp_rows* q,
+                     const vp_kv4* k_cache, const vp_kv4* v_cache,
+                     const int32_t* seq_len, const int32_t* new_len, const vp_visible* visible,
+                     const vp_rows* out, float* lse, void* cuda_stream);
 
 /* Score kernel of later vp_decode_step calls on this context (an
  * implementation choice with no counterpart in the paper; results agree

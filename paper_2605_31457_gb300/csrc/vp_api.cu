@@ -416,6 +416,7 @@ vp_status vp_check_errors(vp_ctx* ctx, void* cuda_stream) {
   if (word & vp::ERR_KEPT) msg += " kept index outside the visual span;";
   if (word & vp::ERR_NONFINITE) msg += " non-finite importance score;";
   if (word & vp::ERR_NEW) msg += " new_len outside [0, min(n_new, seq_len)];";
+  if (word & vp::ERR_POS) msg += " position outside the rotation table;";
   if (word & vp::ERR_TIMEOUT) msg += " an asynchronous copy did not complete in time;";
   return fail(ctx, VP_ERR_DEVICE_PRECOND, msg);
 }
@@ -468,6 +469,7 @@ void vp_free(vp_ctx* ctx) {
   }
   if (ctx->ws) cudaFree(ctx->ws);
   if (ctx->new_ws) cudaFree(ctx->new_ws);
+  if (ctx->ws4) cudaFree(ctx->ws4);
   delete ctx;
 }
 

@@ -1,0 +1,572 @@
+// k_att4: attention of newly appended tokens over a cache held in 4 bits
+// (vp_attend4).
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <math_constants.h>
+#include <stdint.h>
+
+#include <type_traits>
+
+#include "vp_attend_device.h"
+#include "vp_cache4.h"
+#include "vp_device.h"
+
+namespace vp {
+namespace {
+
+// ---------------------------------------------------------------------------
+// k_att4<T, D, NT>: up to 8 NT query rows of a (sequence, kv-head).  A warp takes
+// 16 of the 128 tokens of a tile, with softmax statistics and an output of its
+// own; the warps' are joined at the end of a CTA's part of an item.
+//
+// Codes are not turned into values one by one.  Four bits in the lowest mantissa
+// bits of an fp16 number are a subnormal number, code * 2^-24, which the tensor
+// cores (mma.sync) multiply exactly, and 16 times that one place higher:
+//   S^T = K Q^T   (M = 16 tokens, N = 8 query rows, K = 16 dimensions): the sum of
+//         a group of 32 dimensions starts at -8 sum q (codes have an offset of 8)
+//         and is scaled by the token's scale afterwards, in float;
+//   O^T = V^T P^T (M = 16 dimensions, N = 8 rows, K = 16 tokens): the scale of the
+//         group's dimensions, one a token, goes into P; the offset's part of O is
+//         a product with a constant.
+// So 64 values of a thread take two masks each and few multiplications.  The
+// queries' fp16 form: a row is scaled by a power of two so that its largest
+// magnitude lies in [2^13, 2^14), and the dimensions that meet a code 16 times too
+// large by 1/16; a bf16 number fits exactly (what is more than 2^34 times smaller
+// than the row's largest is rounded), a float takes two terms.
+// P enters in one fp16 term for bf16 outputs: its rounding and that of its
+// product with the scale are 2^-11 each of a term, an eighth of the output's own
+// each; in two terms for float outputs.
+//
+// P = exp2(z - reference).  The reference is 10 (log2 units) below the largest
+// logit that raised it, and is raised when a logit is more than 14 above it, so
+// P <= 2^14 and P * scale < 2^15 for scales below 2.  From the first token with a
+// larger one on, the reference is 15 higher (one term: P is then exact to 2^-20 of
+// the row's largest), or P * scale is taken times 2^-15 (two terms).
+//
+// Tokens that no row sees are not copied: their codes are whatever the ring held
+// before, their scales 0 and their logits masked.
+// ---------------------------------------------------------------------------
+constexpr int kWarps4 = 8, kThreads4 = 32 * kWarps4;
+constexpr float kAbove4 = 10.f, kBig4 = 15.f, kRaise4 = 4.f;
+
+template <typename T, int D, int NT>
+struct Cfg4 {
+  static constexpr int TERMS = std::is_same<T, float>::value ? 2 : 1;
+  static constexpr int GROUPS = D / kGroup4;
+  static constexpr int CPS = NT * TERMS == 1 ? 2 : 1;   // CTAs per SM
+  static constexpr int RS = 8 * NT;                     // query rows of an item
+  static constexpr int CODES = 16 * D / 2;              // a stage: codes of 16 tokens, then their scales, of K and of V
+  static constexpr int SCALES = 16 * GROUPS * 2;
+  static constexpr int STAGE = 2 * (CODES + SCALES);
+  static constexpr int S = 4;                           // stages of a warp's ring
+  static constexpr int OFF_O = kWarps4 * S * STAGE;     // float [warps][RS][D]: outputs to be joined
+  static constexpr int OFF_ML = OFF_O + kWarps4 * RS * D * 4;  // float2 [warps][RS]
+  static constexpr int OFF_MASK = OFF_ML + kWarps4 * RS * 8;   // int [warps][S]: tokens copied
+  static constexpr int OFF_MISC = OFF_MASK + kWarps4 * S * 4;  // int: line_start, a flag
+  static constexpr int LINE = kWarps4 + 7;
+  static constexpr size_t SMEM = OFF_MISC + (LINE + 1) * 4;
+  static_assert(SMEM <= 232448 / CPS - (CPS > 1 ? 1024 : 0), "shared memory of the CTAs of an SM");
+};
+
+__device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                        uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// The transpose of an 8x8 matrix of 16-bit values held as two a lane.
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;\n" : "=r"(y) : "r"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  const __half2 v = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ float2 unpack_f16(uint32_t u) { return __half22float2(*reinterpret_cast<const __half2*>(&u)); }
+__device__ __forceinline__ uint32_t mul_f16(uint32_t a, uint32_t b) {
+  const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+// A copy of N bytes, or N zeros.
+template <int N>
+__device__ __forceinline__ void cp_async_or_zero(unsigned dst, const void* src, bool copy) {
+  const int n = copy ? N : 0;
+  if constexpr (N == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(dst), "l"(src), "r"(n) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], %3, %2;\n" ::"r"(dst), "l"(src), "r"(n), "n"(N) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;\n" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;\n" ::"n"(N) : "memory"); }
+
+// Byte offset of 16-byte chunk `ch` of token `row` in a stage's codes: the chunks
+// are exchanged so that eight rows' same chunk lies in different banks.
+template <int D>
+__device__ __forceinline__ int code_at(int row, int ch) {
+  return D == 128 ? row * 64 + ((ch ^ ((row >> 1) & 3)) << 4) : row * 32 + ((ch ^ ((row >> 2) & 1)) << 4);
+}
+
+template <typename T, int D, int NT>
+__global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const __grid_constant__ Attend4Params p) {
+  using C = Cfg4<T, D, NT>;
+  constexpr int S = C::S, NG = C::GROUPS, TERMS = C::TERMS, RS = C::RS;
+  extern __shared__ __align__(16) unsigned char smem[];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int r = lane >> 2, c = lane & 3;
+  float* o_all = reinterpret_cast<float*>(smem + C::OFF_O);
+  float2* ml_all = reinterpret_cast<float2*>(smem + C::OFF_ML);
+  int* masks = reinterpret_cast<int*>(smem + C::OFF_MASK) + warp * S;
+  int* misc = reinterpret_cast<int*>(smem + C::OFF_MISC);
+  const unsigned ring = smem_u32(smem) + warp * S * C::STAGE;
+  pdl_wait();
+  pdl_trigger();
+  Walk walk = line_start<kThreads4>(p, misc);
+  Part q;
+  unsigned err = 0;
+
+  // Addresses of this lane's matrix rows within a stage (ldmatrix: lane l gives
+  // row l % 8 of matrix l / 8; matrices: tokens 0-7 and 8-15 of one group, then
+  // of the next).
+  const int mrow = (lane & 7) + ((lane >> 3) & 1) * 8, mch = lane >> 4;
+  const uint32_t off8 = 0x80088008u;  // -8 * 2^-24 twice
+
+  while (next_part(p, walk, q)) {
+    const int n = q.u1 - q.u0;
+    const int rows = q.it.rows;
+    // ---- rows that see nothing: padding, or all of an item without tiles
+    if (q.owner) {
+      const int first = q.it.tl.n == 0 ? 0 : rows;
+#pragma unroll 1
+      for (int i = tid; i < (min(p.block, p.R - q.it.row0) - first) * (D / 4); i += kThreads4) {
+        const int row = q.it.row0 + first + i / (D / 4);
+        store4(out_row<T>(p, q.b, q.g, row) + 4 * (i % (D / 4)), make_float4(0.f, 0.f, 0.f, 0.f));
+        if (i % (D / 4) == 0) store_lse(p, q.b, q.g, row, 0.f, 0.f);
+      }
+    }
+    if (n <= 0) continue;
+    const SeenRange& sr = q.it.sr;
+
+    // ---- copies of the warp's 16 tokens of tile u, into stage u % S
+    const int lrow = lane & 15;
+    int kn = -1, vn = -1;  // page ids of token lrow of the next tile to be copied
+    auto lookup = [&](int u) {
+      if (!p.paged || u >= q.u1) return;
+      const int lp = (q.it.tl.tile(u) * kTcTile + 16 * warp + lrow) >> p.page_shift;
+      kn = lp < p.k4.max_pages ? __ldg(p.k4.block_table + (int64_t)q.b * p.k4.max_pages + lp) : -1;
+      vn = lp < p.v4.max_pages ? __ldg(p.v4.block_table + (int64_t)q.b * p.v4.max_pages + lp) : -1;
+    };
+    auto issue = [&](int u) {
+      if (u < q.u1) {
+        const int st = (u - q.u0) % S;
+        const unsigned to = ring + st * C::STAGE;
+        const int j0 = q.it.tl.tile(u) * kTcTile + 16 * warp, j = j0 + lrow;
+        bool live = j < sr.s_end || (j >= sr.lo && j < sr.hi);
+        int kp = q.b, vp = q.b;
+        if (p.paged) {
+          kp = kn;
+          vp = vn;
+          const bool ok = kp >= 0 && kp < p.k4.num_pages && vp >= 0 && vp < p.v4.num_pages;
+          if (live && !ok) err |= ERR_PAGE;
+          live = live && ok;
+        }
+        const unsigned mask = __ballot_sync(0xffffffffu, live) & 0xffffu;
+        if (lane == 0) masks[st] = (int)mask;
+        const int in_page = p.paged ? p.page_size - 1 : -1;
+        constexpr int CH = D / 32, PER = 16 * CH / 32;  // 16-byte chunks of a row; rows this lane copies of K, of V
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+          const int row = lane / CH + i * (32 / CH), ch = lane % CH;
+          const int kr = __shfl_sync(0xffffffffu, kp, row), vr = __shfl_sync(0xffffffffu, vp, row);
+          const bool copy = (mask >> row) & 1u;
+          const int64_t at = (j0 + row) & in_page;
+          cp_async_or_zero<16>(to + code_at<D>(row, ch),
+                               p.k4.codes + (copy ? kr * p.k4.cb + q.g * p.k4.ch + at * p.k4.ct + 16 * ch : 0), copy);
+          cp_async_or_zero<16>(to + C::CODES + code_at<D>(row, ch),
+                               p.v4.codes + (copy ? vr * p.v4.cb + q.g * p.v4.ch + at * p.v4.ct + 16 * ch : 0), copy);
+        }
+        const bool is_v = lane >= 16;
+        const Kv4View& x = is_v ? p.v4 : p.k4;
+        cp_async_or_zero<2 * NG>(to + 2 * C::CODES + (is_v ? C::SCALES : 0) + lrow * 2 * NG,
+                                 x.scales + (live ? (is_v ? vp : kp) * x.sb + q.g * x.sh + (int64_t)(j & in_page) * x.st : 0),
+                                 live);
+        lookup(u + 1);
+      }
+      cp_async_commit();
+    };
+    lookup(q.u0);
+#pragma unroll
+    for (int k = 0; k < S - 1; ++k) issue(q.u0 + k);
+
+    // ---- queries: 8 dimensions of each group a lane, in the order of the codes
+    uint32_t qf[NT][TERMS][NG][4];
+    float init[NT][NG][2], fac[NT][2];
+    int tq[NT][2];
+    const int base = q.sq.len - q.sq.n;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const int row = 8 * t + r;
+      float x[NG][8];
+      float top = 0.f;
+#pragma unroll
+      for (int g = 0; g < NG; ++g) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[g][e] = 0.f;
+        if (row < rows) {
+          const int tok = row_token(p, q.it.row0 + row);
+          const T* src = static_cast<const T*>(p.q.data) + (int64_t)q.b * p.q.sb + (int64_t)tok * p.q.sn +
+                         (int64_t)(q.g * p.G + q.it.row0 + row - tok * p.G) * p.q.sh + 32 * g + 8 * c;
+          if constexpr (TERMS == 1) {
+            const uint4 v = __ldcg(reinterpret_cast<const uint4*>(src));
+            bf2(v.x, x[g][0], x[g][1]); bf2(v.y, x[g][2], x[g][3]); bf2(v.z, x[g][4], x[g][5]); bf2(v.w, x[g][6], x[g][7]);
+          } else {
+            const float4 v = __ldcg(reinterpret_cast<const float4*>(src)), w = __ldcg(reinterpret_cast<const float4*>(src) + 1);
+            x[g][0] = v.x; x[g][1] = v.y; x[g][2] = v.z; x[g][3] = v.w;
+            x[g][4] = w.x; x[g][5] = w.y; x[g][6] = w.z; x[g][7] = w.w;
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[g][e]));
+      }
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      // 2^k and 2^-k, the largest magnitude times 2^k in [2^13, 2^14)
+      const int field = min(267 - (int)(__float_as_uint(top) >> 23), 253);
+      const float up = __uint_as_float((unsigned)field << 23), down = __uint_as_float((unsigned)(254 - field) << 23);
+#pragma unroll
+      for (int g = 0; g < NG; ++g) {
+        float sum = 0.f;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {  // dimensions k and k + 4 meet one mask
+          const float f = (k & 1) ? up * 0.0625f : up;
+          const float a = x[g][k] * f, b = x[g][k + 4] * f;
+          const uint32_t hi = pack_f16(a, b);
+          const float2 h = unpack_f16(hi);
+          qf[t][0][g][k] = hi;
+          float part = h.x + h.y;
+          if constexpr (TERMS == 2) {
+            const uint32_t lo = pack_f16(a - h.x, b - h.y);
+            const float2 l = unpack_f16(lo);
+            qf[t][TERMS - 1][g][k] = lo;
+            part += l.x + l.y;
+          }
+          sum += (k & 1) ? part * 16.f : part;
+        }
+        sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+        sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+        sum *= -8.f * 5.9604644775390625e-08f;
+        init[t][g][0] = __shfl_sync(0xffffffffu, sum, 8 * c);
+        init[t][g][1] = __shfl_sync(0xffffffffu, sum, 8 * c + 4);
+      }
+      const float f = down * 16777216.f * p.c_log2;
+      fac[t][0] = __shfl_sync(0xffffffffu, f, 8 * c);
+      fac[t][1] = __shfl_sync(0xffffffffu, f, 8 * c + 4);
+#pragma unroll
+      for (int k = 0; k < 2; ++k) tq[t][k] = base + row_token(p, q.it.row0 + min(8 * t + 2 * c + k, rows - 1));
+    }
+    const int t0 = base + row_token(p, q.it.row0), t1 = base + row_token(p, q.it.row0 + rows - 1);
+
+    float o[NT][NG][2][4], corr[NT][4], ref[NT][2], l[NT][2];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) corr[t][k] = 0.f;
+      ref[t][0] = ref[t][1] = -CUDART_INF_F;
+      l[t][0] = l[t][1] = 0.f;
+#pragma unroll
+      for (int g = 0; g < NG; ++g)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) o[t][g][h][k] = 0.f;
+    }
+    float above = kAbove4, v_unit = 1.f;  // O is in units of v_unit
+    bool large = false;                    // a scale of 2 or more was met
+
+#pragma unroll 1
+    for (int u = q.u0; u < q.u1; ++u) {
+      cp_async_wait<S - 2>();
+      __syncwarp();
+      issue(u + S - 1);  // into the stage that the last turn read
+      const int st = (u - q.u0) % S;
+      const unsigned at = ring + st * C::STAGE;
+      const unsigned char* sp = smem + (warp * S + st) * C::STAGE;
+      const unsigned mask = (unsigned)masks[st];
+      const int j0 = q.it.tl.tile(u) * kTcTile + 16 * warp;
+
+      // ---- logits: tokens r and r + 8, query rows 2c and 2c + 1
+      uint32_t k0[NG], k1[NG];
+#pragma unroll
+      for (int g = 0; g < NG; g += 2)
+        ldsm_x4(at + code_at<D>(mrow, g + mch), k0[g], k1[g], k0[g + 1], k1[g + 1]);
+      float ks0[NG], ks1[NG];
+      {
+        const unsigned char* ks = sp + 2 * C::CODES;
+#pragma unroll
+        for (int g = 0; g < NG; g += 2) {
+          const float2 a = unpack_f16(*reinterpret_cast<const uint32_t*>(ks + r * 2 * NG + 2 * g));
+          const float2 b = unpack_f16(*reinterpret_cast<const uint32_t*>(ks + (r + 8) * 2 * NG + 2 * g));
+          ks0[g] = a.x; ks0[g + 1] = a.y;
+          ks1[g] = b.x; ks1[g + 1] = b.y;
+        }
+      }
+      float z[NT][4];
+#pragma unroll
+      for (int t = 0; t < NT; ++t) z[t][0] = z[t][1] = z[t][2] = z[t][3] = 0.f;
+#pragma unroll
+      for (int g = 0; g < NG; ++g) {
+        const uint32_t a0 = k0[g] & 0x000f000fu, a1 = k1[g] & 0x000f000fu, a2 = k0[g] & 0x00f000f0u, a3 = k1[g] & 0x00f000f0u;
+        const uint32_t x0 = k0[g] >> 8, x1 = k1[g] >> 8;
+        const uint32_t b0 = x0 & 0x000f000fu, b1 = x1 & 0x000f000fu, b2 = x0 & 0x00f000f0u, b3 = x1 & 0x00f000f0u;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          float s[4] = {init[t][g][0], init[t][g][1], init[t][g][0], init[t][g][1]};
+#pragma unroll
+          for (int m = 0; m < TERMS; ++m) {
+            mma_f16(s, a0, a1, a2, a3, qf[t][m][g][0], qf[t][m][g][1]);
+            mma_f16(s, b0, b1, b2, b3, qf[t][m][g][2], qf[t][m][g][3]);
+          }
+          z[t][0] = fmaf(s[0], ks0[g], z[t][0]);
+          z[t][1] = fmaf(s[1], ks0[g], z[t][1]);
+          z[t][2] = fmaf(s[2], ks1[g], z[t][2]);
+          z[t][3] = fmaf(s[3], ks1[g], z[t][3]);
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        z[t][0] *= fac[t][0]; z[t][1] *= fac[t][1];
+        z[t][2] *= fac[t][0]; z[t][3] *= fac[t][1];
+      }
+      const bool all_see = mask == 0xffffu && j0 + 15 <= t0 && (p.window < 0 || j0 > t1 - p.window || j0 + 16 <= p.sinks);
+      if (!all_see) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const int row = r + 8 * (k >> 1);
+            if (!((mask >> row) & 1u) || !sees(j0 + row, tq[t][k & 1], p.window, p.sinks)) z[t][k] = -CUDART_INF_F;
+          }
+      }
+
+      // ---- V's scales: of tokens 2c, 2c + 1 (s0) and 2c + 8, 2c + 9 (s1), a group each
+      uint32_t s0[NG], s1[NG];
+      uint32_t any = 0;
+      {
+        const unsigned char* vs = sp + 2 * C::CODES + C::SCALES;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          uint32_t w[NG];  // two tokens' scales
+          if constexpr (NG == 4) {
+            const uint4 v = *reinterpret_cast<const uint4*>(vs + (2 * c + 8 * h) * 8);
+            w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+          } else {
+            const uint2 v = *reinterpret_cast<const uint2*>(vs + (2 * c + 8 * h) * 4);
+            w[0] = v.x; w[1] = v.y;
+          }
+#pragma unroll
+          for (int g = 0; g < NG; g += 2) {
+            const uint32_t x = w[g / 2], y = w[NG / 2 + g / 2];
+            any |= x | y;
+            (h ? s1 : s0)[g] = prmt(x, y, 0x5410);
+            (h ? s1 : s0)[g + 1] = prmt(x, y, 0x7632);
+          }
+        }
+      }
+
+      // ---- the references
+      bool need = false;
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) need |= fmaxf(z[t][k], z[t][2 + k]) > ref[t][k] + (above + kRaise4);
+      const bool big = (any & 0x40004000u) != 0;  // a scale of 2 or more
+      if (__any_sync(0xffffffffu, need || (big && !large))) {
+        float fv = 1.f;
+        if (!large && __any_sync(0xffffffffu, big)) {
+          large = true;
+          if constexpr (TERMS == 1) above = kAbove4 - kBig4;
+          else fv = v_unit = 3.0517578125e-05f;  // 2^-kBig4
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const float top = group_max(fmaxf(z[t][k], z[t][2 + k]));
+            const float next = fmaxf(ref[t][k], top - above);
+            const float f = ref[t][k] == -CUDART_INF_F ? 0.f : fexp2(ref[t][k] - next);
+            ref[t][k] = next;
+            l[t][k] *= f;
+            const float fo = TERMS == 1 ? f : f * fv;
+            corr[t][k] *= fo;
+#pragma unroll
+            for (int g = 0; g < NG; ++g)
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                o[t][g][h][k] *= fo;
+                o[t][g][h][2 + k] *= fo;
+              }
+          }
+      }
+
+      // ---- probabilities, transposed: query row r, tokens as in s0 and s1
+      uint32_t ph[NT][2], pl[NT][2];
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const float m0 = ref[t][0] == -CUDART_INF_F ? 0.f : ref[t][0], m1 = ref[t][1] == -CUDART_INF_F ? 0.f : ref[t][1];
+        const float e0 = fexp2(z[t][0] - m0), e1 = fexp2(z[t][1] - m1), e2 = fexp2(z[t][2] - m0), e3 = fexp2(z[t][3] - m1);
+        l[t][0] += e0 + e2;
+        l[t][1] += e1 + e3;
+        const uint32_t h0 = pack_f16(e0, e1), h1 = pack_f16(e2, e3);
+        ph[t][0] = transpose8(h0);
+        ph[t][1] = transpose8(h1);
+        if constexpr (TERMS == 2) {
+          const float2 f0 = unpack_f16(h0), f1 = unpack_f16(h1);
+          pl[t][0] = transpose8(pack_f16(e0 - f0.x, e1 - f0.y));
+          pl[t][1] = transpose8(pack_f16(e2 - f1.x, e3 - f1.y));
+        }
+      }
+
+      // ---- output: dimensions 32 g + 4 r + 2 h and the next, query rows 2c, 2c + 1
+      uint32_t v0[NG], v1[NG];
+#pragma unroll
+      for (int g = 0; g < NG; g += 2)
+        ldsm_x4_t(at + C::CODES + code_at<D>(mrow, g + mch), v0[g], v1[g], v0[g + 1], v1[g + 1]);
+#pragma unroll
+      for (int g = 0; g < NG; ++g) {
+        const uint32_t a0 = v0[g] & 0x000f000fu, a1 = v0[g] & 0x00f000f0u, a2 = v1[g] & 0x000f000fu, a3 = v1[g] & 0x00f000f0u;
+        const uint32_t x0 = v0[g] >> 8, x1 = v1[g] >> 8;
+        const uint32_t b0 = x0 & 0x000f000fu, b1 = x0 & 0x00f000f0u, b2 = x1 & 0x000f000fu, b3 = x1 & 0x00f000f0u;
+        const uint32_t e = r == g ? off8 : 0u;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          uint32_t w[TERMS][2];
+          if constexpr (TERMS == 1) {
+            w[0][0] = mul_f16(ph[t][0], s0[g]);
+            w[0][1] = mul_f16(ph[t][1], s1[g]);
+          } else {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              const float2 x = unpack_f16(ph[t][k]), y = unpack_f16(pl[t][k]), s = unpack_f16(k ? s1[g] : s0[g]);
+              const float a = (x.x + y.x) * (s.x * v_unit), b = (x.y + y.y) * (s.y * v_unit);
+              w[0][k] = pack_f16(a, b);
+              const float2 hi = unpack_f16(w[0][k]);
+              w[TERMS - 1][k] = pack_f16(a - hi.x, b - hi.y);
+            }
+          }
+#pragma unroll
+          for (int m = 0; m < TERMS; ++m) {
+            mma_f16(o[t][g][0], a0, a1, a2, a3, w[m][0], w[m][1]);
+            mma_f16(o[t][g][1], b0, b1, b2, b3, w[m][0], w[m][1]);
+            mma_f16(corr[t], e, 0u, e, 0u, w[m][0], w[m][1]);
+          }
+        }
+      }
+    }
+    cp_async_wait<0>();
+    const float o_unit = TERMS == 1 || !large ? 16777216.f : 16777216.f * 32768.f;
+
+    // ---- the warps' outputs, joined by the CTA into rows of out or a record
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int row = 8 * t + 2 * c + k;
+        const float sum = group_sum(l[t][k]);
+        if (r == 0) ml_all[warp * RS + row] = make_float2(ref[t][k], sum);
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+          const float off = __shfl_sync(0xffffffffu, corr[t][k], 4 * g + c);
+          const float4 x = make_float4(o[t][g][0][k] + off, fmaf(o[t][g][0][2 + k], 0.0625f, off),
+                                       o[t][g][1][k] + off, fmaf(o[t][g][1][2 + k], 0.0625f, off));
+          *reinterpret_cast<float4*>(o_all + (warp * RS + row) * D + 32 * g + 4 * r) =
+              make_float4(x.x * o_unit, x.y * o_unit, x.z * o_unit, x.w * o_unit);
+        }
+      }
+    __syncthreads();
+    const bool direct = !by_ticket(q.parts);
+    const int rec = record_of(blockIdx.x, q.c0) * RS;
+#pragma unroll 1
+    for (int i = tid; i < rows * (D / 4); i += kThreads4) {
+      const int row = i / (D / 4), d = 4 * (i % (D / 4));
+      float m = -CUDART_INF_F;
+#pragma unroll
+      for (int w = 0; w < kWarps4; ++w) m = fmaxf(m, ml_all[w * RS + row].x);
+      const float mu = m == -CUDART_INF_F ? 0.f : m;
+      float sum = 0.f;
+      float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int w = 0; w < kWarps4; ++w) {
+        const float2 st = ml_all[w * RS + row];
+        const float f = exp2f(st.x - mu);
+        const float4 y = *reinterpret_cast<const float4*>(o_all + (w * RS + row) * D + d);
+        sum = fmaf(st.y, f, sum);
+        x.x = fmaf(y.x, f, x.x); x.y = fmaf(y.y, f, x.y); x.z = fmaf(y.z, f, x.z); x.w = fmaf(y.w, f, x.w);
+      }
+      if (direct) {
+        const float inv = sum > 0.f ? 1.f / sum : 0.f;
+        store4(out_row<T>(p, q.b, q.g, q.it.row0 + row) + d, make_float4(x.x * inv, x.y * inv, x.z * inv, x.w * inv));
+        if (d == 0) store_lse(p, q.b, q.g, q.it.row0 + row, m, sum);
+      } else {
+        *reinterpret_cast<float4*>(p.part_o + (int64_t)(rec + row) * D + d) = x;
+        if (d == 0) *reinterpret_cast<float2*>(p.part_st + 2 * (rec + row)) = make_float2(m, sum);
+      }
+    }
+    if (direct) __syncthreads();  // o_all is read before its next use
+    else if (last_to_arrive(p.tickets + q.c0, q.parts, tid, misc + C::LINE, [] { __syncthreads(); }))
+      join_records<T, D, kThreads4, 1, 16>(p, q.b, q.g, q.it.row0, rows, q.parts, RS,
+                                           [&](int k) { return record_of(q.c0 + k, q.c0); }, tid);
+  }
+  if (err) atomicOr(p.err, err);
+}
+
+// f(kernel, shared bytes, rows, CTAs per SM) for the instance that serves R query rows.
+template <typename F>
+auto with_att4(int dtype, int D, int R, F&& f) {
+  auto inst = [&](auto zero, auto dim, auto tiles) {
+    using T = decltype(zero);
+    using C = Cfg4<T, decltype(dim)::value, decltype(tiles)::value>;
+    return f(k_att4<T, decltype(dim)::value, decltype(tiles)::value>, C::SMEM, C::RS, C::CPS);
+  };
+  auto sized = [&](auto zero, auto dim) {
+    if (R <= 8) return inst(zero, dim, std::integral_constant<int, 1>());
+    if (R <= 16 || sizeof(zero) == 4) return inst(zero, dim, std::integral_constant<int, 2>());
+    if constexpr (sizeof(zero) == 2) return inst(zero, dim, std::integral_constant<int, 4>());
+    else return inst(zero, dim, std::integral_constant<int, 2>());
+  };
+  using D64 = std::integral_constant<int, 64>;
+  using D128 = std::integral_constant<int, 128>;
+  if (dtype == 0) return D == 128 ? sized(__nv_bfloat16(), D128()) : sized(__nv_bfloat16(), D64());
+  return D == 128 ? sized(0.f, D128()) : sized(0.f, D64());
+}
+
+}  // namespace
+
+cudaError_t configure_attend4() {
+  cudaError_t e = cudaSuccess;
+  for (int dtype : {0, 1})
+    for (int D : {64, 128})
+      for (int R : {8, 16, 32})
+        if (e == cudaSuccess)
+          e = with_att4(dtype, D, R, [](auto kernel, size_t smem, int, int) {
+            return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+          });
+  return e;
+}
+
+void plan_attend4(Attend4Params& p) {
+  p.block = with_att4(p.dtype, p.D, p.R, [](auto, size_t, int rows, int) { return rows; });
+  p.grid = p.num_sms * with_att4(p.dtype, p.D, p.R, [](auto, size_t, int, int cps) { return cps; });
+  p.nqt = (p.R + p.block - 1) / p.block;
+  p.fixed = kTileUnits;
+}
+
+cudaError_t launch_attend4(const Attend4Params& p, cudaStream_t st) {
+  if (line_bound((int64_t)p.B * p.Hkv * p.nqt, p.max_seq, p.fixed) > INT32_MAX) return cudaErrorInvalidConfiguration;
+  return with_att4(p.dtype, p.D, p.R, [&](auto kernel, size_t smem, int, int) {
+    return launch_dep(kernel, dim3(p.grid), kThreads4, smem, st, p);
+  });
+}
+
+}  // namespace vp

@@ -17,7 +17,8 @@ constexpr float kLn2 = 0.6931471805599453f;
 struct NewSeq {
   int len, n;
 };
-__device__ __forceinline__ NewSeq load_new(const AttendParams& p, int b, bool report) {
+template <typename P>
+__device__ __forceinline__ NewSeq load_new(const P& p, int b, bool report) {
   NewSeq s;
   s.len = __ldcg(p.seq_len + b);
   unsigned e = 0;
@@ -290,8 +291,8 @@ __device__ __forceinline__ void join_records(const AttendParams& p, int b, int g
   }
 }
 
-inline cudaError_t launch_dep(void (*kernel)(AttendParams), dim3 grid, int threads, size_t smem, cudaStream_t st,
-                              const AttendParams& p) {
+template <typename P>
+inline cudaError_t launch_dep(void (*kernel)(P), dim3 grid, int threads, size_t smem, cudaStream_t st, const P& p) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = dim3(threads);

@@ -6,7 +6,6 @@
 #include <string.h>
 
 #include <cmath>
-#include <exception>
 #include <string>
 
 #include "vp.h"
@@ -17,27 +16,14 @@
 using vp::aligned16;
 using vp::cuda_fail;
 using vp::fail;
+using vp::guarded;
 using vp::kv_ok;
+using vp::rows_ok;
+using vp::view;
 
 namespace {
 
 constexpr int kMaxGridY = 65535;  // sequences of a call of vp_evict
-
-vp::KvView view(const vp_kv& c) {
-  return vp::KvView{c.data, c.stride_b, c.stride_h, c.stride_t, c.block_table, c.max_pages, c.num_pages};
-}
-
-bool rows_ok(const vp_ctx* ctx, const vp_rows* r, const char* name, std::string* why) {
-  const size_t esz = ctx->cfg.dtype == VP_BF16 ? 2 : 4;
-  if (!r || !r->data) { *why = std::string(name) + ": NULL"; return false; }
-  if (!aligned16(r->data)) { *why = std::string(name) + ": data must be 16-byte aligned"; return false; }
-  for (int64_t s : {r->stride_b, r->stride_n, r->stride_h})
-    if (s < 0 || ((uint64_t)s * esz) % 16 != 0) {
-      *why = std::string(name) + ": strides must be >= 0 and multiples of 16 bytes";
-      return false;
-    }
-  return true;
-}
 
 bool weights_ok(const vp_weights* w, const char* name, std::string* why) {
   if (!w->data || (reinterpret_cast<uintptr_t>(w->data) & 3u)) {
@@ -218,25 +204,6 @@ vp_status evict(vp_ctx* ctx, int32_t batch, const vp_kv* k_src, const vp_kv* v_s
   const cudaError_t e = vp::launch_evict(p, static_cast<cudaStream_t>(cuda_stream));
   if (e != cudaSuccess) return cuda_fail(ctx, "vp_evict: launch", e);
   return VP_OK;
-}
-
-// No exception may cross the C ABI (a failed allocation of an error text), and
-// nothing is allocated or launched on another device than the context's.
-template <typename F>
-vp_status guarded(vp_ctx* ctx, const char* name, F&& f) {
-  if (!ctx) return VP_ERR_NOT_INITIALIZED;
-  try {
-    ctx->last_error.clear();
-    int device = 0;
-    const cudaError_t e = cudaGetDevice(&device);
-    if (e != cudaSuccess) return cuda_fail(ctx, name, e);
-    if (device != ctx->device)
-      return fail(ctx, VP_ERR_INVALID_ARG, std::string(name) + ": the current device is " + std::to_string(device) +
-                  ", the context's is " + std::to_string(ctx->device));
-    return f();
-  } catch (const std::exception&) {
-    return VP_ERR_CUDA;
-  }
 }
 
 }  // namespace

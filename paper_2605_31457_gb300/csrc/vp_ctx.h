@@ -5,6 +5,7 @@
 #include <stdint.h>
 #include <stdio.h>
 
+#include <exception>
 #include <string>
 #include <vector>
 
@@ -41,6 +42,8 @@ struct vp_ctx {
   int32_t last_kernels = 0;
   void* new_ws = nullptr;  // workspace of vp_attend_new (vp_reserve_new)
   vp::NewLayout new_lay;
+  void* ws4 = nullptr;  // workspace of vp_attend4 (vp_reserve4)
+  vp::NewLayout lay4;
 };
 
 namespace vp {
@@ -77,6 +80,41 @@ inline bool kv_ok(const vp_ctx* ctx, const vp_kv* kv, const char* name, std::str
     snprintf(buf, sizeof buf, "%s: block_table given but the context is not paged", name); *why = buf; return false;
   }
   return true;
+}
+
+inline KvView view(const vp_kv& c) {
+  return KvView{c.data, c.stride_b, c.stride_h, c.stride_t, c.block_table, c.max_pages, c.num_pages};
+}
+
+inline bool rows_ok(const vp_ctx* ctx, const vp_rows* r, const char* name, std::string* why) {
+  const size_t esz = ctx->cfg.dtype == VP_BF16 ? 2 : 4;
+  if (!r || !r->data) { *why = std::string(name) + ": NULL"; return false; }
+  if (!aligned16(r->data)) { *why = std::string(name) + ": data must be 16-byte aligned"; return false; }
+  for (int64_t s : {r->stride_b, r->stride_n, r->stride_h})
+    if (s < 0 || ((uint64_t)s * esz) % 16 != 0) {
+      *why = std::string(name) + ": strides must be >= 0 and multiples of 16 bytes";
+      return false;
+    }
+  return true;
+}
+
+// No exception may cross the C ABI (a failed allocation of an error text), and
+// nothing is allocated or launched on another device than the context's.
+template <typename F>
+vp_status guarded(vp_ctx* ctx, const char* name, F&& f) {
+  if (!ctx) return VP_ERR_NOT_INITIALIZED;
+  try {
+    ctx->last_error.clear();
+    int device = 0;
+    const cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess) return cuda_fail(ctx, name, e);
+    if (device != ctx->device)
+      return fail(ctx, VP_ERR_INVALID_ARG, std::string(name) + ": the current device is " + std::to_string(device) +
+                  ", the context's is " + std::to_string(ctx->device));
+    return f();
+  } catch (const std::exception&) {
+    return VP_ERR_CUDA;
+  }
 }
 
 }  // namespace vp

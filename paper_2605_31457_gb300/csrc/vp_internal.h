@@ -23,7 +23,8 @@ enum : unsigned {
   ERR_KEPT = 16u,      // a kept index outside [0, N_v)
   ERR_NONFINITE = 32u, // a non-finite score reached the selection
   ERR_TIMEOUT = 64u,   // a bounded wait for an asynchronous copy gave up
-  ERR_NEW = 128u       // new_len outside [0, min(n_new, seq_len)]
+  ERR_NEW = 128u,      // new_len outside [0, min(n_new, seq_len)]
+  ERR_POS = 256u       // a rotation position outside the table
 };
 
 // Split statistics written by the score kernel for every (sequence, query

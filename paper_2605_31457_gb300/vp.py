@@ -42,7 +42,7 @@ VP_SCORE_TC = 2
 EXPORTED = ("vp_init", "vp_decode_step", "vp_max_kept", "vp_last_error", "vp_check_errors",
             "vp_timing_enable", "vp_timing_read", "vp_free", "vp_decode_step_noalloc", "vp_decode_gather",
             "vp_set_diagnostics", "vp_set_score_path", "vp_compact_kv", "vp_last_launch", "vp_reserve_new",
-            "vp_attend_new", "vp_evict")
+            "vp_attend_new", "vp_evict", "vp_append", "vp_append4", "vp_reserve4", "vp_attend4")
 VP_NO_WINDOW = -1
 VP_NOALLOC_SCRATCH_BYTES = 16 << 20
 
@@ -89,6 +89,20 @@ class vp_evict_policy(ctypes.Structure):
                 ("granularity", ctypes.c_int32)]
 
 
+class vp_rotation(ctypes.Structure):
+    _fields_ = [("cos_sin", ctypes.c_void_p), ("max_pos", ctypes.c_int32), ("rot_dim", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32), ("pos", ctypes.c_void_p), ("axes", ctypes.c_int32),
+                ("sections", ctypes.c_int32 * 3)]
+
+
+class vp_kv4(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p),
+                ("code_stride_b", ctypes.c_int64), ("code_stride_h", ctypes.c_int64),
+                ("code_stride_t", ctypes.c_int64), ("scale_stride_b", ctypes.c_int64),
+                ("scale_stride_h", ctypes.c_int64), ("scale_stride_t", ctypes.c_int64),
+                ("block_table", ctypes.c_void_p), ("max_pages", ctypes.c_int32), ("num_pages", ctypes.c_int32)]
+
+
 _P = ctypes.c_void_p
 lib.vp_init.argtypes = [ctypes.POINTER(vp_config), ctypes.POINTER(_P)]
 lib.vp_init.restype = ctypes.c_int
@@ -115,6 +129,18 @@ lib.vp_evict.argtypes = [_P, ctypes.c_int32, ctypes.POINTER(vp_kv), ctypes.POINT
                          ctypes.POINTER(vp_evict_policy), ctypes.POINTER(vp_kv), ctypes.POINTER(vp_kv),
                          ctypes.POINTER(vp_weights), ctypes.POINTER(vp_weights), _P, ctypes.c_int32, _P, _P]
 lib.vp_evict.restype = ctypes.c_int
+_ROWS, _KV, _KV4 = ctypes.POINTER(vp_rows), ctypes.POINTER(vp_kv), ctypes.POINTER(vp_kv4)
+lib.vp_append.argtypes = [_P, ctypes.c_int32, ctypes.c_int32, _ROWS, _ROWS, _ROWS, _P, _P,
+                          ctypes.POINTER(vp_rotation), _ROWS, _KV, _KV, _P]
+lib.vp_append.restype = ctypes.c_int
+lib.vp_append4.argtypes = [_P, ctypes.c_int32, ctypes.c_int32, _ROWS, _ROWS, _ROWS, _P, _P,
+                           ctypes.POINTER(vp_rotation), _ROWS, _KV4, _KV4, _ROWS, _ROWS, _P]
+lib.vp_append4.restype = ctypes.c_int
+lib.vp_reserve4.argtypes = [_P, ctypes.c_int32]
+lib.vp_reserve4.restype = ctypes.c_int
+lib.vp_attend4.argtypes = [_P, ctypes.c_int32, ctypes.c_int32, _ROWS, _KV4, _KV4, _P, _P, ctypes.POINTER(vp_visible),
+                           _ROWS, _P, _P]
+lib.vp_attend4.restype = ctypes.c_int
 lib.vp_set_score_path.argtypes = [_P, ctypes.c_int32]
 lib.vp_set_score_path.restype = ctypes.c_int
 lib.vp_last_launch.argtypes = [_P, ctypes.POINTER(ctypes.c_int32), ctypes.POINTER(ctypes.c_int32)]
@@ -250,6 +276,40 @@ def vp_evict(ctx, batch, k_src: vp_kv, v_src: vp_kv, seq_len, policy: vp_evict_p
     return _check(st, ctx) if check else st
 
 
+def vp_append(ctx, batch, n_new, q: vp_rows, k: vp_rows, v: vp_rows, seq_len, rotation: vp_rotation, q_out: vp_rows,
+              k_cache: vp_kv, v_cache: vp_kv, new_len=None, stream=None, check=True):
+    """Enqueues the rotation of the ``n_new`` newest tokens' queries and keys and the
+    appending of their keys and values.  q, k, v and q_out are ``rows(tensor)``
+    (q and q_out may be None), rotation ``make_rotation(...)`` or None; seq_len and
+    new_len are tensors."""
+    st = lib.vp_append(ctx, batch, n_new, _ref(q), _ref(k), _ref(v), _ptr(seq_len), _ptr(new_len), _ref(rotation),
+                       _ref(q_out), _ref(k_cache), _ref(v_cache), _stream(stream))
+    return _check(st, ctx) if check else st
+
+
+def vp_append4(ctx, batch, n_new, q: vp_rows, k: vp_rows, v: vp_rows, seq_len, rotation: vp_rotation, q_out: vp_rows,
+               k_cache: vp_kv4, v_cache: vp_kv4, new_len=None, k_held: vp_rows = None, v_held: vp_rows = None,
+               stream=None, check=True):
+    """``vp_append`` into caches held in 4 bits; k_held and v_held, where given,
+    receive the values that the caches now hold for the new tokens."""
+    st = lib.vp_append4(ctx, batch, n_new, _ref(q), _ref(k), _ref(v), _ptr(seq_len), _ptr(new_len), _ref(rotation),
+                        _ref(q_out), _ref(k_cache), _ref(v_cache), _ref(k_held), _ref(v_held), _stream(stream))
+    return _check(st, ctx) if check else st
+
+
+def vp_reserve4(ctx, max_new):
+    """Allocates the workspace of vp_attend4: up to ``max_new`` new tokens per sequence."""
+    return _check(lib.vp_reserve4(ctx, int(max_new)), ctx)
+
+
+def vp_attend4(ctx, batch, n_new, q: vp_rows, k_cache: vp_kv4, v_cache: vp_kv4, seq_len, visible: vp_visible,
+               out: vp_rows, new_len=None, lse=None, stream=None, check=True):
+    """``vp_attend_new`` over caches held in 4 bits (no accumulated weights)."""
+    st = lib.vp_attend4(ctx, batch, n_new, _ref(q), _ref(k_cache), _ref(v_cache), _ptr(seq_len), _ptr(new_len),
+                        _ref(visible), _ref(out), _ptr(lse), _stream(stream))
+    return _check(st, ctx) if check else st
+
+
 def vp_set_score_path(ctx, path):
     """Score kernel of later vp_decode_step calls: VP_SCORE_AUTO, VP_SCORE_MMA
     or VP_SCORE_TC."""
@@ -341,6 +401,41 @@ def kv_paged(pool, block_table) -> vp_kv:
     assert pool.dim() == 4 and pool.stride(3) == 1 and block_table.dim() == 2
     return vp_kv(pool.data_ptr(), pool.stride(0), pool.stride(1), pool.stride(2),
                  block_table.data_ptr(), block_table.shape[1], pool.shape[0])
+
+
+def kv4_contiguous(codes, scales) -> vp_kv4:
+    """A cache held in 4 bits: uint8 codes [B, Hkv, T, D/2] and float16 scales
+    [B, Hkv, T, D/32] (any strides with a contiguous last axis)."""
+    return _kv4(codes, scales, None)
+
+
+def kv4_paged(codes, scales, block_table) -> vp_kv4:
+    """Pools of codes [pages, Hkv, page_size, D/2] and scales [pages, Hkv, page_size,
+    D/32] plus an int32 [B, max_pages] block table."""
+    assert block_table.dim() == 2
+    return _kv4(codes, scales, block_table)
+
+
+def _kv4(codes, scales, table) -> vp_kv4:
+    assert codes.dim() == 4 and codes.stride(3) == 1 and codes.element_size() == 1
+    assert scales.dim() == 4 and (scales.stride(3) == 1 or scales.shape[3] == 1) and scales.element_size() == 2
+    assert codes.shape[:3] == scales.shape[:3] and codes.shape[3] == 16 * scales.shape[3]
+    paged = (table.data_ptr(), table.shape[1], codes.shape[0]) if table is not None else (None, 0, 0)
+    return vp_kv4(codes.data_ptr(), scales.data_ptr(), *codes.stride()[:3], *scales.stride()[:3], *paged)
+
+
+def make_rotation(cos_sin, interleaved=False, positions=None, sections=None) -> vp_rotation:
+    """Rotation by a float32 [max_pos, rot_dim] table (cosines, then sines) and
+    int32 positions [axes, B, n_new] ([B, n_new]: one axis; None: places in the
+    sequence); ``sections``: pairs of each axis when there are several."""
+    assert cos_sin.dim() == 2 and cos_sin.is_contiguous() and cos_sin.element_size() == 4
+    assert positions is None or (positions.is_contiguous() and positions.element_size() == 4)
+    axes = positions.shape[0] if positions is not None and positions.dim() == 3 else 1
+    parts = list(sections) if sections is not None else [cos_sin.shape[1] // 2]
+    assert len(parts) == axes
+    return vp_rotation(cos_sin.data_ptr(), cos_sin.shape[0], cos_sin.shape[1], int(interleaved),
+                       None if positions is None else positions.data_ptr(), axes,
+                       (ctypes.c_int32 * 3)(*(parts + [0] * (3 - len(parts)))))
 
 
 def rows(t) -> vp_rows:
