@@ -20,23 +20,24 @@ namespace {
 // 16 of the 128 tokens of a tile, with softmax statistics and an output of its
 // own; the warps' are joined at the end of a CTA's part of an item.
 //
-// Codes are not turned into values one by one.  Four bits in the lowest mantissa
-// bits of an fp16 number are a subnormal number, code * 2^-24, which the tensor
-// cores (mma.sync) multiply exactly, and 16 times that one place higher:
+// Codes are not turned into values one by one, but into the whole numbers code - 8
+// in fp16, two at a time: a mask puts four bits into the mantissa of 1024, and one
+// operation takes the 1032 off.  (Left in the mantissa of a subnormal number they
+// would need no operation, but the tensor cores align a subnormal factor by its
+// exponent field and lose up to ten bits of the sum.)  The products on the tensor
+// cores (mma.sync):
 //   S^T = K Q^T   (M = 16 tokens, N = 8 query rows, K = 16 dimensions): the sum of
-//         a group of 32 dimensions starts at -8 sum q (codes have an offset of 8)
-//         and is scaled by the token's scale afterwards, in float;
+//         a group of 32 dimensions is scaled by the token's scale in float;
 //   O^T = V^T P^T (M = 16 dimensions, N = 8 rows, K = 16 tokens): the scale of the
-//         group's dimensions, one a token, goes into P; the offset's part of O is
-//         a product with a constant.
-// So 64 values of a thread take two masks each and few multiplications.  The
-// queries' fp16 form: a row is scaled by a power of two so that its largest
-// magnitude lies in [2^13, 2^14), and the dimensions that meet a code 16 times too
-// large by 1/16; a bf16 number fits exactly (what is more than 2^34 times smaller
-// than the row's largest is rounded), a float takes two terms.
-// P enters in one fp16 term for bf16 outputs: its rounding and that of its
-// product with the scale are 2^-11 each of a term, an eighth of the output's own
-// each; in two terms for float outputs.
+//         group's dimensions, one a token, goes into P.
+// The order of a group's dimensions within a product is that of the masks, four
+// bits here and sixteen higher, so that no value is moved.
+// A query row in fp16 is scaled by a power of two so that its largest magnitude
+// lies in [2^13, 2^14): a bf16 number fits exactly (what is more than 2^30 times
+// smaller than the row's largest is rounded), a float takes two terms.  P enters in
+// one fp16 term for bf16 outputs: its rounding and that of its product with the
+// scale are 2^-11 each of a term, an eighth of the output's own each.  Float
+// outputs: two terms.
 //
 // P = exp2(z - reference).  The reference is 10 (log2 units) below the largest
 // logit that raised it, and is raised when a logit is more than 14 above it, so
@@ -76,6 +77,14 @@ __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1,
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+// D = A * B.
+__device__ __forceinline__ void mma_f16_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                              uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};\n"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
 // The transpose of an 8x8 matrix of 16-bit values held as two a lane.
 __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
   uint32_t y;
@@ -89,6 +98,17 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
 __device__ __forceinline__ float2 unpack_f16(uint32_t u) { return __half22float2(*reinterpret_cast<const __half2*>(&u)); }
 __device__ __forceinline__ uint32_t mul_f16(uint32_t a, uint32_t b) {
   const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+// The whole numbers code - 8 of the codes in bits 0-3 and 16-19, and of those in bits 4-7 and 20-23.
+__device__ __forceinline__ uint32_t less8(uint32_t x) {
+  const uint32_t y = (x & 0x000f000fu) | 0x64006400u;  // 1024 + code
+  const __half2 r = __hsub2(*reinterpret_cast<const __half2*>(&y), __float2half2_rn(1032.f));
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+__device__ __forceinline__ uint32_t less8_high(uint32_t x) {
+  const uint32_t y = (x & 0x00f000f0u) | 0x64006400u;  // 1024 + 16 code
+  const __half2 r = __hfma2(*reinterpret_cast<const __half2*>(&y), __float2half2_rn(0.0625f), __float2half2_rn(-72.f));
   return *reinterpret_cast<const uint32_t*>(&r);
 }
 // A copy of N bytes, or N zeros.
@@ -131,7 +151,6 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
   // row l % 8 of matrix l / 8; matrices: tokens 0-7 and 8-15 of one group, then
   // of the next).
   const int mrow = (lane & 7) + ((lane >> 3) & 1) * 8, mch = lane >> 4;
-  const uint32_t off8 = 0x80088008u;  // -8 * 2^-24 twice
 
   while (next_part(p, walk, q)) {
     const int n = q.u1 - q.u0;
@@ -149,49 +168,64 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
     if (n <= 0) continue;
     const SeenRange& sr = q.it.sr;
 
-    // ---- copies of the warp's 16 tokens of tile u, into stage u % S
+    // ---- copies of the warp's 16 tokens of tile u, into stage u % S.  The tokens
+    // lie in one page, or (pages of fewer than 16) a lane looks up token lane % 16's.
     const int lrow = lane & 15;
-    int kn = -1, vn = -1;  // page ids of token lrow of the next tile to be copied
+    const bool is_v = lane >= 16;  // copies a scale row of V, not of K
+    constexpr int CH = D / 32, ROWS = 32 / CH;  // 16-byte chunks of a row; rows copied at once
+    const int crow = lane / CH, cch = lane % CH;
+    const unsigned char* const k_lane = p.k4.codes + q.g * p.k4.ch + 16 * cch;
+    const unsigned char* const v_lane = p.v4.codes + q.g * p.v4.ch + 16 * cch;
+    const uint16_t* const s_lane = is_v ? p.v4.scales + q.g * p.v4.sh : p.k4.scales + q.g * p.k4.sh;
+    const int64_t s_page = is_v ? p.v4.sb : p.k4.sb, s_tok = is_v ? p.v4.st : p.k4.st;
+    const unsigned s_to = ring + 2 * C::CODES + (is_v ? C::SCALES : 0) + lrow * 2 * NG;
+    int kn = q.b, vn = q.b;  // page ids of the next tile to be copied
     auto lookup = [&](int u) {
       if (!p.paged || u >= q.u1) return;
       const int lp = (q.it.tl.tile(u) * kTcTile + 16 * warp + lrow) >> p.page_shift;
       kn = lp < p.k4.max_pages ? __ldg(p.k4.block_table + (int64_t)q.b * p.k4.max_pages + lp) : -1;
       vn = lp < p.v4.max_pages ? __ldg(p.v4.block_table + (int64_t)q.b * p.v4.max_pages + lp) : -1;
     };
+    const int in_page = p.paged ? p.page_size - 1 : -1;
     auto issue = [&](int u) {
       if (u < q.u1) {
         const int st = (u - q.u0) % S;
         const unsigned to = ring + st * C::STAGE;
-        const int j0 = q.it.tl.tile(u) * kTcTile + 16 * warp, j = j0 + lrow;
-        bool live = j < sr.s_end || (j >= sr.lo && j < sr.hi);
-        int kp = q.b, vp = q.b;
-        if (p.paged) {
-          kp = kn;
-          vp = vn;
-          const bool ok = kp >= 0 && kp < p.k4.num_pages && vp >= 0 && vp < p.v4.num_pages;
+        const int j0 = q.it.tl.tile(u) * kTcTile + 16 * warp;
+        const int kp = kn, vp = vn;
+        const bool ok = !p.paged || ((unsigned)kp < (unsigned)p.k4.num_pages && (unsigned)vp < (unsigned)p.v4.num_pages);
+        const bool whole = (j0 >= sr.lo && j0 + 16 <= sr.hi) || j0 + 16 <= sr.s_end;
+        if (whole && __all_sync(0xffffffffu, ok) && (!p.paged || p.page_size >= 16)) {
+          if (lane == 0) masks[st] = 0xffff;
+          const int64_t jc = (j0 & in_page) + crow;
+          const unsigned char* ks = k_lane + kp * p.k4.cb + jc * p.k4.ct;
+          const unsigned char* vs = v_lane + vp * p.v4.cb + jc * p.v4.ct;
+#pragma unroll
+          for (int i = 0; i < 16; i += ROWS) {
+            cp_async16(to + code_at<D>(crow + i, cch), ks + i * p.k4.ct);
+            cp_async16(to + C::CODES + code_at<D>(crow + i, cch), vs + i * p.v4.ct);
+          }
+          cp_async_or_zero<2 * NG>(s_to + st * C::STAGE,
+                                   s_lane + (is_v ? vp : kp) * s_page + ((j0 & in_page) + lrow) * s_tok, true);
+        } else {
+          const int j = j0 + lrow;
+          bool live = j < sr.s_end || (j >= sr.lo && j < sr.hi);
           if (live && !ok) err |= ERR_PAGE;
           live = live && ok;
+          const unsigned mask = __ballot_sync(0xffffffffu, live) & 0xffffu;
+          if (lane == 0) masks[st] = (int)mask;
+#pragma unroll 1
+          for (int i = 0; i < 16; i += ROWS) {
+            const int row = crow + i;
+            const int kr = __shfl_sync(0xffffffffu, kp, row), vr = __shfl_sync(0xffffffffu, vp, row);
+            const bool copy = (mask >> row) & 1u;
+            const int64_t at = (j0 + row) & in_page;
+            cp_async_or_zero<16>(to + code_at<D>(row, cch), k_lane + (copy ? kr * p.k4.cb + at * p.k4.ct : 0), copy);
+            cp_async_or_zero<16>(to + C::CODES + code_at<D>(row, cch), v_lane + (copy ? vr * p.v4.cb + at * p.v4.ct : 0), copy);
+          }
+          cp_async_or_zero<2 * NG>(s_to + st * C::STAGE,
+                                   s_lane + (live ? (is_v ? vp : kp) * s_page + (int64_t)(j & in_page) * s_tok : 0), live);
         }
-        const unsigned mask = __ballot_sync(0xffffffffu, live) & 0xffffu;
-        if (lane == 0) masks[st] = (int)mask;
-        const int in_page = p.paged ? p.page_size - 1 : -1;
-        constexpr int CH = D / 32, PER = 16 * CH / 32;  // 16-byte chunks of a row; rows this lane copies of K, of V
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-          const int row = lane / CH + i * (32 / CH), ch = lane % CH;
-          const int kr = __shfl_sync(0xffffffffu, kp, row), vr = __shfl_sync(0xffffffffu, vp, row);
-          const bool copy = (mask >> row) & 1u;
-          const int64_t at = (j0 + row) & in_page;
-          cp_async_or_zero<16>(to + code_at<D>(row, ch),
-                               p.k4.codes + (copy ? kr * p.k4.cb + q.g * p.k4.ch + at * p.k4.ct + 16 * ch : 0), copy);
-          cp_async_or_zero<16>(to + C::CODES + code_at<D>(row, ch),
-                               p.v4.codes + (copy ? vr * p.v4.cb + q.g * p.v4.ch + at * p.v4.ct + 16 * ch : 0), copy);
-        }
-        const bool is_v = lane >= 16;
-        const Kv4View& x = is_v ? p.v4 : p.k4;
-        cp_async_or_zero<2 * NG>(to + 2 * C::CODES + (is_v ? C::SCALES : 0) + lrow * 2 * NG,
-                                 x.scales + (live ? (is_v ? vp : kp) * x.sb + q.g * x.sh + (int64_t)(j & in_page) * x.st : 0),
-                                 live);
         lookup(u + 1);
       }
       cp_async_commit();
@@ -202,7 +236,7 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
 
     // ---- queries: 8 dimensions of each group a lane, in the order of the codes
     uint32_t qf[NT][TERMS][NG][4];
-    float init[NT][NG][2], fac[NT][2];
+    float fac[NT][2];
     int tq[NT][2];
     const int base = q.sq.len - q.sq.n;
 #pragma unroll
@@ -237,30 +271,17 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
       const float up = __uint_as_float((unsigned)field << 23), down = __uint_as_float((unsigned)(254 - field) << 23);
 #pragma unroll
       for (int g = 0; g < NG; ++g) {
-        float sum = 0.f;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {  // dimensions k and k + 4 meet one mask
-          const float f = (k & 1) ? up * 0.0625f : up;
-          const float a = x[g][k] * f, b = x[g][k + 4] * f;
-          const uint32_t hi = pack_f16(a, b);
-          const float2 h = unpack_f16(hi);
-          qf[t][0][g][k] = hi;
-          float part = h.x + h.y;
+          const float a = x[g][k] * up, b = x[g][k + 4] * up;
+          qf[t][0][g][k] = pack_f16(a, b);
           if constexpr (TERMS == 2) {
-            const uint32_t lo = pack_f16(a - h.x, b - h.y);
-            const float2 l = unpack_f16(lo);
-            qf[t][TERMS - 1][g][k] = lo;
-            part += l.x + l.y;
+            const float2 h = unpack_f16(qf[t][0][g][k]);
+            qf[t][TERMS - 1][g][k] = pack_f16(a - h.x, b - h.y);
           }
-          sum += (k & 1) ? part * 16.f : part;
         }
-        sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-        sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-        sum *= -8.f * 5.9604644775390625e-08f;
-        init[t][g][0] = __shfl_sync(0xffffffffu, sum, 8 * c);
-        init[t][g][1] = __shfl_sync(0xffffffffu, sum, 8 * c + 4);
       }
-      const float f = down * 16777216.f * p.c_log2;
+      const float f = down * p.c_log2;
       fac[t][0] = __shfl_sync(0xffffffffu, f, 8 * c);
       fac[t][1] = __shfl_sync(0xffffffffu, f, 8 * c + 4);
 #pragma unroll
@@ -268,11 +289,9 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
     }
     const int t0 = base + row_token(p, q.it.row0), t1 = base + row_token(p, q.it.row0 + rows - 1);
 
-    float o[NT][NG][2][4], corr[NT][4], ref[NT][2], l[NT][2];
+    float o[NT][NG][2][4], ref[NT][2], l[NT][2];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-#pragma unroll
-      for (int k = 0; k < 4; ++k) corr[t][k] = 0.f;
       ref[t][0] = ref[t][1] = -CUDART_INF_F;
       l[t][0] = l[t][1] = 0.f;
 #pragma unroll
@@ -314,24 +333,24 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
       }
       float z[NT][4];
 #pragma unroll
-      for (int t = 0; t < NT; ++t) z[t][0] = z[t][1] = z[t][2] = z[t][3] = 0.f;
-#pragma unroll
       for (int g = 0; g < NG; ++g) {
-        const uint32_t a0 = k0[g] & 0x000f000fu, a1 = k1[g] & 0x000f000fu, a2 = k0[g] & 0x00f000f0u, a3 = k1[g] & 0x00f000f0u;
         const uint32_t x0 = k0[g] >> 8, x1 = k1[g] >> 8;
-        const uint32_t b0 = x0 & 0x000f000fu, b1 = x1 & 0x000f000fu, b2 = x0 & 0x00f000f0u, b3 = x1 & 0x00f000f0u;
+        const uint32_t a0 = less8(k0[g]), a1 = less8(k1[g]), a2 = less8_high(k0[g]), a3 = less8_high(k1[g]);
+        const uint32_t b0 = less8(x0), b1 = less8(x1), b2 = less8_high(x0), b3 = less8_high(x1);
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-          float s[4] = {init[t][g][0], init[t][g][1], init[t][g][0], init[t][g][1]};
-#pragma unroll
-          for (int m = 0; m < TERMS; ++m) {
-            mma_f16(s, a0, a1, a2, a3, qf[t][m][g][0], qf[t][m][g][1]);
-            mma_f16(s, b0, b1, b2, b3, qf[t][m][g][2], qf[t][m][g][3]);
+          float s[4];
+          mma_f16_first(s, a0, a1, a2, a3, qf[t][0][g][0], qf[t][0][g][1]);
+          mma_f16(s, b0, b1, b2, b3, qf[t][0][g][2], qf[t][0][g][3]);
+          if constexpr (TERMS == 2) {
+            mma_f16(s, a0, a1, a2, a3, qf[t][TERMS - 1][g][0], qf[t][TERMS - 1][g][1]);
+            mma_f16(s, b0, b1, b2, b3, qf[t][TERMS - 1][g][2], qf[t][TERMS - 1][g][3]);
           }
-          z[t][0] = fmaf(s[0], ks0[g], z[t][0]);
-          z[t][1] = fmaf(s[1], ks0[g], z[t][1]);
-          z[t][2] = fmaf(s[2], ks1[g], z[t][2]);
-          z[t][3] = fmaf(s[3], ks1[g], z[t][3]);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const float step = k < 2 ? ks0[g] : ks1[g];
+            z[t][k] = g == 0 ? s[k] * step : fmaf(s[k], step, z[t][k]);
+          }
         }
       }
 #pragma unroll
@@ -399,7 +418,6 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
             ref[t][k] = next;
             l[t][k] *= f;
             const float fo = TERMS == 1 ? f : f * fv;
-            corr[t][k] *= fo;
 #pragma unroll
             for (int g = 0; g < NG; ++g)
 #pragma unroll
@@ -435,37 +453,35 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
         ldsm_x4_t(at + C::CODES + code_at<D>(mrow, g + mch), v0[g], v1[g], v0[g + 1], v1[g + 1]);
 #pragma unroll
       for (int g = 0; g < NG; ++g) {
-        const uint32_t a0 = v0[g] & 0x000f000fu, a1 = v0[g] & 0x00f000f0u, a2 = v1[g] & 0x000f000fu, a3 = v1[g] & 0x00f000f0u;
         const uint32_t x0 = v0[g] >> 8, x1 = v1[g] >> 8;
-        const uint32_t b0 = x0 & 0x000f000fu, b1 = x0 & 0x00f000f0u, b2 = x1 & 0x000f000fu, b3 = x1 & 0x00f000f0u;
-        const uint32_t e = r == g ? off8 : 0u;
+        const uint32_t a0 = less8(v0[g]), a1 = less8_high(v0[g]), a2 = less8(v1[g]), a3 = less8_high(v1[g]);
+        const uint32_t b0 = less8(x0), b1 = less8_high(x0), b2 = less8(x1), b3 = less8_high(x1);
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-          uint32_t w[TERMS][2];
           if constexpr (TERMS == 1) {
-            w[0][0] = mul_f16(ph[t][0], s0[g]);
-            w[0][1] = mul_f16(ph[t][1], s1[g]);
+            const uint32_t w0 = mul_f16(ph[t][0], s0[g]), w1 = mul_f16(ph[t][1], s1[g]);
+            mma_f16(o[t][g][0], a0, a1, a2, a3, w0, w1);
+            mma_f16(o[t][g][1], b0, b1, b2, b3, w0, w1);
           } else {
+            uint32_t hi[2], lo[2];
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
               const float2 x = unpack_f16(ph[t][k]), y = unpack_f16(pl[t][k]), s = unpack_f16(k ? s1[g] : s0[g]);
               const float a = (x.x + y.x) * (s.x * v_unit), b = (x.y + y.y) * (s.y * v_unit);
-              w[0][k] = pack_f16(a, b);
-              const float2 hi = unpack_f16(w[0][k]);
-              w[TERMS - 1][k] = pack_f16(a - hi.x, b - hi.y);
+              hi[k] = pack_f16(a, b);
+              const float2 h = unpack_f16(hi[k]);
+              lo[k] = pack_f16(a - h.x, b - h.y);
             }
-          }
-#pragma unroll
-          for (int m = 0; m < TERMS; ++m) {
-            mma_f16(o[t][g][0], a0, a1, a2, a3, w[m][0], w[m][1]);
-            mma_f16(o[t][g][1], b0, b1, b2, b3, w[m][0], w[m][1]);
-            mma_f16(corr[t], e, 0u, e, 0u, w[m][0], w[m][1]);
+            mma_f16(o[t][g][0], a0, a1, a2, a3, hi[0], hi[1]);
+            mma_f16(o[t][g][1], b0, b1, b2, b3, hi[0], hi[1]);
+            mma_f16(o[t][g][0], a0, a1, a2, a3, lo[0], lo[1]);
+            mma_f16(o[t][g][1], b0, b1, b2, b3, lo[0], lo[1]);
           }
         }
       }
     }
     cp_async_wait<0>();
-    const float o_unit = TERMS == 1 || !large ? 16777216.f : 16777216.f * 32768.f;
+    const float o_unit = TERMS == 2 && large ? 32768.f : 1.f;
 
     // ---- the warps' outputs, joined by the CTA into rows of out or a record
 #pragma unroll
@@ -477,9 +493,7 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
         if (r == 0) ml_all[warp * RS + row] = make_float2(ref[t][k], sum);
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
-          const float off = __shfl_sync(0xffffffffu, corr[t][k], 4 * g + c);
-          const float4 x = make_float4(o[t][g][0][k] + off, fmaf(o[t][g][0][2 + k], 0.0625f, off),
-                                       o[t][g][1][k] + off, fmaf(o[t][g][1][2 + k], 0.0625f, off));
+          const float4 x = make_float4(o[t][g][0][k], o[t][g][0][2 + k], o[t][g][1][k], o[t][g][1][2 + k]);
           *reinterpret_cast<float4*>(o_all + (warp * RS + row) * D + 32 * g + 4 * r) =
               make_float4(x.x * o_unit, x.y * o_unit, x.z * o_unit, x.w * o_unit);
         }
