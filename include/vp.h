@@ -514,7 +514,8 @@ vp_status vp_reserve4(vp_ctx* ctx, int32_t max_new);
  * vp_attend_new over caches held in 4 bits: the arguments mean what they mean
  * there, without accumulated weights.  Scales need not be vp_append4's: any finite
  * fp16 number is served, and a group whose scale is not finite is as a cache row
- * that is not.  Logits are exact products of queries and codes, scaled and summed
+ * that is not.  Token and page strides must be below 2^31, else
+ * VP_ERR_UNSUPPORTED.  Logits are products of queries and codes, scaled and summed
  * in float.  bf16 contexts: the probabilities, and their products with the values'
  * scales, are rounded to fp16 (2^-11 of each; the output's own rounding is 2^-8);
  * fp32 contexts: both are two fp16 terms.  VP_ERR_CAPACITY when vp_reserve4 has not

@@ -100,17 +100,29 @@ __device__ __forceinline__ uint32_t mul_f16(uint32_t a, uint32_t b) {
   const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
   return *reinterpret_cast<const uint32_t*>(&r);
 }
-// The whole numbers code - 8 of the codes in bits 0-3 and 16-19, and of those in bits 4-7 and 20-23.
-__device__ __forceinline__ uint32_t less8(uint32_t x) {
-  const uint32_t y = (x & 0x000f000fu) | 0x64006400u;  // 1024 + code
-  const __half2 r = __hsub2(*reinterpret_cast<const __half2*>(&y), __float2half2_rn(1032.f));
-  return *reinterpret_cast<const uint32_t*>(&r);
-}
-__device__ __forceinline__ uint32_t less8_high(uint32_t x) {
-  const uint32_t y = (x & 0x00f000f0u) | 0x64006400u;  // 1024 + 16 code
-  const __half2 r = __hfma2(*reinterpret_cast<const __half2*>(&y), __float2half2_rn(0.0625f), __float2half2_rn(-72.f));
-  return *reinterpret_cast<const uint32_t*>(&r);
-}
+// The whole numbers code - 8 of the codes in bits 0-3 and 16-19 (low), and of
+// those in bits 4-7 and 20-23 (high).  The constants are kept in registers: a mask
+// and the exponent are one operation then.
+struct Codes {
+  uint32_t mask, mask_high, k1024, k1032, sixteenth, k72;
+  __device__ __forceinline__ Codes() {
+    asm volatile("mov.b32 %0, 0x000f000f;\n mov.b32 %1, 0x00f000f0;\n mov.b32 %2, 0x64006400;\n"
+                 "mov.b32 %3, 0xe408e408;\n mov.b32 %4, 0x2c002c00;\n mov.b32 %5, 0xd480d480;\n"
+                 : "=r"(mask), "=r"(mask_high), "=r"(k1024), "=r"(k1032), "=r"(sixteenth), "=r"(k72));
+  }
+  __device__ __forceinline__ uint32_t low(uint32_t x) const {
+    uint32_t r;
+    asm("{\n .reg .b32 y;\n lop3.b32 y, %1, %2, %3, 0xea;\n add.f16x2 %0, y, %4;\n}\n"  // 1024 + code
+        : "=r"(r) : "r"(x), "r"(mask), "r"(k1024), "r"(k1032));
+    return r;
+  }
+  __device__ __forceinline__ uint32_t high(uint32_t x) const {
+    uint32_t r;
+    asm("{\n .reg .b32 y;\n lop3.b32 y, %1, %2, %3, 0xea;\n fma.rn.f16x2 %0, y, %4, %5;\n}\n"  // 1024 + 16 code
+        : "=r"(r) : "r"(x), "r"(mask_high), "r"(k1024), "r"(sixteenth), "r"(k72));
+    return r;
+  }
+};
 // A copy of N bytes, or N zeros.
 template <int N>
 __device__ __forceinline__ void cp_async_or_zero(unsigned dst, const void* src, bool copy) {
@@ -146,6 +158,7 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
   Walk walk = line_start<kThreads4>(p, misc);
   Part q;
   unsigned err = 0;
+  const Codes codes;
 
   // Addresses of this lane's matrix rows within a stage (ldmatrix: lane l gives
   // row l % 8 of matrix l / 8; matrices: tokens 0-7 and 8-15 of one group, then
@@ -174,12 +187,19 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
     const bool is_v = lane >= 16;  // copies a scale row of V, not of K
     constexpr int CH = D / 32, ROWS = 32 / CH;  // 16-byte chunks of a row; rows copied at once
     const int crow = lane / CH, cch = lane % CH;
-    const unsigned char* const k_lane = p.k4.codes + q.g * p.k4.ch + 16 * cch;
-    const unsigned char* const v_lane = p.v4.codes + q.g * p.v4.ch + 16 * cch;
-    const uint16_t* const s_lane = is_v ? p.v4.scales + q.g * p.v4.sh : p.k4.scales + q.g * p.k4.sh;
-    const int64_t s_page = is_v ? p.v4.sb : p.k4.sb, s_tok = is_v ? p.v4.st : p.k4.st;
+    const unsigned char* k_lane = p.k4.codes + q.g * p.k4.ch + 16 * cch;
+    const unsigned char* v_lane = p.v4.codes + q.g * p.v4.ch + 16 * cch;
+    const uint16_t* s_lane = is_v ? p.v4.scales + q.g * p.v4.sh : p.k4.scales + q.g * p.k4.sh;
+    if (!p.paged) {
+      k_lane += q.b * p.k4.cb;
+      v_lane += q.b * p.v4.cb;
+      s_lane += q.b * (is_v ? p.v4.sb : p.k4.sb);
+    }
+    // Token and page strides are below 2^31 (vp_attend4 checks them).
+    const int kt = (int)p.k4.ct, vt = (int)p.v4.ct, s_tok = (int)(is_v ? p.v4.st : p.k4.st);
+    const int kpage = (int)p.k4.cb, vpage = (int)p.v4.cb, s_page = (int)(is_v ? p.v4.sb : p.k4.sb);
     const unsigned s_to = ring + 2 * C::CODES + (is_v ? C::SCALES : 0) + lrow * 2 * NG;
-    int kn = q.b, vn = q.b;  // page ids of the next tile to be copied
+    int kn = 0, vn = 0;  // page ids of the next tile to be copied
     auto lookup = [&](int u) {
       if (!p.paged || u >= q.u1) return;
       const int lp = (q.it.tl.tile(u) * kTcTile + 16 * warp + lrow) >> p.page_shift;
@@ -187,26 +207,33 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
       vn = lp < p.v4.max_pages ? __ldg(p.v4.block_table + (int64_t)q.b * p.v4.max_pages + lp) : -1;
     };
     const int in_page = p.paged ? p.page_size - 1 : -1;
+    unsigned partly = 0;  // bit of a stage: masks has which of its tokens were copied; else all of them
     auto issue = [&](int u) {
       if (u < q.u1) {
-        const int st = (u - q.u0) % S;
+        const int st = (unsigned)(u - q.u0) % S;
         const unsigned to = ring + st * C::STAGE;
         const int j0 = q.it.tl.tile(u) * kTcTile + 16 * warp;
-        const int kp = kn, vp = vn;
-        const bool ok = !p.paged || ((unsigned)kp < (unsigned)p.k4.num_pages && (unsigned)vp < (unsigned)p.v4.num_pages);
-        const bool whole = (j0 >= sr.lo && j0 + 16 <= sr.hi) || j0 + 16 <= sr.s_end;
-        if (whole && __all_sync(0xffffffffu, ok) && (!p.paged || p.page_size >= 16)) {
-          if (lane == 0) masks[st] = 0xffff;
-          const int64_t jc = (j0 & in_page) + crow;
-          const unsigned char* ks = k_lane + kp * p.k4.cb + jc * p.k4.ct;
-          const unsigned char* vs = v_lane + vp * p.v4.cb + jc * p.v4.ct;
+        bool ok = true;
+        const unsigned char *kc = k_lane, *vc = v_lane;
+        const uint16_t* sc = s_lane;
+        if (p.paged) {
+          ok = (unsigned)kn < (unsigned)p.k4.num_pages && (unsigned)vn < (unsigned)p.v4.num_pages;
+          kc += (int64_t)kn * kpage;
+          vc += (int64_t)vn * vpage;
+          sc += (int64_t)(is_v ? vn : kn) * s_page;
+        }
+        const int jp = j0 & in_page;
+        const bool whole = ((j0 >= sr.lo && j0 + 16 <= sr.hi) || j0 + 16 <= sr.s_end) && (!p.paged || p.page_size >= 16);
+        if (whole && __all_sync(0xffffffffu, ok)) {
+          partly &= ~(1u << st);
+          kc += (int64_t)(jp + crow) * kt;
+          vc += (int64_t)(jp + crow) * vt;
 #pragma unroll
           for (int i = 0; i < 16; i += ROWS) {
-            cp_async16(to + code_at<D>(crow + i, cch), ks + i * p.k4.ct);
-            cp_async16(to + C::CODES + code_at<D>(crow + i, cch), vs + i * p.v4.ct);
+            cp_async16(to + code_at<D>(crow + i, cch), kc + (int64_t)i * kt);
+            cp_async16(to + C::CODES + code_at<D>(crow + i, cch), vc + (int64_t)i * vt);
           }
-          cp_async_or_zero<2 * NG>(s_to + st * C::STAGE,
-                                   s_lane + (is_v ? vp : kp) * s_page + ((j0 & in_page) + lrow) * s_tok, true);
+          cp_async_or_zero<2 * NG>(s_to + st * C::STAGE, sc + (int64_t)(jp + lrow) * s_tok, true);
         } else {
           const int j = j0 + lrow;
           bool live = j < sr.s_end || (j >= sr.lo && j < sr.hi);
@@ -214,17 +241,17 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
           live = live && ok;
           const unsigned mask = __ballot_sync(0xffffffffu, live) & 0xffffu;
           if (lane == 0) masks[st] = (int)mask;
+          partly |= 1u << st;
 #pragma unroll 1
           for (int i = 0; i < 16; i += ROWS) {
             const int row = crow + i;
-            const int kr = __shfl_sync(0xffffffffu, kp, row), vr = __shfl_sync(0xffffffffu, vp, row);
+            const int kr = __shfl_sync(0xffffffffu, kn, row), vr = __shfl_sync(0xffffffffu, vn, row);
             const bool copy = (mask >> row) & 1u;
             const int64_t at = (j0 + row) & in_page;
-            cp_async_or_zero<16>(to + code_at<D>(row, cch), k_lane + (copy ? kr * p.k4.cb + at * p.k4.ct : 0), copy);
-            cp_async_or_zero<16>(to + C::CODES + code_at<D>(row, cch), v_lane + (copy ? vr * p.v4.cb + at * p.v4.ct : 0), copy);
+            cp_async_or_zero<16>(to + code_at<D>(row, cch), k_lane + (copy ? (int64_t)kr * kpage + at * kt : 0), copy);
+            cp_async_or_zero<16>(to + C::CODES + code_at<D>(row, cch), v_lane + (copy ? (int64_t)vr * vpage + at * vt : 0), copy);
           }
-          cp_async_or_zero<2 * NG>(s_to + st * C::STAGE,
-                                   s_lane + (live ? (is_v ? vp : kp) * s_page + (int64_t)(j & in_page) * s_tok : 0), live);
+          cp_async_or_zero<2 * NG>(s_to + st * C::STAGE, live ? sc + (int64_t)(j & in_page) * s_tok : s_lane, live);
         }
         lookup(u + 1);
       }
@@ -309,10 +336,10 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
       cp_async_wait<S - 2>();
       __syncwarp();
       issue(u + S - 1);  // into the stage that the last turn read
-      const int st = (u - q.u0) % S;
+      const int st = (unsigned)(u - q.u0) % S;
       const unsigned at = ring + st * C::STAGE;
       const unsigned char* sp = smem + (warp * S + st) * C::STAGE;
-      const unsigned mask = (unsigned)masks[st];
+      const unsigned mask = (partly >> st) & 1u ? (unsigned)masks[st] : 0xffffu;
       const int j0 = q.it.tl.tile(u) * kTcTile + 16 * warp;
 
       // ---- logits: tokens r and r + 8, query rows 2c and 2c + 1
@@ -335,8 +362,8 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
 #pragma unroll
       for (int g = 0; g < NG; ++g) {
         const uint32_t x0 = k0[g] >> 8, x1 = k1[g] >> 8;
-        const uint32_t a0 = less8(k0[g]), a1 = less8(k1[g]), a2 = less8_high(k0[g]), a3 = less8_high(k1[g]);
-        const uint32_t b0 = less8(x0), b1 = less8(x1), b2 = less8_high(x0), b3 = less8_high(x1);
+        const uint32_t a0 = codes.low(k0[g]), a1 = codes.low(k1[g]), a2 = codes.high(k0[g]), a3 = codes.high(k1[g]);
+        const uint32_t b0 = codes.low(x0), b1 = codes.low(x1), b2 = codes.high(x0), b3 = codes.high(x1);
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
           float s[4];
@@ -454,8 +481,8 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
 #pragma unroll
       for (int g = 0; g < NG; ++g) {
         const uint32_t x0 = v0[g] >> 8, x1 = v1[g] >> 8;
-        const uint32_t a0 = less8(v0[g]), a1 = less8_high(v0[g]), a2 = less8(v1[g]), a3 = less8_high(v1[g]);
-        const uint32_t b0 = less8(x0), b1 = less8_high(x0), b2 = less8(x1), b3 = less8_high(x1);
+        const uint32_t a0 = codes.low(v0[g]), a1 = codes.high(v0[g]), a2 = codes.low(v1[g]), a3 = codes.high(v1[g]);
+        const uint32_t b0 = codes.low(x0), b1 = codes.high(x0), b2 = codes.low(x1), b3 = codes.high(x1);
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
           if constexpr (TERMS == 1) {

@@ -202,6 +202,9 @@ vp_status attend4(vp_ctx* ctx, int32_t batch, int32_t n_new, const vp_rows* q, c
       !apart_ok(*out, batch, n_new, c.num_q_heads, "out", &why) || !kv4_ok(ctx, k_cache, "k_cache", &why) ||
       !kv4_ok(ctx, v_cache, "v_cache", &why))
     return fail(ctx, VP_ERR_INVALID_ARG, "vp_attend4: " + why);
+  for (const vp_kv4* kv : {k_cache, v_cache})
+    for (int64_t s : {kv->code_stride_t, kv->scale_stride_t, c.paged ? kv->code_stride_b : 0, c.paged ? kv->scale_stride_b : 0})
+      if (s > INT32_MAX) return fail(ctx, VP_ERR_UNSUPPORTED, "vp_attend4: token and page strides must be below 2^31");
 
   vp::Attend4Params p = {};
   const int H = c.num_q_heads, Hkv = c.num_kv_heads, G = H / Hkv;

@@ -350,6 +350,8 @@ def test_refusals(vp):
     assert status(visible=vp.make_visible(scale=-1.0)) == bad and status(visible=vp.make_visible(scale=float("inf"))) == bad
     assert status(out=but(good["out"], stride_n=0)) == bad
     assert status(k_cache=but(a.kc, code_stride_h=8)) == bad and status(v_cache=but(a.vc, max_pages=0)) == bad
+    assert status(k_cache=but(a.kc, code_stride_t=1 << 31)) == vp.VP_ERR_UNSUPPORTED
+    assert status(v_cache=but(a.vc, scale_stride_b=1 << 31)) == vp.VP_ERR_UNSUPPORTED
     assert torch.isnan(a.out).all()
     other = vp.vp_init(vp.make_config(1, 8, 2, 64, 0, 64))
     with pytest.raises(vp.VPError) as e:
