@@ -17,7 +17,7 @@ namespace {
 
 // ---------------------------------------------------------------------------
 // k_att4<T, D, NT>: up to 8 NT query rows of a (sequence, kv-head).  A warp takes
-// 16 of the 128 tokens of a tile, with softmax statistics and an output of its
+// 32 of the 128 tokens of a tile, with softmax statistics and an output of its
 // own; the warps' are joined at the end of a CTA's part of an item.
 //
 // Codes are not turned into values one by one, but into the whole numbers code - 8
@@ -48,26 +48,33 @@ namespace {
 // Tokens that no row sees are not copied: their codes are whatever the ring held
 // before, their scales 0 and their logits masked.
 // ---------------------------------------------------------------------------
-constexpr int kWarps4 = 8, kThreads4 = 32 * kWarps4;
 constexpr float kAbove4 = 10.f, kBig4 = 15.f, kRaise4 = 4.f;
+constexpr int kWarps4 = 4, kThreads4 = 32 * kWarps4;
+constexpr int kStep4 = kTcTile / kWarps4;  // tokens of a warp's turn: a row's lane looks up its page
 
 template <typename T, int D, int NT>
 struct Cfg4 {
   static constexpr int TERMS = std::is_same<T, float>::value ? 2 : 1;
   static constexpr int GROUPS = D / kGroup4;
-  static constexpr int CPS = NT * TERMS == 1 ? 2 : 1;   // CTAs per SM
+  static constexpr int CPS = NT * TERMS == 1 ? 3 : 2;   // CTAs per SM
   static constexpr int RS = 8 * NT;                     // query rows of an item
-  static constexpr int CODES = 16 * D / 2;              // a stage: codes of 16 tokens, then their scales, of K and of V
-  static constexpr int SCALES = 16 * GROUPS * 2;
+  static constexpr int CODES = kStep4 * D / 2;          // a stage: codes of a turn's tokens, then their scales, of K and of V
+  static constexpr int SCALES = kStep4 * GROUPS * 2;
   static constexpr int STAGE = 2 * (CODES + SCALES);
-  static constexpr int S = 4;                           // stages of a warp's ring
-  static constexpr int OFF_O = kWarps4 * S * STAGE;     // float [warps][RS][D]: outputs to be joined
-  static constexpr int OFF_ML = OFF_O + kWarps4 * RS * D * 4;  // float2 [warps][RS]
-  static constexpr int OFF_MASK = OFF_ML + kWarps4 * RS * 8;   // int [warps][S]: tokens copied
+  static constexpr int S = CPS == 3 ? 3 : 4;            // stages of a warp's ring
+  // A warp's ring, and behind it its output to be joined, float [RS][D] (in the ring where there is no room).
+  static constexpr int RING = S * STAGE;
+  static constexpr int OUT = RS * D * 4;
+  static constexpr bool APART = kWarps4 * (RING + OUT) <= 232448 / CPS - 3072;
+  static constexpr int WARP = APART ? RING + OUT : RING > OUT ? RING : OUT;
+  static constexpr int OFF_O = APART ? RING : 0;
+  static constexpr int OFF_ML = kWarps4 * WARP;                // float2 [warps][RS]
+  static constexpr int OFF_MASK = OFF_ML + kWarps4 * RS * 8;   // unsigned [warps][S]: tokens copied
   static constexpr int OFF_MISC = OFF_MASK + kWarps4 * S * 4;  // int: line_start, a flag
   static constexpr int LINE = kWarps4 + 7;
   static constexpr size_t SMEM = OFF_MISC + (LINE + 1) * 4;
   static_assert(SMEM <= 232448 / CPS - (CPS > 1 ? 1024 : 0), "shared memory of the CTAs of an SM");
+  static_assert(STAGE % 128 == 0 && WARP % 128 == 0, "rows keep their banks");
 };
 
 __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
@@ -145,14 +152,14 @@ template <typename T, int D, int NT>
 __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const __grid_constant__ Attend4Params p) {
   using C = Cfg4<T, D, NT>;
   constexpr int S = C::S, NG = C::GROUPS, TERMS = C::TERMS, RS = C::RS;
-  extern __shared__ __align__(16) unsigned char smem[];
+  extern __shared__ __align__(128) unsigned char smem[];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int r = lane >> 2, c = lane & 3;
-  float* o_all = reinterpret_cast<float*>(smem + C::OFF_O);
   float2* ml_all = reinterpret_cast<float2*>(smem + C::OFF_ML);
-  int* masks = reinterpret_cast<int*>(smem + C::OFF_MASK) + warp * S;
+  unsigned* masks = reinterpret_cast<unsigned*>(smem + C::OFF_MASK) + warp * S;
   int* misc = reinterpret_cast<int*>(smem + C::OFF_MISC);
-  const unsigned ring = smem_u32(smem) + warp * S * C::STAGE;
+  unsigned char* const mine = smem + warp * C::WARP;
+  const unsigned ring = smem_u32(mine);
   pdl_wait();
   pdl_trigger();
   Walk walk = line_start<kThreads4>(p, misc);
@@ -164,6 +171,14 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
   // row l % 8 of matrix l / 8; matrices: tokens 0-7 and 8-15 of one group, then
   // of the next).
   const int mrow = (lane & 7) + ((lane >> 3) & 1) * 8, mch = lane >> 4;
+  // Copies: 16-byte chunks of a row of codes, rows copied at once, this lane's.
+  constexpr int CH = D / 32, ROWS = 32 / CH;
+  const int crow = lane / CH, cch = lane % CH;
+  const unsigned s_to = ring + 2 * C::CODES + lane * 2 * NG;
+  // Token and page strides are below 2^31 (vp_attend4 checks them).
+  const int kt = (int)p.k4.ct, vt = (int)p.v4.ct, kst = (int)p.k4.st, vst = (int)p.v4.st;
+  const int kpage = (int)p.k4.cb, vpage = (int)p.v4.cb, kspage = (int)p.k4.sb, vspage = (int)p.v4.sb;
+  const int in_page = p.paged ? p.page_size - 1 : -1;
 
   while (next_part(p, walk, q)) {
     const int n = q.u1 - q.u0;
@@ -180,85 +195,76 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
     }
     if (n <= 0) continue;
     const SeenRange& sr = q.it.sr;
+    auto first_token = [&](int u) { return q.it.tl.tile(u) * kTcTile + kStep4 * warp; };
 
-    // ---- copies of the warp's 16 tokens of tile u, into stage u % S.  The tokens
-    // lie in one page, or (pages of fewer than 16) a lane looks up token lane % 16's.
-    const int lrow = lane & 15;
-    const bool is_v = lane >= 16;  // copies a scale row of V, not of K
-    constexpr int CH = D / 32, ROWS = 32 / CH;  // 16-byte chunks of a row; rows copied at once
-    const int crow = lane / CH, cch = lane % CH;
+    // ---- copies of the warp's 32 tokens of tile u, into stage u % S
     const unsigned char* k_lane = p.k4.codes + q.g * p.k4.ch + 16 * cch;
     const unsigned char* v_lane = p.v4.codes + q.g * p.v4.ch + 16 * cch;
-    const uint16_t* s_lane = is_v ? p.v4.scales + q.g * p.v4.sh : p.k4.scales + q.g * p.k4.sh;
+    const uint16_t *ks_lane = p.k4.scales + q.g * p.k4.sh, *vs_lane = p.v4.scales + q.g * p.v4.sh;
     if (!p.paged) {
-      k_lane += q.b * p.k4.cb;
-      v_lane += q.b * p.v4.cb;
-      s_lane += q.b * (is_v ? p.v4.sb : p.k4.sb);
+      k_lane += q.b * p.k4.cb + (int64_t)crow * kt;
+      v_lane += q.b * p.v4.cb + (int64_t)crow * vt;
+      ks_lane += q.b * p.k4.sb + (int64_t)lane * kst;
+      vs_lane += q.b * p.v4.sb + (int64_t)lane * vst;
     }
-    // Token and page strides are below 2^31 (vp_attend4 checks them).
-    const int kt = (int)p.k4.ct, vt = (int)p.v4.ct, s_tok = (int)(is_v ? p.v4.st : p.k4.st);
-    const int kpage = (int)p.k4.cb, vpage = (int)p.v4.cb, s_page = (int)(is_v ? p.v4.sb : p.k4.sb);
-    const unsigned s_to = ring + 2 * C::CODES + (is_v ? C::SCALES : 0) + lrow * 2 * NG;
-    int kn = 0, vn = 0;  // page ids of the next tile to be copied
+    int kn = 0, vn = 0;  // page ids of token `lane` of the next turn to be copied
     auto lookup = [&](int u) {
       if (!p.paged || u >= q.u1) return;
-      const int lp = (q.it.tl.tile(u) * kTcTile + 16 * warp + lrow) >> p.page_shift;
+      const int lp = (first_token(u) + lane) >> p.page_shift;
       kn = lp < p.k4.max_pages ? __ldg(p.k4.block_table + (int64_t)q.b * p.k4.max_pages + lp) : -1;
       vn = lp < p.v4.max_pages ? __ldg(p.v4.block_table + (int64_t)q.b * p.v4.max_pages + lp) : -1;
     };
-    const int in_page = p.paged ? p.page_size - 1 : -1;
     unsigned partly = 0;  // bit of a stage: masks has which of its tokens were copied; else all of them
     auto issue = [&](int u) {
       if (u < q.u1) {
         const int st = (unsigned)(u - q.u0) % S;
         const unsigned to = ring + st * C::STAGE;
-        const int j0 = q.it.tl.tile(u) * kTcTile + 16 * warp;
-        bool ok = true;
-        const unsigned char *kc = k_lane, *vc = v_lane;
-        const uint16_t* sc = s_lane;
-        if (p.paged) {
-          ok = (unsigned)kn < (unsigned)p.k4.num_pages && (unsigned)vn < (unsigned)p.v4.num_pages;
-          kc += (int64_t)kn * kpage;
-          vc += (int64_t)vn * vpage;
-          sc += (int64_t)(is_v ? vn : kn) * s_page;
-        }
-        const int jp = j0 & in_page;
-        const bool whole = ((j0 >= sr.lo && j0 + 16 <= sr.hi) || j0 + 16 <= sr.s_end) && (!p.paged || p.page_size >= 16);
-        if (whole && __all_sync(0xffffffffu, ok)) {
+        const int j0 = first_token(u);
+        const bool ok = !p.paged || ((unsigned)kn < (unsigned)p.k4.num_pages && (unsigned)vn < (unsigned)p.v4.num_pages);
+        const bool whole = (j0 >= sr.lo && j0 + kStep4 <= sr.hi) || j0 + kStep4 <= sr.s_end;
+        if (whole && !p.paged) {
           partly &= ~(1u << st);
-          kc += (int64_t)(jp + crow) * kt;
-          vc += (int64_t)(jp + crow) * vt;
+          const unsigned char *kc = k_lane + (int64_t)j0 * kt, *vc = v_lane + (int64_t)j0 * vt;
 #pragma unroll
-          for (int i = 0; i < 16; i += ROWS) {
+          for (int i = 0; i < kStep4; i += ROWS) {
             cp_async16(to + code_at<D>(crow + i, cch), kc + (int64_t)i * kt);
             cp_async16(to + C::CODES + code_at<D>(crow + i, cch), vc + (int64_t)i * vt);
           }
-          cp_async_or_zero<2 * NG>(s_to + st * C::STAGE, sc + (int64_t)(jp + lrow) * s_tok, true);
+          cp_async_or_zero<2 * NG>(s_to + st * C::STAGE, ks_lane + (int64_t)j0 * kst, true);
+          cp_async_or_zero<2 * NG>(s_to + st * C::STAGE + C::SCALES, vs_lane + (int64_t)j0 * vst, true);
         } else {
-          const int j = j0 + lrow;
+          // A row's page is known to its lane.  A token that is not copied leaves
+          // zeros, its scale's among them.
+          const int j = j0 + lane;
           bool live = j < sr.s_end || (j >= sr.lo && j < sr.hi);
           if (live && !ok) err |= ERR_PAGE;
           live = live && ok;
-          const unsigned mask = __ballot_sync(0xffffffffu, live) & 0xffffu;
-          if (lane == 0) masks[st] = (int)mask;
-          partly |= 1u << st;
-#pragma unroll 1
-          for (int i = 0; i < 16; i += ROWS) {
+          const unsigned mask = __ballot_sync(0xffffffffu, live);
+          if (mask == 0xffffffffu) partly &= ~(1u << st);
+          else partly |= 1u << st;
+          if (lane == 0) masks[st] = mask;
+#pragma unroll
+          for (int i = 0; i < kStep4; i += ROWS) {
             const int row = crow + i;
             const int kr = __shfl_sync(0xffffffffu, kn, row), vr = __shfl_sync(0xffffffffu, vn, row);
             const bool copy = (mask >> row) & 1u;
-            const int64_t at = (j0 + row) & in_page;
-            cp_async_or_zero<16>(to + code_at<D>(row, cch), k_lane + (copy ? (int64_t)kr * kpage + at * kt : 0), copy);
-            cp_async_or_zero<16>(to + C::CODES + code_at<D>(row, cch), v_lane + (copy ? (int64_t)vr * vpage + at * vt : 0), copy);
+            const int at = p.paged ? (j0 + row) & in_page : j0 + i;  // contiguous: k_lane has the row
+            cp_async_or_zero<16>(to + code_at<D>(row, cch), copy ? k_lane + (int64_t)kr * kpage + (int64_t)at * kt : p.k4.codes, copy);
+            cp_async_or_zero<16>(to + C::CODES + code_at<D>(row, cch),
+                                 copy ? v_lane + (int64_t)vr * vpage + (int64_t)at * vt : p.v4.codes, copy);
           }
-          cp_async_or_zero<2 * NG>(s_to + st * C::STAGE, live ? sc + (int64_t)(j & in_page) * s_tok : s_lane, live);
+          const int at = p.paged ? j & in_page : j0;
+          cp_async_or_zero<2 * NG>(s_to + st * C::STAGE,
+                                   live ? ks_lane + (int64_t)kn * kspage + (int64_t)at * kst : p.k4.scales, live);
+          cp_async_or_zero<2 * NG>(s_to + st * C::STAGE + C::SCALES,
+                                   live ? vs_lane + (int64_t)vn * vspage + (int64_t)at * vst : p.v4.scales, live);
         }
         lookup(u + 1);
       }
       cp_async_commit();
     };
     lookup(q.u0);
-#pragma unroll
+#pragma unroll 1
     for (int k = 0; k < S - 1; ++k) issue(q.u0 + k);
 
     // ---- queries: 8 dimensions of each group a lane, in the order of the codes
@@ -337,177 +343,180 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
       __syncwarp();
       issue(u + S - 1);  // into the stage that the last turn read
       const int st = (unsigned)(u - q.u0) % S;
-      const unsigned at = ring + st * C::STAGE;
-      const unsigned char* sp = smem + (warp * S + st) * C::STAGE;
-      const unsigned mask = (partly >> st) & 1u ? (unsigned)masks[st] : 0xffffu;
-      const int j0 = q.it.tl.tile(u) * kTcTile + 16 * warp;
-
-      // ---- logits: tokens r and r + 8, query rows 2c and 2c + 1
-      uint32_t k0[NG], k1[NG];
+      const unsigned turn = (partly >> st) & 1u ? masks[st] : 0xffffffffu;
+      const int jt = first_token(u);
+      const bool all_see = turn == 0xffffffffu && jt + kStep4 - 1 <= t0 &&
+                           (p.window < 0 || jt > t1 - p.window || jt + kStep4 <= p.sinks);
 #pragma unroll
-      for (int g = 0; g < NG; g += 2)
-        ldsm_x4(at + code_at<D>(mrow, g + mch), k0[g], k1[g], k0[g + 1], k1[g + 1]);
-      float ks0[NG], ks1[NG];
-      {
-        const unsigned char* ks = sp + 2 * C::CODES;
+      for (int half = 0; half < kStep4; half += 16) {
+        const unsigned at = ring + st * C::STAGE;
+        const unsigned char* const scales = mine + st * C::STAGE + 2 * C::CODES + half * 2 * NG;
+        const int j0 = jt + half;
+        // ---- logits: tokens r and r + 8, query rows 2c and 2c + 1
+        uint32_t k0[NG], k1[NG];
 #pragma unroll
-        for (int g = 0; g < NG; g += 2) {
-          const float2 a = unpack_f16(*reinterpret_cast<const uint32_t*>(ks + r * 2 * NG + 2 * g));
-          const float2 b = unpack_f16(*reinterpret_cast<const uint32_t*>(ks + (r + 8) * 2 * NG + 2 * g));
-          ks0[g] = a.x; ks0[g + 1] = a.y;
-          ks1[g] = b.x; ks1[g + 1] = b.y;
-        }
-      }
-      float z[NT][4];
-#pragma unroll
-      for (int g = 0; g < NG; ++g) {
-        const uint32_t x0 = k0[g] >> 8, x1 = k1[g] >> 8;
-        const uint32_t a0 = codes.low(k0[g]), a1 = codes.low(k1[g]), a2 = codes.high(k0[g]), a3 = codes.high(k1[g]);
-        const uint32_t b0 = codes.low(x0), b1 = codes.low(x1), b2 = codes.high(x0), b3 = codes.high(x1);
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          float s[4];
-          mma_f16_first(s, a0, a1, a2, a3, qf[t][0][g][0], qf[t][0][g][1]);
-          mma_f16(s, b0, b1, b2, b3, qf[t][0][g][2], qf[t][0][g][3]);
-          if constexpr (TERMS == 2) {
-            mma_f16(s, a0, a1, a2, a3, qf[t][TERMS - 1][g][0], qf[t][TERMS - 1][g][1]);
-            mma_f16(s, b0, b1, b2, b3, qf[t][TERMS - 1][g][2], qf[t][TERMS - 1][g][3]);
-          }
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const float step = k < 2 ? ks0[g] : ks1[g];
-            z[t][k] = g == 0 ? s[k] * step : fmaf(s[k], step, z[t][k]);
-          }
-        }
-      }
-#pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        z[t][0] *= fac[t][0]; z[t][1] *= fac[t][1];
-        z[t][2] *= fac[t][0]; z[t][3] *= fac[t][1];
-      }
-      const bool all_see = mask == 0xffffu && j0 + 15 <= t0 && (p.window < 0 || j0 > t1 - p.window || j0 + 16 <= p.sinks);
-      if (!all_see) {
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const int row = r + 8 * (k >> 1);
-            if (!((mask >> row) & 1u) || !sees(j0 + row, tq[t][k & 1], p.window, p.sinks)) z[t][k] = -CUDART_INF_F;
-          }
-      }
-
-      // ---- V's scales: of tokens 2c, 2c + 1 (s0) and 2c + 8, 2c + 9 (s1), a group each
-      uint32_t s0[NG], s1[NG];
-      uint32_t any = 0;
-      {
-        const unsigned char* vs = sp + 2 * C::CODES + C::SCALES;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          uint32_t w[NG];  // two tokens' scales
-          if constexpr (NG == 4) {
-            const uint4 v = *reinterpret_cast<const uint4*>(vs + (2 * c + 8 * h) * 8);
-            w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
-          } else {
-            const uint2 v = *reinterpret_cast<const uint2*>(vs + (2 * c + 8 * h) * 4);
-            w[0] = v.x; w[1] = v.y;
-          }
+        for (int g = 0; g < NG; g += 2)
+          ldsm_x4(at + code_at<D>(half + mrow, g + mch), k0[g], k1[g], k0[g + 1], k1[g + 1]);
+        float ks0[NG], ks1[NG];
+        {
 #pragma unroll
           for (int g = 0; g < NG; g += 2) {
-            const uint32_t x = w[g / 2], y = w[NG / 2 + g / 2];
-            any |= x | y;
-            (h ? s1 : s0)[g] = prmt(x, y, 0x5410);
-            (h ? s1 : s0)[g + 1] = prmt(x, y, 0x7632);
+            const float2 a = unpack_f16(*reinterpret_cast<const uint32_t*>(scales + r * 2 * NG + 2 * g));
+            const float2 b = unpack_f16(*reinterpret_cast<const uint32_t*>(scales + (r + 8) * 2 * NG + 2 * g));
+            ks0[g] = a.x; ks0[g + 1] = a.y;
+            ks1[g] = b.x; ks1[g + 1] = b.y;
           }
         }
-      }
-
-      // ---- the references
-      bool need = false;
+        float z[NT][4];
 #pragma unroll
-      for (int t = 0; t < NT; ++t)
+        for (int g = 0; g < NG; ++g) {
+          const uint32_t x0 = k0[g] >> 8, x1 = k1[g] >> 8;
+          const uint32_t a0 = codes.low(k0[g]), a1 = codes.low(k1[g]), a2 = codes.high(k0[g]), a3 = codes.high(k1[g]);
+          const uint32_t b0 = codes.low(x0), b1 = codes.low(x1), b2 = codes.high(x0), b3 = codes.high(x1);
 #pragma unroll
-        for (int k = 0; k < 2; ++k) need |= fmaxf(z[t][k], z[t][2 + k]) > ref[t][k] + (above + kRaise4);
-      const bool big = (any & 0x40004000u) != 0;  // a scale of 2 or more
-      if (__any_sync(0xffffffffu, need || (big && !large))) {
-        float fv = 1.f;
-        if (!large && __any_sync(0xffffffffu, big)) {
-          large = true;
-          if constexpr (TERMS == 1) above = kAbove4 - kBig4;
-          else fv = v_unit = 3.0517578125e-05f;  // 2^-kBig4
+          for (int t = 0; t < NT; ++t) {
+            float s[4];
+            mma_f16_first(s, a0, a1, a2, a3, qf[t][0][g][0], qf[t][0][g][1]);
+            mma_f16(s, b0, b1, b2, b3, qf[t][0][g][2], qf[t][0][g][3]);
+            if constexpr (TERMS == 2) {
+              mma_f16(s, a0, a1, a2, a3, qf[t][TERMS - 1][g][0], qf[t][TERMS - 1][g][1]);
+              mma_f16(s, b0, b1, b2, b3, qf[t][TERMS - 1][g][2], qf[t][TERMS - 1][g][3]);
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const float step = k < 2 ? ks0[g] : ks1[g];
+              z[t][k] = g == 0 ? s[k] * step : fmaf(s[k], step, z[t][k]);
+            }
+          }
         }
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          z[t][0] *= fac[t][0]; z[t][1] *= fac[t][1];
+          z[t][2] *= fac[t][0]; z[t][3] *= fac[t][1];
+        }
+        if (!all_see) {
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const int row = r + 8 * (k >> 1);
+              if (!((turn >> (half + row)) & 1u) || !sees(j0 + row, tq[t][k & 1], p.window, p.sinks)) z[t][k] = -CUDART_INF_F;
+            }
+        }
+
+        // ---- V's scales: of tokens 2c, 2c + 1 (s0) and 2c + 8, 2c + 9 (s1), a group each
+        uint32_t s0[NG], s1[NG];
+        uint32_t any = 0;
+        {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            uint32_t w[NG];  // two tokens' scales
+            if constexpr (NG == 4) {
+              const uint4 v = *reinterpret_cast<const uint4*>(scales + C::SCALES + (2 * c + 8 * h) * 8);
+              w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+            } else {
+              const uint2 v = *reinterpret_cast<const uint2*>(scales + C::SCALES + (2 * c + 8 * h) * 4);
+              w[0] = v.x; w[1] = v.y;
+            }
+#pragma unroll
+            for (int g = 0; g < NG; g += 2) {
+              const uint32_t x = w[g / 2], y = w[NG / 2 + g / 2];
+              any |= x | y;
+              (h ? s1 : s0)[g] = prmt(x, y, 0x5410);
+              (h ? s1 : s0)[g + 1] = prmt(x, y, 0x7632);
+            }
+          }
+        }
+
+        // ---- the references
+        bool need = false;
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            const float top = group_max(fmaxf(z[t][k], z[t][2 + k]));
-            const float next = fmaxf(ref[t][k], top - above);
-            const float f = ref[t][k] == -CUDART_INF_F ? 0.f : fexp2(ref[t][k] - next);
-            ref[t][k] = next;
-            l[t][k] *= f;
-            const float fo = TERMS == 1 ? f : f * fv;
-#pragma unroll
-            for (int g = 0; g < NG; ++g)
-#pragma unroll
-              for (int h = 0; h < 2; ++h) {
-                o[t][g][h][k] *= fo;
-                o[t][g][h][2 + k] *= fo;
-              }
+          for (int k = 0; k < 2; ++k) need |= fmaxf(z[t][k], z[t][2 + k]) > ref[t][k] + (above + kRaise4);
+        const bool big = (any & 0x40004000u) != 0;  // a scale of 2 or more
+        if (__any_sync(0xffffffffu, need || (big && !large))) {
+          float fv = 1.f;
+          if (!large && __any_sync(0xffffffffu, big)) {
+            large = true;
+            if constexpr (TERMS == 1) above = kAbove4 - kBig4;
+            else fv = v_unit = 3.0517578125e-05f;  // 2^-kBig4
           }
-      }
-
-      // ---- probabilities, transposed: query row r, tokens as in s0 and s1
-      uint32_t ph[NT][2], pl[NT][2];
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        const float m0 = ref[t][0] == -CUDART_INF_F ? 0.f : ref[t][0], m1 = ref[t][1] == -CUDART_INF_F ? 0.f : ref[t][1];
-        const float e0 = fexp2(z[t][0] - m0), e1 = fexp2(z[t][1] - m1), e2 = fexp2(z[t][2] - m0), e3 = fexp2(z[t][3] - m1);
-        l[t][0] += e0 + e2;
-        l[t][1] += e1 + e3;
-        const uint32_t h0 = pack_f16(e0, e1), h1 = pack_f16(e2, e3);
-        ph[t][0] = transpose8(h0);
-        ph[t][1] = transpose8(h1);
-        if constexpr (TERMS == 2) {
-          const float2 f0 = unpack_f16(h0), f1 = unpack_f16(h1);
-          pl[t][0] = transpose8(pack_f16(e0 - f0.x, e1 - f0.y));
-          pl[t][1] = transpose8(pack_f16(e2 - f1.x, e3 - f1.y));
-        }
-      }
-
-      // ---- output: dimensions 32 g + 4 r + 2 h and the next, query rows 2c, 2c + 1
-      uint32_t v0[NG], v1[NG];
-#pragma unroll
-      for (int g = 0; g < NG; g += 2)
-        ldsm_x4_t(at + C::CODES + code_at<D>(mrow, g + mch), v0[g], v1[g], v0[g + 1], v1[g + 1]);
-#pragma unroll
-      for (int g = 0; g < NG; ++g) {
-        const uint32_t x0 = v0[g] >> 8, x1 = v1[g] >> 8;
-        const uint32_t a0 = codes.low(v0[g]), a1 = codes.high(v0[g]), a2 = codes.low(v1[g]), a3 = codes.high(v1[g]);
-        const uint32_t b0 = codes.low(x0), b1 = codes.high(x0), b2 = codes.low(x1), b3 = codes.high(x1);
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          if constexpr (TERMS == 1) {
-            const uint32_t w0 = mul_f16(ph[t][0], s0[g]), w1 = mul_f16(ph[t][1], s1[g]);
-            mma_f16(o[t][g][0], a0, a1, a2, a3, w0, w1);
-            mma_f16(o[t][g][1], b0, b1, b2, b3, w0, w1);
-          } else {
-            uint32_t hi[2], lo[2];
+          for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-              const float2 x = unpack_f16(ph[t][k]), y = unpack_f16(pl[t][k]), s = unpack_f16(k ? s1[g] : s0[g]);
-              const float a = (x.x + y.x) * (s.x * v_unit), b = (x.y + y.y) * (s.y * v_unit);
-              hi[k] = pack_f16(a, b);
-              const float2 h = unpack_f16(hi[k]);
-              lo[k] = pack_f16(a - h.x, b - h.y);
+              const float top = group_max(fmaxf(z[t][k], z[t][2 + k]));
+              const float next = fmaxf(ref[t][k], top - above);
+              const float f = ref[t][k] == -CUDART_INF_F ? 0.f : fexp2(ref[t][k] - next);
+              ref[t][k] = next;
+              l[t][k] *= f;
+              const float fo = TERMS == 1 ? f : f * fv;
+#pragma unroll
+              for (int g = 0; g < NG; ++g)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                  o[t][g][h][k] *= fo;
+                  o[t][g][h][2 + k] *= fo;
+                }
             }
-            mma_f16(o[t][g][0], a0, a1, a2, a3, hi[0], hi[1]);
-            mma_f16(o[t][g][1], b0, b1, b2, b3, hi[0], hi[1]);
-            mma_f16(o[t][g][0], a0, a1, a2, a3, lo[0], lo[1]);
-            mma_f16(o[t][g][1], b0, b1, b2, b3, lo[0], lo[1]);
+        }
+
+        // ---- probabilities, transposed: query row r, tokens as in s0 and s1
+        uint32_t ph[NT][2], pl[NT][2];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          const float m0 = ref[t][0] == -CUDART_INF_F ? 0.f : ref[t][0], m1 = ref[t][1] == -CUDART_INF_F ? 0.f : ref[t][1];
+          const float e0 = fexp2(z[t][0] - m0), e1 = fexp2(z[t][1] - m1), e2 = fexp2(z[t][2] - m0), e3 = fexp2(z[t][3] - m1);
+          l[t][0] += e0 + e2;
+          l[t][1] += e1 + e3;
+          const uint32_t h0 = pack_f16(e0, e1), h1 = pack_f16(e2, e3);
+          ph[t][0] = transpose8(h0);
+          ph[t][1] = transpose8(h1);
+          if constexpr (TERMS == 2) {
+            const float2 f0 = unpack_f16(h0), f1 = unpack_f16(h1);
+            pl[t][0] = transpose8(pack_f16(e0 - f0.x, e1 - f0.y));
+            pl[t][1] = transpose8(pack_f16(e2 - f1.x, e3 - f1.y));
+          }
+        }
+
+        // ---- output: dimensions 32 g + 4 r + 2 h and the next, query rows 2c, 2c + 1
+        uint32_t v0[NG], v1[NG];
+#pragma unroll
+        for (int g = 0; g < NG; g += 2)
+          ldsm_x4_t(at + C::CODES + code_at<D>(half + mrow, g + mch), v0[g], v1[g], v0[g + 1], v1[g + 1]);
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+          const uint32_t x0 = v0[g] >> 8, x1 = v1[g] >> 8;
+          const uint32_t a0 = codes.low(v0[g]), a1 = codes.high(v0[g]), a2 = codes.low(v1[g]), a3 = codes.high(v1[g]);
+          const uint32_t b0 = codes.low(x0), b1 = codes.high(x0), b2 = codes.low(x1), b3 = codes.high(x1);
+#pragma unroll
+          for (int t = 0; t < NT; ++t) {
+            if constexpr (TERMS == 1) {
+              const uint32_t w0 = mul_f16(ph[t][0], s0[g]), w1 = mul_f16(ph[t][1], s1[g]);
+              mma_f16(o[t][g][0], a0, a1, a2, a3, w0, w1);
+              mma_f16(o[t][g][1], b0, b1, b2, b3, w0, w1);
+            } else {
+              uint32_t hi[2], lo[2];
+#pragma unroll
+              for (int k = 0; k < 2; ++k) {
+                const float2 x = unpack_f16(ph[t][k]), y = unpack_f16(pl[t][k]), s = unpack_f16(k ? s1[g] : s0[g]);
+                const float a = (x.x + y.x) * (s.x * v_unit), b = (x.y + y.y) * (s.y * v_unit);
+                hi[k] = pack_f16(a, b);
+                const float2 h = unpack_f16(hi[k]);
+                lo[k] = pack_f16(a - h.x, b - h.y);
+              }
+              mma_f16(o[t][g][0], a0, a1, a2, a3, hi[0], hi[1]);
+              mma_f16(o[t][g][1], b0, b1, b2, b3, hi[0], hi[1]);
+              mma_f16(o[t][g][0], a0, a1, a2, a3, lo[0], lo[1]);
+              mma_f16(o[t][g][1], b0, b1, b2, b3, lo[0], lo[1]);
+            }
           }
         }
       }
     }
     cp_async_wait<0>();
+    __syncwarp();
     const float o_unit = TERMS == 2 && large ? 32768.f : 1.f;
 
     // ---- the warps' outputs, joined by the CTA into rows of out or a record
@@ -521,7 +530,7 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
           const float4 x = make_float4(o[t][g][0][k], o[t][g][0][2 + k], o[t][g][1][k], o[t][g][1][2 + k]);
-          *reinterpret_cast<float4*>(o_all + (warp * RS + row) * D + 32 * g + 4 * r) =
+          *reinterpret_cast<float4*>(mine + C::OFF_O + 4 * (row * D + 32 * g + 4 * r)) =
               make_float4(x.x * o_unit, x.y * o_unit, x.z * o_unit, x.w * o_unit);
         }
       }
@@ -541,7 +550,7 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
       for (int w = 0; w < kWarps4; ++w) {
         const float2 st = ml_all[w * RS + row];
         const float f = exp2f(st.x - mu);
-        const float4 y = *reinterpret_cast<const float4*>(o_all + (w * RS + row) * D + d);
+        const float4 y = *reinterpret_cast<const float4*>(smem + w * C::WARP + C::OFF_O + 4 * (row * D + d));
         sum = fmaf(st.y, f, sum);
         x.x = fmaf(y.x, f, x.x); x.y = fmaf(y.y, f, x.y); x.z = fmaf(y.z, f, x.z); x.w = fmaf(y.w, f, x.w);
       }
@@ -554,13 +563,14 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
         if (d == 0) *reinterpret_cast<float2*>(p.part_st + 2 * (rec + row)) = make_float2(m, sum);
       }
     }
-    if (direct) __syncthreads();  // o_all is read before its next use
+    if (direct) __syncthreads();  // the outputs are read before their next use
     else if (last_to_arrive(p.tickets + q.c0, q.parts, tid, misc + C::LINE, [] { __syncthreads(); }))
       join_records<T, D, kThreads4, 1, 16>(p, q.b, q.g, q.it.row0, rows, q.parts, RS,
                                            [&](int k) { return record_of(q.c0 + k, q.c0); }, tid);
   }
   if (err) atomicOr(p.err, err);
 }
+
 
 // f(kernel, shared bytes, rows, CTAs per SM) for the instance that serves R query rows.
 template <typename F>
