@@ -78,9 +78,9 @@ __device__ __forceinline__ void store_raw(T* p, const Raw8<T>& r) {
 
 // The cosine and signed sine of each of this lane's 8 values: value e becomes
 // x c + partner s, the partner the pair's other value.
-__device__ __forceinline__ void load_angles(const AppendParams& p, int b, int i, int place, int chunk, float (&c)[8],
-                                            float (&s)[8], unsigned& err) {
-  const RotView& r = p.rot;
+// at: the token's positions on the axes.
+__device__ __forceinline__ void load_angles(const RotView& r, const int (&at)[3], int chunk, float (&c)[8], float (&s)[8],
+                                            unsigned& err) {
   const int pairs = r.rot / 2;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
@@ -89,19 +89,15 @@ __device__ __forceinline__ void load_angles(const AppendParams& p, int b, int i,
   }
   if (8 * chunk >= r.rot) return;
   auto row = [&](int f) {  // the table's row for pair f
-    int at = place;
-    if (r.pos) {
-      const int axis = f < r.end0 ? 0 : f < r.end1 ? 1 : 2;
-      at = __ldg(r.pos + ((int64_t)axis * p.B + b) * p.n_new + i);
-    }
-    if (at < 0 || at >= r.max_pos) {
+    int x = f < r.end0 ? at[0] : f < r.end1 ? at[1] : at[2];
+    if (x < 0 || x >= r.max_pos) {
       err |= ERR_POS;
-      at = at < 0 ? 0 : r.max_pos - 1;
+      x = x < 0 ? 0 : r.max_pos - 1;
     }
-    return r.cos_sin + (int64_t)at * r.rot;
+    return r.cos_sin + (int64_t)x * r.rot;
   };
   auto one_axis = [&](int f0, int f1) {
-    return !r.pos || (f0 < r.end0) == (f1 < r.end0) && (f0 < r.end1) == (f1 < r.end1);
+    return (f0 < r.end0) == (f1 < r.end0) && (f0 < r.end1) == (f1 < r.end1);
   };
   if (r.interleaved) {
     const int f0 = 4 * chunk;
@@ -152,9 +148,9 @@ __device__ __forceinline__ void load_angles(const AppendParams& p, int b, int i,
 }
 
 // Eight values of a row in 4 bits, their group in this lane and the three beside
-// it (called by the whole warp): the scale, and the codes of the values, the
-// first in the lowest bits.
-__device__ __forceinline__ uint32_t quantise(const float (&x)[8], __half& scale) {
+// it (called by the whole warp): the scale, the codes of the values, the first in
+// the lowest bits, and in x what they stand for.
+__device__ __forceinline__ uint32_t quantise(float (&x)[8], __half& scale) {
   uint32_t top = 0;  // the magnitude's bits: NaN above everything
 #pragma unroll
   for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
@@ -165,12 +161,16 @@ __device__ __forceinline__ uint32_t quantise(const float (&x)[8], __half& scale)
   const float up = __uint_as_float((t + 0xfffffu) & ~0xfffffu);
   const float step = nan ? 1.f : fminf(fmaxf(up, kLeastStep4), kMostStep4);
   scale = nan ? __ushort_as_half(0x7fff) : __float2half_rn(step);
-  const float inv = __frcp_rn(step);
+  const float inv = __frcp_rn(step), held = nan ? __uint_as_float(0x7fffffffu) : step;
+  // Rounding to whole numbers by an addition: floats in [2^23, 2^24) are those, and
+  // 8 more than 1.5 * 2^23 leaves the code in the lowest bits.
+  constexpr float kWhole = 12582920.f;
   uint32_t codes = 0;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const int c = min(7, max(-8, __float2int_rn(__fmul_rn(x[e], inv)))) + 8;
-    codes |= (uint32_t)c << (4 * e);
+    const float whole = __fadd_rn(fminf(fmaxf(__fmul_rn(x[e], inv), -8.f), 7.f), kWhole);
+    codes |= (__float_as_uint(whole) & 15u) << (4 * e);
+    x[e] = (whole - kWhole) * held;
   }
   return codes;
 }
@@ -179,10 +179,35 @@ template <typename T, int D, bool Q4>
 __global__ void __launch_bounds__(kAppendThreads) k_append(const __grid_constant__ AppendParams p) {
   constexpr int L = D / 8, SLOTS = kAppendThreads / L;  // lanes of a row, rows at a time
   const int chunk = threadIdx.x % L, slot = threadIdx.x / L;
+  constexpr int U = 24 / Raw8<T>::N;  // rows of a thread in flight: 48 (D = 128, bf16) of a CTA
   pdl_wait();
   const int token = blockIdx.x / p.parts, part = blockIdx.x - token * p.parts;
   const int b = token / p.n_new, i = token - b * p.n_new;
+  const int rows = p.H + 2 * p.Hkv;
+  Raw8<T> x[U];
+  auto load = [&](int r0) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int r = r0 + u * p.parts * SLOTS + slot;
+      if (r >= rows) continue;
+      const bool is_q = r < p.H, is_k = r < p.H + p.Hkv;
+      const RowView& in = is_q ? p.q : is_k ? p.k : p.v;
+      const int g = is_q ? r : is_k ? r - p.H : r - p.H - p.Hkv;
+      load_raw(x[u], static_cast<const T*>(in.data) + (int64_t)b * in.sb + (int64_t)i * in.sn + (int64_t)g * in.sh + 8 * chunk);
+    }
+  };
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+#pragma unroll
+    for (int k = 0; k < Raw8<T>::N; ++k) x[u].w[k] = 0;
+  load(part * SLOTS);  // on their way while lengths, pages and angles are looked up
   unsigned err = 0;
+  int at[3] = {0, 0, 0};
+  if (p.rot.pos) {
+#pragma unroll
+    for (int a = 0; a < 3; ++a)
+      if (a < p.rot.axes) at[a] = __ldg(p.rot.pos + ((int64_t)a * p.B + b) * p.n_new + i);
+  }
   const int len = __ldcg(p.seq_len + b);
   int n = p.new_len ? __ldcg(p.new_len + b) : len > 0 ? p.n_new : 0;
   if (len < 0 || len > p.max_seq) err |= ERR_LEN;
@@ -190,14 +215,11 @@ __global__ void __launch_bounds__(kAppendThreads) k_append(const __grid_constant
   if (err) n = 0;  // nothing of this sequence is appended
   if (i < n) {
     const int place = len - n + i;
-    float c[8], s[8];
-    if (p.rot.cos_sin) load_angles(p, b, i, place, chunk, c, s, err);
     int64_t kat = b, vat = b;  // sequence or page of the new rows; < 0: nowhere
     int row = place;
     if (p.paged) {
       const int lp = place >> p.page_shift;
-      const auto& kt = Q4 ? p.kc4.block_table : p.kc.block_table;
-      const auto& vt = Q4 ? p.vc4.block_table : p.vc.block_table;
+      const int32_t *kt = Q4 ? p.kc4.block_table : p.kc.block_table, *vt = Q4 ? p.vc4.block_table : p.vc.block_table;
       const int kmax = Q4 ? p.kc4.max_pages : p.kc.max_pages, vmax = Q4 ? p.vc4.max_pages : p.vc.max_pages;
       const int kn = Q4 ? p.kc4.num_pages : p.kc.num_pages, vn = Q4 ? p.vc4.num_pages : p.vc.num_pages;
       kat = lp < kmax ? __ldg(kt + (int64_t)b * kmax + lp) : -1;
@@ -207,69 +229,68 @@ __global__ void __launch_bounds__(kAppendThreads) k_append(const __grid_constant
       if (kat < 0 || vat < 0) err |= ERR_PAGE;
       row = place & (p.page_size - 1);
     }
-    const int rows = p.H + 2 * p.Hkv;
+    float c[8], s[8];
+    if (!p.rot.pos) at[0] = place;
+    if (p.rot.cos_sin) load_angles(p.rot, at, chunk, c, s, err);
     const int pairs = p.rot.rot / 2;
     // The lane that holds the partners of this lane's values.
     const int lane = threadIdx.x & 31;
     const int other = 8 * chunk >= p.rot.rot ? lane : 8 * chunk >= pairs ? lane - pairs / 8 : lane + pairs / 8;
-#pragma unroll 4
-    for (int r0 = part * SLOTS; r0 < rows; r0 += p.parts * SLOTS) {
-      const int r = r0 + slot;
-      const bool is_q = r < p.H, is_k = !is_q && r < p.H + p.Hkv;
-      const int g = is_q ? r : is_k ? r - p.H : r - p.H - p.Hkv;
-      const RowView& in = is_q ? p.q : is_k ? p.k : p.v;
-      Raw8<T> x;
+    for (int r0 = part * SLOTS; r0 < rows; r0 += U * p.parts * SLOTS) {
+      if (r0 != part * SLOTS) load(r0);
 #pragma unroll
-      for (int k = 0; k < Raw8<T>::N; ++k) x.w[k] = 0;
-      if (r < rows)
-        load_raw(x, static_cast<const T*>(in.data) + (int64_t)b * in.sb + (int64_t)i * in.sn + (int64_t)g * in.sh + 8 * chunk);
-      if (p.rot.cos_sin) {
-        Raw8<T> y;
-        float f[8], o[8];
-        x.floats(f);
-        if (p.rot.interleaved) {
+      for (int u = 0; u < U; ++u) {
+        const int r = r0 + u * p.parts * SLOTS + slot;
+        const bool is_q = r < p.H, is_k = !is_q && r < p.H + p.Hkv, is_v = !is_q && !is_k && r < rows;
+        const int g = is_q ? r : is_k ? r - p.H : r - p.H - p.Hkv;
+        if (p.rot.cos_sin && __any_sync(0xffffffffu, is_q || is_k)) {
+          float f[8], o[8];
+          x[u].floats(f);
+          if (p.rot.interleaved) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) o[e] = f[e ^ 1];
-        } else {
+            for (int e = 0; e < 8; ++e) o[e] = f[e ^ 1];
+          } else {
+            Raw8<T> y;
 #pragma unroll
-          for (int k = 0; k < Raw8<T>::N; ++k) y.w[k] = __shfl_sync(0xffffffffu, x.w[k], other);
-          y.floats(o);
-        }
-        if ((is_q || is_k) && 8 * chunk < p.rot.rot) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) f[e] = __fadd_rn(__fmul_rn(f[e], c[e]), __fmul_rn(o[e], s[e]));
-          x.set(f);
-        }
-      }
-      if (is_q) {
-        store_raw(static_cast<T*>(p.q_out.data) + (int64_t)b * p.q_out.sb + (int64_t)i * p.q_out.sn +
-                      (int64_t)g * p.q_out.sh + 8 * chunk, x);
-      }
-      const int64_t at = is_k ? kat : vat;
-      if constexpr (Q4) {
-        float f[8];
-        x.floats(f);
-        __half scale;
-        const uint32_t codes = quantise(f, scale);
-        if (!is_q && r < rows) {
-          if (at >= 0) {
-            const Kv4View& to = is_k ? p.kc4 : p.vc4;
-            *reinterpret_cast<uint32_t*>(to.codes + at * to.cb + (int64_t)g * to.ch + (int64_t)row * to.ct + 4 * chunk) = codes;
-            if (chunk % 4 == 0)
-              to.scales[at * to.sb + (int64_t)g * to.sh + (int64_t)row * to.st + chunk / 4] = __half_as_ushort(scale);
+            for (int k = 0; k < Raw8<T>::N; ++k) y.w[k] = __shfl_sync(0xffffffffu, x[u].w[k], other);
+            y.floats(o);
           }
-          const RowView& held = is_k ? p.k_held : p.v_held;
-          if (held.data) {
-            const float step = __half2float(scale);
+          if ((is_q || is_k) && 8 * chunk < p.rot.rot) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) f[e] = (float)((int)((codes >> (4 * e)) & 15u) - 8) * step;
-            x.set(f);
-            store_raw(static_cast<T*>(held.data) + (int64_t)b * held.sb + (int64_t)i * held.sn + (int64_t)g * held.sh + 8 * chunk, x);
+            for (int e = 0; e < 8; ++e) f[e] = __fadd_rn(__fmul_rn(f[e], c[e]), __fmul_rn(o[e], s[e]));
+            x[u].set(f);
           }
         }
-      } else if (!is_q && r < rows && at >= 0) {
-        const KvView& to = is_k ? p.kc : p.vc;
-        store_raw(static_cast<T*>(const_cast<void*>(to.data)) + at * to.sb + (int64_t)g * to.sh + (int64_t)row * to.st + 8 * chunk, x);
+        if (is_q)
+          store_raw(static_cast<T*>(p.q_out.data) + (int64_t)b * p.q_out.sb + (int64_t)i * p.q_out.sn +
+                        (int64_t)g * p.q_out.sh + 8 * chunk, x[u]);
+        const int64_t to_b = is_k ? kat : vat;
+        if constexpr (Q4) {
+          if (__any_sync(0xffffffffu, is_k || is_v)) {
+            float f[8];
+            x[u].floats(f);
+            __half scale;
+            const uint32_t codes = quantise(f, scale);
+            if (is_k || is_v) {
+              if (to_b >= 0) {
+                const Kv4View& to = is_k ? p.kc4 : p.vc4;
+                *reinterpret_cast<uint32_t*>(to.codes + to_b * to.cb + (int64_t)g * to.ch + (int64_t)row * to.ct + 4 * chunk) = codes;
+                if (chunk % 4 == 0)
+                  to.scales[to_b * to.sb + (int64_t)g * to.sh + (int64_t)row * to.st + chunk / 4] = __half_as_ushort(scale);
+              }
+              const RowView& held = is_k ? p.k_held : p.v_held;
+              if (held.data) {
+                x[u].set(f);
+                store_raw(static_cast<T*>(held.data) + (int64_t)b * held.sb + (int64_t)i * held.sn +
+                              (int64_t)g * held.sh + 8 * chunk, x[u]);
+              }
+            }
+          }
+        } else if ((is_k || is_v) && to_b >= 0) {
+          const KvView& to = is_k ? p.kc : p.vc;
+          store_raw(static_cast<T*>(const_cast<void*>(to.data)) + to_b * to.sb + (int64_t)g * to.sh + (int64_t)row * to.st + 8 * chunk,
+                    x[u]);
+        }
       }
     }
   }

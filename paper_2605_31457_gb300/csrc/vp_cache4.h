@@ -32,7 +32,7 @@ struct RotView {
   const float* cos_sin;  // [max_pos][rot]: rot / 2 cosines, then the sines; NULL: no rotation
   int max_pos, rot, interleaved;
   const int32_t* pos;    // [axes][B][n_new], or NULL: the token's place in its sequence
-  int end0, end1;
+  int axes, end0, end1;  // axes 1: end0 = rot / 2
 };
 
 struct AppendParams {

@@ -144,7 +144,7 @@ vp_status append(vp_ctx* ctx, const char* name, int32_t batch, int32_t n_new, co
   if (rotation) {
     const vp_rotation& r = *rotation;
     const int s0 = r.axes > 1 ? r.sections[0] : r.rot_dim / 2, s1 = r.axes > 1 ? r.sections[1] : 0;
-    p.rot = vp::RotView{r.cos_sin, r.max_pos, r.rot_dim, r.interleaved, r.pos, s0, s0 + s1};
+    p.rot = vp::RotView{r.cos_sin, r.max_pos, r.rot_dim, r.interleaved, r.pos, r.axes, s0, s0 + s1};
   }
   p.err = ctx->err;
   const cudaError_t e = vp::launch_append(p, c.dtype, c.head_dim, kFour, ctx->num_sms, static_cast<cudaStream_t>(cuda_stream));

@@ -235,15 +235,28 @@ def vp_compact_kv(ctx, batch, src: vp_kv, dst: vp_kv, visual_span: vp_span, text
     return _check(st, ctx) if check else st
 
 
-def _stream(stream):
+_torch = None
+
+
+def _raw_stream(stream):
+    """The handle of a torch.cuda.Stream, of a raw handle (itself), or of torch's current stream."""
+    global _torch
     if stream is None:
-        import torch
+        if _torch is None:
+            import torch
+            _torch = torch
         # The handle of torch.cuda.current_stream(), without making the object:
         # a decode step calls this once per layer.
-        stream = torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
-    elif hasattr(stream, "cuda_stream"):
-        stream = stream.cuda_stream
-    return ctypes.c_void_p(stream)
+        return _torch._C._cuda_getCurrentRawStream(_torch.cuda.current_device())
+    return stream.cuda_stream if hasattr(stream, "cuda_stream") else stream
+
+
+def _stream(stream):
+    return ctypes.c_void_p(_raw_stream(stream))
+
+
+def _addr(t):
+    return None if t is None else t.data_ptr()
 
 
 def _ref(struct):
@@ -276,14 +289,16 @@ def vp_evict(ctx, batch, k_src: vp_kv, v_src: vp_kv, seq_len, policy: vp_evict_p
     return _check(st, ctx) if check else st
 
 
+# ctypes passes a structure's address where a pointer to it is declared, and an int
+# as an address: half the time of making the pointer objects here.
 def vp_append(ctx, batch, n_new, q: vp_rows, k: vp_rows, v: vp_rows, seq_len, rotation: vp_rotation, q_out: vp_rows,
               k_cache: vp_kv, v_cache: vp_kv, new_len=None, stream=None, check=True):
     """Enqueues the rotation of the ``n_new`` newest tokens' queries and keys and the
     appending of their keys and values.  q, k, v and q_out are ``rows(tensor)``
     (q and q_out may be None), rotation ``make_rotation(...)`` or None; seq_len and
     new_len are tensors."""
-    st = lib.vp_append(ctx, batch, n_new, _ref(q), _ref(k), _ref(v), _ptr(seq_len), _ptr(new_len), _ref(rotation),
-                       _ref(q_out), _ref(k_cache), _ref(v_cache), _stream(stream))
+    st = lib.vp_append(ctx, batch, n_new, q, k, v, _addr(seq_len), _addr(new_len), rotation,
+                       q_out, k_cache, v_cache, _raw_stream(stream))
     return _check(st, ctx) if check else st
 
 
@@ -292,8 +307,8 @@ def vp_append4(ctx, batch, n_new, q: vp_rows, k: vp_rows, v: vp_rows, seq_len, r
                stream=None, check=True):
     """``vp_append`` into caches held in 4 bits; k_held and v_held, where given,
     receive the values that the caches now hold for the new tokens."""
-    st = lib.vp_append4(ctx, batch, n_new, _ref(q), _ref(k), _ref(v), _ptr(seq_len), _ptr(new_len), _ref(rotation),
-                        _ref(q_out), _ref(k_cache), _ref(v_cache), _ref(k_held), _ref(v_held), _stream(stream))
+    st = lib.vp_append4(ctx, batch, n_new, q, k, v, _addr(seq_len), _addr(new_len), rotation,
+                        q_out, k_cache, v_cache, k_held, v_held, _raw_stream(stream))
     return _check(st, ctx) if check else st
 
 
@@ -305,8 +320,8 @@ def vp_reserve4(ctx, max_new):
 def vp_attend4(ctx, batch, n_new, q: vp_rows, k_cache: vp_kv4, v_cache: vp_kv4, seq_len, visible: vp_visible,
                out: vp_rows, new_len=None, lse=None, stream=None, check=True):
     """``vp_attend_new`` over caches held in 4 bits (no accumulated weights)."""
-    st = lib.vp_attend4(ctx, batch, n_new, _ref(q), _ref(k_cache), _ref(v_cache), _ptr(seq_len), _ptr(new_len),
-                        _ref(visible), _ref(out), _ptr(lse), _stream(stream))
+    st = lib.vp_attend4(ctx, batch, n_new, q, k_cache, v_cache, _addr(seq_len), _addr(new_len),
+                        visible, out, _addr(lse), _raw_stream(stream))
     return _check(st, ctx) if check else st
 
 
