@@ -28,37 +28,32 @@ namespace {
 // bf16.  A code is the value times the scale's rounded reciprocal, rounded to
 // the nearest whole number (ties to even).  A NaN makes its group's scale NaN.
 //
-// Bound by memory for prompts and by the launch for tokens.  A CTA serves rows
-// of one token, so that its threads hold one set of cosines and sines; tokens are
-// few at a decode step, when several CTAs share one token's rows (AppendParams
-// ::parts).  Nothing triggers the next kernel early: what follows may read the
+// Bound by memory for prompts and by the launch for tokens.  A warp serves rows of
+// one token, so that its lanes hold one set of cosines and sines and of addresses;
+// where tokens are few, several warps share one token's rows (AppendParams::parts).  Nothing triggers the next kernel early: what follows may read the
 // caches before it waits.
 // ---------------------------------------------------------------------------
 constexpr int kAppendThreads = 128;
+constexpr int kAppendWarps = 16;  // warps per SM that a call is spread over
 
-template <typename T> struct Raw8;  // eight values as 32-bit words
+template <typename T> struct Raw8;  // eight values as 32-bit words; get and set: the i-th two of them
 template <> struct Raw8<__nv_bfloat16> {
   static constexpr int N = 4;
   uint32_t w[4];
-  __device__ void floats(float (&f)[8]) const {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) bf2(w[i], f[2 * i], f[2 * i + 1]);
+  __device__ float2 get(int i) const {
+    float2 f;
+    bf2(w[i], f.x, f.y);
+    return f;
   }
-  __device__ void set(const float (&f)[8]) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = pack_bf16(f[2 * i], f[2 * i + 1]);
-  }
+  __device__ void set(int i, float2 f) { w[i] = pack_bf16(f.x, f.y); }
 };
 template <> struct Raw8<float> {
   static constexpr int N = 8;
   uint32_t w[8];
-  __device__ void floats(float (&f)[8]) const {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(w[i]);
-  }
-  __device__ void set(const float (&f)[8]) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(f[i]);
+  __device__ float2 get(int i) const { return make_float2(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1])); }
+  __device__ void set(int i, float2 f) {
+    w[2 * i] = __float_as_uint(f.x);
+    w[2 * i + 1] = __float_as_uint(f.y);
   }
 };
 template <typename T>
@@ -177,13 +172,20 @@ __device__ __forceinline__ uint32_t quantise(float (&x)[8], __half& scale) {
 
 template <typename T, int D, bool Q4>
 __global__ void __launch_bounds__(kAppendThreads) k_append(const __grid_constant__ AppendParams p) {
-  constexpr int L = D / 8, SLOTS = kAppendThreads / L;  // lanes of a row, rows at a time
-  const int chunk = threadIdx.x % L, slot = threadIdx.x / L;
-  constexpr int U = 24 / Raw8<T>::N;  // rows of a thread in flight: 48 (D = 128, bf16) of a CTA
+  constexpr int L = D / 8, SLOTS = 32 / L;  // lanes of a row, rows of a warp at a time
+  const int lane = threadIdx.x & 31, chunk = lane % L, slot = lane / L;
+  constexpr int U = 24 / Raw8<T>::N;  // rows of a lane in flight
   pdl_wait();
-  const int token = blockIdx.x / p.parts, part = blockIdx.x - token * p.parts;
-  const int b = token / p.n_new, i = token - b * p.n_new;
+  const unsigned unit = blockIdx.x * (kAppendThreads / 32) + threadIdx.x / 32;
+  const unsigned token = unit / (unsigned)p.parts, part = unit - token * p.parts;
+  const int b = token / (unsigned)p.n_new, i = token - b * p.n_new;
+  if (b >= p.B) return;
   const int rows = p.H + 2 * p.Hkv;
+  // Rows of this lane's chunk at head 0: where they come from and go to.
+  auto from = [&](const RowView& v) {
+    return static_cast<T*>(v.data) + (int64_t)b * v.sb + (int64_t)i * v.sn + 8 * chunk;
+  };
+  const T *q_in = from(p.q), *k_in = from(p.k), *v_in = from(p.v);
   Raw8<T> x[U];
   auto load = [&](int r0) {
 #pragma unroll
@@ -191,9 +193,8 @@ __global__ void __launch_bounds__(kAppendThreads) k_append(const __grid_constant
       const int r = r0 + u * p.parts * SLOTS + slot;
       if (r >= rows) continue;
       const bool is_q = r < p.H, is_k = r < p.H + p.Hkv;
-      const RowView& in = is_q ? p.q : is_k ? p.k : p.v;
-      const int g = is_q ? r : is_k ? r - p.H : r - p.H - p.Hkv;
-      load_raw(x[u], static_cast<const T*>(in.data) + (int64_t)b * in.sb + (int64_t)i * in.sn + (int64_t)g * in.sh + 8 * chunk);
+      const int64_t g = is_q ? r : is_k ? r - p.H : r - p.H - p.Hkv;
+      load_raw(x[u], (is_q ? q_in : is_k ? k_in : v_in) + g * (is_q ? p.q.sh : is_k ? p.k.sh : p.v.sh));
     }
   };
 #pragma unroll
@@ -234,62 +235,76 @@ __global__ void __launch_bounds__(kAppendThreads) k_append(const __grid_constant
     if (p.rot.cos_sin) load_angles(p.rot, at, chunk, c, s, err);
     const int pairs = p.rot.rot / 2;
     // The lane that holds the partners of this lane's values.
-    const int lane = threadIdx.x & 31;
-    const int other = 8 * chunk >= p.rot.rot ? lane : 8 * chunk >= pairs ? lane - pairs / 8 : lane + pairs / 8;
+    const bool turns = 8 * chunk < p.rot.rot;
+    const int other = !turns ? lane : 8 * chunk >= pairs ? lane - pairs / 8 : lane + pairs / 8;
+    T* const q_out = from(p.q_out);
+    // Caches: the new token's row, in T or as codes with their scale.
+    T *k_to = nullptr, *v_to = nullptr, *k_held = nullptr, *v_held = nullptr;
+    uint8_t *k_codes = nullptr, *v_codes = nullptr;
+    uint16_t *k_scale = nullptr, *v_scale = nullptr;
+    if constexpr (Q4) {
+      k_codes = p.kc4.codes + kat * p.kc4.cb + row * p.kc4.ct + 4 * chunk;
+      v_codes = p.vc4.codes + vat * p.vc4.cb + row * p.vc4.ct + 4 * chunk;
+      k_scale = p.kc4.scales + kat * p.kc4.sb + row * p.kc4.st + chunk / 4;
+      v_scale = p.vc4.scales + vat * p.vc4.sb + row * p.vc4.st + chunk / 4;
+      k_held = from(p.k_held);
+      v_held = from(p.v_held);
+    } else {
+      k_to = static_cast<T*>(const_cast<void*>(p.kc.data)) + kat * p.kc.sb + row * p.kc.st + 8 * chunk;
+      v_to = static_cast<T*>(const_cast<void*>(p.vc.data)) + vat * p.vc.sb + row * p.vc.st + 8 * chunk;
+    }
+#pragma unroll 1
     for (int r0 = part * SLOTS; r0 < rows; r0 += U * p.parts * SLOTS) {
-      if (r0 != part * SLOTS) load(r0);
+      if (r0 != (int)part * SLOTS) load(r0);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int r = r0 + u * p.parts * SLOTS + slot;
+        if (r - slot >= rows) break;
         const bool is_q = r < p.H, is_k = !is_q && r < p.H + p.Hkv, is_v = !is_q && !is_k && r < rows;
-        const int g = is_q ? r : is_k ? r - p.H : r - p.H - p.Hkv;
+        const int64_t g = is_q ? r : is_k ? r - p.H : r - p.H - p.Hkv;
         if (p.rot.cos_sin && __any_sync(0xffffffffu, is_q || is_k)) {
-          float f[8], o[8];
-          x[u].floats(f);
-          if (p.rot.interleaved) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) o[e] = f[e ^ 1];
-          } else {
-            Raw8<T> y;
+          Raw8<T> y = x[u];
+          if (!p.rot.interleaved) {
 #pragma unroll
             for (int k = 0; k < Raw8<T>::N; ++k) y.w[k] = __shfl_sync(0xffffffffu, x[u].w[k], other);
-            y.floats(o);
           }
-          if ((is_q || is_k) && 8 * chunk < p.rot.rot) {
+          if (turns && (is_q || is_k)) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) f[e] = __fadd_rn(__fmul_rn(f[e], c[e]), __fmul_rn(o[e], s[e]));
-            x[u].set(f);
+            for (int k = 0; k < 4; ++k) {
+              const float2 a = x[u].get(k), o = y.get(k);
+              const float ox = p.rot.interleaved ? o.y : o.x, oy = p.rot.interleaved ? o.x : o.y;
+              x[u].set(k, make_float2(__fadd_rn(__fmul_rn(a.x, c[2 * k]), __fmul_rn(ox, s[2 * k])),
+                                      __fadd_rn(__fmul_rn(a.y, c[2 * k + 1]), __fmul_rn(oy, s[2 * k + 1]))));
+            }
           }
         }
-        if (is_q)
-          store_raw(static_cast<T*>(p.q_out.data) + (int64_t)b * p.q_out.sb + (int64_t)i * p.q_out.sn +
-                        (int64_t)g * p.q_out.sh + 8 * chunk, x[u]);
-        const int64_t to_b = is_k ? kat : vat;
+        if (is_q) store_raw(q_out + g * p.q_out.sh, x[u]);
+        const bool mapped = (is_k ? kat : vat) >= 0;
         if constexpr (Q4) {
           if (__any_sync(0xffffffffu, is_k || is_v)) {
             float f[8];
-            x[u].floats(f);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              f[2 * k] = x[u].get(k).x;
+              f[2 * k + 1] = x[u].get(k).y;
+            }
             __half scale;
             const uint32_t codes = quantise(f, scale);
             if (is_k || is_v) {
-              if (to_b >= 0) {
-                const Kv4View& to = is_k ? p.kc4 : p.vc4;
-                *reinterpret_cast<uint32_t*>(to.codes + to_b * to.cb + (int64_t)g * to.ch + (int64_t)row * to.ct + 4 * chunk) = codes;
+              if (mapped) {
+                *reinterpret_cast<uint32_t*>((is_k ? k_codes : v_codes) + g * (is_k ? p.kc4.ch : p.vc4.ch)) = codes;
                 if (chunk % 4 == 0)
-                  to.scales[to_b * to.sb + (int64_t)g * to.sh + (int64_t)row * to.st + chunk / 4] = __half_as_ushort(scale);
+                  (is_k ? k_scale : v_scale)[g * (is_k ? p.kc4.sh : p.vc4.sh)] = __half_as_ushort(scale);
               }
-              const RowView& held = is_k ? p.k_held : p.v_held;
-              if (held.data) {
-                x[u].set(f);
-                store_raw(static_cast<T*>(held.data) + (int64_t)b * held.sb + (int64_t)i * held.sn +
-                              (int64_t)g * held.sh + 8 * chunk, x[u]);
+              if ((is_k ? p.k_held.data : p.v_held.data) != nullptr) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) x[u].set(k, make_float2(f[2 * k], f[2 * k + 1]));
+                store_raw((is_k ? k_held : v_held) + g * (is_k ? p.k_held.sh : p.v_held.sh), x[u]);
               }
             }
           }
-        } else if ((is_k || is_v) && to_b >= 0) {
-          const KvView& to = is_k ? p.kc : p.vc;
-          store_raw(static_cast<T*>(const_cast<void*>(to.data)) + to_b * to.sb + (int64_t)g * to.sh + (int64_t)row * to.st + 8 * chunk,
-                    x[u]);
+        } else if ((is_k || is_v) && mapped) {
+          store_raw((is_k ? k_to : v_to) + g * (is_k ? p.kc.sh : p.vc.sh), x[u]);
         }
       }
     }
@@ -299,7 +314,8 @@ __global__ void __launch_bounds__(kAppendThreads) k_append(const __grid_constant
 
 template <typename T, int D, bool Q4>
 cudaError_t launch(const AppendParams& p, cudaStream_t st) {
-  const int64_t ctas = (int64_t)p.B * p.n_new * p.parts;
+  constexpr int kUnits = kAppendThreads / 32;
+  const int64_t ctas = ((int64_t)p.B * p.n_new * p.parts + kUnits - 1) / kUnits;
   if (ctas > INT32_MAX) return cudaErrorInvalidConfiguration;
   return launch_dep(k_append<T, D, Q4>, dim3((unsigned)ctas), kAppendThreads, 0, st, p);
 }
@@ -307,8 +323,8 @@ cudaError_t launch(const AppendParams& p, cudaStream_t st) {
 }  // namespace
 
 cudaError_t launch_append(AppendParams& p, int dtype, int D, bool four, int num_sms, cudaStream_t st) {
-  const int slots = kAppendThreads / (D / 8), most = (p.H + 2 * p.Hkv + slots - 1) / slots;
-  const int64_t tokens = (int64_t)p.B * p.n_new, want = 8 * (int64_t)num_sms / tokens;
+  const int slots = 256 / D, most = (p.H + 2 * p.Hkv + slots - 1) / slots;
+  const int64_t tokens = (int64_t)p.B * p.n_new, want = kAppendWarps * (int64_t)num_sms / tokens;
   p.parts = want < 1 ? 1 : want > most ? most : (int)want;
   auto typed = [&](auto zero) {
     using T = decltype(zero);

@@ -46,7 +46,7 @@ struct AppendParams {
   const int32_t* new_len;         // or NULL
   RotView rot;
   unsigned* err;
-  int parts;                      // CTAs of a token
+  int parts;                      // warps of a token
 };
 
 cudaError_t launch_append(AppendParams& p, int dtype, int D, bool four, int num_sms, cudaStream_t s);
