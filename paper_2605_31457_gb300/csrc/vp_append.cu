@@ -173,35 +173,47 @@ __device__ __forceinline__ uint32_t quantise(float (&x)[8], __half& scale) {
 template <typename T, int D, bool Q4>
 __global__ void __launch_bounds__(kAppendThreads) k_append(const __grid_constant__ AppendParams p) {
   constexpr int L = D / 8, SLOTS = 32 / L;  // lanes of a row, rows of a warp at a time
+  constexpr int U = 24 / Raw8<T>::N;        // of a lane in flight
   const int lane = threadIdx.x & 31, chunk = lane % L, slot = lane / L;
-  constexpr int U = 24 / Raw8<T>::N;  // rows of a lane in flight
   pdl_wait();
-  const unsigned unit = blockIdx.x * (kAppendThreads / 32) + threadIdx.x / 32;
+  const unsigned unit = uniform(blockIdx.x * (kAppendThreads / 32) + threadIdx.x / 32);
   const unsigned token = unit / (unsigned)p.parts, part = unit - token * p.parts;
   const int b = token / (unsigned)p.n_new, i = token - b * p.n_new;
   if (b >= p.B) return;
-  const int rows = p.H + 2 * p.Hkv;
-  // Rows of this lane's chunk at head 0: where they come from and go to.
+  // Turns: SLOTS rows of queries each, then of keys, then of values.
+  const int nq = (p.H + SLOTS - 1) / SLOTS, nk = (p.Hkv + SLOTS - 1) / SLOTS, turns = nq + 2 * nk;
+  struct Turn {
+    bool is_q, is_k;
+    int first;  // its first row
+  };
+  auto turn = [&](int t) {
+    Turn x;
+    x.is_q = t < nq;
+    x.is_k = !x.is_q && t < nq + nk;
+    x.first = (x.is_q ? t : x.is_k ? t - nq : t - nq - nk) * SLOTS;
+    return x;
+  };
+  // This lane's chunk of row `slot`, where it comes from and goes to.
   auto from = [&](const RowView& v) {
-    return static_cast<T*>(v.data) + (int64_t)b * v.sb + (int64_t)i * v.sn + 8 * chunk;
+    return static_cast<T*>(v.data) + (int64_t)b * v.sb + (int64_t)i * v.sn + (int64_t)slot * v.sh + 8 * chunk;
   };
   const T *q_in = from(p.q), *k_in = from(p.k), *v_in = from(p.v);
   Raw8<T> x[U];
-  auto load = [&](int r0) {
+  auto load = [&](int t0) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int r = r0 + u * p.parts * SLOTS + slot;
-      if (r >= rows) continue;
-      const bool is_q = r < p.H, is_k = r < p.H + p.Hkv;
-      const int64_t g = is_q ? r : is_k ? r - p.H : r - p.H - p.Hkv;
-      load_raw(x[u], (is_q ? q_in : is_k ? k_in : v_in) + g * (is_q ? p.q.sh : is_k ? p.k.sh : p.v.sh));
+      const int t = t0 + u * p.parts;
+      if (t >= turns) break;
+      const Turn w = turn(t);
+      if (w.first + slot < (w.is_q ? p.H : p.Hkv))
+        load_raw(x[u], (w.is_q ? q_in : w.is_k ? k_in : v_in) + w.first * (w.is_q ? p.q.sh : w.is_k ? p.k.sh : p.v.sh));
     }
   };
 #pragma unroll
   for (int u = 0; u < U; ++u)
 #pragma unroll
     for (int k = 0; k < Raw8<T>::N; ++k) x[u].w[k] = 0;
-  load(part * SLOTS);  // on their way while lengths, pages and angles are looked up
+  load(part);  // on their way while lengths, pages and angles are looked up
   unsigned err = 0;
   int at[3] = {0, 0, 0};
   if (p.rot.pos) {
@@ -235,76 +247,86 @@ __global__ void __launch_bounds__(kAppendThreads) k_append(const __grid_constant
     if (p.rot.cos_sin) load_angles(p.rot, at, chunk, c, s, err);
     const int pairs = p.rot.rot / 2;
     // The lane that holds the partners of this lane's values.
-    const bool turns = 8 * chunk < p.rot.rot;
-    const int other = !turns ? lane : 8 * chunk >= pairs ? lane - pairs / 8 : lane + pairs / 8;
+    const bool turned = p.rot.cos_sin && 8 * chunk < p.rot.rot;
+    const int other = !turned ? lane : 8 * chunk >= pairs ? lane - pairs / 8 : lane + pairs / 8;
+    auto rotate = [&](Raw8<T>& y) {
+      if (!p.rot.cos_sin) return;
+      if (p.rot.interleaved) {
+        if (!turned) return;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float2 a = y.get(k);
+          y.set(k, make_float2(__fadd_rn(__fmul_rn(a.x, c[2 * k]), __fmul_rn(a.y, s[2 * k])),
+                               __fadd_rn(__fmul_rn(a.y, c[2 * k + 1]), __fmul_rn(a.x, s[2 * k + 1]))));
+        }
+        return;
+      }
+      Raw8<T> o;
+#pragma unroll
+      for (int k = 0; k < Raw8<T>::N; ++k) o.w[k] = __shfl_sync(0xffffffffu, y.w[k], other);
+      if (!turned) return;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float2 a = y.get(k), z = o.get(k);
+        y.set(k, make_float2(__fadd_rn(__fmul_rn(a.x, c[2 * k]), __fmul_rn(z.x, s[2 * k])),
+                             __fadd_rn(__fmul_rn(a.y, c[2 * k + 1]), __fmul_rn(z.y, s[2 * k + 1]))));
+      }
+    };
     T* const q_out = from(p.q_out);
-    // Caches: the new token's row, in T or as codes with their scale.
+    // The new token's rows of the caches, in T or as codes with their scale.
     T *k_to = nullptr, *v_to = nullptr, *k_held = nullptr, *v_held = nullptr;
     uint8_t *k_codes = nullptr, *v_codes = nullptr;
     uint16_t *k_scale = nullptr, *v_scale = nullptr;
     if constexpr (Q4) {
-      k_codes = p.kc4.codes + kat * p.kc4.cb + row * p.kc4.ct + 4 * chunk;
-      v_codes = p.vc4.codes + vat * p.vc4.cb + row * p.vc4.ct + 4 * chunk;
-      k_scale = p.kc4.scales + kat * p.kc4.sb + row * p.kc4.st + chunk / 4;
-      v_scale = p.vc4.scales + vat * p.vc4.sb + row * p.vc4.st + chunk / 4;
+      k_codes = p.kc4.codes + kat * p.kc4.cb + row * p.kc4.ct + slot * p.kc4.ch + 4 * chunk;
+      v_codes = p.vc4.codes + vat * p.vc4.cb + row * p.vc4.ct + slot * p.vc4.ch + 4 * chunk;
+      k_scale = p.kc4.scales + kat * p.kc4.sb + row * p.kc4.st + slot * p.kc4.sh + chunk / 4;
+      v_scale = p.vc4.scales + vat * p.vc4.sb + row * p.vc4.st + slot * p.vc4.sh + chunk / 4;
       k_held = from(p.k_held);
       v_held = from(p.v_held);
     } else {
-      k_to = static_cast<T*>(const_cast<void*>(p.kc.data)) + kat * p.kc.sb + row * p.kc.st + 8 * chunk;
-      v_to = static_cast<T*>(const_cast<void*>(p.vc.data)) + vat * p.vc.sb + row * p.vc.st + 8 * chunk;
+      k_to = static_cast<T*>(const_cast<void*>(p.kc.data)) + kat * p.kc.sb + row * p.kc.st + slot * p.kc.sh + 8 * chunk;
+      v_to = static_cast<T*>(const_cast<void*>(p.vc.data)) + vat * p.vc.sb + row * p.vc.st + slot * p.vc.sh + 8 * chunk;
     }
 #pragma unroll 1
-    for (int r0 = part * SLOTS; r0 < rows; r0 += U * p.parts * SLOTS) {
-      if (r0 != (int)part * SLOTS) load(r0);
+    for (int t0 = part; t0 < turns; t0 += U * p.parts) {
+      if (t0 != (int)part) load(t0);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int r = r0 + u * p.parts * SLOTS + slot;
-        if (r - slot >= rows) break;
-        const bool is_q = r < p.H, is_k = !is_q && r < p.H + p.Hkv, is_v = !is_q && !is_k && r < rows;
-        const int64_t g = is_q ? r : is_k ? r - p.H : r - p.H - p.Hkv;
-        if (p.rot.cos_sin && __any_sync(0xffffffffu, is_q || is_k)) {
-          Raw8<T> y = x[u];
-          if (!p.rot.interleaved) {
-#pragma unroll
-            for (int k = 0; k < Raw8<T>::N; ++k) y.w[k] = __shfl_sync(0xffffffffu, x[u].w[k], other);
-          }
-          if (turns && (is_q || is_k)) {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const float2 a = x[u].get(k), o = y.get(k);
-              const float ox = p.rot.interleaved ? o.y : o.x, oy = p.rot.interleaved ? o.x : o.y;
-              x[u].set(k, make_float2(__fadd_rn(__fmul_rn(a.x, c[2 * k]), __fmul_rn(ox, s[2 * k])),
-                                      __fadd_rn(__fmul_rn(a.y, c[2 * k + 1]), __fmul_rn(oy, s[2 * k + 1]))));
-            }
-          }
+        const int t = t0 + u * p.parts;
+        if (t >= turns) break;
+        const Turn w = turn(t);
+        const bool there = w.first + slot < (w.is_q ? p.H : p.Hkv);
+        Raw8<T>& y = x[u];
+        if (w.is_q) {
+          rotate(y);
+          if (there) store_raw(q_out + w.first * p.q_out.sh, y);
+          continue;
         }
-        if (is_q) store_raw(q_out + g * p.q_out.sh, x[u]);
-        const bool mapped = (is_k ? kat : vat) >= 0;
+        if (w.is_k) rotate(y);
+        const bool mapped = there && (w.is_k ? kat : vat) >= 0;
         if constexpr (Q4) {
-          if (__any_sync(0xffffffffu, is_k || is_v)) {
-            float f[8];
+          float f[8];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              f[2 * k] = x[u].get(k).x;
-              f[2 * k + 1] = x[u].get(k).y;
-            }
-            __half scale;
-            const uint32_t codes = quantise(f, scale);
-            if (is_k || is_v) {
-              if (mapped) {
-                *reinterpret_cast<uint32_t*>((is_k ? k_codes : v_codes) + g * (is_k ? p.kc4.ch : p.vc4.ch)) = codes;
-                if (chunk % 4 == 0)
-                  (is_k ? k_scale : v_scale)[g * (is_k ? p.kc4.sh : p.vc4.sh)] = __half_as_ushort(scale);
-              }
-              if ((is_k ? p.k_held.data : p.v_held.data) != nullptr) {
-#pragma unroll
-                for (int k = 0; k < 4; ++k) x[u].set(k, make_float2(f[2 * k], f[2 * k + 1]));
-                store_raw((is_k ? k_held : v_held) + g * (is_k ? p.k_held.sh : p.v_held.sh), x[u]);
-              }
-            }
+          for (int k = 0; k < 4; ++k) {
+            const float2 a = y.get(k);
+            f[2 * k] = a.x;
+            f[2 * k + 1] = a.y;
           }
-        } else if ((is_k || is_v) && mapped) {
-          store_raw((is_k ? k_to : v_to) + g * (is_k ? p.kc.sh : p.vc.sh), x[u]);
+          __half scale;
+          const uint32_t codes = quantise(f, scale);
+          if (mapped) {
+            *reinterpret_cast<uint32_t*>((w.is_k ? k_codes : v_codes) + w.first * (w.is_k ? p.kc4.ch : p.vc4.ch)) = codes;
+            if (chunk % 4 == 0)
+              (w.is_k ? k_scale : v_scale)[w.first * (w.is_k ? p.kc4.sh : p.vc4.sh)] = __half_as_ushort(scale);
+          }
+          if (there && (w.is_k ? p.k_held.data : p.v_held.data) != nullptr) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) y.set(k, make_float2(f[2 * k], f[2 * k + 1]));
+            store_raw((w.is_k ? k_held : v_held) + w.first * (w.is_k ? p.k_held.sh : p.v_held.sh), y);
+          }
+        } else if (mapped) {
+          store_raw((w.is_k ? k_to : v_to) + w.first * (w.is_k ? p.kc.sh : p.vc.sh), y);
         }
       }
     }
@@ -323,7 +345,7 @@ cudaError_t launch(const AppendParams& p, cudaStream_t st) {
 }  // namespace
 
 cudaError_t launch_append(AppendParams& p, int dtype, int D, bool four, int num_sms, cudaStream_t st) {
-  const int slots = 256 / D, most = (p.H + 2 * p.Hkv + slots - 1) / slots;
+  const int slots = 256 / D, most = (p.H + slots - 1) / slots + 2 * ((p.Hkv + slots - 1) / slots);
   const int64_t tokens = (int64_t)p.B * p.n_new, want = kAppendWarps * (int64_t)num_sms / tokens;
   p.parts = want < 1 ? 1 : want > most ? most : (int)want;
   auto typed = [&](auto zero) {
