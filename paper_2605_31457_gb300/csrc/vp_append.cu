@@ -146,34 +146,45 @@ __device__ __forceinline__ void load_angles(const RotView& r, const int (&at)[3]
 // it (called by the whole warp): the scale, the codes of the values, the first in
 // the lowest bits, and in x what they stand for.
 __device__ __forceinline__ uint32_t quantise(float (&x)[8], __half& scale) {
-  uint32_t top = 0;  // the magnitude's bits: NaN above everything
+  auto larger = [](float a, float b) {  // of magnitudes; NaN above everything
+    float y;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+    return y;
+  };
+  float top = fabsf(x[0]);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
-  top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-  top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-  const bool nan = top > 0x7f800000u;
-  const uint32_t t = __float_as_uint(__fmul_rn(__uint_as_float(top), (float)(1 / 7.5)));
-  const float up = __uint_as_float((t + 0xfffffu) & ~0xfffffu);
+  for (int e = 1; e < 8; ++e) top = larger(top, fabsf(x[e]));
+  top = larger(top, __shfl_xor_sync(0xffffffffu, top, 1));
+  top = larger(top, __shfl_xor_sync(0xffffffffu, top, 2));
+  const bool nan = isnan(top);
+  const float t = __fmul_rn(top, (float)(1 / 7.5));
+  const float up = __uint_as_float((__float_as_uint(t) + 0xfffffu) & ~0xfffffu);
   const float step = nan ? 1.f : fminf(fmaxf(up, kLeastStep4), kMostStep4);
   scale = nan ? __ushort_as_half(0x7fff) : __float2half_rn(step);
   const float inv = __frcp_rn(step), held = nan ? __uint_as_float(0x7fffffffu) : step;
-  // Rounding to whole numbers by an addition: floats in [2^23, 2^24) are those, and
-  // 8 more than 1.5 * 2^23 leaves the code in the lowest bits.
-  constexpr float kWhole = 12582920.f;
-  uint32_t codes = 0;
+  if (up > kMostStep4) {  // cut to what the largest scale holds
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const float whole = __fadd_rn(fminf(fmaxf(__fmul_rn(x[e], inv), -8.f), 7.f), kWhole);
-    codes |= (__float_as_uint(whole) & 15u) << (4 * e);
-    x[e] = (whole - kWhole) * held;
+    for (int e = 0; e < 8; ++e) x[e] = fminf(fmaxf(x[e], -8.f * kMostStep4), 8.f * kMostStep4);
   }
+  // Rounding to whole numbers by an addition, floats from 2^23 to 2^24 being those;
+  // |x / step| <= 7.5 (a little more by rounding) leaves at least -8.
+  constexpr float kWhole = 12582912.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] = __fadd_rn(fminf(__fmul_rn(x[e], inv), 7.f), kWhole) - kWhole;
+  // Four codes side by side, 8 added to each: a whole number below 2^16.
+  auto four = [&](int e) {
+    return __float_as_uint(fmaf(fmaf(x[e + 3], 16.f, x[e + 2]), 256.f, fmaf(x[e + 1], 16.f, x[e])) + (8388608.f + 34952.f));
+  };
+  const uint32_t codes = prmt(four(0), four(4), 0x5410);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] *= held;
   return codes;
 }
 
 template <typename T, int D, bool Q4>
-__global__ void __launch_bounds__(kAppendThreads) k_append(const __grid_constant__ AppendParams p) {
+__global__ void __launch_bounds__(kAppendThreads, Q4 ? 8 : 6) k_append(const __grid_constant__ AppendParams p) {
   constexpr int L = D / 8, SLOTS = 32 / L;  // lanes of a row, rows of a warp at a time
-  constexpr int U = 24 / Raw8<T>::N;        // of a lane in flight
+  constexpr int U = 16 / Raw8<T>::N;        // of a lane in flight
   const int lane = threadIdx.x & 31, chunk = lane % L, slot = lane / L;
   pdl_wait();
   const unsigned unit = uniform(blockIdx.x * (kAppendThreads / 32) + threadIdx.x / 32);
