@@ -503,7 +503,9 @@ vp_status vp_append4(vp_ctx* ctx, int32_t batch, int32_t n_new, const vp_rows* q
                      const vp_rows* k_held, const vp_rows* v_held, void* cuda_stream);
 
 /* Allocates the workspace of vp_attend4 on a context, once, for calls of up to
- * max_new new tokens per sequence: some MB.  Waits for the device; call it outside
+ * max_new new tokens per sequence: tens of MB, and for bf16 contexts where max_new *
+ * G > 64 room for bf16 caches of as many sequences as fit 1 GiB (one at least), by
+ * way of which calls of that many rows go.  Waits for the device; call it outside
  * stream capture.  A second call replaces the first one's workspace: graphs that
  * captured vp_attend4 before it must not be replayed.  VP_ERR_INVALID_ARG for
  * max_new < 1 or max_new > max_seq; VP_ERR_CUDA when the allocation fails (the
@@ -518,7 +520,9 @@ vp_status vp_reserve4(vp_ctx* ctx, int32_t max_new);
  * VP_ERR_UNSUPPORTED.  Logits are products of queries and codes, scaled and summed
  * in float.  bf16 contexts: the probabilities, and their products with the values'
  * scales, are rounded to fp16 (2^-11 of each; the output's own rounding is 2^-8);
- * fp32 contexts: both are two fp16 terms.  VP_ERR_CAPACITY when vp_reserve4 has not
+ * with n_new * G > 64 (pages of at least 8 tokens) the held values are first rounded
+ * to bf16, which vp_append4's are exactly, and vp_attend_new's bounds hold.  fp32
+ * contexts: both are two fp16 terms.  VP_ERR_CAPACITY when vp_reserve4 has not
  * reserved for n_new.  Allocates nothing and never synchronises; every kernel waits
  * for the stream's previous work, so an input may be the output of the preceding
  * call of this library.

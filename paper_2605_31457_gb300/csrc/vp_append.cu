@@ -182,7 +182,7 @@ __device__ __forceinline__ uint32_t quantise(float (&x)[8], __half& scale) {
 }
 
 template <typename T, int D, bool Q4>
-__global__ void __launch_bounds__(kAppendThreads, Q4 ? 8 : 6) k_append(const __grid_constant__ AppendParams p) {
+__global__ void __launch_bounds__(kAppendThreads, Q4 ? 7 : 6) k_append(const __grid_constant__ AppendParams p) {
   constexpr int L = D / 8, SLOTS = 32 / L;  // lanes of a row, rows of a warp at a time
   constexpr int U = 16 / Raw8<T>::N;        // of a lane in flight
   const int lane = threadIdx.x & 31, chunk = lane % L, slot = lane / L;

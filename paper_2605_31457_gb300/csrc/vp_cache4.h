@@ -55,7 +55,56 @@ cudaError_t launch_append(AppendParams& p, int dtype, int D, bool four, int num_
 struct Attend4Params : AttendParams {
   Kv4View k4, v4;
 };
-// The workspace of vp_attend4 (vp_reserve4) is that of vp_attend_new.
+
+// Calls of many query rows unpack the tokens that they see into bf16 caches of the
+// workspace (exactly, for vp_append4's scales) and run the kernels of vp_attend_new
+// on those: a group of sequences at a time, as many as the workspace holds.
+constexpr int kStageRows = 128;  // more query rows than this per (sequence, kv-head)
+constexpr size_t kStageBytes = (size_t)1 << 30;
+inline bool stages(int dtype, int paged, int page_size, int64_t R) {
+  return dtype == 0 && (!paged || page_size >= 8) && R > kStageRows;
+}
+
+// The workspace of vp_attend4 (vp_reserve4): that of vp_attend_new, then the staged
+// caches, K and V each [seqs][Hkv][rows][D] or, paged, [seqs * pages][Hkv][page_size][D]
+// with their block table [seqs][pages].
+struct Layout4 : NewLayout {
+  int seqs = 0, rows = 0, pages = 0;
+  size_t o_k = 0, o_v = 0, o_table = 0;
+};
+inline Layout4 layout4(int max_batch, int H, int Hkv, int D, int max_seq, int max_new, int dtype, int paged, int page_size,
+                       int num_sms) {
+  Layout4 w;
+  static_cast<NewLayout&>(w) = new_layout(max_batch, H, Hkv, D, max_seq, max_new, 0, num_sms);
+  if (!stages(dtype, paged, page_size, (int64_t)max_new * (H / Hkv))) return w;
+  const int unit = paged ? page_size : kTcTile;
+  w.pages = (max_seq + unit - 1) / unit;
+  w.rows = w.pages * unit;
+  const size_t one = (size_t)Hkv * w.rows * D * 2;  // bytes of a sequence's K or V
+  const size_t fit = kStageBytes / (2 * one);
+  w.seqs = fit < 1 ? 1 : fit < (size_t)max_batch ? (int)fit : max_batch;
+  w.o_k = w.total;
+  w.o_v = ws_round(w.o_k + w.seqs * one);
+  w.o_table = ws_round(w.o_v + w.seqs * one);
+  w.total = ws_round(w.o_table + (paged ? (size_t)w.seqs * w.pages * 4 : 0));
+  return w;
+}
+
+struct Unpack4Params {
+  int B, Hkv, D, max_seq, n_new;
+  int paged, page_size, page_shift;
+  Kv4View k4, v4;
+  void *k, *v;         // staged caches
+  int rows, pages;     // Layout4's
+  int32_t* table;      // paged
+  const int32_t* seq_len;
+  const int32_t* new_len;
+  int window, sinks;
+  unsigned* err;
+  int num_sms;
+};
+cudaError_t launch_unpack4(const Unpack4Params& p, cudaStream_t s);
+
 void plan_attend4(Attend4Params& p);
 cudaError_t configure_attend4();
 cudaError_t launch_attend4(const Attend4Params& p, cudaStream_t s);

@@ -162,13 +162,17 @@ vp_status reserve4(vp_ctx* ctx, int32_t max_new) {
   if (e != cudaSuccess) return cuda_fail(ctx, "vp_reserve4", e);
   if (ctx->ws4) cudaFree(ctx->ws4);
   ctx->ws4 = nullptr;
-  ctx->lay4 = vp::NewLayout();
-  const vp::NewLayout lay = vp::new_layout(c.max_batch, c.num_q_heads, c.num_kv_heads, c.head_dim, c.max_seq, max_new, 0,
-                                           ctx->num_sms);
+  ctx->lay4 = vp::Layout4();
+  const vp::Layout4 lay = vp::layout4(c.max_batch, c.num_q_heads, c.num_kv_heads, c.head_dim, c.max_seq, max_new, c.dtype,
+                                      c.paged, c.page_size, ctx->num_sms);
   e = vp::configure_attend4();
+  if (e == cudaSuccess && lay.seqs > 0) e = vp::configure_attend();
   if (e == cudaSuccess) e = cudaMalloc(&ctx->ws4, lay.total);
   if (e == cudaSuccess) {
     e = cudaMemset(static_cast<char*>(ctx->ws4) + lay.o_tk, 0, lay.o_lse - lay.o_tk);
+    if (e == cudaSuccess && lay.seqs > 0) {  // pages that no call has filled are not mapped
+      e = cudaMemset(static_cast<char*>(ctx->ws4) + lay.o_table, 0xff, lay.total - lay.o_table);
+    }
     if (e == cudaSuccess) e = cudaDeviceSynchronize();
     if (e != cudaSuccess) cudaFree(ctx->ws4);
   }
@@ -179,6 +183,51 @@ vp_status reserve4(vp_ctx* ctx, int32_t max_new) {
   }
   ctx->lay4 = lay;
   return VP_OK;
+}
+
+// The call by way of bf16 caches of the workspace, a group of sequences at a time.
+cudaError_t staged(const vp::Attend4Params& all, const vp::Layout4& lay, char* ws, cudaStream_t st) {
+  const int64_t row = (int64_t)lay.rows * all.D;  // elements of a staged (sequence, kv-head)
+  const int64_t page = (int64_t)all.page_size * all.D;
+  for (int b0 = 0; b0 < all.B; b0 += lay.seqs) {
+    vp::Attend4Params p = all;
+    p.B = all.B - b0 < lay.seqs ? all.B - b0 : lay.seqs;
+    p.q.data = static_cast<uint16_t*>(all.q.data) + b0 * all.q.sb;
+    p.out.data = static_cast<uint16_t*>(all.out.data) + b0 * all.out.sb;
+    p.seq_len = all.seq_len + b0;
+    if (all.new_len) p.new_len = all.new_len + b0;
+    if (all.lse) p.lse = all.lse + (int64_t)b0 * all.n_new * all.H;
+    vp::Unpack4Params u = {};
+    u.B = p.B; u.Hkv = p.Hkv; u.D = p.D; u.max_seq = p.max_seq; u.n_new = p.n_new;
+    u.paged = p.paged; u.page_size = p.page_size; u.page_shift = p.page_shift;
+    u.k4 = all.k4; u.v4 = all.v4;
+    for (vp::Kv4View* x : {&u.k4, &u.v4}) {
+      if (p.paged) {
+        x->block_table += (int64_t)b0 * x->max_pages;
+      } else {
+        x->codes += b0 * x->cb;
+        x->scales += b0 * x->sb;
+      }
+    }
+    u.k = ws + lay.o_k; u.v = ws + lay.o_v;
+    u.rows = lay.rows; u.pages = lay.pages;
+    u.table = reinterpret_cast<int32_t*>(ws + lay.o_table);
+    u.seq_len = p.seq_len; u.new_len = p.new_len;
+    u.window = p.window; u.sinks = p.sinks;
+    u.err = p.err; u.num_sms = p.num_sms;
+    cudaError_t e = vp::launch_unpack4(u, st);
+    if (e != cudaSuccess) return e;
+    if (p.paged)
+      p.k = vp::KvView{u.k, p.Hkv * page, page, p.D, u.table, lay.pages, lay.seqs * lay.pages};
+    else
+      p.k = vp::KvView{u.k, p.Hkv * row, row, p.D, nullptr, 0, 0};
+    p.v = p.k;
+    p.v.data = u.v;
+    vp::plan_attend(p);
+    e = vp::launch_attend(p, st);
+    if (e != cudaSuccess) return e;
+  }
+  return cudaSuccess;
 }
 
 vp_status attend4(vp_ctx* ctx, int32_t batch, int32_t n_new, const vp_rows* q, const vp_kv4* k_cache,
@@ -226,8 +275,14 @@ vp_status attend4(vp_ctx* ctx, int32_t batch, int32_t n_new, const vp_rows* q, c
   p.tickets = reinterpret_cast<unsigned*>(ws + ctx->lay4.o_tk);
   p.err = ctx->err;
   p.num_sms = ctx->num_sms;
-  vp::plan_attend4(p);
-  const cudaError_t e = vp::launch_attend4(p, static_cast<cudaStream_t>(cuda_stream));
+  const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  cudaError_t e = cudaSuccess;
+  if (vp::stages(p.dtype, p.paged, p.page_size, p.R)) {
+    e = staged(p, ctx->lay4, ws, st);
+  } else {
+    vp::plan_attend4(p);
+    e = vp::launch_attend4(p, st);
+  }
   if (e != cudaSuccess) return cuda_fail(ctx, "vp_attend4: launch", e);
   return VP_OK;
 }

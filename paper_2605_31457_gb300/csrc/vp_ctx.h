@@ -11,6 +11,7 @@
 
 #include "vp.h"
 #include "vp_attend.h"
+#include "vp_cache4.h"
 #include "vp_internal.h"
 
 struct vp_ctx {
@@ -43,7 +44,7 @@ struct vp_ctx {
   void* new_ws = nullptr;  // workspace of vp_attend_new (vp_reserve_new)
   vp::NewLayout new_lay;
   void* ws4 = nullptr;  // workspace of vp_attend4 (vp_reserve4)
-  vp::NewLayout lay4;
+  vp::Layout4 lay4;
 };
 
 namespace vp {
