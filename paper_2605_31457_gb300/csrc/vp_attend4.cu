@@ -65,10 +65,14 @@ struct Cfg4 {
   // A warp's ring, and behind it its output to be joined, float [RS][D] (in the ring where there is no room).
   static constexpr int RING = S * STAGE;
   static constexpr int OUT = RS * D * 4;
-  static constexpr bool APART = kWarps4 * (RING + OUT) <= 232448 / CPS - 3072;
+  static constexpr bool APART = kWarps4 * (RING + OUT) <= 232448 / CPS - 3072 - NT * TERMS * GROUPS * 512;
   static constexpr int WARP = APART ? RING + OUT : RING > OUT ? RING : OUT;
   static constexpr int OFF_O = APART ? RING : 0;
-  static constexpr int OFF_ML = kWarps4 * WARP;                // float2 [warps][RS]
+  // The queries as the products take them: in registers, or uint4 [NT][TERMS][GROUPS][32] and float [RS] factors.
+  static constexpr bool Q_REGS = NT * TERMS == 1;
+  static constexpr int OFF_Q = kWarps4 * WARP;
+  static constexpr int OFF_FAC = OFF_Q + (Q_REGS ? 0 : NT * TERMS * GROUPS * 512);
+  static constexpr int OFF_ML = OFF_FAC + RS * 4;              // float2 [warps][RS]
   static constexpr int OFF_MASK = OFF_ML + kWarps4 * RS * 8;   // unsigned [warps][S]: tokens copied
   static constexpr int OFF_MISC = OFF_MASK + kWarps4 * S * 4;  // int: line_start, a flag
   static constexpr int LINE = kWarps4 + 7;
@@ -268,12 +272,14 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
     for (int k = 0; k < S - 1; ++k) issue(q.u0 + k);
 
     // ---- queries: 8 dimensions of each group a lane, in the order of the codes
-    uint32_t qf[NT][TERMS][NG][4];
+    uint4 q_regs[C::Q_REGS ? NG : 1];
     float fac[NT][2];
     int tq[NT][2];
     const int base = q.sq.len - q.sq.n;
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
+    uint4* const q_smem = reinterpret_cast<uint4*>(smem + C::OFF_Q) + lane;
+    float* const fac_smem = reinterpret_cast<float*>(smem + C::OFF_FAC);
+#pragma unroll 1
+    for (int t = C::Q_REGS ? 0 : warp; t < NT; t += kWarps4) {  // a warp of the CTA does a tile of 8 rows for all of them
       const int row = 8 * t + r;
       float x[NG][8];
       float top = 0.f;
@@ -304,22 +310,41 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
       const float up = __uint_as_float((unsigned)field << 23), down = __uint_as_float((unsigned)(254 - field) << 23);
 #pragma unroll
       for (int g = 0; g < NG; ++g) {
+        uint32_t hi[4], lo[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {  // dimensions k and k + 4 meet one mask
           const float a = x[g][k] * up, b = x[g][k + 4] * up;
-          qf[t][0][g][k] = pack_f16(a, b);
-          if constexpr (TERMS == 2) {
-            const float2 h = unpack_f16(qf[t][0][g][k]);
-            qf[t][TERMS - 1][g][k] = pack_f16(a - h.x, b - h.y);
-          }
+          hi[k] = pack_f16(a, b);
+          const float2 h = unpack_f16(hi[k]);
+          lo[k] = pack_f16(a - h.x, b - h.y);
+        }
+        if constexpr (C::Q_REGS) {
+          q_regs[g] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+        } else {
+          q_smem[(t * TERMS * NG + g) * 32] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+          if constexpr (TERMS == 2) q_smem[(t * TERMS * NG + NG + g) * 32] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
         }
       }
       const float f = down * p.c_log2;
-      fac[t][0] = __shfl_sync(0xffffffffu, f, 8 * c);
-      fac[t][1] = __shfl_sync(0xffffffffu, f, 8 * c + 4);
-#pragma unroll
-      for (int k = 0; k < 2; ++k) tq[t][k] = base + row_token(p, q.it.row0 + min(8 * t + 2 * c + k, rows - 1));
+      if constexpr (C::Q_REGS) {
+        fac[0][0] = __shfl_sync(0xffffffffu, f, 8 * c);
+        fac[0][1] = __shfl_sync(0xffffffffu, f, 8 * c + 4);
+      } else if (c == 0) {
+        fac_smem[row] = f;
+      }
     }
+    if constexpr (!C::Q_REGS) __syncthreads();  // (the last part's were read before the barrier behind it)
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        if constexpr (!C::Q_REGS) fac[t][k] = fac_smem[8 * t + 2 * c + k];
+        tq[t][k] = base + row_token(p, q.it.row0 + min(8 * t + 2 * c + k, rows - 1));
+      }
+    auto query = [&](int t, int m, int g) {
+      if constexpr (C::Q_REGS) return q_regs[g];
+      else return q_smem[((t * TERMS + m) * NG + g) * 32];
+    };
     const int t0 = base + row_token(p, q.it.row0), t1 = base + row_token(p, q.it.row0 + rows - 1);
 
     float o[NT][NG][2][4], ref[NT][2], l[NT][2];
@@ -347,127 +372,123 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
       const int jt = first_token(u);
       const bool all_see = turn == 0xffffffffu && jt + kStep4 - 1 <= t0 &&
                            (p.window < 0 || jt > t1 - p.window || jt + kStep4 <= p.sinks);
+      const unsigned at = ring + st * C::STAGE;
+      const unsigned char* const scales = mine + st * C::STAGE + 2 * C::CODES;
+
+      // ---- logits: tokens r and r + 8 of each half, query rows 2c and 2c + 1
+      float z[2][NT][4];
 #pragma unroll
-      for (int half = 0; half < kStep4; half += 16) {
-        const unsigned at = ring + st * C::STAGE;
-        const unsigned char* const scales = mine + st * C::STAGE + 2 * C::CODES + half * 2 * NG;
-        const int j0 = jt + half;
-        // ---- logits: tokens r and r + 8, query rows 2c and 2c + 1
-        uint32_t k0[NG], k1[NG];
+      for (int gp = 0; gp < NG; gp += 2) {
+        uint32_t kw[2][2][2];  // half, group, tokens 0-7 or 8-15
+        float2 ks[2][2];       // half, tokens: the two groups' scales
 #pragma unroll
-        for (int g = 0; g < NG; g += 2)
-          ldsm_x4(at + code_at<D>(half + mrow, g + mch), k0[g], k1[g], k0[g + 1], k1[g + 1]);
-        float ks0[NG], ks1[NG];
-        {
+        for (int h = 0; h < 2; ++h) {
+          ldsm_x4(at + code_at<D>(16 * h + mrow, gp + mch), kw[h][0][0], kw[h][0][1], kw[h][1][0], kw[h][1][1]);
 #pragma unroll
-          for (int g = 0; g < NG; g += 2) {
-            const float2 a = unpack_f16(*reinterpret_cast<const uint32_t*>(scales + r * 2 * NG + 2 * g));
-            const float2 b = unpack_f16(*reinterpret_cast<const uint32_t*>(scales + (r + 8) * 2 * NG + 2 * g));
-            ks0[g] = a.x; ks0[g + 1] = a.y;
-            ks1[g] = b.x; ks1[g + 1] = b.y;
-          }
+          for (int k = 0; k < 2; ++k)
+            ks[h][k] = unpack_f16(*reinterpret_cast<const uint32_t*>(scales + (16 * h + 8 * k + r) * 2 * NG + 2 * gp));
         }
-        float z[NT][4];
 #pragma unroll
-        for (int g = 0; g < NG; ++g) {
-          const uint32_t x0 = k0[g] >> 8, x1 = k1[g] >> 8;
-          const uint32_t a0 = codes.low(k0[g]), a1 = codes.low(k1[g]), a2 = codes.high(k0[g]), a3 = codes.high(k1[g]);
-          const uint32_t b0 = codes.low(x0), b1 = codes.low(x1), b2 = codes.high(x0), b3 = codes.high(x1);
+        for (int gg = 0; gg < 2; ++gg) {
+          const int g = gp + gg;
+          uint32_t a[2][8];
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              const uint32_t x = kw[h][gg][k], y = x >> 8;
+              a[h][k] = codes.low(x);
+              a[h][2 + k] = codes.high(x);
+              a[h][4 + k] = codes.low(y);
+              a[h][6 + k] = codes.high(y);
+            }
 #pragma unroll
           for (int t = 0; t < NT; ++t) {
-            float s[4];
-            mma_f16_first(s, a0, a1, a2, a3, qf[t][0][g][0], qf[t][0][g][1]);
-            mma_f16(s, b0, b1, b2, b3, qf[t][0][g][2], qf[t][0][g][3]);
-            if constexpr (TERMS == 2) {
-              mma_f16(s, a0, a1, a2, a3, qf[t][TERMS - 1][g][0], qf[t][TERMS - 1][g][1]);
-              mma_f16(s, b0, b1, b2, b3, qf[t][TERMS - 1][g][2], qf[t][TERMS - 1][g][3]);
-            }
+            const uint4 b = query(t, 0, g);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const float step = k < 2 ? ks0[g] : ks1[g];
-              z[t][k] = g == 0 ? s[k] * step : fmaf(s[k], step, z[t][k]);
-            }
-          }
-        }
+            for (int h = 0; h < 2; ++h) {
+              float s[4];
+              mma_f16_first(s, a[h][0], a[h][1], a[h][2], a[h][3], b.x, b.y);
+              mma_f16(s, a[h][4], a[h][5], a[h][6], a[h][7], b.z, b.w);
+              if constexpr (TERMS == 2) {
+                const uint4 d = query(t, TERMS - 1, g);
+                mma_f16(s, a[h][0], a[h][1], a[h][2], a[h][3], d.x, d.y);
+                mma_f16(s, a[h][4], a[h][5], a[h][6], a[h][7], d.z, d.w);
+              }
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          z[t][0] *= fac[t][0]; z[t][1] *= fac[t][1];
-          z[t][2] *= fac[t][0]; z[t][3] *= fac[t][1];
-        }
-        if (!all_see) {
-#pragma unroll
-          for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const int row = r + 8 * (k >> 1);
-              if (!((turn >> (half + row)) & 1u) || !sees(j0 + row, tq[t][k & 1], p.window, p.sinks)) z[t][k] = -CUDART_INF_F;
-            }
-        }
-
-        // ---- V's scales: of tokens 2c, 2c + 1 (s0) and 2c + 8, 2c + 9 (s1), a group each
-        uint32_t s0[NG], s1[NG];
-        uint32_t any = 0;
-        {
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            uint32_t w[NG];  // two tokens' scales
-            if constexpr (NG == 4) {
-              const uint4 v = *reinterpret_cast<const uint4*>(scales + C::SCALES + (2 * c + 8 * h) * 8);
-              w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
-            } else {
-              const uint2 v = *reinterpret_cast<const uint2*>(scales + C::SCALES + (2 * c + 8 * h) * 4);
-              w[0] = v.x; w[1] = v.y;
-            }
-#pragma unroll
-            for (int g = 0; g < NG; g += 2) {
-              const uint32_t x = w[g / 2], y = w[NG / 2 + g / 2];
-              any |= x | y;
-              (h ? s1 : s0)[g] = prmt(x, y, 0x5410);
-              (h ? s1 : s0)[g + 1] = prmt(x, y, 0x7632);
+              for (int k = 0; k < 4; ++k) {
+                const float step = gg ? ks[h][k >> 1].y : ks[h][k >> 1].x;
+                z[h][t][k] = g == 0 ? s[k] * step : fmaf(s[k], step, z[h][t][k]);
+              }
             }
           }
         }
-
-        // ---- the references
-        bool need = false;
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-          for (int k = 0; k < 2; ++k) need |= fmaxf(z[t][k], z[t][2 + k]) > ref[t][k] + (above + kRaise4);
-        const bool big = (any & 0x40004000u) != 0;  // a scale of 2 or more
-        if (__any_sync(0xffffffffu, need || (big && !large))) {
-          float fv = 1.f;
-          if (!large && __any_sync(0xffffffffu, big)) {
-            large = true;
-            if constexpr (TERMS == 1) above = kAbove4 - kBig4;
-            else fv = v_unit = 3.0517578125e-05f;  // 2^-kBig4
-          }
+          for (int k = 0; k < 4; ++k) z[h][t][k] *= fac[t][k & 1];
+      if (!all_see) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
           for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-              const float top = group_max(fmaxf(z[t][k], z[t][2 + k]));
-              const float next = fmaxf(ref[t][k], top - above);
-              const float f = ref[t][k] == -CUDART_INF_F ? 0.f : fexp2(ref[t][k] - next);
-              ref[t][k] = next;
-              l[t][k] *= f;
-              const float fo = TERMS == 1 ? f : f * fv;
-#pragma unroll
-              for (int g = 0; g < NG; ++g)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                  o[t][g][h][k] *= fo;
-                  o[t][g][h][2 + k] *= fo;
-                }
+            for (int k = 0; k < 4; ++k) {
+              const int row = 16 * h + r + 8 * (k >> 1);
+              if (!((turn >> row) & 1u) || !sees(jt + row, tq[t][k & 1], p.window, p.sinks)) z[h][t][k] = -CUDART_INF_F;
             }
-        }
+      }
 
-        // ---- probabilities, transposed: query row r, tokens as in s0 and s1
+      // ---- the references
+      bool need = false;
+      auto largest = [&](int t, int k) { return fmaxf(fmaxf(z[0][t][k], z[0][t][2 + k]), fmaxf(z[1][t][k], z[1][t][2 + k])); };
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) need |= largest(t, k) > ref[t][k] + (above + kRaise4);
+      uint32_t any = 0;  // of V's scales of token `lane`: one of 2 or more?
+#pragma unroll
+      for (int g = 0; g < NG; g += 2) any |= *reinterpret_cast<const uint32_t*>(scales + C::SCALES + lane * 2 * NG + 2 * g);
+      const bool big = (any & 0x40004000u) != 0;
+      if (__any_sync(0xffffffffu, need || (big && !large))) {
+        float fv = 1.f;
+        if (!large && __any_sync(0xffffffffu, big)) {
+          large = true;
+          if constexpr (TERMS == 1) above = kAbove4 - kBig4;
+          else fv = v_unit = 3.0517578125e-05f;  // 2^-kBig4
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const float top = group_max(largest(t, k));
+            const float next = fmaxf(ref[t][k], top - above);
+            const float f = ref[t][k] == -CUDART_INF_F ? 0.f : fexp2(ref[t][k] - next);
+            ref[t][k] = next;
+            l[t][k] *= f;
+            const float fo = TERMS == 1 ? f : f * fv;
+#pragma unroll
+            for (int g = 0; g < NG; ++g)
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                o[t][g][h][k] *= fo;
+                o[t][g][h][2 + k] *= fo;
+              }
+          }
+      }
+
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        // ---- probabilities, transposed: query row r, tokens 2c, 2c + 1 and 2c + 8, 2c + 9
         uint32_t ph[NT][2], pl[NT][2];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
           const float m0 = ref[t][0] == -CUDART_INF_F ? 0.f : ref[t][0], m1 = ref[t][1] == -CUDART_INF_F ? 0.f : ref[t][1];
-          const float e0 = fexp2(z[t][0] - m0), e1 = fexp2(z[t][1] - m1), e2 = fexp2(z[t][2] - m0), e3 = fexp2(z[t][3] - m1);
+          const float e0 = fexp2(z[h][t][0] - m0), e1 = fexp2(z[h][t][1] - m1);
+          const float e2 = fexp2(z[h][t][2] - m0), e3 = fexp2(z[h][t][3] - m1);
           l[t][0] += e0 + e2;
           l[t][1] += e1 + e3;
           const uint32_t h0 = pack_f16(e0, e1), h1 = pack_f16(e2, e3);
@@ -480,36 +501,64 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
           }
         }
 
-        // ---- output: dimensions 32 g + 4 r + 2 h and the next, query rows 2c, 2c + 1
-        uint32_t v0[NG], v1[NG];
+        // ---- V's scales of those tokens, two of a group in a register
+        uint32_t sc[NG][2];
 #pragma unroll
-        for (int g = 0; g < NG; g += 2)
-          ldsm_x4_t(at + C::CODES + code_at<D>(half + mrow, g + mch), v0[g], v1[g], v0[g + 1], v1[g + 1]);
+        for (int k = 0; k < 2; ++k) {
+          uint32_t w[NG];
+          const unsigned char* const two = scales + C::SCALES + (16 * h + 8 * k + 2 * c) * 2 * NG;
+          if constexpr (NG == 4) {
+            const uint4 v = *reinterpret_cast<const uint4*>(two);
+            w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+          } else {
+            const uint2 v = *reinterpret_cast<const uint2*>(two);
+            w[0] = v.x; w[1] = v.y;
+          }
 #pragma unroll
-        for (int g = 0; g < NG; ++g) {
-          const uint32_t x0 = v0[g] >> 8, x1 = v1[g] >> 8;
-          const uint32_t a0 = codes.low(v0[g]), a1 = codes.high(v0[g]), a2 = codes.low(v1[g]), a3 = codes.high(v1[g]);
-          const uint32_t b0 = codes.low(x0), b1 = codes.high(x0), b2 = codes.low(x1), b3 = codes.high(x1);
+          for (int g = 0; g < NG; g += 2) {
+            sc[g][k] = prmt(w[g / 2], w[NG / 2 + g / 2], 0x5410);
+            sc[g + 1][k] = prmt(w[g / 2], w[NG / 2 + g / 2], 0x7632);
+          }
+        }
+
+        // ---- output: dimensions 32 g + 4 r + 2 x and the next, query rows 2c, 2c + 1
 #pragma unroll
-          for (int t = 0; t < NT; ++t) {
-            if constexpr (TERMS == 1) {
-              const uint32_t w0 = mul_f16(ph[t][0], s0[g]), w1 = mul_f16(ph[t][1], s1[g]);
-              mma_f16(o[t][g][0], a0, a1, a2, a3, w0, w1);
-              mma_f16(o[t][g][1], b0, b1, b2, b3, w0, w1);
-            } else {
-              uint32_t hi[2], lo[2];
+        for (int gp = 0; gp < NG; gp += 2) {
+          uint32_t vw[2][2];
+          ldsm_x4_t(at + C::CODES + code_at<D>(16 * h + mrow, gp + mch), vw[0][0], vw[0][1], vw[1][0], vw[1][1]);
 #pragma unroll
-              for (int k = 0; k < 2; ++k) {
-                const float2 x = unpack_f16(ph[t][k]), y = unpack_f16(pl[t][k]), s = unpack_f16(k ? s1[g] : s0[g]);
-                const float a = (x.x + y.x) * (s.x * v_unit), b = (x.y + y.y) * (s.y * v_unit);
-                hi[k] = pack_f16(a, b);
-                const float2 h = unpack_f16(hi[k]);
-                lo[k] = pack_f16(a - h.x, b - h.y);
+          for (int gg = 0; gg < 2; ++gg) {
+            const int g = gp + gg;
+            uint32_t a[8];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              const uint32_t x = vw[gg][k], y = x >> 8;
+              a[2 * k] = codes.low(x);
+              a[2 * k + 1] = codes.high(x);
+              a[4 + 2 * k] = codes.low(y);
+              a[5 + 2 * k] = codes.high(y);
+            }
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+              if constexpr (TERMS == 1) {
+                const uint32_t w0 = mul_f16(ph[t][0], sc[g][0]), w1 = mul_f16(ph[t][1], sc[g][1]);
+                mma_f16(o[t][g][0], a[0], a[1], a[2], a[3], w0, w1);
+                mma_f16(o[t][g][1], a[4], a[5], a[6], a[7], w0, w1);
+              } else {
+                uint32_t hi[2], lo[2];
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                  const float2 x = unpack_f16(ph[t][k]), y = unpack_f16(pl[t][k]), s = unpack_f16(sc[g][k]);
+                  const float ea = (x.x + y.x) * (s.x * v_unit), eb = (x.y + y.y) * (s.y * v_unit);
+                  hi[k] = pack_f16(ea, eb);
+                  const float2 f = unpack_f16(hi[k]);
+                  lo[k] = pack_f16(ea - f.x, eb - f.y);
+                }
+                mma_f16(o[t][g][0], a[0], a[1], a[2], a[3], hi[0], hi[1]);
+                mma_f16(o[t][g][1], a[4], a[5], a[6], a[7], hi[0], hi[1]);
+                mma_f16(o[t][g][0], a[0], a[1], a[2], a[3], lo[0], lo[1]);
+                mma_f16(o[t][g][1], a[4], a[5], a[6], a[7], lo[0], lo[1]);
               }
-              mma_f16(o[t][g][0], a0, a1, a2, a3, hi[0], hi[1]);
-              mma_f16(o[t][g][1], b0, b1, b2, b3, hi[0], hi[1]);
-              mma_f16(o[t][g][0], a0, a1, a2, a3, lo[0], lo[1]);
-              mma_f16(o[t][g][1], b0, b1, b2, b3, lo[0], lo[1]);
             }
           }
         }
@@ -583,8 +632,9 @@ auto with_att4(int dtype, int D, int R, F&& f) {
   auto sized = [&](auto zero, auto dim) {
     if (R <= 8) return inst(zero, dim, std::integral_constant<int, 1>());
     if (R <= 16 || sizeof(zero) == 4) return inst(zero, dim, std::integral_constant<int, 2>());
-    if constexpr (sizeof(zero) == 2) return inst(zero, dim, std::integral_constant<int, 4>());
-    else return inst(zero, dim, std::integral_constant<int, 2>());
+    if constexpr (sizeof(zero) == 2) {
+      return R <= 24 ? inst(zero, dim, std::integral_constant<int, 3>()) : inst(zero, dim, std::integral_constant<int, 4>());
+    } else return inst(zero, dim, std::integral_constant<int, 2>());
   };
   using D64 = std::integral_constant<int, 64>;
   using D128 = std::integral_constant<int, 128>;
@@ -598,7 +648,7 @@ cudaError_t configure_attend4() {
   cudaError_t e = cudaSuccess;
   for (int dtype : {0, 1})
     for (int D : {64, 128})
-      for (int R : {8, 16, 32})
+      for (int R : {8, 16, 24, 32})
         if (e == cudaSuccess)
           e = with_att4(dtype, D, R, [](auto kernel, size_t smem, int, int) {
             return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);

@@ -59,7 +59,7 @@ struct Attend4Params : AttendParams {
 // Calls of many query rows unpack the tokens that they see into bf16 caches of the
 // workspace (exactly, for vp_append4's scales) and run the kernels of vp_attend_new
 // on those: a group of sequences at a time, as many as the workspace holds.
-constexpr int kStageRows = 128;  // more query rows than this per (sequence, kv-head)
+constexpr int kStageRows = 64;  // more query rows than this per (sequence, kv-head)
 constexpr size_t kStageBytes = (size_t)1 << 30;
 inline bool stages(int dtype, int paged, int page_size, int64_t R) {
   return dtype == 0 && (!paged || page_size >= 8) && R > kStageRows;
