@@ -184,11 +184,18 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
   const int kpage = (int)p.k4.cb, vpage = (int)p.v4.cb, kspage = (int)p.k4.sb, vspage = (int)p.v4.sb;
   const int in_page = p.paged ? p.page_size - 1 : -1;
 
-  while (next_part(p, walk, q)) {
+  uint4* const q_smem = reinterpret_cast<uint4*>(smem + C::OFF_Q) + lane;
+  float* const fac_smem = reinterpret_cast<float*>(smem + C::OFF_FAC);
+  // The part whose output is still to be joined.
+  int d_b = 0, d_g = 0, d_row0 = 0, d_rows = 0, d_c0 = 0, d_parts = 0;
+
+  for (bool more = true; more;) {
+    more = next_part(p, walk, q);
+    const int rows = more ? q.it.rows : 0;
+    if (!more) q.u0 = q.u1 = 0;
     const int n = q.u1 - q.u0;
-    const int rows = q.it.rows;
     // ---- rows that see nothing: padding, or all of an item without tiles
-    if (q.owner) {
+    if (more && q.owner) {
       const int first = q.it.tl.n == 0 ? 0 : rows;
 #pragma unroll 1
       for (int i = tid; i < (min(p.block, p.R - q.it.row0) - first) * (D / 4); i += kThreads4) {
@@ -197,35 +204,42 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
         if (i % (D / 4) == 0) store_lse(p, q.b, q.g, row, 0.f, 0.f);
       }
     }
-    if (n <= 0) continue;
+    if (more && n <= 0) continue;
     const SeenRange& sr = q.it.sr;
     auto first_token = [&](int u) { return q.it.tl.tile(u) * kTcTile + kStep4 * warp; };
 
     // ---- copies of the warp's 32 tokens of tile u, into stage u % S
-    const unsigned char* k_lane = p.k4.codes + q.g * p.k4.ch + 16 * cch;
-    const unsigned char* v_lane = p.v4.codes + q.g * p.v4.ch + 16 * cch;
+    const unsigned char* k_lane = p.k4.codes + q.g * p.k4.ch + (int64_t)crow * kt + 16 * cch;
+    const unsigned char* v_lane = p.v4.codes + q.g * p.v4.ch + (int64_t)crow * vt + 16 * cch;
     const uint16_t *ks_lane = p.k4.scales + q.g * p.k4.sh, *vs_lane = p.v4.scales + q.g * p.v4.sh;
     if (!p.paged) {
-      k_lane += q.b * p.k4.cb + (int64_t)crow * kt;
-      v_lane += q.b * p.v4.cb + (int64_t)crow * vt;
-      ks_lane += q.b * p.k4.sb + (int64_t)lane * kst;
-      vs_lane += q.b * p.v4.sb + (int64_t)lane * vst;
+      k_lane += q.b * p.k4.cb;
+      v_lane += q.b * p.v4.cb;
+      ks_lane += q.b * p.k4.sb;
+      vs_lane += q.b * p.v4.sb;
     }
-    int kn = 0, vn = 0;  // page ids of token `lane` of the next turn to be copied
-    auto lookup = [&](int u) {
+    int kn = 0, vn = 0;   // page ids of the next turn to be copied
+    unsigned partly = 0;  // bit of a stage: masks has which of its tokens were copied; else all of them
+    auto lookup = [&](int u) {  // page ids of token `lane` of tile u
       if (!p.paged || u >= q.u1) return;
       const int lp = (first_token(u) + lane) >> p.page_shift;
       kn = lp < p.k4.max_pages ? __ldg(p.k4.block_table + (int64_t)q.b * p.k4.max_pages + lp) : -1;
       vn = lp < p.v4.max_pages ? __ldg(p.v4.block_table + (int64_t)q.b * p.v4.max_pages + lp) : -1;
     };
-    unsigned partly = 0;  // bit of a stage: masks has which of its tokens were copied; else all of them
     auto issue = [&](int u) {
       if (u < q.u1) {
         const int st = (unsigned)(u - q.u0) % S;
-        const unsigned to = ring + st * C::STAGE;
-        const int j0 = first_token(u);
-        const bool ok = !p.paged || ((unsigned)kn < (unsigned)p.k4.num_pages && (unsigned)vn < (unsigned)p.v4.num_pages);
+        const unsigned to = ring + st * C::STAGE, s_st = s_to + st * C::STAGE;
+        const int j0 = first_token(u), j = j0 + lane;
         const bool whole = (j0 >= sr.lo && j0 + kStep4 <= sr.hi) || j0 + kStep4 <= sr.s_end;
+        unsigned mask = 0xffffffffu;
+        if (!whole || p.paged) {
+          const bool ok = !p.paged || ((unsigned)kn < (unsigned)p.k4.num_pages && (unsigned)vn < (unsigned)p.v4.num_pages);
+          bool live = j < sr.s_end || (j >= sr.lo && j < sr.hi);
+          if (live && !ok) err |= ERR_PAGE;
+          live = live && ok;
+          mask = __ballot_sync(0xffffffffu, live);
+        }
         if (whole && !p.paged) {
           partly &= ~(1u << st);
           const unsigned char *kc = k_lane + (int64_t)j0 * kt, *vc = v_lane + (int64_t)j0 * vt;
@@ -234,50 +248,98 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
             cp_async16(to + code_at<D>(crow + i, cch), kc + (int64_t)i * kt);
             cp_async16(to + C::CODES + code_at<D>(crow + i, cch), vc + (int64_t)i * vt);
           }
-          cp_async_or_zero<2 * NG>(s_to + st * C::STAGE, ks_lane + (int64_t)j0 * kst, true);
-          cp_async_or_zero<2 * NG>(s_to + st * C::STAGE + C::SCALES, vs_lane + (int64_t)j0 * vst, true);
+          cp_async_or_zero<2 * NG>(s_st, ks_lane + (int64_t)j * kst, true);
+          cp_async_or_zero<2 * NG>(s_st + C::SCALES, vs_lane + (int64_t)j * vst, true);
+        } else if (mask == 0xffffffffu && p.page_size >= 16) {
+          partly &= ~(1u << st);
+#pragma unroll
+          for (int h = 0; h < kStep4; h += 16) {
+            const int at = (j0 + h) & in_page;
+            const unsigned char* kc = k_lane + (int64_t)__shfl_sync(0xffffffffu, kn, h) * kpage + (int64_t)at * kt;
+            const unsigned char* vc = v_lane + (int64_t)__shfl_sync(0xffffffffu, vn, h) * vpage + (int64_t)at * vt;
+#pragma unroll
+            for (int i = 0; i < 16; i += ROWS) {
+              cp_async16(to + code_at<D>(h + crow + i, cch), kc + (int64_t)i * kt);
+              cp_async16(to + C::CODES + code_at<D>(h + crow + i, cch), vc + (int64_t)i * vt);
+            }
+          }
+          const int at = j & in_page;
+          cp_async_or_zero<2 * NG>(s_st, ks_lane + (int64_t)kn * kspage + (int64_t)at * kst, true);
+          cp_async_or_zero<2 * NG>(s_st + C::SCALES, vs_lane + (int64_t)vn * vspage + (int64_t)at * vst, true);
         } else {
           // A row's page is known to its lane.  A token that is not copied leaves
           // zeros, its scale's among them.
-          const int j = j0 + lane;
-          bool live = j < sr.s_end || (j >= sr.lo && j < sr.hi);
-          if (live && !ok) err |= ERR_PAGE;
-          live = live && ok;
-          const unsigned mask = __ballot_sync(0xffffffffu, live);
-          if (mask == 0xffffffffu) partly &= ~(1u << st);
-          else partly |= 1u << st;
+          partly |= 1u << st;
           if (lane == 0) masks[st] = mask;
-#pragma unroll
+#pragma unroll 1
           for (int i = 0; i < kStep4; i += ROWS) {
             const int row = crow + i;
             const int kr = __shfl_sync(0xffffffffu, kn, row), vr = __shfl_sync(0xffffffffu, vn, row);
             const bool copy = (mask >> row) & 1u;
-            const int at = p.paged ? (j0 + row) & in_page : j0 + i;  // contiguous: k_lane has the row
-            cp_async_or_zero<16>(to + code_at<D>(row, cch), copy ? k_lane + (int64_t)kr * kpage + (int64_t)at * kt : p.k4.codes, copy);
-            cp_async_or_zero<16>(to + C::CODES + code_at<D>(row, cch),
-                                 copy ? v_lane + (int64_t)vr * vpage + (int64_t)at * vt : p.v4.codes, copy);
+            const int64_t at = ((j0 + row) & in_page) - crow;  // k_lane is of row crow
+            cp_async_or_zero<16>(to + code_at<D>(row, cch), copy ? k_lane + (int64_t)kr * kpage + at * kt : p.k4.codes, copy);
+            cp_async_or_zero<16>(to + C::CODES + code_at<D>(row, cch), copy ? v_lane + (int64_t)vr * vpage + at * vt : p.v4.codes, copy);
           }
-          const int at = p.paged ? j & in_page : j0;
-          cp_async_or_zero<2 * NG>(s_to + st * C::STAGE,
-                                   live ? ks_lane + (int64_t)kn * kspage + (int64_t)at * kst : p.k4.scales, live);
-          cp_async_or_zero<2 * NG>(s_to + st * C::STAGE + C::SCALES,
-                                   live ? vs_lane + (int64_t)vn * vspage + (int64_t)at * vst : p.v4.scales, live);
+          const bool live = (mask >> lane) & 1u;
+          const int64_t at = j & in_page;
+          cp_async_or_zero<2 * NG>(s_st, live ? ks_lane + (int64_t)kn * kspage + at * kst : p.k4.scales, live);
+          cp_async_or_zero<2 * NG>(s_st + C::SCALES, live ? vs_lane + (int64_t)vn * vspage + at * vst : p.v4.scales, live);
         }
         lookup(u + 1);
       }
       cp_async_commit();
     };
-    lookup(q.u0);
+    auto begin = [&] {
+      lookup(q.u0);
 #pragma unroll 1
-    for (int k = 0; k < S - 1; ++k) issue(q.u0 + k);
-
+      for (int v = 0; v < S - 1; ++v) issue(q.u0 + v);
+    };
+    // The first copies are on their way while the last part's output is joined
+    // (unless that lies in the ring).
+    if (C::APART && more) begin();
+    if (d_parts > 0) {
+      // ---- the warps' outputs become rows of out or a record
+      __syncthreads();
+      const bool direct = !by_ticket(d_parts);
+      const int rec = record_of(blockIdx.x, d_c0) * RS;
+#pragma unroll 1
+      for (int i = tid; i < d_rows * (D / 4); i += kThreads4) {
+        const int row = i / (D / 4), d = 4 * (i % (D / 4));
+        float m = -CUDART_INF_F;
+#pragma unroll
+        for (int w = 0; w < kWarps4; ++w) m = fmaxf(m, ml_all[w * RS + row].x);
+        const float mu = m == -CUDART_INF_F ? 0.f : m;
+        float sum = 0.f;
+        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < kWarps4; ++w) {
+          const float2 st = ml_all[w * RS + row];
+          const float f = exp2f(st.x - mu);
+          const float4 y = *reinterpret_cast<const float4*>(smem + w * C::WARP + C::OFF_O + 4 * (row * D + d));
+          sum = fmaf(st.y, f, sum);
+          x.x = fmaf(y.x, f, x.x); x.y = fmaf(y.y, f, x.y); x.z = fmaf(y.z, f, x.z); x.w = fmaf(y.w, f, x.w);
+        }
+        if (direct) {
+          const float inv = sum > 0.f ? 1.f / sum : 0.f;
+          store4(out_row<T>(p, d_b, d_g, d_row0 + row) + d, make_float4(x.x * inv, x.y * inv, x.z * inv, x.w * inv));
+          if (d == 0) store_lse(p, d_b, d_g, d_row0 + row, m, sum);
+        } else {
+          *reinterpret_cast<float4*>(p.part_o + (int64_t)(rec + row) * D + d) = x;
+          if (d == 0) *reinterpret_cast<float2*>(p.part_st + 2 * (rec + row)) = make_float2(m, sum);
+        }
+      }
+      if (direct) __syncthreads();  // the outputs are read before their next use
+      else if (last_to_arrive(p.tickets + d_c0, d_parts, tid, misc + C::LINE, [] { __syncthreads(); }))
+        join_records<T, D, kThreads4, 1, 16>(p, d_b, d_g, d_row0, d_rows, d_parts, RS,
+                                             [&](int k) { return record_of(d_c0 + k, d_c0); }, tid);
+    }
+    if (!more) break;
+    if (!C::APART) begin();
     // ---- queries: 8 dimensions of each group a lane, in the order of the codes
-    uint4 q_regs[C::Q_REGS ? NG : 1];
+    uint4 q_regs[C::Q_REGS ? NG : 1] = {};
     float fac[NT][2];
     int tq[NT][2];
     const int base = q.sq.len - q.sq.n;
-    uint4* const q_smem = reinterpret_cast<uint4*>(smem + C::OFF_Q) + lane;
-    float* const fac_smem = reinterpret_cast<float*>(smem + C::OFF_FAC);
 #pragma unroll 1
     for (int t = C::Q_REGS ? 0 : warp; t < NT; t += kWarps4) {  // a warp of the CTA does a tile of 8 rows for all of them
       const int row = 8 * t + r;
@@ -341,13 +403,16 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
         if constexpr (!C::Q_REGS) fac[t][k] = fac_smem[8 * t + 2 * c + k];
         tq[t][k] = base + row_token(p, q.it.row0 + min(8 * t + 2 * c + k, rows - 1));
       }
+    const int t0 = base + row_token(p, q.it.row0);
+    const int t1 = base + row_token(p, q.it.row0 + rows - 1);
     auto query = [&](int t, int m, int g) {
       if constexpr (C::Q_REGS) return q_regs[g];
       else return q_smem[((t * TERMS + m) * NG + g) * 32];
     };
-    const int t0 = base + row_token(p, q.it.row0), t1 = base + row_token(p, q.it.row0 + rows - 1);
 
     float o[NT][NG][2][4], ref[NT][2], l[NT][2];
+    float above = kAbove4, v_unit = 1.f;  // O is in units of v_unit
+    bool large = false;                    // a scale of 2 or more was met
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
       ref[t][0] = ref[t][1] = -CUDART_INF_F;
@@ -359,8 +424,6 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
 #pragma unroll
           for (int k = 0; k < 4; ++k) o[t][g][h][k] = 0.f;
     }
-    float above = kAbove4, v_unit = 1.f;  // O is in units of v_unit
-    bool large = false;                    // a scale of 2 or more was met
 
 #pragma unroll 1
     for (int u = q.u0; u < q.u1; ++u) {
@@ -566,9 +629,8 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
     }
     cp_async_wait<0>();
     __syncwarp();
+    // ---- this warp's output, to be joined with the others'
     const float o_unit = TERMS == 2 && large ? 32768.f : 1.f;
-
-    // ---- the warps' outputs, joined by the CTA into rows of out or a record
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -583,39 +645,7 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
               make_float4(x.x * o_unit, x.y * o_unit, x.z * o_unit, x.w * o_unit);
         }
       }
-    __syncthreads();
-    const bool direct = !by_ticket(q.parts);
-    const int rec = record_of(blockIdx.x, q.c0) * RS;
-#pragma unroll 1
-    for (int i = tid; i < rows * (D / 4); i += kThreads4) {
-      const int row = i / (D / 4), d = 4 * (i % (D / 4));
-      float m = -CUDART_INF_F;
-#pragma unroll
-      for (int w = 0; w < kWarps4; ++w) m = fmaxf(m, ml_all[w * RS + row].x);
-      const float mu = m == -CUDART_INF_F ? 0.f : m;
-      float sum = 0.f;
-      float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-      for (int w = 0; w < kWarps4; ++w) {
-        const float2 st = ml_all[w * RS + row];
-        const float f = exp2f(st.x - mu);
-        const float4 y = *reinterpret_cast<const float4*>(smem + w * C::WARP + C::OFF_O + 4 * (row * D + d));
-        sum = fmaf(st.y, f, sum);
-        x.x = fmaf(y.x, f, x.x); x.y = fmaf(y.y, f, x.y); x.z = fmaf(y.z, f, x.z); x.w = fmaf(y.w, f, x.w);
-      }
-      if (direct) {
-        const float inv = sum > 0.f ? 1.f / sum : 0.f;
-        store4(out_row<T>(p, q.b, q.g, q.it.row0 + row) + d, make_float4(x.x * inv, x.y * inv, x.z * inv, x.w * inv));
-        if (d == 0) store_lse(p, q.b, q.g, q.it.row0 + row, m, sum);
-      } else {
-        *reinterpret_cast<float4*>(p.part_o + (int64_t)(rec + row) * D + d) = x;
-        if (d == 0) *reinterpret_cast<float2*>(p.part_st + 2 * (rec + row)) = make_float2(m, sum);
-      }
-    }
-    if (direct) __syncthreads();  // the outputs are read before their next use
-    else if (last_to_arrive(p.tickets + q.c0, q.parts, tid, misc + C::LINE, [] { __syncthreads(); }))
-      join_records<T, D, kThreads4, 1, 16>(p, q.b, q.g, q.it.row0, rows, q.parts, RS,
-                                           [&](int k) { return record_of(q.c0 + k, q.c0); }, tid);
+    d_b = q.b; d_g = q.g; d_row0 = q.it.row0; d_rows = rows; d_c0 = q.c0; d_parts = q.parts;
   }
   if (err) atomicOr(p.err, err);
 }
