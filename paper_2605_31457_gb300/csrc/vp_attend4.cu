@@ -49,6 +49,7 @@ namespace {
 // before, their scales 0 and their logits masked.
 // ---------------------------------------------------------------------------
 constexpr float kAbove4 = 10.f, kBig4 = 15.f, kRaise4 = 4.f;
+constexpr float kLowest4 = -3e38f;  // the reference of a row that has seen nothing
 constexpr int kWarps4 = 4, kThreads4 = 32 * kWarps4;
 constexpr int kStep4 = kTcTile / kWarps4;  // tokens of a warp's turn: a row's lane looks up its page
 
@@ -174,15 +175,17 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
   // Addresses of this lane's matrix rows within a stage (ldmatrix: lane l gives
   // row l % 8 of matrix l / 8; matrices: tokens 0-7 and 8-15 of one group, then
   // of the next).
-  const int mrow = (lane & 7) + ((lane >> 3) & 1) * 8, mch = lane >> 4;
+  const int m_off = code_at<D>((lane & 7) + ((lane >> 3) & 1) * 8, lane >> 4);  // of groups 0 and 1
   // Copies: 16-byte chunks of a row of codes, rows copied at once, this lane's.
   constexpr int CH = D / 32, ROWS = 32 / CH;
   const int crow = lane / CH, cch = lane % CH;
+  const unsigned c_to = ring + code_at<D>(crow, cch);  // ROWS further rows have their chunks exchanged alike
   const unsigned s_to = ring + 2 * C::CODES + lane * 2 * NG;
   // Token and page strides are below 2^31 (vp_attend4 checks them).
   const int kt = (int)p.k4.ct, vt = (int)p.v4.ct, kst = (int)p.k4.st, vst = (int)p.v4.st;
   const int kpage = (int)p.k4.cb, vpage = (int)p.v4.cb, kspage = (int)p.k4.sb, vspage = (int)p.v4.sb;
   const int in_page = p.paged ? p.page_size - 1 : -1;
+  const bool dense = kt == D / 2 && vt == D / 2;  // a token's codes lie next to the next one's
 
   uint4* const q_smem = reinterpret_cast<uint4*>(smem + C::OFF_Q) + lane;
   float* const fac_smem = reinterpret_cast<float*>(smem + C::OFF_FAC);
@@ -229,7 +232,7 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
     auto issue = [&](int u) {
       if (u < q.u1) {
         const int st = (unsigned)(u - q.u0) % S;
-        const unsigned to = ring + st * C::STAGE, s_st = s_to + st * C::STAGE;
+        const unsigned to = c_to + st * C::STAGE, s_st = s_to + st * C::STAGE;
         const int j0 = first_token(u), j = j0 + lane;
         const bool whole = (j0 >= sr.lo && j0 + kStep4 <= sr.hi) || j0 + kStep4 <= sr.s_end;
         unsigned mask = 0xffffffffu;
@@ -243,10 +246,18 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
         if (whole && !p.paged) {
           partly &= ~(1u << st);
           const unsigned char *kc = k_lane + (int64_t)j0 * kt, *vc = v_lane + (int64_t)j0 * vt;
+          if (dense) {
 #pragma unroll
-          for (int i = 0; i < kStep4; i += ROWS) {
-            cp_async16(to + code_at<D>(crow + i, cch), kc + (int64_t)i * kt);
-            cp_async16(to + C::CODES + code_at<D>(crow + i, cch), vc + (int64_t)i * vt);
+            for (int i = 0; i < kStep4; i += ROWS) {
+              cp_async16(to + i * (D / 2), kc + i * (D / 2));
+              cp_async16(to + C::CODES + i * (D / 2), vc + i * (D / 2));
+            }
+          } else {
+#pragma unroll
+            for (int i = 0; i < kStep4; i += ROWS) {
+              cp_async16(to + i * (D / 2), kc + (int64_t)i * kt);
+              cp_async16(to + C::CODES + i * (D / 2), vc + (int64_t)i * vt);
+            }
           }
           cp_async_or_zero<2 * NG>(s_st, ks_lane + (int64_t)j * kst, true);
           cp_async_or_zero<2 * NG>(s_st + C::SCALES, vs_lane + (int64_t)j * vst, true);
@@ -259,8 +270,8 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
             const unsigned char* vc = v_lane + (int64_t)__shfl_sync(0xffffffffu, vn, h) * vpage + (int64_t)at * vt;
 #pragma unroll
             for (int i = 0; i < 16; i += ROWS) {
-              cp_async16(to + code_at<D>(h + crow + i, cch), kc + (int64_t)i * kt);
-              cp_async16(to + C::CODES + code_at<D>(h + crow + i, cch), vc + (int64_t)i * vt);
+              cp_async16(to + (h + i) * (D / 2), kc + (dense ? (int64_t)(i * (D / 2)) : (int64_t)i * kt));
+              cp_async16(to + C::CODES + (h + i) * (D / 2), vc + (dense ? (int64_t)(i * (D / 2)) : (int64_t)i * vt));
             }
           }
           const int at = j & in_page;
@@ -277,8 +288,8 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
             const int kr = __shfl_sync(0xffffffffu, kn, row), vr = __shfl_sync(0xffffffffu, vn, row);
             const bool copy = (mask >> row) & 1u;
             const int64_t at = ((j0 + row) & in_page) - crow;  // k_lane is of row crow
-            cp_async_or_zero<16>(to + code_at<D>(row, cch), copy ? k_lane + (int64_t)kr * kpage + at * kt : p.k4.codes, copy);
-            cp_async_or_zero<16>(to + C::CODES + code_at<D>(row, cch), copy ? v_lane + (int64_t)vr * vpage + at * vt : p.v4.codes, copy);
+            cp_async_or_zero<16>(to + i * (D / 2), copy ? k_lane + (int64_t)kr * kpage + at * kt : p.k4.codes, copy);
+            cp_async_or_zero<16>(to + C::CODES + i * (D / 2), copy ? v_lane + (int64_t)vr * vpage + at * vt : p.v4.codes, copy);
           }
           const bool live = (mask >> lane) & 1u;
           const int64_t at = j & in_page;
@@ -387,7 +398,7 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
           if constexpr (TERMS == 2) q_smem[(t * TERMS * NG + NG + g) * 32] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
         }
       }
-      const float f = down * p.c_log2;
+      const float f = fmaxf(down * p.c_log2, 1e-37f);  // above 0: masked logits are multiplied by it
       if constexpr (C::Q_REGS) {
         fac[0][0] = __shfl_sync(0xffffffffu, f, 8 * c);
         fac[0][1] = __shfl_sync(0xffffffffu, f, 8 * c + 4);
@@ -415,7 +426,7 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
     bool large = false;                    // a scale of 2 or more was met
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      ref[t][0] = ref[t][1] = -CUDART_INF_F;
+      ref[t][0] = ref[t][1] = kLowest4;
       l[t][0] = l[t][1] = 0.f;
 #pragma unroll
       for (int g = 0; g < NG; ++g)
@@ -438,18 +449,32 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
       const unsigned at = ring + st * C::STAGE;
       const unsigned char* const scales = mine + st * C::STAGE + 2 * C::CODES;
 
-      // ---- logits: tokens r and r + 8 of each half, query rows 2c and 2c + 1
+      // ---- logits, over the row's factor: tokens r and r + 8 of each half, query rows 2c and 2c + 1
       float z[2][NT][4];
+      uint32_t kscale[2][2][NG / 2];  // half, tokens: two groups' scales each
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const unsigned char* const of = scales + (16 * h + 8 * k + r) * 2 * NG;
+          if constexpr (NG == 4) {
+            const uint2 v = *reinterpret_cast<const uint2*>(of);
+            kscale[h][k][0] = v.x;
+            kscale[h][k][1] = v.y;
+          } else {
+            kscale[h][k][0] = *reinterpret_cast<const uint32_t*>(of);
+          }
+        }
 #pragma unroll
       for (int gp = 0; gp < NG; gp += 2) {
         uint32_t kw[2][2][2];  // half, group, tokens 0-7 or 8-15
         float2 ks[2][2];       // half, tokens: the two groups' scales
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          ldsm_x4(at + code_at<D>(16 * h + mrow, gp + mch), kw[h][0][0], kw[h][0][1], kw[h][1][0], kw[h][1][1]);
+          ldsm_x4(at + (m_off ^ (16 * gp)) + 8 * D * h, kw[h][0][0], kw[h][0][1], kw[h][1][0], kw[h][1][1]);
 #pragma unroll
           for (int k = 0; k < 2; ++k)
-            ks[h][k] = unpack_f16(*reinterpret_cast<const uint32_t*>(scales + (16 * h + 8 * k + r) * 2 * NG + 2 * gp));
+            ks[h][k] = unpack_f16(kscale[h][k][gp / 2]);
         }
 #pragma unroll
         for (int gg = 0; gg < 2; ++gg) {
@@ -487,12 +512,6 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
           }
         }
       }
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-          for (int k = 0; k < 4; ++k) z[h][t][k] *= fac[t][k & 1];
       if (!all_see) {
 #pragma unroll
         for (int h = 0; h < 2; ++h)
@@ -511,7 +530,7 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
 #pragma unroll
       for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int k = 0; k < 2; ++k) need |= largest(t, k) > ref[t][k] + (above + kRaise4);
+        for (int k = 0; k < 2; ++k) need |= fmaf(largest(t, k), fac[t][k], -ref[t][k]) > above + kRaise4;
       uint32_t any = 0;  // of V's scales of token `lane`: one of 2 or more?
 #pragma unroll
       for (int g = 0; g < NG; g += 2) any |= *reinterpret_cast<const uint32_t*>(scales + C::SCALES + lane * 2 * NG + 2 * g);
@@ -527,9 +546,8 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
         for (int t = 0; t < NT; ++t)
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
-            const float top = group_max(largest(t, k));
-            const float next = fmaxf(ref[t][k], top - above);
-            const float f = ref[t][k] == -CUDART_INF_F ? 0.f : fexp2(ref[t][k] - next);
+            const float next = fmaxf(ref[t][k], fmaf(group_max(largest(t, k)), fac[t][k], -above));
+            const float f = fexp2(ref[t][k] - next);
             ref[t][k] = next;
             l[t][k] *= f;
             const float fo = TERMS == 1 ? f : f * fv;
@@ -549,18 +567,18 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
         uint32_t ph[NT][2], pl[NT][2];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-          const float m0 = ref[t][0] == -CUDART_INF_F ? 0.f : ref[t][0], m1 = ref[t][1] == -CUDART_INF_F ? 0.f : ref[t][1];
-          const float e0 = fexp2(z[h][t][0] - m0), e1 = fexp2(z[h][t][1] - m1);
-          const float e2 = fexp2(z[h][t][2] - m0), e3 = fexp2(z[h][t][3] - m1);
-          l[t][0] += e0 + e2;
-          l[t][1] += e1 + e3;
-          const uint32_t h0 = pack_f16(e0, e1), h1 = pack_f16(e2, e3);
+          float e[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) e[k] = fexp2(fmaf(z[h][t][k], fac[t][k & 1], -ref[t][k & 1]));
+          l[t][0] += e[0] + e[2];
+          l[t][1] += e[1] + e[3];
+          const uint32_t h0 = pack_f16(e[0], e[1]), h1 = pack_f16(e[2], e[3]);
           ph[t][0] = transpose8(h0);
           ph[t][1] = transpose8(h1);
           if constexpr (TERMS == 2) {
             const float2 f0 = unpack_f16(h0), f1 = unpack_f16(h1);
-            pl[t][0] = transpose8(pack_f16(e0 - f0.x, e1 - f0.y));
-            pl[t][1] = transpose8(pack_f16(e2 - f1.x, e3 - f1.y));
+            pl[t][0] = transpose8(pack_f16(e[0] - f0.x, e[1] - f0.y));
+            pl[t][1] = transpose8(pack_f16(e[2] - f1.x, e[3] - f1.y));
           }
         }
 
@@ -588,7 +606,7 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
 #pragma unroll
         for (int gp = 0; gp < NG; gp += 2) {
           uint32_t vw[2][2];
-          ldsm_x4_t(at + C::CODES + code_at<D>(16 * h + mrow, gp + mch), vw[0][0], vw[0][1], vw[1][0], vw[1][1]);
+          ldsm_x4_t(at + (m_off ^ (16 * gp)) + C::CODES + 8 * D * h, vw[0][0], vw[0][1], vw[1][0], vw[1][1]);
 #pragma unroll
           for (int gg = 0; gg < 2; ++gg) {
             const int g = gp + gg;
@@ -690,7 +708,9 @@ void plan_attend4(Attend4Params& p) {
   p.block = with_att4(p.dtype, p.D, p.R, [](auto, size_t, int rows, int) { return rows; });
   p.grid = p.num_sms * with_att4(p.dtype, p.D, p.R, [](auto, size_t, int, int cps) { return cps; });
   p.nqt = (p.R + p.block - 1) / p.block;
-  p.fixed = kTileUnits;
+  // An item's start and end take about as long as two tiles; where every item has
+  // CTAs of its own, the least share of one follows from it (min_share).
+  p.fixed = p.B * (int64_t)p.nqt * p.Hkv <= p.grid / 4 ? 2 : 6;
 }
 
 cudaError_t launch_attend4(const Attend4Params& p, cudaStream_t st) {
