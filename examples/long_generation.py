@@ -32,7 +32,6 @@ class Layer:
         self.k = torch.zeros(batch, kv_heads, max_seq, dim, dtype=dtype, device="cuda")
         self.v = torch.zeros_like(self.k)
         self.seq = torch.zeros(batch, dtype=torch.int32, device="cuda")
-        self.at = torch.arange(batch, device="cuda")
         self.ctx = vp.vp_init(vp.make_config(batch, heads, kv_heads, dim, max_visual, max_seq,
                                              vp.VP_FP32 if dtype == torch.float32 else vp.VP_BF16))
         vp.vp_reserve_new(self.ctx, max_new, max_weight_new)
@@ -40,11 +39,10 @@ class Layer:
         self.everything = vp.make_visible()
 
     def append(self, k, v):
-        """k, v [B, Hkv, n, D]: the keys and values of n new tokens."""
-        rows = self.seq.long()[:, None] + torch.arange(k.shape[2], device="cuda")
-        self.k[self.at[:, None], :, rows] = k.transpose(1, 2)
-        self.v[self.at[:, None], :, rows] = v.transpose(1, 2)
+        """k, v [B, Hkv, n, D]: the keys and values of n new tokens (random here, so not rotated)."""
         self.seq += k.shape[2]
+        vp.vp_append(self.ctx, self.B, k.shape[2], None, vp.rows(k.transpose(1, 2)), vp.rows(v.transpose(1, 2)), self.seq,
+                     None, None, self.kc, self.vc)
 
     def attend(self, q, **weights):
         """q [B, n, H, D] of the newest n tokens."""

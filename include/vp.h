@@ -454,6 +454,8 @@ typedef struct {
  * sequence whose seq_len or new_len is out of range is skipped, and flagged; a row
  * whose page the block table does not map is not written (its query is), and
  * flagged (vp_check_errors).  VP_ERR_CAPACITY for n_new > max_seq.
+ * The inputs must not lie in the caches, and no page that a token goes to may
+ * belong to two sequences.
  * Uses no workspace, allocates nothing and never synchronises; waits for the
  * stream's previous work, and a call behind it, vp_decode_step included, may use
  * its outputs.
@@ -494,7 +496,8 @@ typedef struct {
  * is not a number, all of them are held as that (scale 0x7fff).
  *   k_held, v_held  NULL, or [batch][n_new][Hkv] rows of cfg.dtype: the values that
  *                   the cache now holds for the new tokens (of a page that is not
- *                   mapped: would hold).  Rows i >= n_b are left as they were.
+ *                   mapped: would hold).  Rows i >= n_b are left as they were;
+ *                   must not overlap the inputs.
  * Everything else as for vp_append.
  */
 vp_status vp_append4(vp_ctx* ctx, int32_t batch, int32_t n_new, const vp_rows* q, const vp_rows* k, const vp_rows* v,
@@ -523,9 +526,10 @@ vp_status vp_reserve4(vp_ctx* ctx, int32_t max_new);
  * with n_new * G > 64 (pages of at least 8 tokens) the held values are first rounded
  * to bf16, which vp_append4's are exactly, and vp_attend_new's bounds hold.  fp32
  * contexts: both are two fp16 terms.  VP_ERR_CAPACITY when vp_reserve4 has not
- * reserved for n_new.  Allocates nothing and never synchronises; every kernel waits
- * for the stream's previous work, so an input may be the output of the preceding
- * call of this library.
+ * reserved for n_new, VP_ERR_UNSUPPORTED where the call's tiles (of 128 tokens, 32
+ * rows of one kv-head) could pass 2^29.  Allocates nothing and never synchronises;
+ * every kernel waits for the stream's previous work, so an input may be the output
+ * of the preceding call of this library.
  */
 vp_status vp_attend4(vp_ctx* ctx, int32_t batch, int32_t n_new, const vp_rows* q,
                      const vp_kv4* k_cache, const vp_kv4* v_cache,

@@ -714,7 +714,6 @@ void plan_attend4(Attend4Params& p) {
 }
 
 cudaError_t launch_attend4(const Attend4Params& p, cudaStream_t st) {
-  if (line_bound((int64_t)p.B * p.Hkv * p.nqt, p.max_seq, p.fixed) > INT32_MAX) return cudaErrorInvalidConfiguration;
   return with_att4(p.dtype, p.D, p.R, [&](auto kernel, size_t smem, int, int) {
     return launch_dep(kernel, dim3(p.grid), kThreads4, smem, st, p);
   });

@@ -281,6 +281,8 @@ vp_status attend4(vp_ctx* ctx, int32_t batch, int32_t n_new, const vp_rows* q, c
     e = staged(p, ctx->lay4, ws, st);
   } else {
     vp::plan_attend4(p);
+    if (vp::line_bound((int64_t)p.B * p.Hkv * p.nqt, p.max_seq, p.fixed) > INT32_MAX)
+      return fail(ctx, VP_ERR_UNSUPPORTED, "vp_attend4: batch * Hkv * n_new * G * max_seq is too large for one call");
     e = vp::launch_attend4(p, st);
   }
   if (e != cudaSuccess) return cuda_fail(ctx, "vp_attend4: launch", e);
