@@ -33,7 +33,7 @@ def four_bits_up(t):
 
 def quantise(x):
     """x [..., D] float32 -> (codes 0..15 [..., D], scales float32 [..., D/32])."""
-    g = np.asarray(x, F).reshape(*x.shape[:-1], -1, GROUP)
+    g = np.asarray(x, F).reshape(*x.shape[:-1], x.shape[-1] // GROUP, GROUP)
     nan = np.isnan(g).any(-1)
     top = np.abs(np.where(np.isnan(g), 0, g)).max(-1).astype(F)
     with np.errstate(invalid="ignore", over="ignore", divide="ignore"):
@@ -47,7 +47,7 @@ def quantise(x):
 
 def values(codes, scales):
     """What the codes and scales hold, in float64."""
-    g = codes.reshape(*codes.shape[:-1], -1, GROUP).astype(np.float64) - 8.0
+    g = codes.reshape(*codes.shape[:-1], codes.shape[-1] // GROUP, GROUP).astype(np.float64) - 8.0
     return (g * np.asarray(scales, np.float64)[..., None]).reshape(codes.shape)
 
 
@@ -58,4 +58,4 @@ def pack(codes):
 
 def unpack(byts):
     b = np.asarray(byts).astype(np.int64)
-    return np.stack([b & 15, b >> 4], -1).reshape(*b.shape[:-1], -1)
+    return np.stack([b & 15, b >> 4], -1).reshape(*b.shape[:-1], 2 * b.shape[-1])

@@ -66,7 +66,7 @@ struct Cfg4 {
   // A warp's ring, and behind it its output to be joined, float [RS][D] (in the ring where there is no room).
   static constexpr int RING = S * STAGE;
   static constexpr int OUT = RS * D * 4;
-  static constexpr bool APART = kWarps4 * (RING + OUT) <= 232448 / CPS - 3072 - NT * TERMS * GROUPS * 512;
+  static constexpr bool APART = kWarps4 * (RING + OUT) <= 232448 / CPS - 4096 - NT * TERMS * GROUPS * 512;
   static constexpr int WARP = APART ? RING + OUT : RING > OUT ? RING : OUT;
   static constexpr int OFF_O = APART ? RING : 0;
   // The queries as the products take them: in registers, or uint4 [NT][TERMS][GROUPS][32] and float [RS] factors.

@@ -70,7 +70,7 @@ def _near(q, out, lse, k, v, n):
     r = O.attend_new(q.double().cpu().numpy(), k, v, k.shape[1], n)
     got = out.double().cpu().numpy()
     z = 2.0 ** -20 * 16 * r["zmag"] + 2.0 ** -21 * (1 + np.abs(np.where(np.isfinite(r["lse"]), r["lse"], 0)))
-    assert (np.abs(lse.double().cpu().numpy() - r["lse"])[:n] <= z[:n] + 1e-30).all()
+    assert (np.abs(lse.double().cpu().numpy()[:n] - r["lse"][:n]) <= z[:n] + 1e-30).all()
     tol = (2 * z[..., None] + 2.0 ** -9) * r["absout"] + 2.0 ** -8 * np.abs(r["out"]) * (1 + 2.0 ** -6) + 1e-30
     assert (np.abs(got - r["out"]) <= tol).all()
     assert not got[n:].any()
