@@ -260,6 +260,10 @@ __global__ void __launch_bounds__(kAppendThreads, Q4 ? 7 : 6) k_append(const __g
     // The lane that holds the partners of this lane's values.
     const bool turned = p.rot.cos_sin && 8 * chunk < p.rot.rot;
     const int other = !turned ? lane : 8 * chunk >= pairs ? lane - pairs / 8 : lane + pairs / 8;
+    auto turn2 = [&](float2 a, float2 z, int k) {  // products two at a time, sums apart (as pairs they would be fused)
+      const float2 x = mul2(a, make_float2(c[2 * k], c[2 * k + 1])), y = mul2(z, make_float2(s[2 * k], s[2 * k + 1]));
+      return make_float2(__fadd_rn(x.x, y.x), __fadd_rn(x.y, y.y));
+    };
     auto rotate = [&](Raw8<T>& y) {
       if (!p.rot.cos_sin) return;
       if (p.rot.interleaved) {
@@ -267,8 +271,7 @@ __global__ void __launch_bounds__(kAppendThreads, Q4 ? 7 : 6) k_append(const __g
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           const float2 a = y.get(k);
-          y.set(k, make_float2(__fadd_rn(__fmul_rn(a.x, c[2 * k]), __fmul_rn(a.y, s[2 * k])),
-                               __fadd_rn(__fmul_rn(a.y, c[2 * k + 1]), __fmul_rn(a.x, s[2 * k + 1]))));
+          y.set(k, turn2(a, make_float2(a.y, a.x), k));
         }
         return;
       }
@@ -278,9 +281,7 @@ __global__ void __launch_bounds__(kAppendThreads, Q4 ? 7 : 6) k_append(const __g
       if (!turned) return;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const float2 a = y.get(k), z = o.get(k);
-        y.set(k, make_float2(__fadd_rn(__fmul_rn(a.x, c[2 * k]), __fmul_rn(z.x, s[2 * k])),
-                             __fadd_rn(__fmul_rn(a.y, c[2 * k + 1]), __fmul_rn(z.y, s[2 * k + 1]))));
+        y.set(k, turn2(y.get(k), o.get(k), k));
       }
     };
     T* const q_out = from(p.q_out);
