@@ -341,7 +341,7 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
       }
       if (direct) __syncthreads();  // the outputs are read before their next use
       else if (last_to_arrive(p.tickets + d_c0, d_parts, tid, misc + C::LINE, [] { __syncthreads(); }))
-        join_records<T, D, kThreads4, 1, 16>(p, d_b, d_g, d_row0, d_rows, d_parts, RS,
+        join_records<T, D, kThreads4, NT == 1 ? 2 : 4, 8>(p, d_b, d_g, d_row0, d_rows, d_parts, RS,
                                              [&](int k) { return record_of(d_c0 + k, d_c0); }, tid);
     }
     if (!more) break;
