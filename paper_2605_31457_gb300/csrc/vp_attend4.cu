@@ -153,6 +153,22 @@ __device__ __forceinline__ int code_at(int row, int ch) {
   return D == 128 ? row * 64 + ((ch ^ ((row >> 1) & 3)) << 4) : row * 32 + ((ch ^ ((row >> 2) & 1)) << 4);
 }
 
+// True for the CTA that is the last of `expected` to arrive at the ticket, its record
+// written.  One atomic operation releases that record and acquires the others', for
+// the whole CTA by way of the barriers around it.
+__device__ __forceinline__ bool last_of(unsigned* ticket, unsigned expected, int tid, int* flag) {
+  __syncthreads();
+  if (tid == 0) {
+    unsigned before;
+    asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], 1;\n" : "=r"(before) : "l"(ticket) : "memory");
+    const bool last = before == expected - 1;
+    if (last) *ticket = 0;  // for the next call
+    *flag = last;
+  }
+  __syncthreads();
+  return *flag != 0;
+}
+
 template <typename T, int D, int NT>
 __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const __grid_constant__ Attend4Params p) {
   using C = Cfg4<T, D, NT>;
@@ -340,7 +356,7 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
         }
       }
       if (direct) __syncthreads();  // the outputs are read before their next use
-      else if (last_to_arrive(p.tickets + d_c0, d_parts, tid, misc + C::LINE, [] { __syncthreads(); }))
+      else if (last_of(p.tickets + d_c0, d_parts, tid, misc + C::LINE))
         join_records<T, D, kThreads4, NT == 1 ? 2 : 4, 8>(p, d_b, d_g, d_row0, d_rows, d_parts, RS,
                                              [&](int k) { return record_of(d_c0 + k, d_c0); }, tid);
     }
