@@ -438,10 +438,10 @@ typedef struct {
 /*
  * Appends the newest tokens of every sequence: new token i of sequence b, 0 <= i <
  * n_b, goes to place seq_len[b] - n_b + i of its sequence.
- *   q, k, v      rows of H query heads and Hkv keys and values of the new tokens,
- *                cfg.dtype (stride_h steps from head to kv-head in k and v); may be
- *                views of one projection's output.  q may be NULL: keys and values
- *                only.
+ *   q, k, v      n_new rows per sequence of H query heads and Hkv keys and values,
+ *                cfg.dtype (stride_h steps from kv-head to kv-head in k and v); may
+ *                be views of one projection's output.  Rows i >= n_b may hold
+ *                anything.  q may be NULL: keys and values only.
  *   seq_len      device int32 [batch], 0 <= seq_len <= max_seq: tokens of the
  *                sequence, the new ones included (as vp_attend_new takes it).
  *   new_len      device int32 [batch] or NULL: n_b, 0 <= n_b <= min(n_new, seq_len);
@@ -507,7 +507,7 @@ vp_status vp_append4(vp_ctx* ctx, int32_t batch, int32_t n_new, const vp_rows* q
 
 /* Allocates the workspace of vp_attend4 on a context, once, for calls of up to
  * max_new new tokens per sequence: tens of MB, and for bf16 contexts where max_new *
- * G > 64 room for bf16 caches of as many sequences as fit 1 GiB (one at least), by
+ * G > 128 room for bf16 caches of as many sequences as fit 1 GiB (one at least), by
  * way of which calls of that many rows go.  Waits for the device; call it outside
  * stream capture.  A second call replaces the first one's workspace: graphs that
  * captured vp_attend4 before it must not be replayed.  VP_ERR_INVALID_ARG for
@@ -523,7 +523,7 @@ vp_status vp_reserve4(vp_ctx* ctx, int32_t max_new);
  * VP_ERR_UNSUPPORTED.  Logits are products of queries and codes, scaled and summed
  * in float.  bf16 contexts: the probabilities, and their products with the values'
  * scales, are rounded to fp16 (2^-11 of each; the output's own rounding is 2^-8);
- * with n_new * G > 64 (pages of at least 8 tokens) the held values are first rounded
+ * with n_new * G > 128 (pages of at least 8 tokens) the held values are first rounded
  * to bf16, which vp_append4's are exactly, and vp_attend_new's bounds hold.  fp32
  * contexts: both are two fp16 terms.  VP_ERR_CAPACITY when vp_reserve4 has not
  * reserved for n_new, VP_ERR_UNSUPPORTED where the call's tiles (of 128 tokens, 32
