@@ -651,10 +651,16 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
                   const float2 f = unpack_f16(hi[k]);
                   lo[k] = pack_f16(ea - f.x, eb - f.y);
                 }
-                mma_f16(o[t][g][0], a[0], a[1], a[2], a[3], hi[0], hi[1]);
-                mma_f16(o[t][g][1], a[4], a[5], a[6], a[7], hi[0], hi[1]);
-                mma_f16(o[t][g][0], a[0], a[1], a[2], a[3], lo[0], lo[1]);
-                mma_f16(o[t][g][1], a[4], a[5], a[6], a[7], lo[0], lo[1]);
+                // The tensor cores cut what they add to a sum, which over a long range adds up:
+                // sixteen tokens' products are summed by themselves, and added in float.
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                  float sum[4];
+                  mma_f16_first(sum, a[4 * x], a[4 * x + 1], a[4 * x + 2], a[4 * x + 3], lo[0], lo[1]);
+                  mma_f16(sum, a[4 * x], a[4 * x + 1], a[4 * x + 2], a[4 * x + 3], hi[0], hi[1]);
+#pragma unroll
+                  for (int k = 0; k < 4; ++k) o[t][g][x][k] += sum[k];
+                }
               }
             }
           }
