@@ -10,6 +10,7 @@
 
 #include "vp_attend_device.h"
 #include "vp_cache4.h"
+#include "vp_codes4.h"
 #include "vp_device.h"
 
 namespace vp {
@@ -103,38 +104,10 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;\n" : "=r"(y) : "r"(x));
   return y;
 }
-__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
-  const __half2 v = __floats2half2_rn(lo, hi);
-  return *reinterpret_cast<const uint32_t*>(&v);
-}
-__device__ __forceinline__ float2 unpack_f16(uint32_t u) { return __half22float2(*reinterpret_cast<const __half2*>(&u)); }
 __device__ __forceinline__ uint32_t mul_f16(uint32_t a, uint32_t b) {
   const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
   return *reinterpret_cast<const uint32_t*>(&r);
 }
-// The whole numbers code - 8 of the codes in bits 0-3 and 16-19 (low), and of
-// those in bits 4-7 and 20-23 (high).  The constants are kept in registers: a mask
-// and the exponent are one operation then.
-struct Codes {
-  uint32_t mask, mask_high, k1024, k1032, sixteenth, k72;
-  __device__ __forceinline__ Codes() {
-    asm volatile("mov.b32 %0, 0x000f000f;\n mov.b32 %1, 0x00f000f0;\n mov.b32 %2, 0x64006400;\n"
-                 "mov.b32 %3, 0xe408e408;\n mov.b32 %4, 0x2c002c00;\n mov.b32 %5, 0xd480d480;\n"
-                 : "=r"(mask), "=r"(mask_high), "=r"(k1024), "=r"(k1032), "=r"(sixteenth), "=r"(k72));
-  }
-  __device__ __forceinline__ uint32_t low(uint32_t x) const {
-    uint32_t r;
-    asm("{\n .reg .b32 y;\n lop3.b32 y, %1, %2, %3, 0xea;\n add.f16x2 %0, y, %4;\n}\n"  // 1024 + code
-        : "=r"(r) : "r"(x), "r"(mask), "r"(k1024), "r"(k1032));
-    return r;
-  }
-  __device__ __forceinline__ uint32_t high(uint32_t x) const {
-    uint32_t r;
-    asm("{\n .reg .b32 y;\n lop3.b32 y, %1, %2, %3, 0xea;\n fma.rn.f16x2 %0, y, %4, %5;\n}\n"  // 1024 + 16 code
-        : "=r"(r) : "r"(x), "r"(mask_high), "r"(k1024), "r"(sixteenth), "r"(k72));
-    return r;
-  }
-};
 // A copy of N bytes, or N zeros.
 template <int N>
 __device__ __forceinline__ void cp_async_or_zero(unsigned dst, const void* src, bool copy) {

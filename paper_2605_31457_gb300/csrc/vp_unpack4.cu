@@ -7,6 +7,7 @@
 
 #include "vp_attend_device.h"
 #include "vp_cache4.h"
+#include "vp_codes4.h"
 #include "vp_device.h"
 
 namespace vp {
@@ -22,18 +23,19 @@ namespace {
 // ---------------------------------------------------------------------------
 constexpr int kUnpackThreads = 256, kUnpackTokens = 64;
 
-__device__ __forceinline__ uint4 values(uint32_t codes, uint16_t scale) {
+__device__ __forceinline__ uint4 values(const Codes& codes, uint32_t x, uint16_t scale) {
   const float s = __half2float(__ushort_as_half(scale));
-  auto two = [&](int e) {
-    return pack_bf16((float)((int)((codes >> (4 * e)) & 15u) - 8) * s, (float)((int)((codes >> (4 * e + 4)) & 15u) - 8) * s);
-  };
-  return make_uint4(two(0), two(2), two(4), two(6));
+  const uint32_t y = x >> 8;
+  // Dimensions k and k + 4 meet one mask.
+  const float2 a = unpack_f16(codes.low(x)), b = unpack_f16(codes.high(x)), c = unpack_f16(codes.low(y)), d = unpack_f16(codes.high(y));
+  return make_uint4(pack_bf16(a.x * s, b.x * s), pack_bf16(c.x * s, d.x * s), pack_bf16(a.y * s, b.y * s), pack_bf16(c.y * s, d.y * s));
 }
 
 template <int D>
 __global__ void __launch_bounds__(kUnpackThreads) k_unpack4(const __grid_constant__ Unpack4Params p) {
   constexpr int L = D / 8, ROWS = kUnpackThreads / L;
   const int chunk = threadIdx.x % L, slot = threadIdx.x / L;
+  const Codes codes;
   pdl_wait();
   pdl_trigger();
   const int blocks = (p.max_seq + kUnpackTokens - 1) / kUnpackTokens;
@@ -65,8 +67,8 @@ __global__ void __launch_bounds__(kUnpackThreads) k_unpack4(const __grid_constan
       const uint32_t vc = __ldcs(reinterpret_cast<const uint32_t*>(p.v4.codes + vat * p.v4.cb + g * p.v4.ch + row * p.v4.ct) + chunk);
       const uint16_t ks = __ldg(p.k4.scales + kat * p.k4.sb + g * p.k4.sh + row * p.k4.st + chunk / 4);
       const uint16_t vs = __ldg(p.v4.scales + vat * p.v4.sb + g * p.v4.sh + row * p.v4.st + chunk / 4);
-      static_cast<uint4*>(p.k)[to * L + chunk] = values(kc, ks);
-      static_cast<uint4*>(p.v)[to * L + chunk] = values(vc, vs);
+      static_cast<uint4*>(p.k)[to * L + chunk] = values(codes, kc, ks);
+      static_cast<uint4*>(p.v)[to * L + chunk] = values(codes, vc, vs);
     }
   }
 }
