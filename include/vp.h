@@ -410,9 +410,8 @@ vp_status vp_evict(vp_ctx* ctx, int32_t batch, const vp_kv* k_src, const vp_kv* 
  * vp_append takes a layer's new queries, keys and values as the projections leave
  * them, rotates queries and keys by their positions and writes keys and values to
  * their places in the caches, in one kernel.  vp_append4 writes them to caches held
- * in 4 bits, which vp_attend4 attends over: a fifth more than a quarter of the
- * memory, and of the time where that is what bounds it.  The entry points use the
- * contexts, error codes and device checks of those above and return
+ * in 4 bits (9/32 of the memory of bf16), which vp_attend4 attends over.  The entry
+ * points use the contexts, error codes and device checks of those above and return
  * VP_ERR_INVALID_ARG when the current CUDA device is not the context's.
  */
 

@@ -46,8 +46,28 @@ namespace {
 // larger one on, the reference is 15 higher (one term: P is then exact to 2^-20 of
 // the row's largest), or P * scale is taken times 2^-15 (two terms).
 //
-// Tokens that no row sees are not copied: their codes are whatever the ring held
-// before, their scales 0 and their logits masked.
+// Float outputs: the tensor cores cut what they add to a sum, so 16 tokens' products
+// are summed by themselves and added in float; bf16 outputs, whose rounding is far
+// larger, are summed in the accumulators (2^-24 of the sum per 16 tokens of a warp).
+//
+// Tokens that no row sees are not copied: the ring gets zeros for them, their scales
+// among these, and their logits are masked.
+//
+// A warp's ring is filled by its own asynchronous copies, two turns ahead, so warps
+// need no barrier until a part ends; a part's first copies run while the part before
+// it is joined (where shared memory holds both: up to 16 rows of 128 dimensions).  mma.sync takes its operands from
+// registers, where the codes are converted: a tcgen05 operand would go through shared
+// memory, 512 bytes for every 144 that are read.
+//
+// Bound by issue slots: 330 instructions of a warp for 16 tokens of K and V with 8
+// rows, 144 of them the conversion, at 60% of the issue rate; at the measured copy rate
+// an SM gets these tokens' bytes in the time of 390.
+// Heads of 128, 32/8: 64 sequences of 17408 tokens in 243 us (5.3 TB/s); 16 of 2305 to
+// 9001 with five new tokens in 52 us; 28/4: 32 of 2816 to 6400 in 28 us, one of 3857 in
+// 11.0 us.  Slower, the first of these: 16 tokens a turn and 8 warps a CTA (304 us), 16
+// warps per SM at 128 registers (250), constants of the conversion left to the compiler,
+// which loads them again for every use (348).  Two warps sharing 24 rows' registers,
+// with two barriers a turn, took 68 us for the drafted tokens (then 55).
 // ---------------------------------------------------------------------------
 constexpr float kAbove4 = 10.f, kBig4 = 15.f, kRaise4 = 4.f;
 constexpr float kLowest4 = -3e38f;  // the reference of a row that has seen nothing
