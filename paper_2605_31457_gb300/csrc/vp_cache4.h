@@ -106,8 +106,9 @@ struct Unpack4Params {
   int window, sinks;
   unsigned* err;
   int num_sms;
+  int splits;          // CTAs of a (sequence, kv-head), set by launch_unpack4
 };
-cudaError_t launch_unpack4(const Unpack4Params& p, cudaStream_t s);
+cudaError_t launch_unpack4(Unpack4Params& p, cudaStream_t s);
 
 void plan_attend4(Attend4Params& p);
 cudaError_t configure_attend4();
