@@ -235,28 +235,25 @@ def vp_compact_kv(ctx, batch, src: vp_kv, dst: vp_kv, visual_span: vp_span, text
     return _check(st, ctx) if check else st
 
 
-_torch = None
+_current = None  # torch's (raw stream of a device, current device), once it is needed
 
 
 def _raw_stream(stream):
     """The handle of a torch.cuda.Stream, of a raw handle (itself), or of torch's current stream."""
-    global _torch
+    global _current
     if stream is None:
-        if _torch is None:
+        if _current is None:
             import torch
-            _torch = torch
+            torch.cuda.init()
+            _current = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
         # The handle of torch.cuda.current_stream(), without making the object:
         # a decode step calls this once per layer.
-        return _torch._C._cuda_getCurrentRawStream(_torch.cuda.current_device())
+        return _current[0](_current[1]())
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else stream
 
 
 def _stream(stream):
     return ctypes.c_void_p(_raw_stream(stream))
-
-
-def _addr(t):
-    return None if t is None else t.data_ptr()
 
 
 def _ref(struct):
@@ -290,16 +287,20 @@ def vp_evict(ctx, batch, k_src: vp_kv, v_src: vp_kv, seq_len, policy: vp_evict_p
 
 
 # ctypes passes a structure's address where a pointer to it is declared, and an int
-# as an address: half the time of making the pointer objects here.
+# as an address, in half the time of making the pointer objects here.
+_append, _append4, _attend4 = lib.vp_append, lib.vp_append4, lib.vp_attend4
+
+
 def vp_append(ctx, batch, n_new, q: vp_rows, k: vp_rows, v: vp_rows, seq_len, rotation: vp_rotation, q_out: vp_rows,
               k_cache: vp_kv, v_cache: vp_kv, new_len=None, stream=None, check=True):
     """Enqueues the rotation of the ``n_new`` newest tokens' queries and keys and the
     appending of their keys and values.  q, k, v and q_out are ``rows(tensor)``
     (q and q_out may be None), rotation ``make_rotation(...)`` or None; seq_len and
     new_len are tensors."""
-    st = lib.vp_append(ctx, batch, n_new, q, k, v, _addr(seq_len), _addr(new_len), rotation,
-                       q_out, k_cache, v_cache, _raw_stream(stream))
-    return _check(st, ctx) if check else st
+    seq = None if seq_len is None else seq_len.data_ptr()
+    new = None if new_len is None else new_len.data_ptr()
+    st = _append(ctx, batch, n_new, q, k, v, seq, new, rotation, q_out, k_cache, v_cache, _raw_stream(stream))
+    return _check(st, ctx) if st and check else st
 
 
 def vp_append4(ctx, batch, n_new, q: vp_rows, k: vp_rows, v: vp_rows, seq_len, rotation: vp_rotation, q_out: vp_rows,
@@ -307,9 +308,11 @@ def vp_append4(ctx, batch, n_new, q: vp_rows, k: vp_rows, v: vp_rows, seq_len, r
                stream=None, check=True):
     """``vp_append`` into caches held in 4 bits; k_held and v_held, where given,
     receive the values that the caches now hold for the new tokens."""
-    st = lib.vp_append4(ctx, batch, n_new, q, k, v, _addr(seq_len), _addr(new_len), rotation,
-                        q_out, k_cache, v_cache, k_held, v_held, _raw_stream(stream))
-    return _check(st, ctx) if check else st
+    seq = None if seq_len is None else seq_len.data_ptr()
+    new = None if new_len is None else new_len.data_ptr()
+    st = _append4(ctx, batch, n_new, q, k, v, seq, new, rotation, q_out, k_cache, v_cache, k_held, v_held,
+                  _raw_stream(stream))
+    return _check(st, ctx) if st and check else st
 
 
 def vp_reserve4(ctx, max_new):
@@ -320,9 +323,11 @@ def vp_reserve4(ctx, max_new):
 def vp_attend4(ctx, batch, n_new, q: vp_rows, k_cache: vp_kv4, v_cache: vp_kv4, seq_len, visible: vp_visible,
                out: vp_rows, new_len=None, lse=None, stream=None, check=True):
     """``vp_attend_new`` over caches held in 4 bits (no accumulated weights)."""
-    st = lib.vp_attend4(ctx, batch, n_new, q, k_cache, v_cache, _addr(seq_len), _addr(new_len),
-                        visible, out, _addr(lse), _raw_stream(stream))
-    return _check(st, ctx) if check else st
+    seq = None if seq_len is None else seq_len.data_ptr()
+    new = None if new_len is None else new_len.data_ptr()
+    st = _attend4(ctx, batch, n_new, q, k_cache, v_cache, seq, new, visible, out,
+                  None if lse is None else lse.data_ptr(), _raw_stream(stream))
+    return _check(st, ctx) if st and check else st
 
 
 def vp_set_score_path(ctx, path):

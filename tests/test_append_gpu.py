@@ -82,7 +82,7 @@ class Append:
             self.k_mag = np.maximum(np.abs(self.k_mag), np.abs(O4.rotate(np.abs(f[:, :, H: H + Hkv]), np.abs(cos),
                                                                          np.abs(sin), interleaved, np.float64)))
         else:
-            self.k_mag = 0 * self.k64
+            self.k_mag = np.zeros_like(self.k64)
         self.want_q = torch.from_numpy(q32).to(dt)
         self.want_k, self.want_v = torch.from_numpy(k32).to(dt), qkv[:, :, H + Hkv:]
         for b, n in enumerate(self.ns):  # rows that are no new tokens
