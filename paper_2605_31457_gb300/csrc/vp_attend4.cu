@@ -83,7 +83,9 @@ struct Cfg4 {
   static constexpr int CODES = kStep4 * D / 2;          // a stage: codes of a turn's tokens, then their scales, of K and of V
   static constexpr int SCALES = kStep4 * GROUPS * 2;
   static constexpr int STAGE = 2 * (CODES + SCALES);
-  static constexpr int S = CPS == 3 ? 3 : 4;            // stages of a warp's ring
+  // Stages of a warp's ring (three also for 32 rows: 64 us against 67 with four and 74
+  // with two; 24 rows: 51 with four, 55 with three).
+  static constexpr int S = CPS == 3 || NT == 4 ? 3 : 4;
   // A warp's ring, and behind it its output to be joined, float [RS][D] (in the ring where there is no room).
   static constexpr int RING = S * STAGE;
   static constexpr int OUT = RS * D * 4;
@@ -721,11 +723,19 @@ cudaError_t configure_attend4() {
 
 void plan_attend4(Attend4Params& p) {
   p.block = with_att4(p.dtype, p.D, p.R, [](auto, size_t, int rows, int) { return rows; });
-  p.grid = p.num_sms * with_att4(p.dtype, p.D, p.R, [](auto, size_t, int, int cps) { return cps; });
   p.nqt = (p.R + p.block - 1) / p.block;
+  // No more CTAs than shares of two tiles: idle ones cost a microsecond (one sequence of
+  // 3857 tokens, 4 kv-heads: 11.0 us with 456 CTAs, 9.2 with 152).
+  const int64_t items = p.B * (int64_t)p.nqt * p.Hkv;
+  int64_t span = p.max_seq;
+  if (p.window >= 0 && (int64_t)p.window + p.n_new + p.sinks + 2 * kTcTile < span)
+    span = (int64_t)p.window + p.n_new + p.sinks + 2 * kTcTile;
+  const int64_t shares = items * ((span + 2 * kTcTile - 1) / (2 * kTcTile)), waves = (shares + p.num_sms - 1) / p.num_sms;
+  const int cps = with_att4(p.dtype, p.D, p.R, [](auto, size_t, int, int cps) { return cps; });
+  p.grid = p.num_sms * (int)(waves < cps ? waves : cps);
   // An item's start and end take about as long as two tiles; where every item has
   // CTAs of its own, the least share of one follows from it (min_share).
-  p.fixed = p.B * (int64_t)p.nqt * p.Hkv <= p.grid / 4 ? 2 : 6;
+  p.fixed = items <= p.grid / 4 ? 2 : 6;
 }
 
 cudaError_t launch_attend4(const Attend4Params& p, cudaStream_t st) {

@@ -81,7 +81,7 @@ def test_line_of_vp_attend4(tmp_path):
     for old, new in [("block = R > kTcTile ? 2 * kTcTile : R,", "block = R <= 8 ? 8 : R <= 16 ? 16 : R <= 24 ? 24 : 32,"),
                      ("Hkv = pick(1, 8), fixed = (dec ? 1 : 2) * kTileUnits;\n", "Hkv = pick(1, 8);\n"),
                      ("const int ctas = pick(0, 1) ? 152 : pick(1, 320);",
-                      "const int ctas = pick(0, 1) ? 456 : 304, fixed = B * nqt * Hkv <= ctas / 4 ? 2 : 6; (void)dec;")]:
+                      "const int ctas = 152 * pick(1, 3), fixed = B * nqt * Hkv <= ctas / 4 ? 2 : 6; (void)dec;")]:
         assert s.count(old) == 1, old
         s = s.replace(old, new)
     _run(s, tmp_path)
