@@ -63,8 +63,8 @@ namespace {
 // rows, 144 of them the conversion, at 60% of the issue rate; at the measured copy rate
 // an SM gets these tokens' bytes in the time of 390.
 // Heads of 128, 32/8: 64 sequences of 17408 tokens in 243 us (5.3 TB/s); 16 of 2305 to
-// 9001 with five new tokens in 52 us; 28/4: 32 of 2816 to 6400 in 28 us, one of 3857 in
-// 11.0 us.  Slower, the first of these: 16 tokens a turn and 8 warps a CTA (304 us), 16
+// 9001 with five new tokens in 51 us; 28/4: 32 of 2816 to 6400 in 28 us, one of 3857 in
+// 9.3 us.  Slower, the first of these: 16 tokens a turn and 8 warps a CTA (304 us), 16
 // warps per SM at 128 registers (250), constants of the conversion left to the compiler,
 // which loads them again for every use (348).  Two warps sharing 24 rows' registers,
 // with two barriers a turn, took 68 us for the drafted tokens (then 55).
@@ -725,7 +725,7 @@ void plan_attend4(Attend4Params& p) {
   p.block = with_att4(p.dtype, p.D, p.R, [](auto, size_t, int rows, int) { return rows; });
   p.nqt = (p.R + p.block - 1) / p.block;
   // No more CTAs than shares of two tiles: idle ones cost a microsecond (one sequence of
-  // 3857 tokens, 4 kv-heads: 11.0 us with 456 CTAs, 9.2 with 152).
+  // 3857 tokens, 4 kv-heads: 11.0 us with 456 CTAs, 9.3 with 152).
   const int64_t items = p.B * (int64_t)p.nqt * p.Hkv;
   int64_t span = p.max_seq;
   if (p.window >= 0 && (int64_t)p.window + p.n_new + p.sinks + 2 * kTcTile < span)
