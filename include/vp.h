@@ -524,7 +524,10 @@ vp_status vp_reserve4(vp_ctx* ctx, int32_t max_new);
  * scales, are rounded to fp16 (2^-11 of each; the output's own rounding is 2^-8);
  * with n_new * G > 128 (pages of at least 8 tokens) the held values are first rounded
  * to bf16, which vp_append4's are exactly, and vp_attend_new's bounds hold.  fp32
- * contexts: both are two fp16 terms.  VP_ERR_CAPACITY when vp_reserve4 has not
+ * contexts: both are two fp16 terms (2^-22 of each).  A product that is far below the
+ * row's largest probability times its own scale is rounded at 2^-28 of that (fp32:
+ * 2^-38) instead; other groups' and other tokens' scales do not matter.  (Scales
+ * below 2^-22 count as 2^-22 in this.)  VP_ERR_CAPACITY when vp_reserve4 has not
  * reserved for n_new, VP_ERR_UNSUPPORTED where the call's tiles (of 128 tokens, 32
  * rows of one kv-head) could pass 2^29.  Allocates nothing and never synchronises;
  * every kernel waits for the stream's previous work, so an input may be the output

@@ -42,9 +42,14 @@ namespace {
 //
 // P = exp2(z - reference).  The reference is 10 (log2 units) below the largest
 // logit that raised it, and is raised when a logit is more than 14 above it, so
-// P <= 2^14 and P * scale < 2^15 for scales below 2.  From the first token with a
-// larger one on, the reference is 15 higher (one term: P is then exact to 2^-20 of
-// the row's largest), or P * scale is taken times 2^-15 (two terms).
+// P <= 2^14.  V's scales are taken in units, a power of two for each group of
+// dimensions (and so is the group's output): a turn's scales lie within [2^-7, 2) of
+// theirs, so that P * scale < 2^15, and below 2^-14, where fp16's step is fixed, only
+// for a P more than 2^17 below the row's largest: 2^-28 of that at worst (a second
+// term is held times 2^11: 2^-39).  Each lane puts one token's scales into their
+// units, in the ring, where they are read eight times.  When a turn does not fit,
+// units follow the largest scales, up or down; where a group's scales lie further
+// apart than that, the turn is done again for those that were left out, until none is.
 //
 // Float outputs: the tensor cores cut what they add to a sum, so 16 tokens' products
 // are summed by themselves and added in float; bf16 outputs, whose rounding is far
@@ -69,7 +74,9 @@ namespace {
 // which loads them again for every use (348).  Two warps sharing 24 rows' registers,
 // with two barriers a turn, took 68 us for the drafted tokens (then 55).
 // ---------------------------------------------------------------------------
-constexpr float kAbove4 = 10.f, kBig4 = 15.f, kRaise4 = 4.f;
+constexpr float kAbove4 = 10.f, kRaise4 = 4.f;
+constexpr uint32_t kLeastUnit4 = 0x7800;  // 2^15, one over the least unit, in fp16
+constexpr float kSecond4 = 2048.f;        // a second term is held times this
 constexpr float kLowest4 = -3e38f;  // the reference of a row that has seen nothing
 constexpr int kWarps4 = 4, kThreads4 = 32 * kWarps4;
 constexpr int kStep4 = kTcTile / kWarps4;  // tokens of a warp's turn: a row's lane looks up its page
@@ -129,6 +136,11 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
 __device__ __forceinline__ uint32_t mul_f16(uint32_t a, uint32_t b) {
   const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
   return *reinterpret_cast<const uint32_t*>(&r);
+}
+// A group's unit from one over it (a power of two, the low or high half of a register).
+__device__ __forceinline__ float unit_of(uint32_t one_over, int high) {
+  const float2 x = unpack_f16(one_over);
+  return __uint_as_float((254u << 23) - __float_as_uint(high ? x.y : x.x));
 }
 // A copy of N bytes, or N zeros.
 template <int N>
@@ -433,8 +445,15 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
     };
 
     float o[NT][NG][2][4], ref[NT][2], l[NT][2];
-    float above = kAbove4, v_unit = 1.f;  // O is in units of v_unit
-    bool large = false;                    // a scale of 2 or more was met
+    // One over the groups' units, two of them in a register; what is left of the turn's
+    // scales, this lane's token's, when it is done again.
+    uint32_t one_over[NG / 2], left[NG / 2];
+    bool again = false;
+#pragma unroll
+    for (int m = 0; m < NG / 2; ++m) {
+      one_over[m] = 0x3c003c00;
+      left[m] = 0;
+    }
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
       ref[t][0] = ref[t][1] = kLowest4;
@@ -448,17 +467,32 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
     }
 
 #pragma unroll 1
-    for (int u = q.u0; u < q.u1; ++u) {
+    for (int u = q.u0; u < q.u1; u += again ? 0 : 1) {
+      const bool repeat = again;
+      again = false;
       cp_async_wait<S - 2>();
       __syncwarp();
-      issue(u + S - 1);  // into the stage that the last turn read
+      if (!repeat) issue(u + S - 1);  // into the stage that the last turn read
       const int st = (unsigned)(u - q.u0) % S;
       const unsigned turn = (partly >> st) & 1u ? masks[st] : 0xffffffffu;
       const int jt = first_token(u);
       const bool all_see = turn == 0xffffffffu && jt + kStep4 - 1 <= t0 &&
                            (p.window < 0 || jt > t1 - p.window || jt + kStep4 <= p.sinks);
       const unsigned at = ring + st * C::STAGE;
-      const unsigned char* const scales = mine + st * C::STAGE + 2 * C::CODES;
+      unsigned char* const scales = mine + st * C::STAGE + 2 * C::CODES;
+
+      // ---- V's scales of token `lane`, in their units
+      uint32_t* const of_mine = reinterpret_cast<uint32_t*>(scales + C::SCALES + lane * 2 * NG);
+      uint32_t held[NG / 2], out_of = 0;
+#pragma unroll
+      for (int m = 0; m < NG / 2; ++m) held[m] = repeat ? left[m] : of_mine[m];
+#pragma unroll
+      for (int m = 0; m < NG / 2; ++m) {
+        const uint32_t in_units = mul_f16(held[m], one_over[m]);
+        of_mine[m] = in_units;
+        out_of |= in_units ^ 0x20002000;
+      }
+      const bool off = (out_of & 0x60006000) != 0;  // an exponent is not one of 2^-7 to 2^0
 
       // ---- logits, over the row's factor: tokens r and r + 8 of each half, query rows 2c and 2c + 1
       float z[2][NT][4];
@@ -535,42 +569,65 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
             }
       }
 
-      // ---- the references
+      // ---- the references and units
       bool need = false;
       auto largest = [&](int t, int k) { return fmaxf(fmaxf(z[0][t][k], z[0][t][2 + k]), fmaxf(z[1][t][k], z[1][t][2 + k])); };
 #pragma unroll
       for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int k = 0; k < 2; ++k) need |= fmaf(largest(t, k), fac[t][k], -ref[t][k]) > above + kRaise4;
-      uint32_t any = 0;  // of V's scales of token `lane`: one of 2 or more?
+        for (int k = 0; k < 2; ++k) need |= fmaf(largest(t, k), fac[t][k], -ref[t][k]) > kAbove4 + kRaise4;
+      if (__any_sync(0xffffffffu, need || off)) {
+        float change[NG];
 #pragma unroll
-      for (int g = 0; g < NG; g += 2) any |= *reinterpret_cast<const uint32_t*>(scales + C::SCALES + lane * 2 * NG + 2 * g);
-      const bool big = (any & 0x40004000u) != 0;
-      if (__any_sync(0xffffffffu, need || (big && !large))) {
-        float fv = 1.f;
-        if (!large && __any_sync(0xffffffffu, big)) {
-          large = true;
-          if constexpr (TERMS == 1) above = kAbove4 - kBig4;
-          else fv = v_unit = 3.0517578125e-05f;  // 2^-kBig4
+        for (int g = 0; g < NG; ++g) change[g] = 1.f;
+        if (__any_sync(0xffffffffu, off)) {
+          uint32_t rest = 0;
+#pragma unroll
+          for (int m = 0; m < NG / 2; ++m) {
+            uint32_t next = one_over[m];
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+              const uint32_t top = __reduce_max_sync(0xffffffffu, (held[m] >> (16 * x)) & 0x7fff);
+              const uint32_t field = top >> 10;
+              const float was = unit_of(one_over[m], x), size = __half2float(__ushort_as_half((unsigned short)top));
+              if (top != 0 && !(size >= 0.0078125f * was && size < 2.f * was)) {  // it becomes the unit that is next below
+                const float unit = __uint_as_float((min(field, 30u) + 112u) << 23);
+                change[2 * m + x] = was * (1.f / unit);
+                const uint32_t bits = __half_as_ushort(__float2half_rn(1.f / unit));
+                next = x ? prmt(next, bits, 0x5410) : prmt(next, bits, 0x3254);
+              }
+            }
+            one_over[m] = next;
+            uint32_t in_units = mul_f16(held[m], next);
+            // What lies below the unit's reach is left for later, unless there is no smaller unit.
+            const uint32_t small = __hlt2_mask(__habs2(*reinterpret_cast<const __half2*>(&in_units)),
+                                               __float2half2_rn(0.0078125f)) &
+                                   ~((next & 0xffff) == kLeastUnit4 ? 0xffffu : 0u) &
+                                   ~((next >> 16) == kLeastUnit4 ? 0xffff0000u : 0u);
+            left[m] = held[m] & small;
+            of_mine[m] = in_units & ~small;
+            rest |= left[m] & 0x7fff7fff;
+          }
+          again = __any_sync(0xffffffffu, rest != 0);
         }
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
-            const float next = fmaxf(ref[t][k], fmaf(group_max(largest(t, k)), fac[t][k], -above));
+            const float next = fmaxf(ref[t][k], fmaf(group_max(largest(t, k)), fac[t][k], -kAbove4));
             const float f = fexp2(ref[t][k] - next);
             ref[t][k] = next;
             l[t][k] *= f;
-            const float fo = TERMS == 1 ? f : f * fv;
 #pragma unroll
             for (int g = 0; g < NG; ++g)
 #pragma unroll
               for (int h = 0; h < 2; ++h) {
-                o[t][g][h][k] *= fo;
-                o[t][g][h][2 + k] *= fo;
+                o[t][g][h][k] *= f * change[g];
+                o[t][g][h][2 + k] *= f * change[g];
               }
           }
       }
+      __syncwarp();
 
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -581,15 +638,17 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
           float e[4];
 #pragma unroll
           for (int k = 0; k < 4; ++k) e[k] = fexp2(fmaf(z[h][t][k], fac[t][k & 1], -ref[t][k & 1]));
-          l[t][0] += e[0] + e[2];
-          l[t][1] += e[1] + e[3];
+          if (!repeat) {
+            l[t][0] += e[0] + e[2];
+            l[t][1] += e[1] + e[3];
+          }
           const uint32_t h0 = pack_f16(e[0], e[1]), h1 = pack_f16(e[2], e[3]);
           ph[t][0] = transpose8(h0);
           ph[t][1] = transpose8(h1);
           if constexpr (TERMS == 2) {
             const float2 f0 = unpack_f16(h0), f1 = unpack_f16(h1);
-            pl[t][0] = transpose8(pack_f16(e[0] - f0.x, e[1] - f0.y));
-            pl[t][1] = transpose8(pack_f16(e[2] - f1.x, e[3] - f1.y));
+            pl[t][0] = transpose8(pack_f16((e[0] - f0.x) * kSecond4, (e[1] - f0.y) * kSecond4));
+            pl[t][1] = transpose8(pack_f16((e[2] - f1.x) * kSecond4, (e[3] - f1.y) * kSecond4));
           }
         }
 
@@ -641,20 +700,20 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                   const float2 x = unpack_f16(ph[t][k]), y = unpack_f16(pl[t][k]), s = unpack_f16(sc[g][k]);
-                  const float ea = (x.x + y.x) * (s.x * v_unit), eb = (x.y + y.y) * (s.y * v_unit);
+                  const float ea = fmaf(y.x, 1.f / kSecond4, x.x) * s.x, eb = fmaf(y.y, 1.f / kSecond4, x.y) * s.y;
                   hi[k] = pack_f16(ea, eb);
                   const float2 f = unpack_f16(hi[k]);
-                  lo[k] = pack_f16(ea - f.x, eb - f.y);
+                  lo[k] = pack_f16((ea - f.x) * kSecond4, (eb - f.y) * kSecond4);
                 }
                 // The tensor cores cut what they add to a sum, which over a long range adds up:
                 // sixteen tokens' products are summed by themselves, and added in float.
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
-                  float sum[4];
-                  mma_f16_first(sum, a[4 * x], a[4 * x + 1], a[4 * x + 2], a[4 * x + 3], lo[0], lo[1]);
-                  mma_f16(sum, a[4 * x], a[4 * x + 1], a[4 * x + 2], a[4 * x + 3], hi[0], hi[1]);
+                  float sum[4], second[4];
+                  mma_f16_first(sum, a[4 * x], a[4 * x + 1], a[4 * x + 2], a[4 * x + 3], hi[0], hi[1]);
+                  mma_f16_first(second, a[4 * x], a[4 * x + 1], a[4 * x + 2], a[4 * x + 3], lo[0], lo[1]);
 #pragma unroll
-                  for (int k = 0; k < 4; ++k) o[t][g][x][k] += sum[k];
+                  for (int k = 0; k < 4; ++k) o[t][g][x][k] += fmaf(second[k], 1.f / kSecond4, sum[k]);
                 }
               }
             }
@@ -665,7 +724,6 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
     cp_async_wait<0>();
     __syncwarp();
     // ---- this warp's output, to be joined with the others'
-    const float o_unit = TERMS == 2 && large ? 32768.f : 1.f;
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -675,9 +733,9 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
         if (r == 0) ml_all[warp * RS + row] = make_float2(ref[t][k], sum);
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
-          const float4 x = make_float4(o[t][g][0][k], o[t][g][0][2 + k], o[t][g][1][k], o[t][g][1][2 + k]);
+          const float unit = unit_of(one_over[g / 2], g & 1);
           *reinterpret_cast<float4*>(mine + C::OFF_O + 4 * (row * D + 32 * g + 4 * r)) =
-              make_float4(x.x * o_unit, x.y * o_unit, x.z * o_unit, x.w * o_unit);
+              make_float4(o[t][g][0][k] * unit, o[t][g][0][2 + k] * unit, o[t][g][1][k] * unit, o[t][g][1][2 + k] * unit);
         }
       }
     d_b = q.b; d_g = q.g; d_row0 = q.it.row0; d_rows = rows; d_c0 = q.c0; d_parts = q.parts;
