@@ -454,7 +454,9 @@ typedef struct {
  * whose page the block table does not map is not written (its query is), and
  * flagged (vp_check_errors).  VP_ERR_CAPACITY for n_new > max_seq.
  * The inputs must not lie in the caches, and no page that a token goes to may
- * belong to two sequences.
+ * belong to two sequences.  Rows of q_out and of the caches must not overlap:
+ * VP_ERR_INVALID_ARG for a stride below a row's length along an axis of more than one
+ * element (sequences or pages, heads, tokens; a broadcast cache, for instance).
  * Uses no workspace, allocates nothing and never synchronises; waits for the
  * stream's previous work, and a call behind it, vp_decode_step included, may use
  * its outputs.

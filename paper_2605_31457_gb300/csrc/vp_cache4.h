@@ -35,6 +35,12 @@ struct RotView {
   int axes, end0, end1;  // axes 1: end0 = rot / 2
 };
 
+// Whether rows of `row` elements do not overlap: nb, nh and nt of them along axes of
+// these strides.  (An axis of one element may have any stride.)
+inline bool rows_apart(int64_t sb, int64_t sh, int64_t st, int64_t nb, int64_t nh, int64_t nt, int64_t row) {
+  return (nb <= 1 || sb >= row) && (nh <= 1 || sh >= row) && (nt <= 1 || st >= row);
+}
+
 struct AppendParams {
   int B, n_new, H, Hkv, max_seq;  // H: query heads to rotate; 0: none
   int paged, page_size, page_shift;

@@ -80,13 +80,28 @@ bool rotation_ok(const vp_ctx* ctx, const vp_rotation& r, std::string* why) {
   return true;
 }
 
-// Rows that a call writes: no two of them in one place.
-bool apart_ok(const vp_rows& r, int batch, int n_new, int heads, const char* name, std::string* why) {
-  if ((batch > 1 && r.stride_b == 0) || (n_new > 1 && r.stride_n == 0) || (heads > 1 && r.stride_h == 0)) {
-    *why = std::string(name) + ": rows that are written need strides above 0";
-    return false;
-  }
-  return true;
+// Rows that a call writes: no two of them overlap.
+bool apart_ok(const vp_ctx* ctx, const vp_rows& r, int batch, int n_new, int heads, const char* name, std::string* why) {
+  if (vp::rows_apart(r.stride_b, r.stride_h, r.stride_n, batch, heads, n_new, ctx->cfg.head_dim)) return true;
+  *why = std::string(name) + ": rows that are written need strides of at least head_dim";
+  return false;
+}
+// The same of a cache: its strides, its sequences or pages, elements of a row.
+bool apart_ok(const vp_ctx* ctx, int64_t sb, int64_t sh, int64_t st, int64_t lead, int64_t row, const char* name,
+              std::string* why) {
+  const vp_config& c = ctx->cfg;
+  if (vp::rows_apart(sb, sh, st, lead, c.num_kv_heads, c.paged ? c.page_size : c.max_seq, row)) return true;
+  *why = std::string(name) + ": a cache that is written needs strides of at least a row";
+  return false;
+}
+bool apart_ok(const vp_ctx* ctx, const vp_kv& kv, int batch, const char* name, std::string* why) {
+  return apart_ok(ctx, kv.stride_b, kv.stride_h, kv.stride_t, ctx->cfg.paged ? kv.num_pages : batch, ctx->cfg.head_dim,
+                  name, why);
+}
+bool apart_ok(const vp_ctx* ctx, const vp_kv4& kv, int batch, const char* name, std::string* why) {
+  const int64_t lead = ctx->cfg.paged ? kv.num_pages : batch, D = ctx->cfg.head_dim;
+  return apart_ok(ctx, kv.code_stride_b, kv.code_stride_h, kv.code_stride_t, lead, D / 2, name, why) &&
+         apart_ok(ctx, kv.scale_stride_b, kv.scale_stride_h, kv.scale_stride_t, lead, D / vp::kGroup4, name, why);
 }
 
 // Kv: vp_kv or vp_kv4.
@@ -110,12 +125,12 @@ vp_status append(vp_ctx* ctx, const char* name, int32_t batch, int32_t n_new, co
   if (batch == 0 || n_new == 0) return VP_OK;
   if (!seq_len) return fail(ctx, VP_ERR_INVALID_ARG, at + "seq_len is NULL");
   if ((q && (!rows_ok(ctx, q, "q", &why) || !rows_ok(ctx, q_out, "q_out", &why) ||
-             !apart_ok(*q_out, batch, n_new, c.num_q_heads, "q_out", &why))) ||
+             !apart_ok(ctx, *q_out, batch, n_new, c.num_q_heads, "q_out", &why))) ||
       !rows_ok(ctx, k, "k", &why) || !rows_ok(ctx, v, "v", &why))
     return fail(ctx, VP_ERR_INVALID_ARG, at + why);
   for (const vp_rows* held : {k_held, v_held})
     if (held && (!rows_ok(ctx, held, "k_held, v_held", &why) ||
-                 !apart_ok(*held, batch, n_new, c.num_kv_heads, "k_held, v_held", &why)))
+                 !apart_ok(ctx, *held, batch, n_new, c.num_kv_heads, "k_held, v_held", &why)))
       return fail(ctx, VP_ERR_INVALID_ARG, at + why);
   if (q && q->data == q_out->data &&
       (q->stride_b != q_out->stride_b || q->stride_n != q_out->stride_n || q->stride_h != q_out->stride_h))
@@ -123,12 +138,14 @@ vp_status append(vp_ctx* ctx, const char* name, int32_t batch, int32_t n_new, co
 
   vp::AppendParams p = {};
   if constexpr (kFour) {
-    if (!kv4_ok(ctx, k_cache, "k_cache", &why) || !kv4_ok(ctx, v_cache, "v_cache", &why))
+    if (!kv4_ok(ctx, k_cache, "k_cache", &why) || !kv4_ok(ctx, v_cache, "v_cache", &why) ||
+        !apart_ok(ctx, *k_cache, batch, "k_cache", &why) || !apart_ok(ctx, *v_cache, batch, "v_cache", &why))
       return fail(ctx, VP_ERR_INVALID_ARG, at + why);
     p.kc4 = view(*k_cache);
     p.vc4 = view(*v_cache);
   } else {
-    if (!kv_ok(ctx, k_cache, "k_cache", &why) || !kv_ok(ctx, v_cache, "v_cache", &why))
+    if (!kv_ok(ctx, k_cache, "k_cache", &why) || !kv_ok(ctx, v_cache, "v_cache", &why) ||
+        !apart_ok(ctx, *k_cache, batch, "k_cache", &why) || !apart_ok(ctx, *v_cache, batch, "v_cache", &why))
       return fail(ctx, VP_ERR_INVALID_ARG, at + why);
     p.kc = vp::view(*k_cache);
     p.vc = vp::view(*v_cache);
@@ -248,7 +265,7 @@ vp_status attend4(vp_ctx* ctx, int32_t batch, int32_t n_new, const vp_rows* q, c
   std::string why;
   if (!seq_len) return fail(ctx, VP_ERR_INVALID_ARG, "vp_attend4: seq_len is NULL");
   if (!rows_ok(ctx, q, "q", &why) || !rows_ok(ctx, out, "out", &why) ||
-      !apart_ok(*out, batch, n_new, c.num_q_heads, "out", &why) || !kv4_ok(ctx, k_cache, "k_cache", &why) ||
+      !apart_ok(ctx, *out, batch, n_new, c.num_q_heads, "out", &why) || !kv4_ok(ctx, k_cache, "k_cache", &why) ||
       !kv4_ok(ctx, v_cache, "v_cache", &why))
     return fail(ctx, VP_ERR_INVALID_ARG, "vp_attend4: " + why);
   for (const vp_kv4* kv : {k_cache, v_cache})
