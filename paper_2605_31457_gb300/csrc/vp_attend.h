@@ -26,6 +26,9 @@ constexpr int kAnyRows = 16;         // most query rows per CTA of k_att_any
 
 constexpr int kTcTile = 128;         // cached tokens per tile of k_att_tc; query rows per accumulator
 
+// Of the workspaces, per SM: partial rows and tickets.
+constexpr int kPartRows = 4 * kTcTile, kTickets = 4;
+
 // The workspace of vp_attend_new (vp_reserve_new), offsets in bytes.
 struct NewLayout {
   int max_new = 0, max_weight_new = 0;
@@ -63,9 +66,9 @@ struct AttendParams {
   int weigh;                  // weights asked for
   WeightView w_in, w_out;     // w_in.data may be NULL
   // workspace
-  unsigned* tickets;          // [4 * num_sms] records written of the items cut between CTAs; 0 between calls:
-                              // a CTA's (two of them per SM) or one for each 16 or 128 of its rows, or k_att_any's
-                              // for its row blocks, which it splits where there are at most four per SM
+  unsigned* tickets;          // [kTickets * num_sms] records written of the items cut between CTAs; 0 between calls:
+                              // a CTA's (two of them per SM, k_att4: three) or one for each 16 or 128 of its rows,
+                              // or k_att_any's for its row blocks, which it splits where there are at most four per SM
   float* lse2;                // [B * Hkv][R] log-sum-exp in log2 units (+inf: an empty row), when weigh
   float* part_o;              // partial outputs, unnormalised
   float* part_st;             // their {maximum in log2 units, sum}
@@ -238,12 +241,13 @@ inline NewLayout new_layout(int max_batch, int H, int Hkv, int D, int max_seq, i
   const size_t G = (size_t)(H / Hkv);
   // Partial rows.  The tensor-core kernels leave up to two records per CTA (the
   // item it goes on with and the one it begins), of 16 rows at two CTAs per SM, of
-  // 64 or of 256 at one; k_att_any, whose CTAs number at most 8 per SM where it
-  // splits (any_splits), one of up to kAnyRows rows each.
-  const size_t rows = (size_t)2 * num_sms * 2 * kTcTile;
-  static_assert(8 * kAnyRows <= 4 * kTcTile, "k_att_any's partial rows fit");
+  // 64 or of 256 at one, k_att4 of 8 rows at three CTAs per SM or of up to 32 at
+  // two; k_att_any, whose CTAs number at most 8 per SM where it splits
+  // (any_splits), one of up to kAnyRows rows each.
+  const size_t rows = (size_t)kPartRows * num_sms;
+  static_assert(8 * kAnyRows <= kPartRows, "k_att_any's partial rows fit");
   size_t off = 0;
-  w.o_tk = off; off = ws_round(off + (size_t)4 * num_sms * 4);
+  w.o_tk = off; off = ws_round(off + (size_t)kTickets * num_sms * 4);
   w.o_lse = off; off = ws_round(off + (size_t)max_batch * Hkv * max_weight_new * G * 4);
   w.o_st = off; off = ws_round(off + rows * 2 * 4);
   w.o_o = off; off = ws_round(off + rows * D * 4);

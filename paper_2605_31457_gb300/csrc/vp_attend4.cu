@@ -110,6 +110,7 @@ struct Cfg4 {
   static constexpr size_t SMEM = OFF_MISC + (LINE + 1) * 4;
   static_assert(SMEM <= 232448 / CPS - (CPS > 1 ? 1024 : 0), "shared memory of the CTAs of an SM");
   static_assert(STAGE % 128 == 0 && WARP % 128 == 0, "rows keep their banks");
+  static_assert(2 * CPS * RS <= kPartRows && CPS <= kTickets, "two records and a ticket of a CTA");
 };
 
 __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,

@@ -253,7 +253,7 @@ __device__ __forceinline__ void join_records(const AttendParams& p, int b, int g
 #pragma unroll
         for (int i = 0; i < EU; ++i) x[k][i] = make_float4(0.f, 0.f, 0.f, 0.f);
         if (k0 + k < n) {
-          const int at = rec(k0 + k) * RS + r;  // at most 4 records per SM of up to 128 rows
+          const int at = rec(k0 + k) * RS + r;  // below kPartRows rows per SM
           st[k] = __ldcg(reinterpret_cast<const float2*>(p.part_st) + at);
 #pragma unroll
           for (int i = 0; i < EU; ++i)
