@@ -410,8 +410,11 @@ vp_status vp_evict(vp_ctx* ctx, int32_t batch, const vp_kv* k_src, const vp_kv* 
  * vp_append takes a layer's new queries, keys and values as the projections leave
  * them, rotates queries and keys by their positions and writes keys and values to
  * their places in the caches, in one kernel.  vp_append4 writes them to caches held
- * in 4 bits (9/32 of the memory of bf16), which vp_attend4 attends over.  The entry
- * points use the contexts, error codes and device checks of those above and return
+ * in 4 bits (9/32 of the memory of bf16), which vp_attend4 attends over.  The other
+ * entry points (vp_decode_step, vp_decode_gather, vp_compact_kv, vp_attend_new with its
+ * weights, vp_evict) take caches of the context's type only: a layer that is pruned or
+ * bounded by eviction keeps its cache in that.  The entry points here
+ * use the contexts, error codes and device checks of those above and return
  * VP_ERR_INVALID_ARG when the current CUDA device is not the context's.
  */
 
@@ -518,22 +521,24 @@ vp_status vp_reserve4(vp_ctx* ctx, int32_t max_new);
 
 /*
  * vp_attend_new over caches held in 4 bits: the arguments mean what they mean
- * there, without accumulated weights.  Scales need not be vp_append4's: any finite
- * fp16 number is served, and a group whose scale is not finite is as a cache row
- * that is not.  Token and page strides must be below 2^31, else
- * VP_ERR_UNSUPPORTED.  Logits are products of queries and codes, scaled and summed
- * in float.  bf16 contexts: the probabilities, and their products with the values'
- * scales, are rounded to fp16 (2^-11 of each; the output's own rounding is 2^-8);
- * with n_new * G > 128 (pages of at least 8 tokens) the held values are first rounded
- * to bf16, which vp_append4's are exactly, and vp_attend_new's bounds hold.  fp32
- * contexts: both are two fp16 terms (2^-22 of each).  A product that is far below the
- * row's largest probability times its own scale is rounded at 2^-28 of that (fp32:
- * 2^-38) instead; other groups' and other tokens' scales do not matter.  (Scales
- * below 2^-22 count as 2^-22 in this.)  VP_ERR_CAPACITY when vp_reserve4 has not
- * reserved for n_new, VP_ERR_UNSUPPORTED where the call's tiles (of 128 tokens, 32
- * rows of one kv-head) could pass 2^29.  Allocates nothing and never synchronises;
- * every kernel waits for the stream's previous work, so an input may be the output
- * of the preceding call of this library.
+ * there, without accumulated weights; rows of out must not overlap.  Scales need not
+ * be vp_append4's: any finite fp16 number is served, and a group whose scale is not
+ * finite is as a cache row that is not.  Token and page strides must be below 2^31,
+ * else VP_ERR_UNSUPPORTED.
+ * Logits are products of queries and codes, scaled and summed in float; a query's
+ * values are exact where they are within 2^30 of its row's largest (fp32 contexts:
+ * held to 2^-22, or 2^-38 of the row's largest).  bf16 contexts: the probabilities,
+ * and their products with the values' scales, are rounded to fp16 (2^-11 of each; the
+ * output's own rounding is 2^-8); with n_new * G > 128 (pages of at least 8 tokens)
+ * the held values are first rounded to bf16, which vp_append4's are exactly, and
+ * vp_attend_new's bounds hold.  fp32 contexts: both are two fp16 terms (2^-22 of
+ * each).  A product that is far below the row's largest probability times its own
+ * scale is rounded at 2^-28 of that (fp32: 2^-38) instead; the scales of other groups
+ * and tokens do not matter.  (Scales below 2^-22 count as 2^-22 in this.)
+ * VP_ERR_CAPACITY when vp_reserve4 has not reserved for n_new, VP_ERR_UNSUPPORTED
+ * where the call's tiles (of 128 tokens, 8 to 32 rows of one kv-head) could pass 2^29.
+ * Allocates nothing and never synchronises; every kernel waits for the stream's
+ * previous work, so an input may be the output of the preceding call of this library.
  */
 vp_status vp_attend4(vp_ctx* ctx, int32_t batch, int32_t n_new, const vp_rows* q,
                      const vp_kv4* k_cache, const vp_kv4* v_cache,

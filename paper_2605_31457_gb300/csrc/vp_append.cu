@@ -34,7 +34,9 @@ namespace {
 // ::parts).  Its turns are of one kind each, queries, keys or values, so that nothing
 // is chosen per lane, and the loads of four rows are on their way while lengths, pages
 // and angles are looked up.  In a graph, heads of 128: one token of 32 sequences, 28/4,
-// in 2.8 us (4 bits: 3.1); a prompt of 3857, 28/4, in 12.1 us (6.0 TB/s); four of up to
+// in 2.8 us (4 bits: 3.1); a prompt of 3857, 28/4, in 15.5 us (4.7 TB/s; 12.1 us time
+// after time on one set of inputs, half of which stays in L2), where the loads of the next
+// four rows wait for the stores of these; four of up to
 // 2305, 32/8, in 4 bits in 43 us (4.6 TB/s; three quarters of the issue slots).  A CTA
 // per token took 17.1 and 52 us, six rows in flight 15.5 and 50.
 // Nothing triggers the next kernel early: what follows may read the caches before it

@@ -58,18 +58,23 @@ namespace {
 // Tokens that no row sees are not copied: the ring gets zeros for them, their scales
 // among these, and their logits are masked.
 //
-// A warp's ring is filled by its own asynchronous copies, two turns ahead, so warps
-// need no barrier until a part ends; a part's first copies run while the part before
-// it is joined (where shared memory holds both: up to 16 rows of 128 dimensions).  mma.sync takes its operands from
-// registers, where the codes are converted: a tcgen05 operand would go through shared
-// memory, 512 bytes for every 144 that are read.
+// A warp's ring is filled by its own asynchronous copies, two or three turns ahead, so
+// warps need no barrier until a part ends; a part's first copies run while the part
+// before it is joined (where shared memory holds both: up to 16 rows of 128 dimensions).
+// mma.sync takes its operands from registers, where the codes are converted.  For
+// tcgen05 they would first be written to shared memory (512 bytes for every 144 that are
+// read) or, K's, to tensor memory.  For 8 rows that is more than the products themselves;
+// a form that converts each tile once for all of 9 to 128 rows has not been built, and
+// this one converts it again for every 32.
 //
-// Bound by issue slots: 330 instructions of a warp for 16 tokens of K and V with 8
+// Bound by issue slots: 337 instructions of a warp for 16 tokens of K and V with 8
 // rows, 144 of them the conversion, at 60% of the issue rate; at the measured copy rate
 // an SM gets these tokens' bytes in the time of 390.
-// Heads of 128, 32/8: 64 sequences of 17408 tokens in 243 us (5.3 TB/s); 16 of 2305 to
-// 9001 with five new tokens in 51 us; 28/4: 32 of 2816 to 6400 in 28 us, one of 3857 in
-// 9.3 us.  Slower, the first of these: 16 tokens a turn and 8 warps a CTA (304 us), 16
+// Heads of 128, 32/8: 64 sequences of 17408 tokens in 247 us (5.2 TB/s); 16 of 2305 to
+// 9001 with five new tokens in 53 us; 28/4: 32 of 2816 to 6400 in 29 us, one of 3857 in
+// 9.7 us.  fp32: the first of these in 380 us.  Units of V's scales cost 7 instructions
+// of those 337 (243, 51, 28 and 9.3 us without; scales put into them behind the logits
+// instead of before, 255 us).  Slower, against 243: 16 tokens a turn and 8 warps a CTA (304 us), 16
 // warps per SM at 128 registers (250), constants of the conversion left to the compiler,
 // which loads them again for every use (348).  Two warps sharing 24 rows' registers,
 // with two barriers a turn, took 68 us for the drafted tokens (then 55).

@@ -64,7 +64,9 @@ struct Attend4Params : AttendParams {
 
 // Calls of many query rows unpack the tokens that they see into bf16 caches of the
 // workspace (exactly, for vp_append4's scales) and run the kernels of vp_attend_new
-// on those: a group of sequences at a time, as many as the workspace holds.  Measured,
+// on those: a group of sequences at a time, as many as the workspace holds (which follows
+// from max_seq, not from their lengths).  The rule goes by rows alone: where there are
+// few items, as with one sequence, k_att4 is still the faster way somewhat above it.  Measured,
 // 32/8 heads of 128, k_att4 against this way: one sequence of 9001 tokens, 128 rows
 // 35 us against 97, 256 rows 60 against 72; four of up to 9001, 128 rows 65 against
 // 93, 192 rows 94 against 89; 16 of them, 128 rows 227 against 255, 160 rows 283

@@ -15,7 +15,9 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
 __device__ __forceinline__ float2 unpack_f16(uint32_t u) { return __half22float2(*reinterpret_cast<const __half2*>(&u)); }
 
 // The whole numbers code - 8 of the codes in bits 0-3 and 16-19 (low), and of
-// those in bits 4-7 and 20-23 (high).  The constants are kept in registers: a mask
+// those in bits 4-7 and 20-23 (high), in the widely published way: the bits become the
+// mantissa of 1024 and an addition takes the offset off, for the high ones with a factor
+// of 1/16; the constants follow from fp16's format.  They are kept in registers: a mask
 // and the exponent are one operation then.
 struct Codes {
   uint32_t mask, mask_high, k1024, k1032, sixteenth, k72;
