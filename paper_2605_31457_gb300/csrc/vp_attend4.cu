@@ -605,7 +605,8 @@ __global__ void __launch_bounds__(kThreads4, Cfg4<T, D, NT>::CPS) k_att4(const _
             }
             one_over[m] = next;
             uint32_t in_units = mul_f16(held[m], next);
-            // What lies below the unit's reach is left for later, unless there is no smaller unit.
+            // What lies below the unit's reach is left for later, unless there is no smaller unit; the
+            // group's largest never is, so that passes end.
             const uint32_t small = __hlt2_mask(__habs2(*reinterpret_cast<const __half2*>(&in_units)),
                                                __float2half2_rn(0.0078125f)) &
                                    ~((next & 0xffff) == kLeastUnit4 ? 0xffffu : 0u) &

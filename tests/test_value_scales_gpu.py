@@ -37,11 +37,15 @@ def vp(lib):
     return lib
 
 
-def check(a, nothing=0.9):
-    """Runs the case; of the elements, at least the share `nothing` must tell a zero from the result."""
+def check(a, nothing=0.9, lost=None):
+    """Runs the case; of the elements, at least the share `nothing` must tell a zero from the result.
+    lost: dimensions of sequence 0 that must not come out finite."""
     a.call()
     torch.cuda.synchronize()
     a.vp.vp_check_errors(a.ctx)
+    if lost is not None:
+        assert not torch.isfinite(a.out[0, :, :, lost]).any()
+        a.out[0, :, :, lost] = torch.from_numpy(a.ref[0]["out"]).to(a.out)[:, :, lost]
     vstep = a.held[1][1].astype(np.float64)                          # [B, Hkv, T, groups]
     told = total = 0
     for b, ref in enumerate(a.ref):
@@ -219,6 +223,21 @@ def test_windows_and_pages(vp, dtype, page, window, sinks):
         vstep[:, :, ::50, 1] = 300.0
 
     check(case(vp, (8, 2), 64, dtype, lens=(400, 77, 130), n_new=2, page=page, window=window, sinks=sinks, steps=steps))
+
+
+@TYPES
+@pytest.mark.parametrize("heads,dim", [((8, 2), 64), ((28, 4), 128), ((32, 2), 128)])
+@pytest.mark.parametrize("scale", [float("inf"), float("-inf"), float("nan")])
+def test_a_scale_that_is_not_finite_stays_in_its_group(vp, dtype, heads, dim, scale):
+    """Among scales of every size, which take several passes; the other groups and sequences are as without it."""
+    def steps(held, rng):
+        vstep = held[1][1]
+        vstep[:] = np.clip(fit_bits(2.0 ** rng.uniform(-14, 16, vstep.shape)), 2.0 ** -14, 61440.0)
+
+    a = case(vp, heads, dim, dtype, lens=(300, 77), steps=steps)
+    a.tensors[3][0, :, 130, 1] = scale
+    a.tensors[3][0, :, 131, 1] = float("inf")
+    check(a, lost=slice(32, 64))
 
 
 @TYPES
